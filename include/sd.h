@@ -390,6 +390,128 @@ sd_status sd_accept_sample(const float* z_target, const float* z_draft, int B, i
                            void* ws, size_t ws_bytes, sd_stream_t stream);
 
 /*
+ * An 8-bit KV cache of one attention layer. k and v are [B][Hkv][capacity][D]
+ * e4m3 codes (1 byte each: 4 significant bits, magnitude at most 448);
+ * k_scale and v_scale are fp32 [B][Hkv][ceil(capacity / block)], one scale for
+ * each block of `block` consecutive rows of a KV head:
+ *   key n = k_code[n] * k_scale[n / block],  value n likewise.
+ * len as in sd_kv_cache. Rows at or past len[b], and the scales of blocks that
+ * hold none before it, are never read (but as older rows of an append).
+ * ticket: device uint32 [B], zero-filled before the cache's first use and left
+ * zeroed by every completed call.
+ * D in {64, 128}, block in {32, 64, 128}.
+ */
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int32_t* len;
+  uint32_t* ticket;
+  int32_t batch;
+  int32_t n_kv_heads;
+  int32_t capacity;
+  int32_t head_dim;
+  int32_t block;
+} sd_kv8_cache;
+
+/*
+ * Append R new rows per scene to an 8-bit cache: sd_kv_append with the rows
+ * quantised on the way.
+ *   k_new, v_new: [B][R][Hkv][D] bf16, contiguous.
+ * A block that begins with new rows takes the smallest power of two s =
+ * 2^e, e >= -100, with amax <= 448 s, amax the largest finite magnitude of its
+ * new rows (2^-100 when that is 0). A block that holds older rows keeps its
+ * scale s times the least 2^g, g >= 0, with amax <= 448 s 2^g, and the older
+ * codes move by 2^-g: that rounds only the ones that become subnormal. (Any
+ * positive scale may stand there; the division is then fp32's.) A code is the
+ * value over its block's scale, rounded to the nearest e4m3, ties to even:
+ * infinities become +-448, NaN stays NaN.
+ * A scene with len[b] + R > capacity is left untouched and sets
+ * SD_DEVERR_KV_OVERFLOW. sd_kv_rollback rolls the length back; a block's scale
+ * stays what it was until the block begins anew.
+ */
+sd_status sd_kv8_append(const sd_kv8_cache* cache, const void* k_new, const void* v_new, int R,
+                        sd_stream_t stream);
+
+/*
+ * Store a whole bf16 cache in 8 bits: for every scene b rows 0 .. src->len[b] - 1
+ * as if appended to an empty cache, then cache->len[b] = src->len[b]. The two
+ * caches agree in batch, heads and head dim; their capacities may differ. A scene
+ * whose src->len[b] passes src->capacity sets SD_DEVERR_LENGTH, one that passes
+ * cache->capacity SD_DEVERR_KV_OVERFLOW, and is left untouched.
+ */
+sd_status sd_kv8_store(const sd_kv8_cache* cache, const sd_kv_cache* src, sd_stream_t stream);
+
+/*
+ * Verify attention over an 8-bit cache: sd_verify_attention_ex (the same rows,
+ * masks, q and out) on the keys and values that the codes stand for.
+ * flags: SD_ATTN_BLOCK_MASK; other bits SD_ERR_INVALID_ARG. Needs no workspace.
+ * D in {64, 128}, Hq % Hkv == 0 and G*R <= 128. A scene with len[b] < R or
+ * len[b] > capacity sets SD_DEVERR_LENGTH and its output is left unwritten.
+ */
+sd_status sd_kv8_attention(const void* q, const sd_kv8_cache* cache, void* out, int R, int Hq, float scale,
+                           int flags, sd_stream_t stream);
+
+/*
+ * The attention weight that each cached key gathers from a pass's rows. With
+ * p[b][i][h] the softmax of row i of head h over the keys it sees, as in
+ * sd_verify_attention (the R rows appended, causal mask):
+ *   weights[b][g][n] = decay * weights_in[b][g][n]
+ *                      + sum_{i < committed[b]} sum_{h of KV head g} p[b][i][h][n]
+ * for n < len[b], where a key of this pass (n >= len[b] - R) has no weight from
+ * before; entries from len[b] on are left unwritten.
+ *   q: [B][R][Hq][D] bf16 (rotated), cache: keys appended (v is not read),
+ *   committed: int32 [B] device, rows that count (the accepted ones), in [0, R];
+ *   NULL: all R. weights_in, weights: fp32 [B][Hkv][capacity] device;
+ *   weights_in may be NULL (nothing before) or weights itself; scale as for
+ *   sd_verify_attention.
+ * D in {64, 128}, Hq % Hkv == 0; any R. A scene with len[b] < R or len[b] >
+ * capacity sets SD_DEVERR_LENGTH, one with committed[b] outside [0, R]
+ * SD_DEVERR_ROLLBACK; both are left unwritten.
+ */
+sd_status sd_attention_weights(const void* q, const sd_kv_cache* cache, int R, int Hq, float scale,
+                               const int32_t* committed, const float* weights_in, float decay,
+                               float* weights, sd_stream_t stream);
+
+/*
+ * Evict the keys that hold least weight: of scene b's n = src->len[b] keys each
+ * KV head keeps min(n, keep) -- the first `sinks`, the last `recent`, and of
+ * the others those with the largest weights[b][g] (of equal ones the lowest
+ * index; NaN below every number) -- and copies their rows, in their order, to
+ * dst; dst->len[b] = min(n, keep). Keys carry their rotation with them, so an
+ * attention over dst sees the kept keys at their own positions.
+ *   weights: fp32 [B][Hkv][src->capacity] device.
+ *   weights_out: fp32 [B][Hkv][dst->capacity] device or NULL: the kept keys' weights.
+ *   kept: int32 [B][Hkv][keep] device or NULL: their indices in src, then -1.
+ * src and dst agree in batch, heads and head dim, keep <= dst->capacity,
+ * sinks + recent <= keep, and nothing written may overlap what is read. D in
+ * {64, 128}. A scene with n < 0 or n > src->capacity sets SD_DEVERR_LENGTH and
+ * is left unwritten.
+ */
+sd_status sd_kv_evict(const sd_kv_cache* src, const float* weights, int keep, int sinks, int recent,
+                      const sd_kv_cache* dst, float* weights_out, int32_t* kept, sd_stream_t stream);
+
+/*
+ * Log probabilities of given tokens under softmax(z / T), with the entropy of
+ * the rows and their top alternatives.
+ *   logits: `rows` rows of V values of `dtype`, row_stride elements apart (>= V);
+ *   tokens: int32 [rows] device. Token -1 (what the acceptance leaves past
+ *   n_emit) gives logprob 0; any other outside [0, V) gives NaN and sets
+ *   SD_DEVERR_TOKEN_RANGE.
+ * Outputs (device): logprob fp32 [rows]; entropy fp32 [rows] in nats, or NULL;
+ * for top_n > 0 (at most 32 and at most V) top_ids int32 [rows][top_n], the
+ * largest logits in descending order, of equal ones the lowest index first
+ * (+0 == -0), and top_logprobs fp32 [rows][top_n].
+ * A logit of -inf is a token of probability 0. A row of nothing else, or with
+ * +inf or NaN in it, has NaN for its log probabilities and entropy (its ids are
+ * in [0, V)). One pass over the logits, fp32 arithmetic in a fixed order.
+ */
+sd_status sd_token_logprobs(const void* logits, sd_dtype dtype, int rows, int V, long long row_stride,
+                            const int32_t* tokens, float temperature, int top_n, float* logprob,
+                            float* entropy, int32_t* top_ids, float* top_logprobs, sd_stream_t stream);
+
+/*
  * Synchronise `stream`, return the device error bits accumulated on the
  * current device since the last call in *bits, and clear them.
  * Returns SD_OK when no bit is set, SD_ERR_DEVICE when some bit is set

@@ -13,6 +13,9 @@ Driving", arxiv 2606.31160):
   kv.py         KV-cache append and rollback to the committed length (Eq. commit)
   budget.py     per-segment attention mass and normalised entropy of the verify
                 rows (Sec. 4.2, Table tab:attn-budget)
+  kv8.py        the 8-bit KV cache: e4m3 codes with a scale for each block of tokens
+  evict.py      the weight that keys accumulate, and which of them an eviction keeps
+  logprobs.py   log probabilities of given tokens, entropy, top alternatives
 
 Only tests/, __graft_entry__.smoke() and bench.py (its cpu_baseline leg and
 its --impl reference arm) may import it. The CUDA library and its Python
@@ -31,10 +34,14 @@ from .attention import verify_attention
 from .accept import accept_greedy, accept_sample, argmax_lowest
 from .kv import kv_append, kv_rollback
 from .budget import attention_budget
+from .kv8 import dequantise, e4m3_values, kv8_append, round_e4m3
+from .evict import attention_weights, kept_keys
+from .logprobs import token_logprobs
 
 __all__ = [
     "rope_frequencies", "axis_assignment", "mrope_apply", "rope_1d",
     "rope_1d_matrix", "flatrope_positions", "verify_attention",
     "accept_greedy", "accept_sample", "argmax_lowest", "kv_append",
-    "kv_rollback", "attention_budget",
+    "kv_rollback", "attention_budget", "dequantise", "e4m3_values", "kv8_append",
+    "round_e4m3", "attention_weights", "kept_keys", "token_logprobs",
 ]

@@ -31,7 +31,8 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-O2",
               "--expt-relaxed-constexpr", "-I" + INCLUDE] + ARCH
 SOURCES = ["api.cu", "rope.cu", "kv.cu", "attention.cu", "attention_tc.cu", "attention_wide.cu", "layer.cu",
-           "accept_greedy.cu", "accept_sample.cu", "budget.cu"]
+           "accept_greedy.cu", "accept_sample.cu", "budget.cu", "kv8.cu", "attention_kv8.cu", "key_weights.cu", "evict.cu",
+           "logprobs.cu"]
 
 
 def nvcc_path():

@@ -27,7 +27,9 @@ extern "C" sd_status sd_get_device_error(sd_stream_t stream, uint32_t* bits) {
   cudaError_t (*take[])(uint32_t*) = {sd_take_error_rope, sd_take_error_kv,
                                       sd_take_error_attention, sd_take_error_attention_tc, sd_take_error_attention_wide,
                                       sd_take_error_greedy,
-                                      sd_take_error_sample, sd_take_error_budget};
+                                      sd_take_error_sample, sd_take_error_budget, sd_take_error_kv8,
+                                      sd_take_error_attention_kv8, sd_take_error_weights, sd_take_error_evict,
+                                      sd_take_error_logprobs};
   for (auto fn : take) {
     if (fn(bits) != cudaSuccess) {
       (void)cudaGetLastError();

@@ -38,6 +38,13 @@ class KVCacheStruct(ctypes.Structure):
                 ("capacity", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
+class KV8CacheStruct(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("len", ctypes.c_void_p), ("ticket", ctypes.c_void_p),
+                ("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("capacity", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32)]
+
+
 _lib = None
 
 _vp, _i, _f, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
@@ -65,6 +72,12 @@ _SIGNATURES = {
     "sd_verify_kernel": ([_i, _i, _i, _i, _i, _i, _i], ctypes.c_char_p),
     "sd_verify_cluster_size": ([_i, _i, _i, _i, _i, _i, _i], _i),
     "sd_attention_budget": ([_vp, ctypes.POINTER(KVCacheStruct), _i, _i, _f, _vp, _vp, _vp, _vp], _i),
+    "sd_kv8_append": ([ctypes.POINTER(KV8CacheStruct), _vp, _vp, _i, _vp], _i),
+    "sd_kv8_store": ([ctypes.POINTER(KV8CacheStruct), ctypes.POINTER(KVCacheStruct), _vp], _i),
+    "sd_kv8_attention": ([_vp, ctypes.POINTER(KV8CacheStruct), _vp, _i, _i, _f, _i, _vp], _i),
+    "sd_attention_weights": ([_vp, ctypes.POINTER(KVCacheStruct), _i, _i, _f, _vp, _vp, _f, _vp, _vp], _i),
+    "sd_kv_evict": ([ctypes.POINTER(KVCacheStruct), _vp, _i, _i, _i, ctypes.POINTER(KVCacheStruct), _vp, _vp, _vp], _i),
+    "sd_token_logprobs": ([_vp, _i, _i, _i, ctypes.c_longlong, _vp, _f, _i, _vp, _vp, _vp, _vp, _vp], _i),
 }
 
 
@@ -314,6 +327,182 @@ def verify_layer(q, k_new, v_new, pos, sections, cache, interleaved=0, base=1e6,
                                  (SD_LAYER_PREFIX_EARLY if early else 0) | (SD_LAYER_BLOCK_MASK if block else 0),
                                  _stream()), "sd_verify_layer")
     return out
+
+
+# ----------------------------------------------------------- 8-bit KV cache
+
+class KV8Cache:
+    """One layer's 8-bit KV cache: e4m3 codes [B, Hkv, cap, D] (torch.float8_e4m3fn), fp32
+    scales [B, Hkv, ceil(cap / block)] and device lengths [B]; value = code * scale of the
+    row's block."""
+
+    def __init__(self, k, v, k_scale, v_scale, lens, block=64):
+        if k.shape != v.shape or k.dim() != 4:
+            raise ValueError("k and v must both be [B, Hkv, cap, D]")
+        B, H, cap, D = k.shape
+        block = int(block)
+        if block <= 0:
+            raise ValueError("block must be positive")
+        want = (B, H, -(-cap // block))
+        if tuple(k_scale.shape) != want or tuple(v_scale.shape) != want or tuple(lens.shape) != (B,):
+            raise ValueError("scales must be %s and len (%d,)" % (want, B))
+        for t, name in ((k, "k"), (v, "v")):
+            _dev(t, name, torch.float8_e4m3fn)
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            _dev(t, name, torch.float32)
+        _dev(lens, "len", torch.int32)
+        _same_device(k, v, k_scale, v_scale, lens)
+        self.k, self.v, self.k_scale, self.v_scale, self.len, self.block = k, v, k_scale, v_scale, lens, block
+        self._ticket = torch.zeros(max(B, 1), dtype=torch.int32, device=k.device)
+        self._struct = KV8CacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                                      lens.data_ptr(), self._ticket.data_ptr(), B, H, cap, D, block)
+        self._ref, self._shape = ctypes.byref(self._struct), (B, H, cap, D)
+
+    @classmethod
+    def empty(cls, B, Hkv, cap, D, block=64, device="cuda"):
+        k = torch.zeros((B, Hkv, cap, D), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+        s = torch.ones((B, Hkv, -(-cap // block)), dtype=torch.float32, device=device)
+        return cls(k, torch.zeros_like(k), s, s.clone(), torch.zeros(B, dtype=torch.int32, device=device), block)
+
+    @property
+    def struct(self):
+        return self._ref
+
+    @property
+    def shape(self):
+        return self._shape
+
+
+def _same_device(*tensors):
+    for t in tensors[1:]:
+        if t.device != tensors[0].device:
+            raise ValueError("all tensors must be on one device")
+
+
+def kv8_append(cache, k_new, v_new):
+    """Quantise and write k_new / v_new [B,R,Hkv,D] bf16 at len[b] .. len[b]+R-1; len += R."""
+    B, H, _, D = cache.shape
+    R = k_new.shape[1]
+    if tuple(k_new.shape) != (B, R, H, D) or k_new.shape != v_new.shape:
+        raise ValueError("shape mismatch")
+    _check(lib().sd_kv8_append(cache.struct, _dev(k_new, "k_new", torch.bfloat16), _dev(v_new, "v_new", torch.bfloat16),
+                               R, _stream()), "sd_kv8_append")
+
+
+def kv8_store(cache, src):
+    """Quantise a whole bf16 KVCache into the 8-bit cache, its lengths included."""
+    if (cache.shape[0], cache.shape[1], cache.shape[3]) != (src.shape[0], src.shape[1], src.shape[3]):
+        raise ValueError("the caches disagree")
+    _check(lib().sd_kv8_store(cache.struct, src.struct, _stream()), "sd_kv8_store")
+
+
+def kv8_attention(q, cache, out=None, scale=0.0, block=False):
+    """Verify attention of q [B,R,Hq,D] bf16 (rotated) over an 8-bit cache (rows appended):
+    verify_attention on the keys and values that the codes stand for. block=True selects
+    the block mask."""
+    B, R, Hq, D = q.shape
+    if cache.shape[0] != B or cache.shape[3] != D:
+        raise ValueError("q and cache disagree")
+    if out is None:
+        out = torch.empty_like(q)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    _check(lib().sd_kv8_attention(_dev(q, "q", torch.bfloat16), cache.struct, _dev(out, "out", torch.bfloat16), R, Hq,
+                                  float(scale), SD_ATTN_BLOCK_MASK if block else 0, _stream()), "sd_kv8_attention")
+    return out
+
+
+# ------------------------------------------------------ weights and eviction
+
+def attention_weights(q, cache, weights_in=None, weights=None, decay=1.0, committed=None, scale=0.0):
+    """The attention weight that each cached key gathers from the rows q [B,R,Hq,D] (keys
+    appended): weights = decay * weights_in + the sum over the committed rows and the KV
+    head's query heads, fp32 [B,Hkv,cap]. committed: int32 [B] rows that count, or all."""
+    B, R, Hq, D = q.shape
+    _, Hkv, cap, _ = cache.shape
+    if cache.shape[0] != B or cache.shape[3] != D:
+        raise ValueError("q and cache disagree")
+    if weights is None:
+        weights = torch.zeros((B, Hkv, cap), dtype=torch.float32, device=q.device)
+    if tuple(weights.shape) != (B, Hkv, cap) or (weights_in is not None and weights_in.shape != weights.shape):
+        raise ValueError("weights must be [B, Hkv, cap]")
+    if committed is not None and tuple(committed.shape) != (B,):
+        raise ValueError("committed must be [B]")
+    _check(lib().sd_attention_weights(_dev(q, "q", torch.bfloat16), cache.struct, R, Hq, float(scale),
+                                      None if committed is None else _dev(committed, "committed", torch.int32),
+                                      None if weights_in is None else _dev(weights_in, "weights_in", torch.float32),
+                                      float(decay), _dev(weights, "weights", torch.float32), _stream()),
+           "sd_attention_weights")
+    return weights
+
+
+def kv_evict(src, weights, dst, keep, sinks=0, recent=0, weights_out=None, kept=None):
+    """Copy to dst the min(len, keep) keys of each KV head of src that hold the most weight
+    (fp32 [B,Hkv,cap]), the first `sinks` and the last `recent` among them, in their order.
+    weights_out [B,Hkv,dst cap] takes their weights, kept [B,Hkv,keep] int32 their indices."""
+    B, Hkv, cap, D = src.shape
+    keep = int(keep)
+    if (dst.shape[0], dst.shape[1], dst.shape[3]) != (B, Hkv, D):
+        raise ValueError("the caches disagree")
+    if tuple(weights.shape) != (B, Hkv, cap):
+        raise ValueError("weights must be [B, Hkv, cap]")
+    if weights_out is not None and tuple(weights_out.shape) != (B, Hkv, dst.shape[2]):
+        raise ValueError("weights_out must be [B, Hkv, cap of dst]")
+    if kept is not None and tuple(kept.shape) != (B, Hkv, keep):
+        raise ValueError("kept must be [B, Hkv, keep]")
+    _check(lib().sd_kv_evict(src.struct, _dev(weights, "weights", torch.float32), keep, int(sinks), int(recent), dst.struct,
+                             None if weights_out is None else _dev(weights_out, "weights_out", torch.float32),
+                             None if kept is None else _dev(kept, "kept", torch.int32), _stream()), "sd_kv_evict")
+
+
+# ------------------------------------------------------------ log probabilities
+
+def token_logprobs(logits, tokens, temperature=1.0, top_n=0, logprob=None, entropy=None, top_ids=None, top_logprobs=None):
+    """Log probabilities of tokens [...] int32 under softmax(logits [..., V] / temperature)
+    (bf16 or fp32), the rows' entropies (nats) and their top_n alternatives. A token -1
+    gives 0. Returns (logprob [...], entropy [...], top_ids [..., top_n] int32,
+    top_logprobs [..., top_n])."""
+    V, lead = logits.shape[-1], tuple(logits.shape[:-1])
+    dt = {torch.bfloat16: SD_BF16, torch.float32: SD_F32}.get(logits.dtype)
+    if dt is None:
+        raise ValueError("logits must be bf16 or fp32")
+    if tuple(tokens.shape) != lead:
+        raise ValueError("tokens must be %s" % (lead,))
+    top_n, dev, rows = int(top_n), logits.device, tokens.numel()
+    if logits.is_contiguous():
+        ptr, stride = _dev(logits, "logits"), V
+    else:
+        ptr, stride = _padded_rows(logits, rows)
+    logprob = torch.empty(lead, dtype=torch.float32, device=dev) if logprob is None else logprob
+    entropy = torch.empty(lead, dtype=torch.float32, device=dev) if entropy is None else entropy
+    if tuple(logprob.shape) != lead or tuple(entropy.shape) != lead:
+        raise ValueError("logprob and entropy must be %s" % (lead,))
+    top_ids = torch.empty(lead + (max(top_n, 0),), dtype=torch.int32, device=dev) if top_ids is None else top_ids
+    top_logprobs = torch.empty(lead + (max(top_n, 0),), dtype=torch.float32, device=dev) if top_logprobs is None else top_logprobs
+    if tuple(top_ids.shape) != lead + (top_n,) or tuple(top_logprobs.shape) != lead + (top_n,):
+        raise ValueError("top_ids and top_logprobs must be %s" % (lead + (top_n,),))
+    _check(lib().sd_token_logprobs(ptr, dt, rows, V, stride, _dev(tokens, "tokens", torch.int32), float(temperature), top_n,
+                                   _dev(logprob, "logprob", torch.float32), _dev(entropy, "entropy", torch.float32),
+                                   _dev(top_ids, "top_ids", torch.int32),
+                                   _dev(top_logprobs, "top_logprobs", torch.float32), _stream()), "sd_token_logprobs")
+    return logprob, entropy, top_ids, top_logprobs
+
+
+def _padded_rows(logits, rows):
+    """Address and row stride of logits whose rows are contiguous and evenly spaced (a
+    padded vocabulary)."""
+    if not logits.is_cuda:
+        raise ValueError("logits must be on a CUDA device (no CPU path exists)")
+    lead, strides = logits.shape[:-1], logits.stride()
+    step = next((s for n, s in zip(reversed(lead), reversed(strides[:-1])) if n > 1), logits.shape[-1])
+    want = step
+    for n, s in zip(reversed(lead), reversed(strides[:-1])):
+        if n > 1 and s != want:
+            raise ValueError("logits' rows must be evenly spaced")
+        want *= n
+    if (logits.shape[-1] > 1 and strides[-1] != 1) or step < logits.shape[-1]:
+        raise ValueError("logits' rows must be contiguous")
+    return logits.data_ptr(), step
 
 
 # -------------------------------------------------------------- acceptance

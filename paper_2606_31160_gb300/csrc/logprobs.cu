@@ -1,11 +1,23 @@
 // Log probabilities of given tokens with the entropy and the top alternatives of their
-// rows (sm_103a). With x = (z - max z) / T over a row's vocabulary, S = sum e^x and
-// W = sum x e^x:
+// rows (sm_103a). With x = (z - m) / T, m the row's largest logit, S = sum e^x and
+// W = sum x e^x over the vocabulary:
 //     log p(t) = x_t - ln S,    entropy = ln S - W / S,
 //     alternatives: the top_n largest logits, equal ones by the lowest index.
 //
-// The plainest form: a CTA a row; the alternatives one by one, each the largest below
-// the one before it.
+// One pass over the logits. A cluster of CTAs has a row, each a contiguous segment; a
+// thread folds 4 chunks of 16 bytes at a time into (m, S, W) under its running maximum,
+// which it moves only when a chunk's maximum passes it. S and W merge over lanes, warps
+// and CTAs in a fixed order.
+//
+// Alternatives without a second pass: the threads' maxima are kept anyway, and every
+// warp's j-th largest of them, j = ceil(top_n / warps), gives a bound that at least
+// top_n elements of the segment reach, and few more do (the least of 16 warps' maxima
+// leaves about 50). Only threads whose maximum reaches the bound hold such elements:
+// their warps read those threads' chunks again, a chunk a lane, and list what reaches
+// it. A list is ranked by counting; the cluster's first CTA ranks the CTAs' lists. A
+// bound of -inf (a masked vocabulary) lists the finite logits only, the lowest masked
+// indices fill the rest; a list that overflows (thousands of equal logits) is replaced
+// by top_n passes for the next largest.
 #include "common.cuh"
 
 #include <math.h>
@@ -14,71 +26,402 @@ SD_DEFINE_ERROR_ACCESSOR(sd_take_error_logprobs)
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+constexpr int kTopMax = 32;
+constexpr int kList = 1024;      // candidates a CTA lists
+constexpr int kUnroll = 4;       // 16-byte chunks a thread has in flight
+constexpr int kMaxCluster = 8;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 
-// (value, lowest index first) as one integer that orders descending preference upward.
-__device__ __forceinline__ uint64_t key_of(float z, int i) {
+// An integer that orders as the logit does (-0 as +0).
+__device__ __forceinline__ uint32_t order_of(float z) {
   const uint32_t u = __float_as_uint(z + 0.f);
-  const uint32_t o = u & 0x80000000u ? ~u : u | 0x80000000u;
-  return (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~i);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
+constexpr uint32_t kOrderNegInf = 0x007fffffu;  // order_of(-inf)
+// (value, lowest index first) as one integer
+__device__ __forceinline__ uint64_t key_of(float z, int i) {
+  return (static_cast<uint64_t>(order_of(z)) << 32) | static_cast<uint32_t>(~i);
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float redux_max(float x) {
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ uint4 load16(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+// Address of the same shared variable in the cluster's CTA 0.
+__device__ __forceinline__ uint32_t in_first_cta(const void* p) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_addr(p)));
+  return r;
 }
 
 template <bool kBf16>
-__device__ __forceinline__ float load(const void* z, long long i) {
-  return kBf16 ? sd_ldcg_bf16(static_cast<const __nv_bfloat16*>(z) + i) : __ldcg(static_cast<const float*>(z) + i);
+struct Type {
+  static constexpr int kPer = kBf16 ? 8 : 4;  // logits a chunk
+  static __device__ __forceinline__ void unpack(const uint4& c, float (&z)[kPer]) {
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (kBf16) {
+        z[2 * j] = sd_bf16_lo(w[j]);
+        z[2 * j + 1] = sd_bf16_hi(w[j]);
+      } else {
+        z[j] = __uint_as_float(w[j]);
+      }
+    }
+  }
+  static __device__ __forceinline__ float load(const void* z, long long i) {
+    return kBf16 ? sd_ldcg_bf16(static_cast<const __nv_bfloat16*>(z) + i) : __ldcg(static_cast<const float*>(z) + i);
+  }
+};
+
+// Sums relative to a maximum m, x in units of log 2: S = sum 2^x, W = sum x 2^x.
+struct Stat {
+  float m, S, W;
+};
+// s moved to the maximum M >= s.m (c = log2(e) / T). Nothing seen: m = -inf, and S is 0 or NaN.
+__device__ __forceinline__ void move_to(Stat& s, float M, float c) {
+  if (s.m == M) return;
+  if (s.m == -INFINITY) {
+    s.S *= 0.f;
+    s.W = s.S;
+  } else {
+    const float d = (s.m - M) * c, f = ex2(d);
+    s.W = f * fmaf(d, s.S, s.W);
+    s.S *= f;
+  }
+  s.m = M;
 }
 
+template <bool kBf16, int kN>
+__device__ __forceinline__ void fold(Stat& s, const float (&z)[kN], float c) {
+  float bm = z[0];
+#pragma unroll
+  for (int j = 1; j < kN; ++j) bm = max_nan(bm, z[j]);
+  if (bm == -INFINITY) return;  // nothing but tokens of probability 0
+  if (bm > s.m) move_to(s, bm, c);
+#pragma unroll
+  for (int j = 0; j < kN; ++j) {
+    const float x = max_nan((z[j] - s.m) * c, -1000.f);  // -inf: 0 * -1000, not 0 * -inf
+    const float e = ex2(x);
+    s.S += e;
+    s.W = fmaf(e, x, s.W);
+  }
+}
+
+// Grid (cluster size, rows).
 template <bool kBf16>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(const void* z, long long stride, int V, const int32_t* tokens,
-                                                            float inv_t, int top_n, float* logprob, float* entropy,
-                                                            int32_t* top_ids, float* top_logprobs) {
+__global__ void __launch_bounds__(kThreads, 2)
+    logprobs_kernel(const void* logits, long long stride, int V, const int32_t* tokens, float inv_t, int top_n,
+                    float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs) {
+  using T = Type<kBf16>;
+  constexpr int kPer = T::kPer, kElem = kBf16 ? 2 : 4;
+  __shared__ uint64_t list[kList];
+  __shared__ uint64_t best[kMaxCluster][kTopMax];  // [0]: this CTA's; the first CTA's: every rank's
+  __shared__ Stat stat[kWarps];
+  __shared__ Stat cta_stat[kMaxCluster];
+  __shared__ uint32_t warp_bound[kWarps];
+  __shared__ int n_list;
+  const int csize = gridDim.x, rank = blockIdx.x;
+  if (csize > 1) cluster_arrive();  // waited for before the first store into another CTA
   sd_pdl_enter();
-  __shared__ double reds[kThreads], redw[kThreads];
-  __shared__ uint64_t redk[kThreads];
-  const long long row = blockIdx.x, base = row * stride;
-  const int t = threadIdx.x;
-  auto best_below = [&](uint64_t limit) {
-    uint64_t k = 0;
-    for (int i = t; i < V; i += kThreads) {
-      const uint64_t x = key_of(load<kBf16>(z, base + i), i);
-      if (x < limit && x > k) k = x;
+  const long long row = blockIdx.y;
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  const char* z0 = static_cast<const char*>(logits) + row * stride * kElem;
+  const float c = inv_t * kLog2e;
+  if (t == 0) n_list = 0;
+  // the token's logit travels with the rest
+  int tok = -1;
+  float z_tok = 0.f;
+  if (rank == 0 && t == 0) {
+    tok = __ldcg(tokens + row);
+    if (tok >= 0 && tok < V) z_tok = T::load(z0, tok);
+  }
+  // whole chunks of the row: [lead, lead + n_vec * kPer); the ends are single elements
+  const int lead = min(V, static_cast<int>(((16 - (reinterpret_cast<uintptr_t>(z0) & 15)) & 15) / kElem));
+  const int n_vec = (V - lead) / kPer;
+  const int tail = lead + n_vec * kPer;
+  const uint4* vec = reinterpret_cast<const uint4*>(z0 + static_cast<long long>(lead) * kElem);
+  const int v_lo = static_cast<int>(static_cast<long long>(rank) * n_vec / csize);
+  const int v_hi = static_cast<int>(static_cast<long long>(rank + 1) * n_vec / csize);
+  // single elements: thread t < lead of the first CTA, the next ones the tail's
+  int edge = -1;
+  if (rank == 0) edge = t < lead ? t : (t - lead < V - tail ? tail + t - lead : -1);
+
+  Stat s{-INFINITY, 0.f, 0.f};
+  {
+    int v = v_lo + t;
+    for (; v + (kUnroll - 1) * kThreads < v_hi; v += kUnroll * kThreads) {
+      uint4 r[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) r[u] = load16(vec + v + u * kThreads);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        float z[kPer];
+        T::unpack(r[u], z);
+        fold<kBf16>(s, z, c);
+      }
+    }
+    uint4 r[kUnroll - 1];
+#pragma unroll
+    for (int u = 0; u < kUnroll - 1; ++u)
+      if (v + u * kThreads < v_hi) r[u] = load16(vec + v + u * kThreads);
+#pragma unroll
+    for (int u = 0; u < kUnroll - 1; ++u)
+      if (v + u * kThreads < v_hi) {
+        float z[kPer];
+        T::unpack(r[u], z);
+        fold<kBf16>(s, z, c);
+      }
+  }
+  float z_edge = -INFINITY;
+  if (edge >= 0) {
+    z_edge = T::load(z0, edge);
+    float z[1] = {z_edge};
+    fold<kBf16>(s, z, c);
+  }
+  const float mine = s.m;  // this thread's largest
+
+  // ---- (m, S, W) over the warp, the CTA and the cluster
+  {
+    const float M = redux_max(s.m);
+    move_to(s, M, c);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      s.S += __shfl_xor_sync(0xffffffffu, s.S, o);
+      s.W += __shfl_xor_sync(0xffffffffu, s.W, o);
+    }
+    if (lane == 0) stat[warp] = s;
+  }
+  if (top_n > 0) {
+    // the warp's j-th largest of its threads' maxima
+    uint32_t o = order_of(mine), bound = 0;
+    for (int j = (top_n + kWarps - 1) / kWarps; j > 0; --j) {
+      bound = __reduce_max_sync(0xffffffffu, o);
+      const uint32_t who = __ballot_sync(0xffffffffu, o == bound);
+      if (lane == __ffs(who) - 1) o = 0;
+    }
+    if (lane == 0) warp_bound[warp] = bound;
+  }
+  __syncthreads();
+  if (csize > 1) cluster_wait();  // every CTA of the cluster has started
+  if (warp == 0) {
+    Stat a = lane < kWarps ? stat[lane] : Stat{-INFINITY, 0.f, 0.f};
+    move_to(a, redux_max(a.m), c);
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) {
+      a.S += __shfl_xor_sync(0xffffffffu, a.S, o);
+      a.W += __shfl_xor_sync(0xffffffffu, a.W, o);
+    }
+    if (lane == 0) {
+      const uint32_t to = in_first_cta(&cta_stat[rank]);
+      if (csize == 1) {
+        cta_stat[0] = a;
+      } else {
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(a.m) : "memory");
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4), "f"(a.S) : "memory");
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 8), "f"(a.W) : "memory");
+      }
+    }
+  }
+  if (top_n > 0) {
+    uint32_t bound = 0xffffffffu;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) bound = min(bound, warp_bound[w]);
+    bound = max(bound, kOrderNegInf + 1);  // finite logits only
+    auto offer = [&](float z, int i) {
+      if (order_of(z) >= bound) {
+        const int at = atomicAdd(&n_list, 1);
+        if (at < kList) list[at] = key_of(z, i);
+      }
+    };
+    if (edge >= 0) offer(z_edge, edge);
+    uint32_t who = __ballot_sync(0xffffffffu, order_of(mine) >= bound);
+    while (who) {
+      const int first = v_lo + warp * 32 + __ffs(who) - 1;
+      who &= who - 1;
+      for (int v = first + lane * kThreads; v < v_hi; v += 32 * kThreads) {
+        float z[kPer];
+        T::unpack(__ldcg(vec + v), z);
+        const int i = lead + v * kPer;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) offer(z[j], i + j);
+      }
     }
     __syncthreads();
-    redk[t] = k;
-    __syncthreads();
-    for (int w = 0; w < kThreads; ++w) k = max(k, redk[w]);
-    return k;
-  };
-  uint64_t k = best_below(~0ull);
-  const float m = load<kBf16>(z, base + static_cast<int>(~static_cast<uint32_t>(k)));
-  double S = 0, W = 0;
-  for (int i = t; i < V; i += kThreads) {
-    const float x = (load<kBf16>(z, base + i) - m) * inv_t, e = expf(x);
-    S += e;
-    W += e > 0.f ? e * x : 0.f;
+    int n = n_list;
+    uint64_t* mine_best = best[0];
+    uint64_t got = 0;  // thread j < top_n: the list's j-th largest, 0 past its end
+    if (n <= kList) {
+      // rank by counting
+      __shared__ uint64_t sorted[kTopMax];
+      if (t < kTopMax) sorted[t] = 0;
+      __syncthreads();
+      for (int i = t; i < n; i += kThreads) {
+        const uint64_t k = list[i];
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += list[j] > k;
+        if (above < top_n) sorted[above] = k;
+      }
+      __syncthreads();
+      if (t < top_n) got = sorted[t];
+    } else {
+      // too many equals: the next largest, one by one
+      __shared__ uint64_t part[kWarps];
+      uint64_t limit = ~0ull;
+      for (int j = 0; j < top_n; ++j) {
+        uint64_t k = 0;
+        auto look = [&](float z, int i) {
+          const uint64_t x = key_of(z, i);
+          if (x < limit && x > k) k = x;
+        };
+        if (edge >= 0) look(z_edge, edge);
+        for (int v = v_lo + t; v < v_hi; v += kThreads) {
+          float z[kPer];
+          T::unpack(__ldcg(vec + v), z);
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) look(z[e], lead + v * kPer + e);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, o));
+        __syncthreads();
+        if (lane == 0) part[warp] = k;
+        __syncthreads();
+        for (int w = 0; w < kWarps; ++w) k = max(k, part[w]);
+        limit = k;
+        if (t == j) got = k;
+      }
+    }
+    if (t < top_n) {
+      if (csize == 1) {
+        mine_best[t] = got;
+      } else {
+        const uint32_t to = in_first_cta(&best[rank][t]);
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to), "l"(got) : "memory");
+      }
+    }
   }
-  reds[t] = S;
-  redw[t] = W;
-  __syncthreads();
-  S = W = 0;
-  for (int w = 0; w < kThreads; ++w) S += reds[w], W += redw[w];
-  const double ln = m == -INFINITY ? NAN : log(S);
+  if (csize > 1) {
+    cluster_arrive();
+    cluster_wait();
+    if (rank != 0) return;
+  } else {
+    __syncthreads();
+  }
+  // ---- the first CTA: the row's statistics
+  float m, ln, W_over_S;
+  {
+    Stat a = lane < csize ? cta_stat[lane] : Stat{-INFINITY, 0.f, 0.f};
+    m = redux_max(a.m);
+    move_to(a, m, c);
+#pragma unroll
+    for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
+      a.S += __shfl_xor_sync(0xffffffffu, a.S, o);
+      a.W += __shfl_xor_sync(0xffffffffu, a.W, o);
+    }
+    a.S = __shfl_sync(0xffffffffu, a.S, 0);
+    a.W = __shfl_sync(0xffffffffu, a.W, 0);
+    ln = m == -INFINITY ? __uint_as_float(0x7fc00000u) : logf(a.S);
+    W_over_S = a.W * kLn2 / a.S;
+  }
   if (t == 0) {
-    if (entropy) entropy[row] = static_cast<float>(ln - W / S);
-    const int tok = __ldcg(tokens + row);
+    if (entropy) entropy[row] = ln - W_over_S;
     float lp = 0.f;
-    if (tok >= 0 && tok < V) lp = static_cast<float>((load<kBf16>(z, base + tok) - m) * inv_t - ln);
-    else if (tok != -1) sd_set_error(SD_DEVERR_TOKEN_RANGE), lp = NAN;
+    if (tok >= 0 && tok < V) {
+      lp = (z_tok - m) * inv_t - ln;
+    } else if (tok != -1) {
+      sd_set_error(SD_DEVERR_TOKEN_RANGE);
+      lp = __uint_as_float(0x7fc00000u);
+    }
     logprob[row] = lp;
   }
-  for (int j = 0; j < top_n; ++j) {
-    if (j > 0) k = best_below(k);
-    if (t == 0) {
-      const int i = static_cast<int>(~static_cast<uint32_t>(k));
-      top_ids[row * top_n + j] = i;
-      top_logprobs[row * top_n + j] = static_cast<float>((load<kBf16>(z, base + i) - m) * inv_t - ln);
+  if (top_n == 0) return;
+  // ---- its alternatives: rank by counting over the CTAs' sorted lists
+  __shared__ int n_found;
+  if (t == 0) n_found = 0;
+  __syncthreads();
+  auto write = [&](int at, float z, int i) {
+    top_ids[row * top_n + at] = i;
+    top_logprobs[row * top_n + at] = (z - m) * inv_t - ln;
+  };
+  if (t < csize * top_n) {
+    const int r = t / top_n, j = t - r * top_n;
+    const uint64_t k = best[r][j];
+    if (k) {
+      int above = j;
+      for (int q = 0; q < csize; ++q)
+        if (q != r)
+          for (int e = 0; e < top_n && best[q][e] > k; ++e) ++above;
+      if (above < top_n) {
+        write(above, value_of(static_cast<uint32_t>(k >> 32)), static_cast<int>(~static_cast<uint32_t>(k)));
+        atomicAdd(&n_found, 1);
+      }
     }
   }
+  __syncthreads();
+  if (warp == 0 && n_found < top_n) {
+    // tokens of probability 0, the lowest indices first (a row with NaN in it may have too
+    // few of both: any index then)
+    int at = n_found;
+    for (int i0 = 0; i0 < V && at < top_n; i0 += 32) {
+      const int i = i0 + lane;
+      const bool is = i < V && T::load(z0, i) == -INFINITY;
+      const uint32_t all = __ballot_sync(0xffffffffu, is);
+      const int place = at + __popc(all & ((1u << lane) - 1));
+      if (is && place < top_n) write(place, -INFINITY, i);
+      at += __popc(all);
+    }
+    if (lane >= at && lane < top_n) write(lane, __uint_as_float(0x7fc00000u), lane);
+  }
+}
+
+// CTAs a row: enough for two an SM over all rows, as long as each keeps 32 KB of the row
+// or so (at least one batch of chunks a thread).
+int cluster_size(int rows, long long row_bytes) {
+  int s = 1;
+  while (s < kMaxCluster && static_cast<long long>(rows) * s * 2 <= 2LL * sd_num_sms() && row_bytes / (2 * s) >= 16384) s *= 2;
+  return s;
+}
+
+template <bool kBf16>
+cudaError_t launch(cudaStream_t st, int S, const void* logits, int rows, long long stride, int V, const int32_t* tokens,
+                   float inv_t, int top_n, float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = S;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(S, rows);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, logprobs_kernel<kBf16>, logits, stride, V, tokens, inv_t, top_n, logprob, entropy,
+                            top_ids, top_logprobs);
 }
 
 }  // namespace
@@ -90,15 +433,25 @@ extern "C" sd_status sd_token_logprobs(const void* logits, sd_dtype dtype, int r
   if (dtype != SD_BF16 && dtype != SD_F32) return SD_ERR_INVALID_ARG;
   if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature)) return SD_ERR_INVALID_ARG;
   if (top_n < 0 || top_n > V) return SD_ERR_INVALID_ARG;
-  if (top_n > 32) return SD_ERR_UNSUPPORTED;
+  if (top_n > kTopMax) return SD_ERR_UNSUPPORTED;
+  if (V > (1 << 30)) return SD_ERR_UNSUPPORTED;
   if (rows == 0) return SD_OK;
   if (!logits || !tokens || !logprob || (top_n > 0 && (!top_ids || !top_logprobs))) return SD_ERR_INVALID_ARG;
   if (!sd_aligned16(logits)) return SD_ERR_INVALID_ARG;
-  if (sd_launch_pdl(dtype == SD_BF16 ? logprobs_kernel<true> : logprobs_kernel<false>, dim3(rows), dim3(kThreads), 0,
-                    reinterpret_cast<cudaStream_t>(stream), logits, row_stride, V, tokens, 1.f / temperature, top_n,
-                    logprob, entropy, top_ids, top_logprobs) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return SD_ERR_CUDA;
+  const int elem = dtype == SD_BF16 ? 2 : 4;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  for (int r0 = 0; r0 < rows; r0 += 65535) {  // a grid's second dimension ends at 65535
+    const int n = rows - r0 < 65535 ? rows - r0 : 65535;
+    const int S = cluster_size(n, static_cast<long long>(V) * elem);
+    const char* z = static_cast<const char*>(logits) + static_cast<long long>(r0) * row_stride * elem;
+    const long long o = static_cast<long long>(r0) * top_n;
+    const cudaError_t e = (dtype == SD_BF16 ? launch<true> : launch<false>)(
+        st, S, z, n, row_stride, V, tokens + r0, 1.f / temperature, top_n, logprob + r0, entropy ? entropy + r0 : nullptr,
+        top_ids ? top_ids + o : nullptr, top_logprobs ? top_logprobs + o : nullptr);
+    if (e != cudaSuccess) {
+      (void)cudaGetLastError();
+      return SD_ERR_CUDA;
+    }
   }
   return SD_OK;
 }

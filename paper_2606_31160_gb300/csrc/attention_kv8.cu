@@ -1,76 +1,830 @@
-// Verify attention over the 8-bit KV cache (sm_103a): the rows, masks and results of
-// the bf16 verify attention, with key n = k_code[n] * k_scale[n / block] and value
-// n = v_code[n] * v_scale[n / block].
+// Verify attention over the 8-bit KV cache on the 5th-generation tensor cores (sm_103a):
+// the rows, masks and results of the bf16 verify attention, with key n = k_code[n] *
+// k_scale[n / block] and value n = v_code[n] * v_scale[n / block].
 //
-// The plainest form: a warp a query row, its lanes over the head dim, one pass over the
-// row's keys with the running maximum and sum of its softmax.
-#include "common.cuh"
+// The codes go from HBM to the tensor cores as they are (kind::f8f6f4, e4m3 by e4m3, fp32
+// sums): nothing widens a key or a value. What meets them has 8 significant bits and an
+// e4m3 number 4, so queries and weights go in as two terms each, x = hi + lo with hi =
+// e4m3(x) and lo = e4m3(x - hi), both products into the same sum:
+//   * a query row, scaled by the power of two that brings its largest element into [128,
+//     256), is exact in two terms (bf16 has 8 bits; elements below 2^-10 of the largest
+//     to 2^-18 of it);
+//   * a weight keeps 8 bits, as a bf16 one would, down to 2^-12 of its row's largest, and
+//     below that is off by 2^-17 of it at most.
+// The packed query rows of a KV head (G * R) are few, so both products run transposed,
+//     S^T[128 keys][kR rows] = K_tile . Q^T,   O^T[128 d][kR rows] += V_tile^T . P^T
+// with kR = 32 or 64 and, above 64 rows, two m-blocks. Scales enter between the two: a
+// thread has one key, t = S * k_scale * c, and
+//     P = 2^(t * qscale[row] + log2 v_scale - ref[row]),   l[row] += P / v_scale,
+// so O / l is the attention whatever the scales are.
+//
+// Reference. P has to stay within e4m3's 448, so ref[row] is 2^6 below the largest weight
+// that the first tile shows, and moves when a later one would pass 2^8.75: every thread
+// compares its largest exponent and the group votes once a tile (an OR in its barrier).
+// Moving takes the tile's exact row maxima (redux over the lanes), and rescales l and O
+// in tensor memory.
+//
+// Warps (608 threads): 0 the TMA producer; 1 issues S and owns tensor memory; 2 issues
+// PV; 3..18 two softmax groups of eight, which take alternate tiles. The groups are two
+// independent softmaxes (own references, own O in tensor memory, own P buffer), joined
+// at the end: neither waits for the other's references. One cluster per (scene, KV head,
+// m-block); its CTAs take contiguous ranges of the keys and merge their partials through
+// distributed shared memory.
+#include "tc_common.cuh"
 
 #include <math.h>
+
+#include <atomic>
 
 SD_DEFINE_ERROR_ACCESSOR(sd_take_error_attention_kv8)
 
 namespace {
 
-__device__ __forceinline__ float2 code2(uint32_t w) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(w)));
-  float lo, hi;
-  asm("{\n\t.reg .f16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}"
-      : "=f"(lo), "=f"(hi)
-      : "r"(h));
-  return make_float2(lo, hi);
+constexpr int kTile = 128;               // keys a tile
+constexpr int kStages = 4;               // K slots, V slots and S buffers
+constexpr int kSoftWarps = 16;
+constexpr int kSoftThreads = 32 * kSoftWarps;
+constexpr int kGroupThreads = kSoftThreads / 2;
+constexpr int kFirstSoft = 3;
+constexpr int kSoft0 = 32 * kFirstSoft;
+constexpr int kThreads = kSoft0 + kSoftThreads;
+constexpr float kTop = 6.f;              // log2 of the weight that a reference gives the largest key
+constexpr float kHot = 8.75f;            // log2 of the largest weight a reference may leave (e4m3 ends at 448 = 2^8.81)
+
+struct Args {
+  const __nv_bfloat16* q;
+  __nv_bfloat16* out;
+  const float* ks;
+  const float* vs;
+  const int32_t* len;
+  int R, Hq, Hkv, G, M, cap, nblk, block_shift;
+  int block_mask;
+  float inv_g;       // 1 / G: p / G == int((p + 0.5) / G) exactly for the p < 128 used here
+  float scale_log2;
+};
+
+template <int kR, int kDim>
+struct Cfg {
+  static_assert(kR == 32 || kR == 64, "row tile");
+  static_assert(kDim == 64 || kDim == 128, "head dim");
+  static constexpr int kRpt = kR / 2;             // rows of a softmax thread
+  static constexpr int kKV = kTile * kDim;        // one K (or V) tile
+  static constexpr int kRingV = kStages * kKV;
+  static constexpr int kRing = 2 * kStages * kKV;
+  static constexpr int kQ = kR * kDim;            // one term of the query rows
+  // P^T: MN-major, 32-byte swizzle: 32 rows x 8 keys an atom; the 32-row groups kPGroup apart
+  static constexpr int kPGroup = kTile * 32;
+  static constexpr int kP = kR / 32 * kPGroup;    // one term of a group's weights
+  static constexpr int kOffQ = kRing;             // hi, lo
+  static constexpr int kOffP = kOffQ + 2 * kQ;    // [group][hi, lo]
+  static constexpr int kOffBar = kOffP + 4 * kP;
+  // full_k[4] full_v[4] s_ready[4] s_free[4] pv_done[4] p_full[2] recv tmem_done
+  static constexpr int kNumBars = 5 * kStages + 4;
+  static constexpr int kOffMisc = round_up(kOffBar + kNumBars * 8, 16);
+  static constexpr int kOffRow = kOffMisc + 16;             // [group][kR / 2] {-ref, -ref, qscale, qscale} of row pairs
+  static constexpr int kOffRef = kOffRow + 2 * kR * 8;      // [group][kR] references
+  static constexpr int kOffFac = kOffRef + 2 * kR * 4;      // [group][kR] rescale factors
+  static constexpr int kOffMax = kOffFac + 2 * kR * 4;      // [group][4 lane quarters][kR] tile maxima
+  static constexpr int kOffSum = kOffMax + 8 * kR * 4;      // [kR][8] row sums by group and lane quarter
+  static constexpr int kOffJoin = kOffSum + kR * 32;        // [kR] {weight of O_0, of O_1, 1 / l or l, ref}
+  static constexpr int kSmemBytes = kOffJoin + kR * 16 + 1024;
+  static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
+  static_assert(kOffQ % 1024 == 0 && kOffP % 1024 == 0, "swizzle atoms");
+  static constexpr int kTmemO = 4 * kR;                     // S0..S3 | O_0 | O_1
+  static constexpr int kTmemCols = kR == 32 ? 256 : 512;
+  static constexpr uint64_t kLayout = kDim == 128 ? 2 : 4;  // swizzle of K, V and Q rows: their whole width
+  // a partial row sent to its owner: [O(kDim) | l | ref | 2 pad] fp32
+  static constexpr int kRowF = kDim + 4;
+  static constexpr int kRowBytes = kRowF * 4;
+  // incoming rows in the K ring, this CTA's in the V ring; ceil(n / c) * c < n + 16
+  static_assert((kR + 15) * kRowBytes <= kRingV && kR * kRowBytes <= kRingV, "merge buffers");
+};
+
+// kind::f8f6f4: fp32 sums, A and B e4m3
+constexpr uint32_t idesc8(int M, int N, int a_mn_major, int b_mn_major) {
+  return (1u << 4) | (static_cast<uint32_t>(a_mn_major) << 15) | (static_cast<uint32_t>(b_mn_major) << 16) |
+         (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+__device__ __forceinline__ void umma8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, int accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// 16 fp32 columns of this warp's 32 TMEM lanes from 16 registers
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint64_t pack2f(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void unpack2(uint64_t d, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(d));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float warp_max(float x) {
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
-// Grid (warps of packed rows, Hkv, B).
-template <int D>
-__global__ void __launch_bounds__(128) kv8_attention_kernel(const __nv_bfloat16* q, const uint8_t* kc, const uint8_t* vc,
-                                                            const float* ks, const float* vs, const int32_t* len,
-                                                            __nv_bfloat16* out, int R, int Hq, int Hkv, int cap,
-                                                            int block, int nblk, float scale_log2, bool block_mask) {
-  sd_pdl_enter();
-  constexpr int kPer = D / 32;
-  const int G = Hq / Hkv, lane = threadIdx.x & 31;
-  const int p = blockIdx.x * 4 + (threadIdx.x >> 5), kvh = blockIdx.y, b = blockIdx.z;
-  const int n = __ldcg(len + b);
-  if (n < R || n > cap) {
-    if (threadIdx.x == 0) sd_set_error(SD_DEVERR_LENGTH);
-    return;
-  }
-  if (p >= G * R) return;
-  const int i = p / G, h = kvh * G + (p - i * G);
-  const long long row = ((static_cast<long long>(b) * R + i) * Hq + h) * D + lane * kPer;
-  float qv[kPer], o[kPer];
-  for (int j = 0; j < kPer; ++j) {
-    qv[j] = sd_ldcg_bf16(q + row + j);
-    o[j] = 0.f;
-  }
-  const long long plane = static_cast<long long>(b) * Hkv + kvh;
-  kc += plane * cap * D + lane * kPer;
-  vc += plane * cap * D + lane * kPer;
-  ks += plane * nblk;
-  vs += plane * nblk;
-  const int seen = block_mask ? n : n - R + i + 1;
-  float m = -INFINITY, l = 0.f;
-  for (int t = 0; t < seen; ++t) {
-    float x = 0.f;
-    float v[kPer];
-    for (int j = 0; j < kPer; j += 2) {
-      const float2 kk = code2(__ldcg(reinterpret_cast<const unsigned short*>(kc + static_cast<long long>(t) * D + j)));
-      const float2 vv = code2(__ldcg(reinterpret_cast<const unsigned short*>(vc + static_cast<long long>(t) * D + j)));
-      x = fmaf(qv[j], kk.x, fmaf(qv[j + 1], kk.y, x));
-      v[j] = vv.x;
-      v[j + 1] = vv.y;
+// Two numbers of magnitude up to 448 as two e4m3 terms (by way of fp16, whose 11 bits
+// both terms together do not reach): hi and lo codes in the low 16 bits of each.
+__device__ __forceinline__ void two_terms(float x0, float x1, uint32_t& hi, uint32_t& lo) {
+  asm("{\n\t.reg .b32 f, b, d;\n\t.reg .b16 h, l;\n\t"
+      "cvt.rn.f16x2.f32 f, %3, %2;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 h, f;\n\t"
+      "cvt.rn.f16x2.e4m3x2 b, h;\n\t"
+      "sub.f16x2 d, f, b;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 l, d;\n\t"
+      "cvt.u32.u16 %0, h;\n\tcvt.u32.u16 %1, l;\n\t}"
+      : "=r"(hi), "=r"(lo)
+      : "f"(x0), "f"(x1));
+}
+
+// Sum over the 32 lanes of a warp of each of 8 per-lane values: lane L ends with the sum
+// of value (L >> 2).
+__device__ __forceinline__ float warp_sum8(float (&v)[8], int lane) {
+#pragma unroll
+  for (int n = 8, s = 16; n > 1; n >>= 1, s >>= 1) {
+    const bool hi = (lane & s) != 0;
+#pragma unroll
+    for (int i = 0; i < n / 2; ++i) {
+      const float keep = hi ? v[i + n / 2] : v[i];
+      const float give = hi ? v[i] : v[i + n / 2];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, s);
     }
-    for (int s = 16; s > 0; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
-    x *= __ldcg(ks + t / block) * scale_log2;
-    const float mn = fmaxf(m, x), f = exp2f(m - mn), e = exp2f(x - mn);
-    const float w = e * __ldcg(vs + t / block);
-    l = fmaf(l, f, e);
-    for (int j = 0; j < kPer; ++j) o[j] = fmaf(o[j], f, w * v[j]);
-    m = mn;
   }
-  for (int j = 0; j < kPer; ++j) out[row + j] = __float2bfloat16_rn(o[j] / l);
+  float x = v[0];
+  x += __shfl_xor_sync(0xffffffffu, x, 2);
+  x += __shfl_xor_sync(0xffffffffu, x, 1);
+  return x;
+}
+
+// ------------------------------------------------------------------ kernel
+// Grid: (cluster size, Hkv * m-blocks, B); m-block mb takes packed rows mb * kR ..
+// mb * kR + kR - 1 (packed row p = i * G + g: new row i, query head g of the group).
+template <int kR, int kDim>
+__global__ void __launch_bounds__(kThreads, 1)
+    kv8_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Args a) {
+  using C = Cfg<kR, kDim>;
+  constexpr int kRpt = C::kRpt, kKV = C::kKV, kRowF = C::kRowF, kRowBytes = C::kRowBytes;
+  constexpr uint32_t kIdescS = idesc8(128, kR, 0, 0);
+  constexpr uint32_t kIdescO = idesc8(128, kR, 1, 1);
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const uint32_t base = smem_addr(smem);
+  auto bar = [&](int i) { return base + C::kOffBar + 8u * i; };
+  // A wait names a phase by its parity: the phase before has completed by then, and the
+  // next one cannot complete before the waiter has looked. Slot and buffer of tile T are
+  // T % 4, so their next phase is tile T + 4, of the same group: K(T + 4) waits for S(T),
+  // V(T + 4) for PV(T), S(T + 4) for the group's reading of S(T), P(T + 2) for PV(T).
+  auto FULLK = [&](int T) { return bar(T % kStages); };
+  auto FULLV = [&](int T) { return bar(kStages + T % kStages); };
+  auto SREADY = [&](int T) { return bar(2 * kStages + T % kStages); };
+  auto SFREE = [&](int T) { return bar(3 * kStages + T % kStages); };
+  auto PVDONE = [&](int T) { return bar(4 * kStages + T % kStages); };
+  auto PFULL = [&](int T) { return bar(5 * kStages + (T & 1)); };
+  const uint32_t RECV = bar(5 * kStages + 2);
+  const uint32_t TMEMDONE = bar(5 * kStages + 3);
+  auto par = [](int T) { return static_cast<uint32_t>((T / kStages) & 1); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
+  float4* row_const = reinterpret_cast<float4*>(smem + C::kOffRow);
+  float* row_ref = reinterpret_cast<float*>(smem + C::kOffRef);
+  float* row_fac = reinterpret_cast<float*>(smem + C::kOffFac);
+  float* row_max = reinterpret_cast<float*>(smem + C::kOffMax);
+  float* row_sum = reinterpret_cast<float*>(smem + C::kOffSum);
+  float4* row_join = reinterpret_cast<float4*>(smem + C::kOffJoin);
+
+  auto gdiv = [&](int p) { return __float2int_rz((static_cast<float>(p) + 0.5f) * a.inv_g); };
+  const int rank = blockIdx.x, csize = gridDim.x;
+  const int kvh = blockIdx.y % a.Hkv, mblock = blockIdx.y / a.Hkv, b = blockIdx.z;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (warp == 0 && lane == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(FULLK(s), 1);
+      mbar_init(FULLV(s), 1);
+      mbar_init(SREADY(s), 1);
+      mbar_init(SFREE(s), kSoftWarps / 2);
+      mbar_init(PVDONE(s), 1);
+    }
+    mbar_init(PFULL(0), kSoftWarps / 2);
+    mbar_init(PFULL(1), kSoftWarps / 2);
+    mbar_init(RECV, 1);
+    mbar_init(TMEMDONE, kSoftWarps);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  __syncwarp();
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_slot)),
+                 "r"(C::kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  griddep_wait();  // nothing before this touches global memory
+  const int n_keys = __ldcg(a.len + b);
+  const bool valid = n_keys >= a.R && n_keys <= a.cap;
+  // this CTA's share of the keys, in blocks of 32
+  const int nblk32 = valid ? (n_keys + 31) / 32 : 0;
+  const int blk_begin = static_cast<int>(static_cast<long long>(rank) * nblk32 / csize);
+  const int blk_end = static_cast<int>(static_cast<long long>(rank + 1) * nblk32 / csize);
+  const int key_begin = blk_begin * 32, key_end = min(blk_end * 32, valid ? n_keys : 0);
+  const int n_tiles = (blk_end - blk_begin + 3) / 4;
+  auto tile_keys = [&](int t) { return min(kTile, key_end - key_begin - t * kTile); };
+
+  if (warp == 0) {
+    // -------------------------------------------------------------- producer
+    if (!valid && rank == 0 && lane == 0 && blockIdx.y == 0) sd_set_error(SD_DEVERR_LENGTH);
+    const int z = b * a.Hkv + kvh;
+    const uint64_t policy = l2_evict_first_policy();
+    // a whole box even for a short last tile: keys past the range are masked, rows past
+    // the capacity arrive zero-filled
+    auto issue_k = [&](int T) {
+      if (T >= kStages) mbar_wait(SREADY(T), par(T - kStages));
+      if (elect_one()) {
+        mbar_expect_tx(FULLK(T), static_cast<uint32_t>(kKV));
+        tma_load_3d_hint(base + (T % kStages) * kKV, &tm_k, FULLK(T), 0, key_begin + T * kTile, z, policy);
+      }
+      __syncwarp();
+    };
+    auto issue_v = [&](int T) {
+      if (T >= kStages) mbar_wait(PVDONE(T), par(T - kStages));
+      if (elect_one()) {
+        mbar_expect_tx(FULLV(T), static_cast<uint32_t>(kKV));
+        tma_load_3d_hint(base + C::kRingV + (T % kStages) * kKV, &tm_v, FULLV(T), 0, key_begin + T * kTile, z, policy);
+      }
+      __syncwarp();
+    };
+    const int n0 = min(n_tiles, kStages);
+#pragma unroll 1
+    for (int T = 0; T < n0; ++T) {
+      issue_k(T);
+      issue_v(T);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    // past the ring the keys go one tile ahead of the values: their slot is free earlier
+#pragma unroll 1
+    for (int T = n0; T <= n_tiles; ++T) {
+      if (T < n_tiles) issue_k(T);
+      if (T > n0) issue_v(T - 1);
+    }
+    if (csize > 1) {
+      cluster_arrive_relaxed();
+      cluster_wait();
+    }
+  } else if (warp == 1) {
+    // -------------------------------------------------------------- S issue
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const uint64_t dK0 = umma_desc(base, 16, kDim * 8, C::kLayout);
+    const uint64_t dQ = umma_desc(base + C::kOffQ, 16, kDim * 8, C::kLayout);
+#pragma unroll 1
+    for (int T = 0; T < n_tiles; ++T) {
+      if (T >= kStages) mbar_wait(SFREE(T), par(T - kStages));
+      mbar_wait(FULLK(T), par(T));
+      tc_fence_after();
+      const uint32_t ts = tmem + kR * (T % kStages);
+      const uint64_t dk = dK0 + static_cast<uint64_t>(((T % kStages) * kKV) >> 4);
+      if (elect_one()) {
+#pragma unroll
+        for (int term = 0; term < 2; ++term)
+#pragma unroll
+          for (int kk = 0; kk < kDim / 32; ++kk)
+            umma8(ts, dk + (kk * 32 >> 4), dQ + ((term * C::kQ + kk * 32) >> 4), kIdescS, term + kk > 0 ? 1 : 0);
+        umma_commit(SREADY(T));
+      }
+      __syncwarp();
+    }
+    if (csize > 1) cluster_arrive_relaxed();
+    mbar_wait(TMEMDONE, 0);  // every softmax warp has read its last column
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
+    if (csize > 1) cluster_wait();
+  } else if (warp == 2) {
+    // -------------------------------------------------------------- PV issue
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_o = *tmem_slot + C::kTmemO;
+    // V^T: MN-major. Head dim 64 keeps M = 128 with both 64-row halves of the operand on
+    // the same rows (stride 0): O's lanes 64..127 repeat 0..63 and are not read
+    const uint64_t dV0 = umma_desc(base + C::kRingV, 0, kDim * 8, C::kLayout);
+    const uint64_t dP0 = umma_desc(base + C::kOffP, C::kPGroup, 256, 6);  // MN-major, 32-byte swizzle
+#pragma unroll 1
+    for (int T = 0; T < n_tiles; ++T) {
+      mbar_wait(PFULL(T), (T >> 1) & 1);
+      mbar_wait(FULLV(T), par(T));
+      tc_fence_after();
+      const uint64_t dv = dV0 + static_cast<uint64_t>(((T % kStages) * kKV) >> 4);
+      const uint64_t dp = dP0 + static_cast<uint64_t>(((T & 1) * 2 * C::kP) >> 4);
+      const uint32_t to = tmem_o + kR * (T & 1);
+      const int n_steps = (tile_keys(T) + 31) >> 5;
+      if (elect_one()) {
+#pragma unroll
+        for (int kk = 0; kk < kTile / 32; ++kk)
+          if (kk < n_steps) {
+            umma8(to, dv + (kk * 32 * kDim >> 4), dp + (kk * 1024 >> 4), kIdescO, T > 1 || kk > 0 ? 1 : 0);
+            umma8(to, dv + (kk * 32 * kDim >> 4), dp + ((C::kP + kk * 1024) >> 4), kIdescO, 1);
+          }
+        umma_commit(PVDONE(T));
+      }
+      __syncwarp();
+    }
+    if (csize > 1) {
+      cluster_arrive_relaxed();
+      cluster_wait();
+    }
+  } else {
+    // -------------------------------------------------------------- softmax
+    const int st = static_cast<int>(threadIdx.x) - kSoft0;  // 0 .. 511
+    const int sw = warp - kFirstSoft;
+    const int group = sw >> 3;
+    const int gt = st & (kGroupThreads - 1);
+    const int half = (sw >> 2) & 1;      // rows kRpt * half .. + kRpt - 1
+    const int quarter = warp & 3;        // TMEM lane quarter of this warp
+    const int kl = quarter * 32 + lane;  // key lane of S^T / d lane of O^T
+    const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
+    const int row0 = kRpt * half;
+    const int rows_in = max(1, min(kR, a.M - mblock * kR));
+    auto q_off = [&](int p) {
+      const int i = gdiv(p);
+      return ((static_cast<long long>(b) * a.R + i) * a.Hq + kvh * a.G + (p - i * a.G)) * kDim;
+    };
+    // ---- the query rows as two terms (rows past M zero), a 16-byte chunk a thread
+    constexpr int kChunks = kDim / 8;
+    constexpr int kQc = kR * kChunks / kSoftThreads > 0 ? kR * kChunks / kSoftThreads : 1;
+    uint4 qv[kQc];
+#pragma unroll
+    for (int u = 0; u < kQc; ++u) {
+      const int idx = st + u * kSoftThreads, p = mblock * kR + idx / kChunks;
+      qv[u] = idx < kR * kChunks && p < a.M ? __ldcg(reinterpret_cast<const uint4*>(a.q + q_off(p) + (idx % kChunks) * 8))
+                                            : make_uint4(0, 0, 0, 0);
+    }
+    if (st == 0) griddep_launch();  // every older kernel has finished: the next may launch
+#pragma unroll
+    for (int u = 0; u < kQc; ++u) {
+      const int idx = st + u * kSoftThreads, row = idx / kChunks, c = idx % kChunks;
+      if (idx >= kR * kChunks) break;  // warp-uniform
+      const uint32_t w[4] = {qv[u].x, qv[u].y, qv[u].z, qv[u].w};
+      uint32_t m = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m = max(m, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
+#pragma unroll
+      for (int x = kChunks / 2; x > 0; x >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, x));
+      // qscale = 2^(e - 7) of the largest element's 2^e (of 2^-119 at least: its inverse is a number)
+      const int e = max(static_cast<int>(m >> 7), 8);
+      const float inv = __uint_as_float(static_cast<uint32_t>(min(254 - e + 7, 254)) << 23);
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) two_terms(sd_bf16_lo(w[j]) * inv, sd_bf16_hi(w[j]) * inv, hi[j], lo[j]);
+      // the swizzle moves 16-byte chunks: of 8 rows of 128 bytes, or of 4 pairs of rows of 64
+      const uint32_t sw16 = kDim == 128 ? ((c >> 1) ^ (row & 7)) : ((c >> 1) ^ ((row >> 1) & 3));
+      const uint32_t dst = base + C::kOffQ + row * kDim + (sw16 << 4) + (c & 1) * 8;
+      asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dst), "r"(hi[0] | (hi[1] << 16)), "r"(hi[2] | (hi[3] << 16)) : "memory");
+      asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dst + C::kQ), "r"(lo[0] | (lo[1] << 16)), "r"(lo[2] | (lo[3] << 16))
+                   : "memory");
+      if (c == 0) {
+        // a row with infinities or NaN in it has no attention: NaN throughout
+        const float qs = m >= 0x7f80u ? __uint_as_float(0x7fc00000u) : __uint_as_float(static_cast<uint32_t>(max(e - 7, 1)) << 23);
+        float* rc = reinterpret_cast<float*>(row_const + (row >> 1)) + (row & 1);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          rc[g * kR * 2] = INFINITY;  // no reference yet: any key's weight passes every bound
+          rc[g * kR * 2 + 2] = qs;
+          row_ref[g * kR + row] = -INFINITY;
+        }
+      }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    // ---- this group's tiles
+    const float4* rconst = row_const + group * (kR / 2) + row0 / 2;
+    uint64_t lp2[kRpt / 2];
+#pragma unroll
+    for (int j = 0; j < kRpt / 2; ++j) lp2[j] = 0ull;
+    const uint32_t pbuf = base + C::kOffP + group * 2 * C::kP;
+    const uint32_t pkey = pbuf + kl * 32;
+    const uint32_t psw = (kl >> 2) & 1;  // 32-byte swizzle
+    const long long plane = static_cast<long long>(b) * a.Hkv + kvh;
+    const float* ks = a.ks + plane * a.nblk;
+    const float* vs = a.vs + plane * a.nblk;
+    // rows of this tile below which a key is masked (causal: new row i sees new keys 0..i;
+    // kR: every row)
+    auto first_row = [&](int key) {
+      if (key >= key_end) return kR;
+      const int i = key - (n_keys - a.R);
+      return a.block_mask || i <= 0 ? 0 : min(kR, max(0, i * a.G - mblock * kR));
+    };
+    const bool idle = row0 >= rows_in;  // none of this warp's rows exists: barriers only
+    float ks_next = 0.f, vs_next = 1.f;
+    auto load_scales = [&](int t) {
+      const int key = key_begin + t * kTile + kl;
+      if (t < n_tiles && key < key_end) {
+        ks_next = __ldcg(ks + (key >> a.block_shift));
+        vs_next = __ldcg(vs + (key >> a.block_shift));
+      }
+    };
+    load_scales(group);
+#pragma unroll 1
+    for (int T = group; T < n_tiles; T += 2) {
+      const int key = key_begin + T * kTile + kl;
+      const float kc = ks_next * a.scale_log2, v_scale = vs_next, lv = lg2(v_scale), iv = 1.f / v_scale;
+      load_scales(T + 2);
+      const int below = first_row(key) - row0;  // this thread's rows j < below are masked
+      const uint64_t kc2 = pack2f(kc, kc), lv2 = pack2f(lv, lv), iv2 = pack2f(iv, iv);
+      const uint32_t ts = tmem + kR * (T % kStages) + row0 + lane_off;
+      mbar_wait(SREADY(T), par(T));
+      tc_fence_after();
+      float y[kRpt];
+      // y = log2 of the weights of this thread's key under the present references
+      auto exponents = [&](bool raw) {
+#pragma unroll
+        for (int j0 = 0; j0 < kRpt; j0 += 16) {
+          uint32_t r[16];
+          tmem_ld16(ts + j0, r);
+#pragma unroll
+          for (int j = 0; j < 16; j += 2) {
+            const float4 rc = rconst[(j0 + j) / 2];
+            const uint64_t t = mul2(pack2f(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), kc2);
+            const uint64_t at = raw ? lv2 : add2(lv2, pack2f(rc.x, rc.y));
+            unpack2(fma2(t, pack2f(rc.z, rc.w), at), y[j0 + j], y[j0 + j + 1]);
+          }
+        }
+        if (__any_sync(0xffffffffu, below > 0)) {  // whatever the score, NaN included
+#pragma unroll
+          for (int j = 0; j < kRpt; ++j)
+            if (j < below) y[j] = -INFINITY;
+        }
+      };
+      bool hot = false;
+      if (!idle) {
+        exponents(false);
+        float m = y[0];
+#pragma unroll
+        for (int j = 1; j < kRpt; ++j) m = fmaxf(m, y[j]);
+        hot = m > kHot;
+      }
+      if (__builtin_expect(named_bar_or(4 + group, kGroupThreads, hot), 0)) {
+        // ---- move the references: the tile's exact row maxima
+        if (!idle) {
+          exponents(true);
+          float mine = 0.f;
+#pragma unroll
+          for (int j = 0; j < kRpt; ++j) {
+            const float m = warp_max(y[j]);
+            if (lane == j) mine = m;
+          }
+          if (lane < kRpt) row_max[(group * 4 + quarter) * kR + row0 + lane] = mine;
+        }
+        named_bar_sync(4 + group, kGroupThreads);
+        if (gt < kR && gt < ((rows_in + kRpt - 1) / kRpt) * kRpt) {
+          const float* rm = row_max + group * 4 * kR + gt;
+          const float m = fmaxf(fmaxf(rm[0], rm[kR]), fmaxf(rm[2 * kR], rm[3 * kR]));
+          const float old = row_ref[group * kR + gt], now = fmaxf(old, m - kTop);
+          row_ref[group * kR + gt] = now;
+          row_fac[group * kR + gt] = old == -INFINITY ? 0.f : ex2(old - now);
+          reinterpret_cast<float*>(row_const + group * (kR / 2) + (gt >> 1))[gt & 1] = -now;
+        }
+        if (T >= 2) mbar_wait(PVDONE(T - 2), par(T - 2));
+        named_bar_sync(4 + group, kGroupThreads);
+        if (!idle) {
+          const float* fac = row_fac + group * kR + row0;
+#pragma unroll
+          for (int j = 0; j < kRpt / 2; ++j) lp2[j] = mul2(lp2[j], pack2f(fac[2 * j], fac[2 * j + 1]));
+          if (T >= 2) {
+            tc_fence_after();
+#pragma unroll
+            for (int j0 = 0; j0 < kRpt; j0 += 16) {
+              uint32_t o[16];
+              const uint32_t to = tmem + C::kTmemO + group * kR + row0 + j0 + lane_off;
+              tmem_ld16(to, o);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * fac[j0 + j]);
+              tmem_st16(to, o);
+            }
+          }
+          exponents(false);
+        }
+      }
+      // the tile's scores are all in registers: its buffer may take S(T + 4)
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(SFREE(T));
+      if (T >= 2) mbar_wait(PVDONE(T - 2), par(T - 2));  // PV(T - 2) has read the P buffer
+      if (!idle) {
+#pragma unroll
+        for (int j0 = 0; j0 < kRpt; j0 += 16) {
+          uint32_t ph[4], pl[4];
+#pragma unroll
+          for (int j = 0; j < 16; j += 4) {
+            uint32_t h[2], l[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int i = j0 + j + 2 * e;
+              const float e0 = ex2(y[i]), e1 = ex2(y[i + 1]);
+              lp2[i / 2] = fma2(pack2f(e0, e1), iv2, lp2[i / 2]);
+              two_terms(e0, e1, h[e], l[e]);
+            }
+            ph[j / 4] = h[0] | (h[1] << 16);
+            pl[j / 4] = l[0] | (l[1] << 16);
+          }
+          const int ch = (row0 + j0) / 16;
+          const uint32_t dst = pkey + (ch >> 1) * C::kPGroup + (((ch & 1) ^ psw) << 4);
+          st_shared_v4(dst, ph[0], ph[1], ph[2], ph[3]);
+          st_shared_v4(dst + C::kP, pl[0], pl[1], pl[2], pl[3]);
+        }
+      }
+      const int n_here = tile_keys(T);
+      if (n_here & 31) {
+        // stale rows that the product reads may hold NaN, whose product with 0 is not 0:
+        // zeros, once the tile has landed
+        mbar_wait(FULLV(T), par(T));
+        const int stale = 32 - (n_here & 31);
+        if (gt < stale * (kDim / 16))
+          st_shared_v4(base + C::kRingV + (T % kStages) * kKV + n_here * kDim + gt * 16, 0u, 0u, 0u, 0u);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(PFULL(T));
+    }
+    const int n_mine = (n_tiles - group + 1) / 2;
+    // ---- row sums: lane L ends with that of row row0 + 8 c + (L >> 2)
+#pragma unroll
+    for (int c = 0; c < kRpt / 8; ++c) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) unpack2(lp2[4 * c + j], v[2 * j], v[2 * j + 1]);
+      const float x = warp_sum8(v, lane);
+      if ((lane & 3) == 0) row_sum[(row0 + 8 * c + (lane >> 2)) * 8 + group * 4 + quarter] = x;
+    }
+    const bool merge = csize > 1;
+    if (merge) cluster_arrive_relaxed();  // the group has seen its last S, and the MMA warps arrive after theirs
+    if (n_mine > 0) {
+      const int T = group + 2 * (n_mine - 1);
+      mbar_wait(PVDONE(T), par(T));
+    }
+    named_bar_sync(2, kSoftThreads);
+    // ---- the groups' softmaxes joined: O = w_0 O_0 + w_1 O_1, l likewise
+    const int rpc = (rows_in + csize - 1) / csize;  // rank c merges rows [c * rpc, ...)
+    auto rows_of = [&](int c) { return max(0, min(rpc, rows_in - c * rpc)); };
+    const int my_rows = rows_of(rank);
+    if (st < kR) {
+      const float4 s0 = reinterpret_cast<const float4*>(row_sum + st * 8)[0];
+      const float4 s1 = reinterpret_cast<const float4*>(row_sum + st * 8)[1];
+      const float l0 = (s0.x + s0.y) + (s0.z + s0.w), l1 = (s1.x + s1.y) + (s1.z + s1.w);
+      const float r0 = row_ref[st], r1 = row_ref[kR + st], ref = fmaxf(r0, r1);
+      // a group without a key for the row counts for nothing
+      const float w0 = r0 == -INFINITY ? 0.f : ex2(r0 - ref), w1 = r1 == -INFINITY ? 0.f : ex2(r1 - ref);
+      const float l = (w0 > 0.f ? w0 * l0 : 0.f) + (w1 > 0.f ? w1 * l1 : 0.f);
+      row_join[st] = make_float4(w0, w1, merge ? l : 1.f / l, ref);
+    }
+    named_bar_sync(2, kSoftThreads);
+    tc_fence_after();
+    constexpr int kOr = kR / 4;  // this warp: its 32 d lanes of a quarter of the rows
+    const int orow0 = (sw >> 2) * kOr;
+    float o[kOr];
+#pragma unroll
+    for (int j = 0; j < kOr; ++j) o[j] = 0.f;
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+      if (g < n_tiles) {
+#pragma unroll
+        for (int j0 = 0; j0 < kOr; j0 += 8) {
+          uint32_t r[8];
+          asm volatile(
+              "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\t"
+              "tcgen05.wait::ld.sync.aligned;"
+              : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+              : "r"(tmem + C::kTmemO + g * kR + orow0 + j0 + lane_off)
+              : "memory");
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float4 jn = row_join[orow0 + j0 + j];
+            const float w = g == 0 ? jn.x : jn.y;
+            if (w != 0.f) o[j0 + j] = fmaf(w, __uint_as_float(r[j]), o[j0 + j]);
+          }
+        }
+      }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(TMEMDONE);
+    if (!merge) {
+#pragma unroll
+      for (int j = 0; j < kOr; ++j) {
+        const int row = orow0 + j, p = mblock * kR + row;
+        if (valid && p < a.M && kl < kDim) a.out[q_off(p) + kl] = __float2bfloat16_rn(o[j] * row_join[row].z);
+      }
+    } else {
+      float* send = reinterpret_cast<float*>(smem + C::kRingV);
+      if (kl < kDim)
+#pragma unroll
+        for (int j = 0; j < kOr; ++j) send[(orow0 + j) * kRowF + kl] = o[j];
+      if (st < kR) *reinterpret_cast<float2*>(send + st * kRowF + kDim) = make_float2(row_join[st].z, row_join[st].w);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      named_bar_sync(2, kSoftThreads);
+      if (st == 0) mbar_expect_tx(RECV, static_cast<uint32_t>(csize * my_rows * kRowBytes));
+      cluster_wait();  // every peer's K ring is free to receive
+      // softmax warp w sends rank w's rows to it, into its slots [rank * rpc, ...)
+      if (elect_one()) {
+        if (sw < csize && rows_of(sw) > 0)
+          bulk_copy_s2s(cluster_map(base + rank * rpc * kRowBytes, sw), base + C::kRingV + sw * rpc * kRowBytes,
+                        static_cast<uint32_t>(rows_of(sw) * kRowBytes), cluster_map(RECV, sw));
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+      }
+      __syncwarp();
+      // ---- merge of the rows this CTA owns, a warp a row; slot c * rpc + r came from rank c
+      const float* recv = reinterpret_cast<const float*>(smem);
+      const int cstep = rpc * kRowF;
+      constexpr int kPer = kDim / 32;
+      struct alignas(kPer * 4) Row {
+        float v[kPer];
+      };
+#pragma unroll 1
+      for (int r = sw; r < my_rows; r += kSoftWarps) {
+        const float* part = recv + r * kRowF;
+        const int p = mblock * kR + rank * rpc + r;
+        if (r == sw) mbar_wait(RECV, 0);
+        const float2 lr = lane < csize ? *reinterpret_cast<const float2*>(part + lane * cstep + kDim)
+                                       : make_float2(0.f, -INFINITY);
+        const float ref = warp_max(lr.y);
+        const float w = lr.y == -INFINITY ? 0.f : ex2(lr.y - ref);
+        float l = w > 0.f ? w * lr.x : 0.f;
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+        Row ov = {};
+#pragma unroll 4
+        for (int c = 0; c < csize; ++c) {
+          const float wc = __shfl_sync(0xffffffffu, w, c);
+          const Row x = reinterpret_cast<const Row*>(part + c * cstep)[lane];
+#pragma unroll
+          for (int j = 0; j < kPer; ++j)
+            if (wc != 0.f) ov.v[j] = fmaf(wc, x.v[j], ov.v[j]);
+        }
+        if (valid && p < a.M) {
+          const float inv_l = 1.f / l;
+          __nv_bfloat16* dst = a.out + q_off(p) + lane * kPer;
+#pragma unroll
+          for (int j = 0; j < kPer; j += 2)
+            *reinterpret_cast<uint32_t*>(dst + j) = cvt_bf16x2(ov.v[j] * inv_l, ov.v[j + 1] * inv_l);
+        }
+      }
+      if (elect_one()) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      __syncwarp();
+    }
+  }
+  // no CTA-wide barrier at the end: every warp leaves when its own work is done
+}
+
+// ------------------------------------------------------------------ host
+constexpr int kClusterSizes[] = {1, 2, 4, 5, 6, 8, 10, 12, 16};
+constexpr int kNumSizes = sizeof(kClusterSizes) / sizeof(int);
+
+template <int kR, int kDim>
+bool set_attributes(int* active) {
+  const void* k = reinterpret_cast<const void*>(kv8_attention_kernel<kR, kDim>);
+  constexpr int smem = Cfg<kR, kDim>::kSmemBytes;
+  if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+      cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return false;
+  }
+  for (int i = 0; i < kNumSizes; ++i) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kClusterSizes[i];
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(kClusterSizes[i], 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int m = 0;
+    if (cudaOccupancyMaxActiveClusters(&m, k, &cfg) != cudaSuccess) {
+      (void)cudaGetLastError();
+      m = 0;
+    }
+    active[i] = m;
+  }
+  return true;
+}
+
+struct DevState {
+  std::once_flag once;
+  bool ok = false;
+  int active[4][kNumSizes] = {};  // [head dim 64, 128][rows 32, 64]
+};
+
+DevState* state() {
+  static DevState states[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+    (void)cudaGetLastError();
+    return nullptr;
+  }
+  DevState& s = states[dev];
+  std::call_once(s.once, [&s] {
+    s.ok = set_attributes<32, 64>(s.active[0]) && set_attributes<64, 64>(s.active[1]) &&
+           set_attributes<32, 128>(s.active[2]) && set_attributes<64, 128>(s.active[3]);
+  });
+  return &s;
+}
+
+// Cluster size: the least waves x (128-key tiles a CTA + a fixed cost a wave), in tiles.
+int pick_cluster(const int* active, long long units, int cap) {
+  const double nblk = (cap + 31) / 32;
+  double best_cost = -1;
+  int best = 0;
+  for (int i = 0; i < kNumSizes; ++i) {
+    const int cs = kClusterSizes[i];
+    if (active[i] <= 0 || (cs > 1 && nblk < 2.0 * cs)) continue;
+    const long long waves = (units + active[i] - 1) / active[i];
+    const double fixed = (waves > 1 ? 3.0 : 1.0) + (cs > 8 ? 0.8 : 0.0);
+    const double cost = static_cast<double>(waves) * (nblk / (4.0 * cs) + fixed);
+    if (best_cost < 0 || cost < best_cost) {
+      best_cost = cost;
+      best = cs;
+    }
+  }
+  return best;
+}
+
+// [planes][cap][D] codes in boxes of one whole row x 128 rows, swizzled by the row's width
+bool make_map8(CUtensorMap* map, void* base, int cap, int planes, int D) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(cap), static_cast<cuuint64_t>(planes)};
+  cuuint64_t strides[2] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(cap) * static_cast<cuuint64_t>(D)};
+  cuuint32_t box[3] = {static_cast<cuuint32_t>(D), kTile, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int kR, int kDim>
+sd_status launch(const sd_kv8_cache* c, const Args& a, int mblocks, int cs, cudaStream_t stream) {
+  CUtensorMap k, v;
+  if (!make_map8(&k, c->k, c->capacity, c->batch * c->n_kv_heads, kDim) ||
+      !make_map8(&v, c->v, c->capacity, c->batch * c->n_kv_heads, kDim))
+    return SD_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cs;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(cs, c->n_kv_heads * mblocks, c->batch);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = Cfg<kR, kDim>::kSmemBytes;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  if (cudaLaunchKernelEx(&cfg, kv8_attention_kernel<kR, kDim>, k, v, a) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return SD_ERR_CUDA;
+  }
+  return SD_OK;
 }
 
 }  // namespace
@@ -86,17 +840,30 @@ extern "C" sd_status sd_kv8_attention(const void* q, const sd_kv8_cache* cache, 
   if (B == 0) return SD_OK;
   if (!q || !out || !sd_aligned16(q) || !sd_aligned16(out)) return SD_ERR_INVALID_ARG;
   const double sc = scale > 0.f ? scale : 1.0 / sqrt(static_cast<double>(D));
-  const float scale_log2 = static_cast<float>(sc * 1.4426950408889634);
-  const int M = Hq / Hkv * R;
-  if (sd_launch_pdl(D == 64 ? kv8_attention_kernel<64> : kv8_attention_kernel<128>, dim3((M + 3) / 4, Hkv, B), dim3(128), 0,
-                    reinterpret_cast<cudaStream_t>(stream), static_cast<const __nv_bfloat16*>(q),
-                    static_cast<const uint8_t*>(cache->k), static_cast<const uint8_t*>(cache->v),
-                    static_cast<const float*>(cache->k_scale), static_cast<const float*>(cache->v_scale),
-                    static_cast<const int32_t*>(cache->len), static_cast<__nv_bfloat16*>(out), R, Hq, Hkv,
-                    cache->capacity, cache->block, (cache->capacity + cache->block - 1) / cache->block, scale_log2,
-                    (flags & SD_ATTN_BLOCK_MASK) != 0) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return SD_ERR_CUDA;
-  }
-  return SD_OK;
+  Args a = {};
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.ks = cache->k_scale;
+  a.vs = cache->v_scale;
+  a.len = cache->len;
+  a.R = R;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.G = Hq / Hkv;
+  a.M = a.G * R;
+  a.cap = cache->capacity;
+  a.nblk = (cache->capacity + cache->block - 1) / cache->block;
+  a.block_shift = cache->block == 32 ? 5 : (cache->block == 64 ? 6 : 7);
+  a.block_mask = (flags & SD_ATTN_BLOCK_MASK) != 0;
+  a.inv_g = 1.0f / static_cast<float>(a.G);
+  a.scale_log2 = static_cast<float>(sc * 1.4426950408889634);
+  const int rows = a.M <= 32 ? 32 : 64, mblocks = (a.M + rows - 1) / rows;
+  DevState* dev = state();
+  if (!dev || !dev->ok) return SD_ERR_CUDA;
+  const int cs = pick_cluster(dev->active[(D == 128 ? 2 : 0) + (rows == 64)], static_cast<long long>(B) * Hkv * mblocks,
+                              cache->capacity);
+  if (cs <= 0) return SD_ERR_CUDA;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (D == 128) return rows == 32 ? launch<32, 128>(cache, a, mblocks, cs, st) : launch<64, 128>(cache, a, mblocks, cs, st);
+  return rows == 32 ? launch<32, 64>(cache, a, mblocks, cs, st) : launch<64, 64>(cache, a, mblocks, cs, st);
 }

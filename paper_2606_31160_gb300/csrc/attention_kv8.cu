@@ -4,22 +4,24 @@
 //
 // The codes go from HBM to the tensor cores as they are (kind::f8f6f4, e4m3 by e4m3, fp32
 // sums): nothing widens a key or a value. What meets them has 8 significant bits and an
-// e4m3 number 4, so queries and weights go in as two terms each, x = hi + lo with hi =
-// e4m3(x) and lo = e4m3(x - hi), both products into the same sum:
+// e4m3 number 4, so queries and weights go in as two terms each, the second what rounding
+// the first left over:
 //   * a query row, scaled by the power of two that brings its largest element into [128,
 //     256), is exact in two terms (bf16 has 8 bits; elements below 2^-10 of the largest
-//     to 2^-18 of it);
-//   * a weight keeps 8 bits, as a bf16 one would, down to 2^-12 of its row's largest, and
-//     below that is off by 2^-17 of it at most.
+//     to 2^-18 of it), both products into the same sum;
+//   * a weight is hi + lo / 16, hi = e4m3(P), lo = e4m3(16 (P - hi)): 8 bits, as a bf16
+//     one would keep, down to 2^-12 of its row's largest, and off by 2^-16 of it at most
+//     below that. The terms are columns of one product, 2 kR wide (four of N = 2 kR take
+//     200 cycles at kR = 32, eight of N = kR 330).
 // The packed query rows of a KV head (G * R) are few, so both products run transposed,
-//     S^T[128 keys][kR rows] = K_tile . Q^T,   O^T[128 d][kR rows] += V_tile^T . P^T
-// with kR = 32 or 64 and, above 64 rows, two m-blocks. Scales enter between the two: a
+//     S^T[128 keys][kR rows] = K_tile . Q^T,   O^T[128 d][2 kR] += V_tile^T . P^T
+// with kR = 32, 48 or 64 and, above 64 rows, two m-blocks. Scales enter between the two: a
 // thread has one key, t = S * k_scale * c, and
 //     P = 2^(t * qscale[row] + log2 v_scale - ref[row]),   l[row] += P / v_scale,
 // so O / l is the attention whatever the scales are.
 //
-// Reference. P has to stay within e4m3's 448, so ref[row] is 2^6 below the largest weight
-// that the first tile shows, and moves when a later one would pass 2^8.75: every thread
+// Reference. P has to stay within e4m3's 448, so ref[row] gives the largest weight that
+// the first tile shows 2^2, and moves when a later one would pass 2^8.75: every thread
 // compares its largest exponent and the group votes once a tile (an OR in its barrier).
 // Moving takes the tile's exact row maxima (redux over the lanes), and rescales l and O
 // in tensor memory.
@@ -48,7 +50,7 @@ constexpr int kGroupThreads = kSoftThreads / 2;
 constexpr int kFirstSoft = 3;
 constexpr int kSoft0 = 32 * kFirstSoft;
 constexpr int kThreads = kSoft0 + kSoftThreads;
-constexpr float kTop = 6.f;              // log2 of the weight that a reference gives the largest key
+constexpr float kTop = 2.f;              // log2 of the weight that a reference gives the largest key
 constexpr float kHot = 8.75f;            // log2 of the largest weight a reference may leave (e4m3 ends at 448 = 2^8.81)
 
 struct Args {
@@ -65,19 +67,20 @@ struct Args {
 
 template <int kR, int kDim>
 struct Cfg {
-  static_assert(kR == 32 || kR == 64, "row tile");
+  static_assert(kR == 32 || kR == 48 || kR == 64, "row tile");
   static_assert(kDim == 64 || kDim == 128, "head dim");
   static constexpr int kRpt = kR / 2;             // rows of a softmax thread
   static constexpr int kKV = kTile * kDim;        // one K (or V) tile
   static constexpr int kRingV = kStages * kKV;
   static constexpr int kRing = 2 * kStages * kKV;
   static constexpr int kQ = kR * kDim;            // one term of the query rows
-  // P^T: MN-major, 32-byte swizzle: 32 rows x 8 keys an atom; the 32-row groups kPGroup apart
+  // P^T: 2 kR rows (hi, then lo), MN-major, 32-byte swizzle: 32 rows x 8 keys an atom; the
+  // 32-row groups kPGroup apart
   static constexpr int kPGroup = kTile * 32;
-  static constexpr int kP = kR / 32 * kPGroup;    // one term of a group's weights
+  static constexpr int kP = 2 * kR / 32 * kPGroup;  // a group's weights
   static constexpr int kOffQ = kRing;             // hi, lo
-  static constexpr int kOffP = kOffQ + 2 * kQ;    // [group][hi, lo]
-  static constexpr int kOffBar = kOffP + 4 * kP;
+  static constexpr int kOffP = kOffQ + 2 * kQ;    // [group]
+  static constexpr int kOffBar = kOffP + 2 * kP;
   // full_k[4] full_v[4] s_ready[4] s_free[4] pv_done[4] p_full[2] recv tmem_done
   static constexpr int kNumBars = 5 * kStages + 4;
   static constexpr int kOffMisc = round_up(kOffBar + kNumBars * 8, 16);
@@ -90,7 +93,7 @@ struct Cfg {
   static constexpr int kSmemBytes = kOffJoin + kR * 16 + 1024;
   static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
   static_assert(kOffQ % 1024 == 0 && kOffP % 1024 == 0, "swizzle atoms");
-  static constexpr int kTmemO = 4 * kR;                     // S0..S3 | O_0 | O_1
+  static constexpr int kTmemO = 4 * kR;                     // S0..S3 | O_0 hi, lo | O_1 hi, lo
   static constexpr int kTmemCols = kR == 32 ? 256 : 512;
   static constexpr uint64_t kLayout = kDim == 128 ? 2 : 4;  // swizzle of K, V and Q rows: their whole width
   // a partial row sent to its owner: [O(kDim) | l | ref | 2 pad] fp32
@@ -112,14 +115,32 @@ __device__ __forceinline__ void umma8(uint32_t d_tmem, uint64_t a, uint64_t b, u
       "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// 16 fp32 columns of this warp's 32 TMEM lanes from 16 registers
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]),
-      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
-      : "memory");
-  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+// fp32 columns of this warp's 32 TMEM lanes to and from registers; a load's registers
+// hold them after tmem_wait_ld
+__device__ __forceinline__ void tmem_ld4(uint32_t taddr, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+template <int kN>
+__device__ __forceinline__ void tmem_wait_ld(float* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < kN; j += 8)  // no use of the registers moves above the wait
+    asm volatile("" : "+f"(r[j]), "+f"(r[j + 1]), "+f"(r[j + 2]), "+f"(r[j + 3]), "+f"(r[j + 4]), "+f"(r[j + 5]),
+                 "+f"(r[j + 6]), "+f"(r[j + 7]));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"f"(r[0]), "f"(r[1]), "f"(r[2]),
+               "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "r"(taddr)
+               : "memory");
 }
 __device__ __forceinline__ uint64_t pack2f(float lo, float hi) {
   uint64_t d;
@@ -155,18 +176,21 @@ __device__ __forceinline__ float lg2(float x) {
   return y;
 }
 
-// Two numbers of magnitude up to 448 as two e4m3 terms (by way of fp16, whose 11 bits
-// both terms together do not reach): hi and lo codes in the low 16 bits of each.
+// Two numbers of magnitude up to 448 as two e4m3 terms each, x = hi + lo / kLo (by way of
+// fp16, whose 11 bits both terms together do not reach): codes in the low 16 bits.
+template <int kLo>
 __device__ __forceinline__ void two_terms(float x0, float x1, uint32_t& hi, uint32_t& lo) {
+  static_assert(kLo == 1 || kLo == 16, "as fp16 below");
   asm("{\n\t.reg .b32 f, b, d;\n\t.reg .b16 h, l;\n\t"
       "cvt.rn.f16x2.f32 f, %3, %2;\n\t"
       "cvt.rn.satfinite.e4m3x2.f16x2 h, f;\n\t"
       "cvt.rn.f16x2.e4m3x2 b, h;\n\t"
       "sub.f16x2 d, f, b;\n\t"
+      "mul.f16x2 d, d, %4;\n\t"
       "cvt.rn.satfinite.e4m3x2.f16x2 l, d;\n\t"
       "cvt.u32.u16 %0, h;\n\tcvt.u32.u16 %1, l;\n\t}"
       : "=r"(hi), "=r"(lo)
-      : "f"(x0), "f"(x1));
+      : "f"(x0), "f"(x1), "r"(kLo == 1 ? 0x3c003c00u : 0x4c004c00u));
 }
 
 // Sum over the 32 lanes of a warp of each of 8 per-lane values: lane L ends with the sum
@@ -197,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   using C = Cfg<kR, kDim>;
   constexpr int kRpt = C::kRpt, kKV = C::kKV, kRowF = C::kRowF, kRowBytes = C::kRowBytes;
   constexpr uint32_t kIdescS = idesc8(128, kR, 0, 0);
-  constexpr uint32_t kIdescO = idesc8(128, kR, 1, 1);
+  constexpr uint32_t kIdescO = idesc8(128, 2 * kR, 1, 1);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const uint32_t base = smem_addr(smem);
@@ -349,16 +373,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_wait(FULLV(T), par(T));
       tc_fence_after();
       const uint64_t dv = dV0 + static_cast<uint64_t>(((T % kStages) * kKV) >> 4);
-      const uint64_t dp = dP0 + static_cast<uint64_t>(((T & 1) * 2 * C::kP) >> 4);
-      const uint32_t to = tmem_o + kR * (T & 1);
+      const uint64_t dp = dP0 + static_cast<uint64_t>(((T & 1) * C::kP) >> 4);
+      const uint32_t to = tmem_o + 2 * kR * (T & 1);
       const int n_steps = (tile_keys(T) + 31) >> 5;
       if (elect_one()) {
 #pragma unroll
         for (int kk = 0; kk < kTile / 32; ++kk)
-          if (kk < n_steps) {
+          if (kk < n_steps)
             umma8(to, dv + (kk * 32 * kDim >> 4), dp + (kk * 1024 >> 4), kIdescO, T > 1 || kk > 0 ? 1 : 0);
-            umma8(to, dv + (kk * 32 * kDim >> 4), dp + ((C::kP + kk * 1024) >> 4), kIdescO, 1);
-          }
         umma_commit(PVDONE(T));
       }
       __syncwarp();
@@ -385,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     // ---- the query rows as two terms (rows past M zero), a 16-byte chunk a thread
     constexpr int kChunks = kDim / 8;
-    constexpr int kQc = kR * kChunks / kSoftThreads > 0 ? kR * kChunks / kSoftThreads : 1;
+    constexpr int kQc = (kR * kChunks + kSoftThreads - 1) / kSoftThreads;
     uint4 qv[kQc];
 #pragma unroll
     for (int u = 0; u < kQc; ++u) {
@@ -409,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float inv = __uint_as_float(static_cast<uint32_t>(min(254 - e + 7, 254)) << 23);
       uint32_t hi[4], lo[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) two_terms(sd_bf16_lo(w[j]) * inv, sd_bf16_hi(w[j]) * inv, hi[j], lo[j]);
+      for (int j = 0; j < 4; ++j) two_terms<1>(sd_bf16_lo(w[j]) * inv, sd_bf16_hi(w[j]) * inv, hi[j], lo[j]);
       // the swizzle moves 16-byte chunks: of 8 rows of 128 bytes, or of 4 pairs of rows of 64
       const uint32_t sw16 = kDim == 128 ? ((c >> 1) ^ (row & 7)) : ((c >> 1) ^ ((row >> 1) & 3));
       const uint32_t dst = base + C::kOffQ + row * kDim + (sw16 << 4) + (c & 1) * 8;
@@ -439,8 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint64_t lp2[kRpt / 2];
 #pragma unroll
     for (int j = 0; j < kRpt / 2; ++j) lp2[j] = 0ull;
-    const uint32_t pbuf = base + C::kOffP + group * 2 * C::kP;
-    const uint32_t pkey = pbuf + kl * 32;
+    const uint32_t pkey = base + C::kOffP + group * C::kP + kl * 32;
     const uint32_t psw = (kl >> 2) & 1;  // 32-byte swizzle
     const long long plane = static_cast<long long>(b) * a.Hkv + kvh;
     const float* ks = a.ks + plane * a.nblk;
@@ -476,16 +497,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       // y = log2 of the weights of this thread's key under the present references
       auto exponents = [&](bool raw) {
 #pragma unroll
-        for (int j0 = 0; j0 < kRpt; j0 += 16) {
-          uint32_t r[16];
-          tmem_ld16(ts + j0, r);
+        for (int j = 0; j < kRpt; j += 8) tmem_ld8(ts + j, y + j);
+        tmem_wait_ld<kRpt>(y);
 #pragma unroll
-          for (int j = 0; j < 16; j += 2) {
-            const float4 rc = rconst[(j0 + j) / 2];
-            const uint64_t t = mul2(pack2f(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), kc2);
-            const uint64_t at = raw ? lv2 : add2(lv2, pack2f(rc.x, rc.y));
-            unpack2(fma2(t, pack2f(rc.z, rc.w), at), y[j0 + j], y[j0 + j + 1]);
-          }
+        for (int j = 0; j < kRpt; j += 2) {
+          const float4 rc = rconst[j / 2];
+          const uint64_t t = mul2(pack2f(y[j], y[j + 1]), kc2);
+          const uint64_t at = raw ? lv2 : add2(lv2, pack2f(rc.x, rc.y));
+          unpack2(fma2(t, pack2f(rc.z, rc.w), at), y[j], y[j + 1]);
         }
         if (__any_sync(0xffffffffu, below > 0)) {  // whatever the score, NaN included
 #pragma unroll
@@ -531,14 +550,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (T >= 2) {
             tc_fence_after();
 #pragma unroll
-            for (int j0 = 0; j0 < kRpt; j0 += 16) {
-              uint32_t o[16];
-              const uint32_t to = tmem + C::kTmemO + group * kR + row0 + j0 + lane_off;
-              tmem_ld16(to, o);
+            for (int term = 0; term < 2; ++term)
 #pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * fac[j0 + j]);
-              tmem_st16(to, o);
-            }
+              for (int j0 = 0; j0 < kRpt; j0 += 8) {
+                float o[8];
+                const uint32_t to = tmem + C::kTmemO + (2 * group + term) * kR + row0 + j0 + lane_off;
+                tmem_ld8(to, o);
+                tmem_wait_ld<8>(o);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] *= fac[j0 + j];
+                tmem_st8(to, o);
+              }
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
           }
           exponents(false);
         }
@@ -550,25 +573,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (T >= 2) mbar_wait(PVDONE(T - 2), par(T - 2));  // PV(T - 2) has read the P buffer
       if (!idle) {
 #pragma unroll
-        for (int j0 = 0; j0 < kRpt; j0 += 16) {
-          uint32_t ph[4], pl[4];
+        for (int j0 = 0; j0 < kRpt; j0 += 8) {
+          uint32_t h[4], l[4];
 #pragma unroll
-          for (int j = 0; j < 16; j += 4) {
-            uint32_t h[2], l[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int i = j0 + j + 2 * e;
-              const float e0 = ex2(y[i]), e1 = ex2(y[i + 1]);
-              lp2[i / 2] = fma2(pack2f(e0, e1), iv2, lp2[i / 2]);
-              two_terms(e0, e1, h[e], l[e]);
-            }
-            ph[j / 4] = h[0] | (h[1] << 16);
-            pl[j / 4] = l[0] | (l[1] << 16);
+          for (int e = 0; e < 4; ++e) {
+            const int i = j0 + 2 * e;
+            const float e0 = ex2(y[i]), e1 = ex2(y[i + 1]);
+            lp2[i / 2] = fma2(pack2f(e0, e1), iv2, lp2[i / 2]);
+            two_terms<16>(e0, e1, h[e], l[e]);
           }
-          const int ch = (row0 + j0) / 16;
-          const uint32_t dst = pkey + (ch >> 1) * C::kPGroup + (((ch & 1) ^ psw) << 4);
-          st_shared_v4(dst, ph[0], ph[1], ph[2], ph[3]);
-          st_shared_v4(dst + C::kP, pl[0], pl[1], pl[2], pl[3]);
+          auto store = [&](int row, const uint32_t (&x)[4]) {  // rows row .. row + 7 of 2 kR
+            const uint32_t dst = pkey + (row >> 5) * C::kPGroup + ((((row >> 4) & 1) ^ psw) << 4) + (row & 8);
+            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dst), "r"(x[0] | (x[1] << 16)), "r"(x[2] | (x[3] << 16))
+                         : "memory");
+          };
+          store(row0 + j0, h);
+          store(kR + row0 + j0, l);
         }
       }
       const int n_here = tile_keys(T);
@@ -626,19 +646,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int g = 0; g < 2; ++g)
       if (g < n_tiles) {
 #pragma unroll
-        for (int j0 = 0; j0 < kOr; j0 += 8) {
-          uint32_t r[8];
-          asm volatile(
-              "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\t"
-              "tcgen05.wait::ld.sync.aligned;"
-              : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-              : "r"(tmem + C::kTmemO + g * kR + orow0 + j0 + lane_off)
-              : "memory");
+        for (int j0 = 0; j0 < kOr; j0 += 4) {
+          float r[8];  // hi and lo of 4 rows
+          const uint32_t to = tmem + C::kTmemO + 2 * g * kR + orow0 + j0 + lane_off;
+          tmem_ld4(to, r);
+          tmem_ld4(to + kR, r + 4);
+          tmem_wait_ld<8>(r);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
+          for (int j = 0; j < 4; ++j) {
             const float4 jn = row_join[orow0 + j0 + j];
             const float w = g == 0 ? jn.x : jn.y;
-            if (w != 0.f) o[j0 + j] = fmaf(w, __uint_as_float(r[j]), o[j0 + j]);
+            if (w != 0.f) o[j0 + j] = fmaf(w, fmaf(r[4 + j], 0.0625f, r[j]), o[j0 + j]);
           }
         }
       }
@@ -750,7 +768,7 @@ bool set_attributes(int* active) {
 struct DevState {
   std::once_flag once;
   bool ok = false;
-  int active[4][kNumSizes] = {};  // [head dim 64, 128][rows 32, 64]
+  int active[6][kNumSizes] = {};  // [head dim 64, 128][rows 32, 48, 64]
 };
 
 DevState* state() {
@@ -762,8 +780,9 @@ DevState* state() {
   }
   DevState& s = states[dev];
   std::call_once(s.once, [&s] {
-    s.ok = set_attributes<32, 64>(s.active[0]) && set_attributes<64, 64>(s.active[1]) &&
-           set_attributes<32, 128>(s.active[2]) && set_attributes<64, 128>(s.active[3]);
+    s.ok = set_attributes<32, 64>(s.active[0]) && set_attributes<48, 64>(s.active[1]) &&
+           set_attributes<64, 64>(s.active[2]) && set_attributes<32, 128>(s.active[3]) &&
+           set_attributes<48, 128>(s.active[4]) && set_attributes<64, 128>(s.active[5]);
   });
   return &s;
 }
@@ -857,13 +876,17 @@ extern "C" sd_status sd_kv8_attention(const void* q, const sd_kv8_cache* cache, 
   a.block_mask = (flags & SD_ATTN_BLOCK_MASK) != 0;
   a.inv_g = 1.0f / static_cast<float>(a.G);
   a.scale_log2 = static_cast<float>(sc * 1.4426950408889634);
-  const int rows = a.M <= 32 ? 32 : 64, mblocks = (a.M + rows - 1) / rows;
+  // the smallest tile that holds the rows in one m-block, else in two
+  const int rows = a.M <= 32 ? 32 : (a.M <= 48 ? 48 : (a.M <= 64 ? 64 : (a.M <= 96 ? 48 : 64)));
+  const int mblocks = (a.M + rows - 1) / rows;
   DevState* dev = state();
   if (!dev || !dev->ok) return SD_ERR_CUDA;
-  const int cs = pick_cluster(dev->active[(D == 128 ? 2 : 0) + (rows == 64)], static_cast<long long>(B) * Hkv * mblocks,
+  const int cs = pick_cluster(dev->active[(D == 128 ? 3 : 0) + rows / 16 - 2], static_cast<long long>(B) * Hkv * mblocks,
                               cache->capacity);
   if (cs <= 0) return SD_ERR_CUDA;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (D == 128) return rows == 32 ? launch<32, 128>(cache, a, mblocks, cs, st) : launch<64, 128>(cache, a, mblocks, cs, st);
-  return rows == 32 ? launch<32, 64>(cache, a, mblocks, cs, st) : launch<64, 64>(cache, a, mblocks, cs, st);
+  auto go = [&](auto f32, auto f48, auto f64) {
+    return rows == 32 ? f32(cache, a, mblocks, cs, st) : (rows == 48 ? f48(cache, a, mblocks, cs, st) : f64(cache, a, mblocks, cs, st));
+  };
+  return D == 128 ? go(launch<32, 128>, launch<48, 128>, launch<64, 128>) : go(launch<32, 64>, launch<48, 64>, launch<64, 64>);
 }

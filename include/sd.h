@@ -207,7 +207,8 @@ sd_status sd_verify_attention_ex(const void* q, const sd_kv_cache* cache, void* 
 
 /*
  * Cluster size of the tcgen05 verify-attention kernels (sd_verify_attention
- * and sd_verify_layer; sd_verify_kernel says which shapes take them): one
+ * and sd_verify_layer; sd_verify_kernel says which shapes take them; and
+ * sd_kv8_attention): one
  * thread-block cluster of `cluster_size` CTAs per (scene, KV head) splits that
  * head's keys evenly and merges the partial softmax states in distributed
  * shared memory (the split-L form of Eq. verify). 0 (the default) lets every

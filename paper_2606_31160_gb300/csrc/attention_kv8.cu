@@ -6,18 +6,18 @@
 // sums): nothing widens a key or a value. What meets them has 8 significant bits and an
 // e4m3 number 4, so queries and weights go in as two terms each, the second what rounding
 // the first left over:
-//   * a query row, scaled by the power of two that brings its largest element into [128,
-//     256), is exact in two terms (bf16 has 8 bits; elements below 2^-10 of the largest
-//     to 2^-18 of it), both products into the same sum;
+//   * the query rows, scaled by the power of two that brings their largest element into
+//     [128, 256), are exact in two terms (bf16 has 8 bits; elements below 2^-10 of the
+//     largest to 2^-18 of it), both products into the same sum;
 //   * a weight is hi + lo / 16, hi = e4m3(P), lo = e4m3(16 (P - hi)): 8 bits, as a bf16
 //     one would keep, down to 2^-12 of its row's largest, and off by 2^-16 of it at most
 //     below that. The terms are columns of one product, 2 kR wide (four of N = 2 kR take
 //     200 cycles at kR = 32, eight of N = kR 330).
 // The packed query rows of a KV head (G * R) are few, so both products run transposed,
 //     S^T[128 keys][kR rows] = K_tile . Q^T,   O^T[128 d][2 kR] += V_tile^T . P^T
-// with kR = 32, 48 or 64 and, above 64 rows, two m-blocks. Scales enter between the two: a
+// with kR = 32 or 48 and, above 48 rows, two or three m-blocks. Scales enter between the two: a
 // thread has one key, t = S * k_scale * c, and
-//     P = 2^(t * qscale[row] + log2 v_scale - ref[row]),   l[row] += P / v_scale,
+//     P = 2^(t * qscale + log2 v_scale - ref[row]),   l[row] += P / v_scale,
 // so O / l is the attention whatever the scales are.
 //
 // Reference. P has to stay within e4m3's 448, so ref[row] gives the largest weight that
@@ -44,12 +44,8 @@ namespace {
 
 constexpr int kTile = 128;               // keys a tile
 constexpr int kStages = 4;               // K slots, V slots and S buffers
-constexpr int kSoftWarps = 16;
-constexpr int kSoftThreads = 32 * kSoftWarps;
-constexpr int kGroupThreads = kSoftThreads / 2;
-constexpr int kFirstSoft = 3;
+constexpr int kFirstSoft = 3;            // the first softmax warp
 constexpr int kSoft0 = 32 * kFirstSoft;
-constexpr int kThreads = kSoft0 + kSoftThreads;
 constexpr float kTop = 2.f;              // log2 of the weight that a reference gives the largest key
 constexpr float kHot = 8.75f;            // log2 of the largest weight a reference may leave (e4m3 ends at 448 = 2^8.81)
 
@@ -59,7 +55,7 @@ struct Args {
   const float* ks;
   const float* vs;
   const int32_t* len;
-  int R, Hq, Hkv, G, M, cap, nblk, block_shift;
+  int R, Hq, Hkv, G, M, cap, nblk, block_shift, mblocks;
   int block_mask;
   float inv_g;       // 1 / G: p / G == int((p + 0.5) / G) exactly for the p < 128 used here
   float scale_log2;
@@ -67,9 +63,14 @@ struct Args {
 
 template <int kR, int kDim>
 struct Cfg {
-  static_assert(kR == 32 || kR == 48 || kR == 64, "row tile");
+  static_assert(kR == 32 || kR == 48, "row tile");
   static_assert(kDim == 64 || kDim == 128, "head dim");
-  static constexpr int kRpt = kR / 2;             // rows of a softmax thread
+  // a softmax thread has one key and kUnits units of 8 rows: of its half every second one
+  static constexpr int kUnits = kR / 16;
+  static constexpr int kSoftWarps = 16;
+  static constexpr int kSoftThreads = 32 * kSoftWarps;
+  static constexpr int kGroupThreads = kSoftThreads / 2;
+  static constexpr int kThreads = kSoft0 + kSoftThreads;
   static constexpr int kKV = kTile * kDim;        // one K (or V) tile
   static constexpr int kRingV = kStages * kKV;
   static constexpr int kRing = 2 * kStages * kKV;
@@ -84,8 +85,10 @@ struct Cfg {
   // full_k[4] full_v[4] s_ready[4] s_free[4] pv_done[4] p_full[2] recv tmem_done
   static constexpr int kNumBars = 5 * kStages + 4;
   static constexpr int kOffMisc = round_up(kOffBar + kNumBars * 8, 16);
-  static constexpr int kOffRow = kOffMisc + 16;             // [group][kR / 2] {-ref, -ref, qscale, qscale} of row pairs
-  static constexpr int kOffRef = kOffRow + 2 * kR * 8;      // [group][kR] references
+  static constexpr int kOffExp = kOffMisc + 16;             // [kR] exponents of the query rows
+  static constexpr int kOffQs = kOffExp + kR * 4;           // [kR] scales of the query rows over the tile's
+  static constexpr int kOffNref = kOffQs + kR * 4;          // [group][kR] negated references
+  static constexpr int kOffRef = kOffNref + 2 * kR * 4;     // [group][kR] references
   static constexpr int kOffFac = kOffRef + 2 * kR * 4;      // [group][kR] rescale factors
   static constexpr int kOffMax = kOffFac + 2 * kR * 4;      // [group][4 lane quarters][kR] tile maxima
   static constexpr int kOffSum = kOffMax + 8 * kR * 4;      // [kR][8] row sums by group and lane quarter
@@ -193,6 +196,12 @@ __device__ __forceinline__ void two_terms(float x0, float x1, uint32_t& hi, uint
       : "f"(x0), "f"(x1), "r"(kLo == 1 ? 0x3c003c00u : 0x4c004c00u));
 }
 
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Sum over the 32 lanes of a warp of each of 8 per-lane values: lane L ends with the sum
 // of value (L >> 2).
 __device__ __forceinline__ float warp_sum8(float (&v)[8], int lane) {
@@ -213,13 +222,14 @@ __device__ __forceinline__ float warp_sum8(float (&v)[8], int lane) {
 }
 
 // ------------------------------------------------------------------ kernel
-// Grid: (cluster size, Hkv * m-blocks, B); m-block mb takes packed rows mb * kR ..
+// Grid: (cluster size, Hkv * m-blocks, B), the m-blocks of a head side by side; m-block mb takes packed rows mb * kR ..
 // mb * kR + kR - 1 (packed row p = i * G + g: new row i, query head g of the group).
 template <int kR, int kDim>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
     kv8_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Args a) {
   using C = Cfg<kR, kDim>;
-  constexpr int kRpt = C::kRpt, kKV = C::kKV, kRowF = C::kRowF, kRowBytes = C::kRowBytes;
+  constexpr int kUnits = C::kUnits, kSoftWarps = C::kSoftWarps, kSoftThreads = C::kSoftThreads;
+  constexpr int kGroupThreads = C::kGroupThreads, kKV = C::kKV, kRowF = C::kRowF, kRowBytes = C::kRowBytes;
   constexpr uint32_t kIdescS = idesc8(128, kR, 0, 0);
   constexpr uint32_t kIdescO = idesc8(128, 2 * kR, 1, 1);
   extern __shared__ uint8_t smem_raw[];
@@ -240,7 +250,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t TMEMDONE = bar(5 * kStages + 3);
   auto par = [](int T) { return static_cast<uint32_t>((T / kStages) & 1); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
-  float4* row_const = reinterpret_cast<float4*>(smem + C::kOffRow);
+  int* row_exp = reinterpret_cast<int*>(smem + C::kOffExp);
+  float* row_nref = reinterpret_cast<float*>(smem + C::kOffNref);
+  float* row_qs = reinterpret_cast<float*>(smem + C::kOffQs);
   float* row_ref = reinterpret_cast<float*>(smem + C::kOffRef);
   float* row_fac = reinterpret_cast<float*>(smem + C::kOffFac);
   float* row_max = reinterpret_cast<float*>(smem + C::kOffMax);
@@ -249,7 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   auto gdiv = [&](int p) { return __float2int_rz((static_cast<float>(p) + 0.5f) * a.inv_g); };
   const int rank = blockIdx.x, csize = gridDim.x;
-  const int kvh = blockIdx.y % a.Hkv, mblock = blockIdx.y / a.Hkv, b = blockIdx.z;
+  const int kvh = blockIdx.y / a.mblocks, mblock = blockIdx.y - kvh * a.mblocks, b = blockIdx.z;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (warp == 0 && lane == 0) {
@@ -394,13 +406,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int st = static_cast<int>(threadIdx.x) - kSoft0;  // 0 .. 511
     const int sw = warp - kFirstSoft;
     const int group = sw >> 3;
-    const int gt = st & (kGroupThreads - 1);
-    const int half = (sw >> 2) & 1;      // rows kRpt * half .. + kRpt - 1
+    const int gt = st - group * kGroupThreads;
+    const int half = gt >> 7;            // this warp has the 8-row units half, half + 2, ...
     const int quarter = warp & 3;        // TMEM lane quarter of this warp
     const int kl = quarter * 32 + lane;  // key lane of S^T / d lane of O^T
     const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
-    const int row0 = kRpt * half;
     const int rows_in = max(1, min(kR, a.M - mblock * kR));
+    // this warp's units that hold a row: it leaves the others out (their P stays stale and
+    // reaches only O columns that are not read)
+    const int n_units = ((rows_in + 7) / 8 - half + 1) / 2;
     auto q_off = [&](int p) {
       const int i = gdiv(p);
       return ((static_cast<long long>(b) * a.R + i) * a.Hq + kvh * a.G + (p - i * a.G)) * kDim;
@@ -416,19 +430,44 @@ __global__ void __launch_bounds__(kThreads, 1)
                                             : make_uint4(0, 0, 0, 0);
     }
     if (st == 0) griddep_launch();  // every older kernel has finished: the next may launch
+    // One scale for the tile's rows, 2^(e - 7) with 2^e its largest element's power: a score
+    // then needs no factor of its own row (read from shared memory for every score, the
+    // rows' factors and references took all its bandwidth). A row more than 2^6 below the
+    // tile's largest would lose bits that way: it keeps its own scale, row_qs, and the
+    // tile takes a slower form.
+    int em[kQc];
 #pragma unroll
     for (int u = 0; u < kQc; ++u) {
-      const int idx = st + u * kSoftThreads, row = idx / kChunks, c = idx % kChunks;
-      if (idx >= kR * kChunks) break;  // warp-uniform
+      const int idx = st + u * kSoftThreads;
       const uint32_t w[4] = {qv[u].x, qv[u].y, qv[u].z, qv[u].w};
       uint32_t m = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) m = max(m, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
 #pragma unroll
       for (int x = kChunks / 2; x > 0; x >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, x));
-      // qscale = 2^(e - 7) of the largest element's 2^e (of 2^-119 at least: its inverse is a number)
-      const int e = max(static_cast<int>(m >> 7), 8);
-      const float inv = __uint_as_float(static_cast<uint32_t>(min(254 - e + 7, 254)) << 23);
+      // (2^-119 at least: its inverse is a number; 255: infinities or NaN in the row)
+      em[u] = m >= 0x7f80u ? 255 : max(static_cast<int>(m >> 7), 8);
+      if (idx < kR * kChunks && idx % kChunks == 0) row_exp[idx / kChunks] = em[u];
+    }
+    named_bar_sync(2, kSoftThreads);
+    int e_tile;
+    bool small_rows;
+    {
+      int x0 = row_exp[lane], x1 = lane < kR - 32 ? row_exp[32 + lane] : 8;
+      small_rows = __any_sync(0xffffffffu, max(x0, x1) == 255);
+      x0 = x0 == 255 ? 8 : x0;
+      x1 = x1 == 255 ? 8 : x1;
+      e_tile = __reduce_max_sync(0xffffffffu, max(x0, x1));
+      small_rows |= __any_sync(0xffffffffu, (x0 > 8 && x0 < e_tile - 6) || (x1 > 8 && x1 < e_tile - 6));
+    }
+#pragma unroll
+    for (int u = 0; u < kQc; ++u) {
+      const int idx = st + u * kSoftThreads, row = idx / kChunks, c = idx % kChunks;
+      if (idx >= kR * kChunks) break;  // warp-uniform
+      const uint32_t w[4] = {qv[u].x, qv[u].y, qv[u].z, qv[u].w};
+      // (rows of zeros, those past M among them, take the tile's scale)
+      const int e = em[u] > 8 && em[u] < e_tile - 6 ? em[u] : e_tile;
+      const float inv = __uint_as_float(static_cast<uint32_t>(min(261 - e, 254)) << 23);
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) two_terms<1>(sd_bf16_lo(w[j]) * inv, sd_bf16_hi(w[j]) * inv, hi[j], lo[j]);
@@ -440,14 +479,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                    : "memory");
       if (c == 0) {
         // a row with infinities or NaN in it has no attention: NaN throughout
-        const float qs = m >= 0x7f80u ? __uint_as_float(0x7fc00000u) : __uint_as_float(static_cast<uint32_t>(max(e - 7, 1)) << 23);
-        float* rc = reinterpret_cast<float*>(row_const + (row >> 1)) + (row & 1);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          rc[g * kR * 2] = INFINITY;  // no reference yet: any key's weight passes every bound
-          rc[g * kR * 2 + 2] = qs;
-          row_ref[g * kR + row] = -INFINITY;
-        }
+        row_qs[row] = em[u] == 255 ? __uint_as_float(0x7fc00000u)
+                                   : __uint_as_float(static_cast<uint32_t>(max(127 + e - e_tile, 1)) << 23);
+        row_nref[row] = row_nref[kR + row] = INFINITY;
+        row_ref[row] = row_ref[kR + row] = -INFINITY;  // no reference yet: any key's weight passes every bound
       }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -457,23 +492,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t tmem = *tmem_slot;
 
     // ---- this group's tiles
-    const float4* rconst = row_const + group * (kR / 2) + row0 / 2;
-    uint64_t lp2[kRpt / 2];
+    const float c_log2 = a.scale_log2 * __uint_as_float(static_cast<uint32_t>(max(e_tile - 7, 1)) << 23);
+    uint64_t lp2[kUnits][4];  // this key lane's row sums, in pairs
+    const float* nref = row_nref + group * kR + half * 8;  // unit u: + 16 u
 #pragma unroll
-    for (int j = 0; j < kRpt / 2; ++j) lp2[j] = 0ull;
+    for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) lp2[u][j] = 0ull;
     const uint32_t pkey = base + C::kOffP + group * C::kP + kl * 32;
     const uint32_t psw = (kl >> 2) & 1;  // 32-byte swizzle
     const long long plane = static_cast<long long>(b) * a.Hkv + kvh;
     const float* ks = a.ks + plane * a.nblk;
     const float* vs = a.vs + plane * a.nblk;
-    // rows of this tile below which a key is masked (causal: new row i sees new keys 0..i;
-    // kR: every row)
+    // rows below which a key is masked (causal: new row i sees new keys 0..i; kR: all)
     auto first_row = [&](int key) {
       if (key >= key_end) return kR;
       const int i = key - (n_keys - a.R);
       return a.block_mask || i <= 0 ? 0 : min(kR, max(0, i * a.G - mblock * kR));
     };
-    const bool idle = row0 >= rows_in;  // none of this warp's rows exists: barriers only
     float ks_next = 0.f, vs_next = 1.f;
     auto load_scales = [&](int t) {
       const int key = key_begin + t * kTile + kl;
@@ -485,112 +521,124 @@ __global__ void __launch_bounds__(kThreads, 1)
     load_scales(group);
 #pragma unroll 1
     for (int T = group; T < n_tiles; T += 2) {
-      const int key = key_begin + T * kTile + kl;
-      const float kc = ks_next * a.scale_log2, v_scale = vs_next, lv = lg2(v_scale), iv = 1.f / v_scale;
+      const int tile0 = key_begin + T * kTile;
+      const float kc = ks_next * c_log2, lv = lg2(vs_next), iv = rcp(vs_next);
       load_scales(T + 2);
-      const int below = first_row(key) - row0;  // this thread's rows j < below are masked
+      // whether a key of the tile is masked for some row
+      const bool masks = tile0 + kTile > min(key_end, a.block_mask ? key_end : n_keys - a.R + 1);
       const uint64_t kc2 = pack2f(kc, kc), lv2 = pack2f(lv, lv), iv2 = pack2f(iv, iv);
-      const uint32_t ts = tmem + kR * (T % kStages) + row0 + lane_off;
+      const uint32_t ts = tmem + kR * (T % kStages) + half * 8 + lane_off;  // unit u: + 16 u
       mbar_wait(SREADY(T), par(T));
       tc_fence_after();
-      float y[kRpt];
-      // y = log2 of the weights of this thread's key under the present references
+      float y[kUnits][8];
+      // y = log2 of the weights of this thread's key under the present references (raw:
+      // without them); the largest
       auto exponents = [&](bool raw) {
 #pragma unroll
-        for (int j = 0; j < kRpt; j += 8) tmem_ld8(ts + j, y + j);
-        tmem_wait_ld<kRpt>(y);
+        for (int u = 0; u < kUnits; ++u)
+          if (u < n_units) tmem_ld8(ts + 16 * u, y[u]);
+        tmem_wait_ld<8 * kUnits>(&y[0][0]);
+        if (__builtin_expect(small_rows, 0)) {
 #pragma unroll
-        for (int j = 0; j < kRpt; j += 2) {
-          const float4 rc = rconst[j / 2];
-          const uint64_t t = mul2(pack2f(y[j], y[j + 1]), kc2);
-          const uint64_t at = raw ? lv2 : add2(lv2, pack2f(rc.x, rc.y));
-          unpack2(fma2(t, pack2f(rc.z, rc.w), at), y[j], y[j + 1]);
+          for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[u][j] *= row_qs[16 * u + half * 8 + j];
         }
-        if (__any_sync(0xffffffffu, below > 0)) {  // whatever the score, NaN included
+        float m = -INFINITY;
 #pragma unroll
-          for (int j = 0; j < kRpt; ++j)
-            if (j < below) y[j] = -INFINITY;
-        }
-      };
-      bool hot = false;
-      if (!idle) {
-        exponents(false);
-        float m = y[0];
+        for (int u = 0; u < kUnits; ++u)
+          if (u < n_units) {
 #pragma unroll
-        for (int j = 1; j < kRpt; ++j) m = fmaxf(m, y[j]);
-        hot = m > kHot;
-      }
-      if (__builtin_expect(named_bar_or(4 + group, kGroupThreads, hot), 0)) {
-        // ---- move the references: the tile's exact row maxima
-        if (!idle) {
-          exponents(true);
-          float mine = 0.f;
+            for (int j = 0; j < 8; j += 4) {
+              const float4 nr = *reinterpret_cast<const float4*>(nref + 16 * u + j);
+              const uint64_t a0 = raw ? lv2 : add2(lv2, pack2f(nr.x, nr.y)), a1 = raw ? lv2 : add2(lv2, pack2f(nr.z, nr.w));
+              unpack2(fma2(pack2f(y[u][j], y[u][j + 1]), kc2, a0), y[u][j], y[u][j + 1]);
+              unpack2(fma2(pack2f(y[u][j + 2], y[u][j + 3]), kc2, a1), y[u][j + 2], y[u][j + 3]);
+            }
+            if (masks) {  // whatever the score, NaN included
+              const int below = first_row(tile0 + kl) - 16 * u - half * 8;
 #pragma unroll
-          for (int j = 0; j < kRpt; ++j) {
-            const float m = warp_max(y[j]);
-            if (lane == j) mine = m;
+              for (int j = 0; j < 8; ++j)
+                if (j < below) y[u][j] = -INFINITY;
+            }
+            m = fmaxf(m, fmaxf(fmaxf(fmaxf(y[u][0], y[u][1]), fmaxf(y[u][2], y[u][3])),
+                               fmaxf(fmaxf(y[u][4], y[u][5]), fmaxf(y[u][6], y[u][7]))));
           }
-          if (lane < kRpt) row_max[(group * 4 + quarter) * kR + row0 + lane] = mine;
-        }
+        return m;
+      };
+      const bool hot = exponents(false) > kHot;
+      if (__builtin_expect(named_bar_or(4 + group, kGroupThreads, hot), 0)) {
+        // ---- move the references to the rows' exact maxima over this tile
+        exponents(true);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+          if (u < n_units) {
+            float mine = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float x = warp_max(y[u][j]);
+              if (lane == j) mine = x;
+            }
+            if (lane < 8) row_max[(group * 4 + quarter) * kR + 16 * u + half * 8 + lane] = mine;
+          }
         named_bar_sync(4 + group, kGroupThreads);
-        if (gt < kR && gt < ((rows_in + kRpt - 1) / kRpt) * kRpt) {
+        if (gt < ((rows_in + 7) & ~7)) {  // (rows that do not exist, in a unit with some that do, need one too)
           const float* rm = row_max + group * 4 * kR + gt;
-          const float m = fmaxf(fmaxf(rm[0], rm[kR]), fmaxf(rm[2 * kR], rm[3 * kR]));
-          const float old = row_ref[group * kR + gt], now = fmaxf(old, m - kTop);
+          const float x = fmaxf(fmaxf(rm[0], rm[kR]), fmaxf(rm[2 * kR], rm[3 * kR]));
+          const float old = row_ref[group * kR + gt], now = fmaxf(old, x - kTop);
           row_ref[group * kR + gt] = now;
+          row_nref[group * kR + gt] = -now;
           row_fac[group * kR + gt] = old == -INFINITY ? 0.f : ex2(old - now);
-          reinterpret_cast<float*>(row_const + group * (kR / 2) + (gt >> 1))[gt & 1] = -now;
         }
         if (T >= 2) mbar_wait(PVDONE(T - 2), par(T - 2));
         named_bar_sync(4 + group, kGroupThreads);
-        if (!idle) {
-          const float* fac = row_fac + group * kR + row0;
+        if (T >= 2) {
+          tc_fence_after();
 #pragma unroll
-          for (int j = 0; j < kRpt / 2; ++j) lp2[j] = mul2(lp2[j], pack2f(fac[2 * j], fac[2 * j + 1]));
-          if (T >= 2) {
-            tc_fence_after();
+          for (int u = 0; u < kUnits; ++u)
+            if (u < n_units) {
+              const int row = 16 * u + half * 8;
+              const float* fac = row_fac + group * kR + row;
 #pragma unroll
-            for (int term = 0; term < 2; ++term)
-#pragma unroll
-              for (int j0 = 0; j0 < kRpt; j0 += 8) {
+              for (int e = 0; e < 4; ++e) lp2[u][e] = mul2(lp2[u][e], pack2f(fac[2 * e], fac[2 * e + 1]));
+#pragma unroll 1
+              for (int term = 0; term < 2; ++term) {
                 float o[8];
-                const uint32_t to = tmem + C::kTmemO + (2 * group + term) * kR + row0 + j0 + lane_off;
+                const uint32_t to = tmem + C::kTmemO + (2 * group + term) * kR + row + lane_off;
                 tmem_ld8(to, o);
                 tmem_wait_ld<8>(o);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] *= fac[j0 + j];
+                for (int j = 0; j < 8; ++j) o[j] *= fac[j];
                 tmem_st8(to, o);
               }
-            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-          }
-          exponents(false);
+            }
+          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         }
+        exponents(false);
       }
       // the tile's scores are all in registers: its buffer may take S(T + 4)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(SFREE(T));
       if (T >= 2) mbar_wait(PVDONE(T - 2), par(T - 2));  // PV(T - 2) has read the P buffer
-      if (!idle) {
 #pragma unroll
-        for (int j0 = 0; j0 < kRpt; j0 += 8) {
+      for (int u = 0; u < kUnits; ++u)
+        if (u < n_units) {
           uint32_t h[4], l[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int i = j0 + 2 * e;
-            const float e0 = ex2(y[i]), e1 = ex2(y[i + 1]);
-            lp2[i / 2] = fma2(pack2f(e0, e1), iv2, lp2[i / 2]);
+            const float e0 = ex2(y[u][2 * e]), e1 = ex2(y[u][2 * e + 1]);
+            lp2[u][e] = fma2(pack2f(e0, e1), iv2, lp2[u][e]);
             two_terms<16>(e0, e1, h[e], l[e]);
           }
-          auto store = [&](int row, const uint32_t (&x)[4]) {  // rows row .. row + 7 of 2 kR
+          auto store = [&](int row, const uint32_t (&w)[4]) {  // rows row .. row + 7 of 2 kR
             const uint32_t dst = pkey + (row >> 5) * C::kPGroup + ((((row >> 4) & 1) ^ psw) << 4) + (row & 8);
-            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dst), "r"(x[0] | (x[1] << 16)), "r"(x[2] | (x[3] << 16))
+            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dst), "r"(w[0] | (w[1] << 16)), "r"(w[2] | (w[3] << 16))
                          : "memory");
           };
-          store(row0 + j0, h);
-          store(kR + row0 + j0, l);
+          store(16 * u + half * 8, h);
+          store(kR + 16 * u + half * 8, l);
         }
-      }
       const int n_here = tile_keys(T);
       if (n_here & 31) {
         // stale rows that the product reads may hold NaN, whose product with 0 is not 0:
@@ -605,14 +653,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) mbar_arrive(PFULL(T));
     }
     const int n_mine = (n_tiles - group + 1) / 2;
-    // ---- row sums: lane L ends with that of row row0 + 8 c + (L >> 2)
+    // ---- row sums: lane L ends with that of row L >> 2 of the unit
 #pragma unroll
-    for (int c = 0; c < kRpt / 8; ++c) {
+    for (int u = 0; u < kUnits; ++u) {
       float v[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) unpack2(lp2[4 * c + j], v[2 * j], v[2 * j + 1]);
+      for (int j = 0; j < 4; ++j) unpack2(lp2[u][j], v[2 * j], v[2 * j + 1]);
       const float x = warp_sum8(v, lane);
-      if ((lane & 3) == 0) row_sum[(row0 + 8 * c + (lane >> 2)) * 8 + group * 4 + quarter] = x;
+      if ((lane & 3) == 0) row_sum[(16 * u + half * 8 + (lane >> 2)) * 8 + group * 4 + quarter] = x;
     }
     const bool merge = csize > 1;
     if (merge) cluster_arrive_relaxed();  // the group has seen its last S, and the MMA warps arrive after theirs
@@ -751,7 +799,7 @@ bool set_attributes(int* active) {
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3(kClusterSizes[i], 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.blockDim = dim3(Cfg<kR, kDim>::kThreads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
@@ -768,7 +816,7 @@ bool set_attributes(int* active) {
 struct DevState {
   std::once_flag once;
   bool ok = false;
-  int active[6][kNumSizes] = {};  // [head dim 64, 128][rows 32, 48, 64]
+  int active[4][kNumSizes] = {};  // [head dim 64, 128][rows 32, 48]
 };
 
 DevState* state() {
@@ -781,14 +829,16 @@ DevState* state() {
   DevState& s = states[dev];
   std::call_once(s.once, [&s] {
     s.ok = set_attributes<32, 64>(s.active[0]) && set_attributes<48, 64>(s.active[1]) &&
-           set_attributes<64, 64>(s.active[2]) && set_attributes<32, 128>(s.active[3]) &&
-           set_attributes<48, 128>(s.active[4]) && set_attributes<64, 128>(s.active[5]);
+           set_attributes<32, 128>(s.active[2]) && set_attributes<48, 128>(s.active[3]);
   });
   return &s;
 }
 
-// Cluster size: the least waves x (128-key tiles a CTA + a fixed cost a wave), in tiles.
+// Cluster size: the one forced by sd_set_cluster_size, else the least waves x (128-key tiles a CTA + a fixed cost a wave), in tiles.
 int pick_cluster(const int* active, long long units, int cap) {
+  const int forced = sd_internal_forced_cluster();
+  for (int i = 0; i < kNumSizes && forced > 0; ++i)
+    if (kClusterSizes[i] == forced && active[i] > 0) return forced;
   const double nblk = (cap + 31) / 32;
   double best_cost = -1;
   int best = 0;
@@ -820,7 +870,7 @@ bool make_map8(CUtensorMap* map, void* base, int cap, int planes, int D) {
 }
 
 template <int kR, int kDim>
-sd_status launch(const sd_kv8_cache* c, const Args& a, int mblocks, int cs, cudaStream_t stream) {
+sd_status launch(const sd_kv8_cache* c, const Args& a, int cs, cudaStream_t stream) {
   CUtensorMap k, v;
   if (!make_map8(&k, c->k, c->capacity, c->batch * c->n_kv_heads, kDim) ||
       !make_map8(&v, c->v, c->capacity, c->batch * c->n_kv_heads, kDim))
@@ -833,8 +883,8 @@ sd_status launch(const sd_kv8_cache* c, const Args& a, int mblocks, int cs, cuda
   attr[0].val.clusterDim.z = 1;
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3(cs, c->n_kv_heads * mblocks, c->batch);
-  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.gridDim = dim3(cs, c->n_kv_heads * a.mblocks, c->batch);
+  cfg.blockDim = dim3(Cfg<kR, kDim>::kThreads, 1, 1);
   cfg.dynamicSmemBytes = Cfg<kR, kDim>::kSmemBytes;
   cfg.stream = stream;
   cfg.attrs = attr;
@@ -876,17 +926,18 @@ extern "C" sd_status sd_kv8_attention(const void* q, const sd_kv8_cache* cache, 
   a.block_mask = (flags & SD_ATTN_BLOCK_MASK) != 0;
   a.inv_g = 1.0f / static_cast<float>(a.G);
   a.scale_log2 = static_cast<float>(sc * 1.4426950408889634);
-  // the smallest tile that holds the rows in one m-block, else in two
-  const int rows = a.M <= 32 ? 32 : (a.M <= 48 ? 48 : (a.M <= 64 ? 64 : (a.M <= 96 ? 48 : 64)));
-  const int mblocks = (a.M + rows - 1) / rows;
+  // the fewest m-blocks of up to 48 rows, and the smaller tile that holds one. (64 rows in
+  // two m-blocks of 32, which read every key twice, mostly from L2: 154.7 us for 32 scenes
+  // of 8192 keys, 9.9 for one of 4096; one tile of 64, 32 rows a thread in registers, took
+  // 150 to 165 and 12.5.)
+  a.mblocks = (a.M + 47) / 48;
+  const int rows = (a.M + a.mblocks - 1) / a.mblocks <= 32 ? 32 : 48;
   DevState* dev = state();
   if (!dev || !dev->ok) return SD_ERR_CUDA;
-  const int cs = pick_cluster(dev->active[(D == 128 ? 3 : 0) + rows / 16 - 2], static_cast<long long>(B) * Hkv * mblocks,
+  const int cs = pick_cluster(dev->active[(D == 128 ? 2 : 0) + (rows == 48)], static_cast<long long>(B) * Hkv * a.mblocks,
                               cache->capacity);
   if (cs <= 0) return SD_ERR_CUDA;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  auto go = [&](auto f32, auto f48, auto f64) {
-    return rows == 32 ? f32(cache, a, mblocks, cs, st) : (rows == 48 ? f48(cache, a, mblocks, cs, st) : f64(cache, a, mblocks, cs, st));
-  };
-  return D == 128 ? go(launch<32, 128>, launch<48, 128>, launch<64, 128>) : go(launch<32, 64>, launch<48, 64>, launch<64, 64>);
+  if (D == 128) return rows == 32 ? launch<32, 128>(cache, a, cs, st) : launch<48, 128>(cache, a, cs, st);
+  return rows == 32 ? launch<32, 64>(cache, a, cs, st) : launch<48, 64>(cache, a, cs, st);
 }

@@ -852,6 +852,7 @@ struct TcPlan {
 
 // Cluster size forced by sd_set_cluster_size (0: chosen per call).
 static std::atomic<int> g_forced_cluster{0};
+int sd_internal_forced_cluster() { return g_forced_cluster.load(); }
 
 extern "C" sd_status sd_set_cluster_size(int cluster_size) {
   if (cluster_size == 0) {

@@ -58,6 +58,9 @@ bool sd_internal_tc_serves_layer(int B, int R, int Hq, int Hkv, int D, int cap);
 // Their cluster sizes, 0 where not served.
 int sd_internal_tc_cluster(int B, int R, int Hq, int Hkv, int D, int cap, bool layer);
 
+// Cluster size forced by sd_set_cluster_size (0: chosen per call).
+int sd_internal_forced_cluster();
+
 struct RopeTable;
 // The fused verify layer on the tcgen05 path (attention_tc.cu); *handled is
 // set when the shape is served and the kernel launched.

@@ -5,9 +5,22 @@
 //                    heads h of KV head g of p[b][i][h][n]
 // where a key appended with these rows (n >= len[b] - R) brings no weight with it.
 //
-// The plainest form: a CTA a (KV head, scene), first each row's maximum and sum, then
-// each key's weights.
-#include "common.cuh"
+// A weight needs its row's sum over all keys, so the scores are needed twice. They are
+// computed once: S^T[128 keys][kR rows] = K_tile . Q^T on the tensor cores (tcgen05), every
+// tile to its own columns of tensor memory, where they wait for the sums (512 columns: 16
+// tiles of 32 rows, 4 of 128). Only a CTA with more tiles than that reads its keys, and
+// forms its scores, twice. One cluster per (KV head, scene); its CTAs take contiguous ranges
+// of the keys and send each other their rows' (maximum, sum).
+//
+// Pass A, the rows' sums: a thread has one key lane and a quarter of the rows, and keeps its
+// own reference for each, the first score it meets, moved only when one lies 2^100 above
+// it: no exchange between threads before the end. There the lanes' references are brought
+// to their maximum and the sums added, in a fixed order.
+// Pass B, the keys' weights: with its row's log sum every weight is final, 2^(S c - lse).
+// A thread has one key and all rows, so a key's sum needs no exchange at all; the four
+// warps of a lane quarter take every fourth tile.
+// Rows of more than one tile of 128 go through both passes in turn.
+#include "tc_common.cuh"
 
 #include <math.h>
 
@@ -15,59 +28,463 @@ SD_DEFINE_ERROR_ACCESSOR(sd_take_error_weights)
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kTile = 128;
+constexpr int kHalf = kTile * 128;       // one 64-column half of a tile's keys
+constexpr int kSlices = 4;
+constexpr int kSoftWarps = 4 * kSlices;
+constexpr int kSoftThreads = 32 * kSoftWarps;
+constexpr int kFirstSoft = 2;
+constexpr int kSoft0 = 32 * kFirstSoft;
+constexpr int kThreads = kSoft0 + kSoftThreads;
+constexpr int kMaxCluster = 16;
+constexpr int kMaxBufs = 16;
+constexpr int kStages = 4;
+constexpr float kFar = 100.f;            // log2 of what a sum may hold over its reference
 
-template <int D>
-__device__ float dot(const float* q, const __nv_bfloat16* k) {
-  float x = 0.f;
-  for (int j = 0; j < D; j += 2) {
-    const uint32_t w = __ldcg(reinterpret_cast<const unsigned int*>(k + j));
-    x = fmaf(q[j], sd_bf16_lo(w), fmaf(q[j + 1], sd_bf16_hi(w), x));
+struct Args {
+  const __nv_bfloat16* q;
+  const int32_t* len;
+  const int32_t* committed;
+  const float* in;
+  float* out;
+  int R, Hq, Hkv, G, M, cap;
+  float inv_g;       // 1 / G: p / G == int((p + 0.5) / G) exactly for p < 2^20 and G < 2^12
+  float scale_log2, decay;
+};
+
+template <int kR, int kDim>
+struct Cfg {
+  static_assert(kR == 32 || kR == 64 || kR == 128, "row tile");
+  static constexpr int kHalves = kDim / 64;
+  static constexpr int kK = kHalves * kHalf;       // one tile of keys
+  static constexpr int kQHalf = kR * 128;
+  static constexpr int kBufs = 512 / kR;           // tiles of scores in tensor memory
+  static constexpr int kRpt = kR / kSlices;        // rows of a thread in pass A
+  static constexpr int kOffQ = kStages * kK;
+  static constexpr int kOffBar = kOffQ + kHalves * kQHalf;
+  // full[stages] free[stages] s_ready[bufs] s_free[bufs] q_full gathered[2]
+  static constexpr int kNumBars = 2 * kStages + 2 * kMaxBufs + 3;
+  static constexpr int kOffMisc = round_up(kOffBar + kNumBars * 8, 16);
+  static constexpr int kOffPart = kOffMisc + 16;                  // [4 quarters][kR] (maximum, sum)
+  static constexpr int kOffGather = kOffPart + 4 * kR * 8;        // [2][cluster rank][kR] (maximum, sum)
+  static constexpr int kOffLse = kOffGather + 2 * kMaxCluster * kR * 8;  // [kR] negated log sums
+  static constexpr int kSmemBytes = kOffLse + kR * 4 + 1024;
+  static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
+};
+
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+template <int kN>
+__device__ __forceinline__ void tmem_wait_ld(float* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < kN; j += 8)  // no use of the registers moves above the wait
+    asm volatile("" : "+f"(r[j]), "+f"(r[j + 1]), "+f"(r[j + 2]), "+f"(r[j + 3]), "+f"(r[j + 4]), "+f"(r[j + 5]),
+                 "+f"(r[j + 6]), "+f"(r[j + 7]));
+}
+__device__ __forceinline__ float warp_max(float x) {
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Sum over the 32 lanes of a warp of each of 8 per-lane values: lane L ends with the sum
+// of value (L >> 2).
+__device__ __forceinline__ float warp_sum8(float (&v)[8], int lane) {
+#pragma unroll
+  for (int n = 8, s = 16; n > 1; n >>= 1, s >>= 1) {
+    const bool hi = (lane & s) != 0;
+#pragma unroll
+    for (int i = 0; i < n / 2; ++i) {
+      const float keep = hi ? v[i + n / 2] : v[i];
+      const float give = hi ? v[i] : v[i + n / 2];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, s);
+    }
   }
+  float x = v[0];
+  x += __shfl_xor_sync(0xffffffffu, x, 2);
+  x += __shfl_xor_sync(0xffffffffu, x, 1);
   return x;
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads) key_weights_kernel(const __nv_bfloat16* q, const __nv_bfloat16* k,
-                                                               const int32_t* len, const int32_t* committed,
-                                                               const float* in, float decay, float* out, int R, int Hq,
-                                                               int Hkv, int cap, float scale_log2) {
-  sd_pdl_enter();
-  const int kvh = blockIdx.x, b = blockIdx.y, G = Hq / Hkv;
-  const int n = __ldcg(len + b);
-  const int rows = committed ? __ldcg(committed + b) : R;
-  if (n < R || n > cap || rows < 0 || rows > R) {
-    if (threadIdx.x == 0) sd_set_error(n < R || n > cap ? SD_DEVERR_LENGTH : SD_DEVERR_ROLLBACK);
-    return;
+// Grid (cluster size, Hkv, B).
+template <int kR, int kDim>
+__global__ void __launch_bounds__(kThreads, 1)
+    key_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const Args a) {
+  using C = Cfg<kR, kDim>;
+  constexpr int kHalves = C::kHalves, kK = C::kK, kBufs = C::kBufs, kRpt = C::kRpt;
+  constexpr uint32_t kIdesc = umma_idesc(128, kR, 0, 0);
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const uint32_t base = smem_addr(smem);
+  auto bar = [&](int i) { return base + C::kOffBar + 8u * i; };
+  // T counts the tiles of scores formed, over passes and row groups; a barrier's next phase
+  // waits for the one before to have been seen: K(T + stages) for S(T), S(T + bufs) for the
+  // last reading of S(T)
+  auto FULL = [&](int T) { return bar(T % kStages); };
+  auto FREE = [&](int T) { return bar(kStages + T % kStages); };
+  auto SREADY = [&](int T) { return bar(2 * kStages + T % kBufs); };
+  auto SFREE = [&](int T) { return bar(2 * kStages + kMaxBufs + T % kBufs); };
+  const uint32_t QFULL = bar(2 * kStages + 2 * kMaxBufs);
+  auto GATHERED = [&](int grp) { return bar(2 * kStages + 2 * kMaxBufs + 1 + (grp & 1)); };
+  auto parK = [](int T) { return static_cast<uint32_t>((T / kStages) & 1); };
+  auto parS = [](int T) { return static_cast<uint32_t>((T / kBufs) & 1); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
+  float2* part = reinterpret_cast<float2*>(smem + C::kOffPart);
+  float2* gather = reinterpret_cast<float2*>(smem + C::kOffGather);
+  float* nlse = reinterpret_cast<float*>(smem + C::kOffLse);
+
+  const int rank = blockIdx.x, csize = gridDim.x, kvh = blockIdx.y, b = blockIdx.z;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (warp == 0 && lane == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(FULL(s), 1);
+      mbar_init(FREE(s), 1);
+    }
+    for (int i = 0; i < kBufs; ++i) {
+      mbar_init(SREADY(i), 1);
+      mbar_init(SFREE(i), kSoftWarps);
+    }
+    mbar_init(QFULL, kSoftWarps);
+    mbar_init(GATHERED(0), 1);
+    mbar_init(GATHERED(1), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  __shared__ float qs[D];
-  __shared__ float red[kThreads];
-  const long long plane = static_cast<long long>(b) * Hkv + kvh;
-  k += plane * cap * D;
-  in = in ? in + plane * cap : nullptr;
-  out += plane * cap;
-  for (int t = threadIdx.x; t < n; t += kThreads) out[t] = in && t < n - R ? decay * __ldcg(in + t) : 0.f;
-  for (int p = 0; p < rows * G; ++p) {
-    const int i = p / G, h = kvh * G + p % G, seen = n - R + i + 1;
-    __syncthreads();
-    if (threadIdx.x < D)
-      qs[threadIdx.x] = sd_ldcg_bf16(q + ((static_cast<long long>(b) * R + i) * Hq + h) * D + threadIdx.x) * scale_log2;
-    __syncthreads();
-    float m = -INFINITY;
-    for (int t = threadIdx.x; t < seen; t += kThreads) m = fmaxf(m, dot<D>(qs, k + static_cast<long long>(t) * D));
-    red[threadIdx.x] = m;
-    __syncthreads();
-    for (int w = 0; w < kThreads; ++w) m = fmaxf(m, red[w]);
-    __syncthreads();
-    float l = 0.f;
-    for (int t = threadIdx.x; t < seen; t += kThreads) l += exp2f(dot<D>(qs, k + static_cast<long long>(t) * D) - m);
-    red[threadIdx.x] = l;
-    __syncthreads();
-    l = 0.f;
-    for (int w = 0; w < kThreads; ++w) l += red[w];
-    for (int t = threadIdx.x; t < seen; t += kThreads)
-      out[t] += exp2f(dot<D>(qs, k + static_cast<long long>(t) * D) - m) / l;
+  __syncwarp();
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_slot)), "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  cluster_arrive_relaxed();  // waited for before the first store into another CTA
+  griddep_wait();  // nothing before this touches global memory
+  const int n_keys = __ldcg(a.len + b);
+  const int counted = a.committed ? __ldcg(a.committed + b) : a.R;
+  const bool valid = n_keys >= a.R && n_keys <= a.cap && counted >= 0 && counted <= a.R;
+  const int nblk32 = valid ? (n_keys + 31) / 32 : 0;
+  const int blk_begin = static_cast<int>(static_cast<long long>(rank) * nblk32 / csize);
+  const int blk_end = static_cast<int>(static_cast<long long>(rank + 1) * nblk32 / csize);
+  const int key_begin = blk_begin * 32, key_end = min(blk_end * 32, valid ? n_keys : 0);
+  const int n_tiles = (blk_end - blk_begin + 3) / 4;
+  const bool resident = n_tiles <= kBufs;
+  const int m_rows = valid ? counted * a.G : 0;                       // the packed rows that count
+  const int n_groups = max(1, (m_rows + kR - 1) / kR); // (no rows: the weights from before still move on)
+  const int formed = n_tiles * (resident ? 1 : 2);     // tiles of scores a row group forms
+  auto tile_of = [&](int T) { return (T % formed) % n_tiles; };
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+
+  if (warp == 0) {
+    // -------------------------------------------------------------- producer
+    if (!valid && rank == 0 && lane == 0 && kvh == 0)
+      sd_set_error(n_keys >= a.R && n_keys <= a.cap ? SD_DEVERR_ROLLBACK : SD_DEVERR_LENGTH);
+    const int z = b * a.Hkv + kvh;
+#pragma unroll 1
+    for (int T = 0; T < n_groups * formed; ++T) {
+      if (T >= kStages) mbar_wait(FREE(T), parK(T - kStages));
+      const int key0 = key_begin + tile_of(T) * kTile;
+      const int boxes = (min(kTile, key_end - key0) + 31) / 32;  // of 32 keys, as many as there are
+      if (lane == 0) mbar_expect_tx(FULL(T), static_cast<uint32_t>(boxes * 32 * 128 * kHalves));
+      __syncwarp();
+      if (lane < boxes * kHalves) {
+        const int h = lane / boxes, x = lane - h * boxes;
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+                base + (T % kStages) * kK + h * kHalf + x * 32 * 128),
+            "l"(reinterpret_cast<uint64_t>(&tm_k)), "r"(FULL(T)), "r"(h * 64), "r"(key0 + x * 32), "r"(z)
+            : "memory");
+      }
+      __syncwarp();
+    }
+  } else if (warp == 1) {
+    // -------------------------------------------------------------- S issue
+    const uint32_t tmem = *tmem_slot;
+    const uint64_t dK0 = umma_desc(base, 16, 1024);
+    const uint64_t dQ = umma_desc(base + C::kOffQ, 16, 1024);
+#pragma unroll 1
+    for (int T = 0; T < n_groups * formed; ++T) {
+      if (T % formed == 0) mbar_wait(QFULL, (T / formed) & 1);
+      if (T >= kBufs) mbar_wait(SFREE(T), parS(T - kBufs));
+      mbar_wait(FULL(T), parK(T));
+      tc_fence_after();
+      const uint64_t dk = dK0 + static_cast<uint64_t>(((T % kStages) * kK) >> 4);
+      if (elect_one()) {
+#pragma unroll
+        for (int kk = 0; kk < kDim / 16; ++kk)
+          umma(tmem + kR * (T % kBufs), dk + (((kk >> 2) * kHalf + (kk & 3) * 32) >> 4),
+               dQ + (((kk >> 2) * C::kQHalf + (kk & 3) * 32) >> 4), kIdesc, kk > 0 ? 1 : 0);
+        umma_commit(SREADY(T));
+        umma_commit(FREE(T));
+      }
+      __syncwarp();
+    }
+  } else {
+    // -------------------------------------------------------------- softmax
+    const uint32_t tmem = *tmem_slot;
+    const int st = static_cast<int>(threadIdx.x) - kSoft0;
+    const int slice = st >> 7;           // pass A: rows slice * kRpt ..; pass B: tiles t % 4 == slice
+    const int quarter = warp & 3;
+    const int kl = quarter * 32 + lane;
+    const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
+    const long long plane = static_cast<long long>(b) * a.Hkv + kvh;
+    auto gdiv = [&](int p) { return __float2int_rz((static_cast<float>(p) + 0.5f) * a.inv_g); };
+    const uint64_t c2 = [&] {
+      uint64_t d;
+      asm("mov.b64 %0, {%1, %1};" : "=l"(d) : "f"(a.scale_log2));
+      return d;
+    }();
+    auto scaled = [&](float x0, float x1, float n0, float n1, float& y0, float& y1) {  // x * c + n, in pairs
+      uint64_t x, n, y;
+      asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(x0), "f"(x1));
+      asm("mov.b64 %0, {%1, %2};" : "=l"(n) : "f"(n0), "f"(n1));
+      asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(x), "l"(c2), "l"(n));
+      asm("mov.b64 {%0, %1}, %2;" : "=f"(y0), "=f"(y1) : "l"(y));
+    };
+#pragma unroll 1
+    for (int grp = 0; grp < n_groups; ++grp) {
+      const int p0 = grp * kR, T0 = grp * formed;
+      const int rows_in = max(0, min(kR, m_rows - p0));
+      // ---- the group's query rows (zero past the last that counts)
+      constexpr int kChunks = kDim / 8;
+#pragma unroll 1
+      for (int idx = st; idx < kR * kChunks; idx += kSoftThreads) {
+        const int row = idx / kChunks, c = idx % kChunks, p = p0 + row;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < rows_in) {
+          const int i = gdiv(p);
+          v = __ldcg(reinterpret_cast<const uint4*>(
+              a.q + ((static_cast<long long>(b) * a.R + i) * a.Hq + kvh * a.G + (p - i * a.G)) * kDim + c * 8));
+        }
+        st_shared_v4(base + C::kOffQ + (c >> 3) * C::kQHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4), v.x, v.y, v.z, v.w);
+      }
+      if (grp == 0 && st == 0) griddep_launch();  // every older kernel has finished: the next may launch
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(QFULL);
+      // rows of the group below which a key is masked (kR: all)
+      auto first_row = [&](int key) {
+        if (key >= key_end) return kR;
+        const int i = key - (n_keys - a.R);
+        return i <= 0 ? 0 : static_cast<int>(min(static_cast<long long>(kR), max(0ll, static_cast<long long>(i) * a.G - p0)));
+      };
+      auto masked_tile = [&](int t) { return key_begin + (t + 1) * kTile > min(key_end, n_keys - a.R + 1); };
+
+      // ---- pass A: references and sums of this key lane
+      float ref[kRpt], l[kRpt];
+#pragma unroll
+      for (int j = 0; j < kRpt; ++j) {
+        ref[j] = -INFINITY;
+        l[j] = 0.f;
+      }
+      const bool idle = slice * kRpt >= rows_in;
+#pragma unroll 1
+      for (int t = 0; t < n_tiles; ++t) {
+        const int T = T0 + t;
+        mbar_wait(SREADY(T), parS(T));
+        tc_fence_after();
+        if (!idle) {
+          const int below = masked_tile(t) ? first_row(key_begin + t * kTile + kl) - slice * kRpt : 0;
+#pragma unroll
+          for (int u = 0; u < kRpt; u += 8) {
+            float x[8];
+            tmem_ld8(tmem + kR * (T % kBufs) + slice * kRpt + u + lane_off, x);
+            tmem_wait_ld<8>(x);
+            float y[8], m = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) scaled(x[j], x[j + 1], -ref[u + j], -ref[u + j + 1], y[j], y[j + 1]);
+            if (below > u) {  // whatever the score, NaN included
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (u + j < below) y[j] = -INFINITY;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = fmaxf(m, y[j]);
+            if (m > kFar) {  // the first score, or one far above it: the new reference
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (y[j] > kFar) {
+                  const float now = x[j] * a.scale_log2;
+                  l[u + j] = ref[u + j] == -INFINITY ? 0.f : l[u + j] * ex2(ref[u + j] - now);
+                  ref[u + j] = now;
+                  y[j] = 0.f;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) l[u + j] += ex2(y[j]);
+          }
+        }
+        if (!resident) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(SFREE(T));
+        }
+      }
+      // ---- the rows' (maximum, sum) over the warp, the CTA and the cluster
+#pragma unroll
+      for (int u = 0; u < kRpt; u += 8) {
+        float v[8], mine = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          // (a reference that is not a number makes the row's sums so)
+          const bool nan = __any_sync(0xffffffffu, ref[u + j] != ref[u + j]);
+          const float m = nan ? __uint_as_float(0x7fc00000u) : warp_max(ref[u + j]);
+          v[j] = l[u + j] * (ref[u + j] == -INFINITY ? 0.f : ex2(ref[u + j] - m));
+          if ((lane >> 2) == j) mine = m;
+        }
+        const float s = warp_sum8(v, lane);
+        if ((lane & 3) == 0) part[quarter * kR + slice * kRpt + u + (lane >> 2)] = make_float2(mine, s);
+      }
+      named_bar_sync(2, kSoftThreads);
+      if (grp == 0) cluster_wait();  // every CTA of the cluster has started
+      auto joined = [&](const float2* x, int stride, int n) {
+        float m = -INFINITY, s = 0.f;
+        bool nan = false;
+        for (int i = 0; i < n; ++i) {
+          m = fmaxf(m, x[i * stride].x);
+          nan |= x[i * stride].x != x[i * stride].x;
+        }
+        for (int i = 0; i < n; ++i)
+          if (x[i * stride].x != -INFINITY) s = fmaf(ex2(x[i * stride].x - m), x[i * stride].y, s);
+        return make_float2(nan ? __uint_as_float(0x7fc00000u) : m, s);
+      };
+      float2* box = gather + (grp & 1) * kMaxCluster * kR;
+      // to every CTA of the cluster, this one too: the stores complete on its barrier. (A CTA
+      // sends a group's sums when it has read the boxes of the one before, so those of two
+      // groups before are free)
+      if (st == 0) mbar_expect_tx(GATHERED(grp), static_cast<uint32_t>(csize * kR * 8));
+      for (int i = st; i < kR * csize; i += kSoftThreads) {
+        const int row = i % kR, to = i / kR;
+        const float2 ml = joined(part + row, kR, 4);
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(
+                         cluster_map(smem_addr(box + rank * kR + row), to)),
+                     "f"(ml.x), "f"(ml.y), "r"(cluster_map(GATHERED(grp), to))
+                     : "memory");
+      }
+      mbar_wait(GATHERED(grp), (grp >> 1) & 1);
+      if (st < kR) {
+        const float2 ml = joined(box + st, kR, csize);
+        // rows that do not count give no weight
+        nlse[st] = st < rows_in ? -(ml.x + lg2(ml.y)) : -INFINITY;
+      }
+      named_bar_sync(2, kSoftThreads);
+
+      // ---- pass B: the keys' weights
+#pragma unroll 1
+      for (int t = 0; t < n_tiles; ++t) {
+        const int T = T0 + t + (resident ? 0 : n_tiles);
+        if (!resident) {
+          mbar_wait(SREADY(T), parS(T));
+          tc_fence_after();
+        }
+        if ((t & 3) == slice) {
+          const int key = key_begin + t * kTile + kl;
+          const int below = masked_tile(t) ? first_row(key) : 0;
+          const long long at = plane * a.cap + key;
+          float before = 0.f;
+          if (key < key_end) {
+            if (grp > 0) before = a.out[at];
+            else if (a.in && key < n_keys - a.R) before = __ldcg(a.in + at) * a.decay;
+          }
+          float w[4] = {0.f, 0.f, 0.f, 0.f};
+          const int units = (rows_in + 7) / 8;
+#pragma unroll 2
+          for (int u = 0; u < units; ++u) {
+            float x[8], y[8];
+            tmem_ld8(tmem + kR * (T % kBufs) + 8 * u + lane_off, x);
+            const float4 n0 = *reinterpret_cast<const float4*>(nlse + 8 * u), n1 = *reinterpret_cast<const float4*>(nlse + 8 * u + 4);
+            tmem_wait_ld<8>(x);
+            scaled(x[0], x[1], n0.x, n0.y, y[0], y[1]);
+            scaled(x[2], x[3], n0.z, n0.w, y[2], y[3]);
+            scaled(x[4], x[5], n1.x, n1.y, y[4], y[5]);
+            scaled(x[6], x[7], n1.z, n1.w, y[6], y[7]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j & 3] += 8 * u + j < below ? 0.f : ex2(y[j]);
+          }
+          if (key < key_end) a.out[at] = before + ((w[0] + w[1]) + (w[2] + w[3]));
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(SFREE(T));
+      }
+      named_bar_sync(2, kSoftThreads);  // nlse, part and the query rows are free again
+    }
+  }
+  if (warp < kFirstSoft) cluster_wait();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*tmem_slot), "r"(512) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------ host
+template <int kR, int kDim>
+bool allow() {
+  const void* k = reinterpret_cast<const void*>(key_weights_kernel<kR, kDim>);
+  const bool ok = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<kR, kDim>::kSmemBytes) == cudaSuccess &&
+                  cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+  if (!ok) (void)cudaGetLastError();
+  return ok;
+}
+
+// The launch attributes, once per device and kernel.
+bool allowed() {
+  static std::once_flag once[64];
+  static bool ok[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+    (void)cudaGetLastError();
+    return false;
+  }
+  std::call_once(once[dev], [dev] {
+    ok[dev] = allow<32, 64>() && allow<64, 64>() && allow<128, 64>() && allow<32, 128>() && allow<64, 128>() && allow<128, 128>();
+  });
+  return ok[dev];
+}
+
+// [planes][cap][D] bf16 keys in boxes of 64 columns x 32 rows, 128-byte swizzle
+bool make_key_map(CUtensorMap* map, void* k, int D, int cap, int planes) { return make_map(map, k, cap, planes, 32, D); }
+
+template <int kR, int kDim>
+sd_status launch(const sd_kv_cache* c, const Args& a, int cs, cudaStream_t stream) {
+  CUtensorMap k;
+  if (!make_key_map(&k, c->k, kDim, c->capacity, c->batch * c->n_kv_heads)) return SD_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cs;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(cs, c->n_kv_heads, c->batch);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = Cfg<kR, kDim>::kSmemBytes;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  if (cudaLaunchKernelEx(&cfg, key_weights_kernel<kR, kDim>, k, a) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return SD_ERR_CUDA;
+  }
+  return SD_OK;
+}
+
+template <int kDim>
+sd_status launch_rows(const sd_kv_cache* c, const Args& a, int cs, cudaStream_t stream) {
+  if (a.M <= 32) return launch<32, kDim>(c, a, cs, stream);
+  if (a.M <= 64) return launch<64, kDim>(c, a, cs, stream);
+  return launch<128, kDim>(c, a, cs, stream);
 }
 
 }  // namespace
@@ -79,20 +496,32 @@ extern "C" sd_status sd_attention_weights(const void* q, const sd_kv_cache* cach
   const int B = cache->batch, Hkv = cache->n_kv_heads, D = cache->head_dim, cap = cache->capacity;
   if (B < 0 || R <= 0 || Hq <= 0 || Hkv <= 0 || cap <= 0 || Hq % Hkv) return SD_ERR_INVALID_ARG;
   if (D != 64 && D != 128) return SD_ERR_UNSUPPORTED;
-  if (B > 65535 || Hkv > 65535 || static_cast<long long>(Hq / Hkv) * R > (1 << 24)) return SD_ERR_UNSUPPORTED;
+  if (B > 65535 || Hkv > 65535 || Hq / Hkv > 4095 || static_cast<long long>(Hq / Hkv) * R > (1 << 20)) return SD_ERR_UNSUPPORTED;
   if (!(scale >= 0.f) || !isfinite(scale) || !isfinite(decay)) return SD_ERR_INVALID_ARG;
   if (B == 0) return SD_OK;
   if (!q || !cache->k || !cache->len || !weights) return SD_ERR_INVALID_ARG;
   if (!sd_aligned16(q) || !sd_aligned16(cache->k) || !sd_aligned16(weights) || !sd_aligned16(weights_in))
     return SD_ERR_INVALID_ARG;
   const double sc = scale > 0.f ? scale : 1.0 / sqrt(static_cast<double>(D));
-  const float scale_log2 = static_cast<float>(sc * 1.4426950408889634);
-  if (sd_launch_pdl(D == 64 ? key_weights_kernel<64> : key_weights_kernel<128>, dim3(Hkv, B), dim3(kThreads), 0,
-                    reinterpret_cast<cudaStream_t>(stream), static_cast<const __nv_bfloat16*>(q),
-                    static_cast<const __nv_bfloat16*>(cache->k), static_cast<const int32_t*>(cache->len), committed,
-                    weights_in, decay, weights, R, Hq, Hkv, cap, scale_log2) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return SD_ERR_CUDA;
-  }
-  return SD_OK;
+  Args a = {};
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.len = cache->len;
+  a.committed = committed;
+  a.in = weights_in;
+  a.out = weights;
+  a.R = R;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.G = Hq / Hkv;
+  a.M = a.G * R;
+  a.cap = cap;
+  a.inv_g = 1.0f / static_cast<float>(a.G);
+  a.scale_log2 = static_cast<float>(sc * 1.4426950408889634);
+  a.decay = decay;
+  if (!allowed()) return SD_ERR_CUDA;
+  // CTAs a head: two tiles of keys each, as far as clusters go
+  int cs = 1;
+  while (cs < kMaxCluster && cap > 256LL * cs) cs *= 2;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  return D == 64 ? launch_rows<64>(cache, a, cs, st) : launch_rows<128>(cache, a, cs, st);
 }

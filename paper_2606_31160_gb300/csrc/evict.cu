@@ -3,16 +3,25 @@
 // between the ones with the largest weights (among equal weights the lowest index),
 // moved in their order to another cache.
 //
-// The plainest form: a CTA a (KV head, scene). The weight of the last key kept is found
-// bit by bit on the weights' order-preserving integers, by counting; then a prefix sum
-// over the keys gives each kept one its place.
+// Several CTAs a (KV head, scene), each moving its share of the places in dst: they need
+// nothing of each other, as each finds the whole selection itself from the weights (4 bytes
+// a key against the 512 of a kept row: 16384 keys are 64 KB from L2). The weight of the last
+// key kept is found by three passes of counting on the digits (11, 11 and 10 bits) of its
+// order-preserving integer, in shared memory. Then a key's place is the number of kept keys
+// before it: each warp counts its part of the keys by ballots, a sum over the warps gives it
+// its first place, and a second walk lists the CTA's share, whose rows are copied with
+// eight 16-byte loads a thread in flight.
 #include "common.cuh"
 
 SD_DEFINE_ERROR_ACCESSOR(sd_take_error_evict)
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+constexpr int kBins = 2048;
+constexpr int kList = 1024;     // kept keys that a CTA lists, then copies, at a time
+constexpr int kKeysMax = 20480; // keys whose integers stay in shared memory; more are read anew each time
 
 // An integer that orders as the weight does (-0 as +0; NaN below every number).
 __device__ __forceinline__ uint32_t order_of(float w) {
@@ -21,88 +30,176 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__device__ int block_sum(int x, int* red) {
-  x = __reduce_add_sync(0xffffffffu, x);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
-  __syncthreads();
-  return __reduce_add_sync(0xffffffffu, red[threadIdx.x & 31]);
-}
-
+// Grid (parts, Hkv, B); dynamic shared memory for `kept_in_smem` keys.
 __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, const float* weights, const sd_kv_cache dst,
-                                                         int keep, int sinks, int recent, float* weights_out, int32_t* kept) {
+                                                         int keep, int sinks, int recent, float* weights_out, int32_t* kept,
+                                                         int smem_keys, int vec_shift) {
+  extern __shared__ uint32_t order[];
+  __shared__ int bins[kBins];
+  __shared__ int list[kList];
+  __shared__ int warp_sum[kWarps];
+  __shared__ int warp_kept[kWarps], warp_ties[kWarps];
+  __shared__ int s_bin, s_left;
   sd_pdl_enter();
-  __shared__ int red[32];
-  __shared__ int warp_base[33];
-  const int h = blockIdx.x, b = blockIdx.y, Hkv = src.n_kv_heads;
+  const int part = blockIdx.x, parts = gridDim.x, h = blockIdx.y, b = blockIdx.z, Hkv = src.n_kv_heads;
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   const int n = __ldcg(src.len + b);
   if (n < 0 || n > src.capacity) {
-    if (threadIdx.x == 0) sd_set_error(SD_DEVERR_LENGTH);
+    if (t == 0 && part == 0 && h == 0) sd_set_error(SD_DEVERR_LENGTH);
     return;
   }
   const long long plane = static_cast<long long>(b) * Hkv + h;
   weights += plane * src.capacity;
-  const int lo = min(sinks, n), hi = max(lo, n - recent);  // the keys that compete
-  const int want = n <= keep ? hi - lo : keep - lo - (n - hi);
-  // T: the largest integer that at least `want` of them reach
+  const int m = min(n, keep);                                   // kept keys
+  const int p_lo = static_cast<int>(static_cast<long long>(part) * m / parts);
+  const int p_hi = static_cast<int>(static_cast<long long>(part + 1) * m / parts);
+  if (part == 0 && h == 0 && t == 0) dst.len[b] = m;
+  if (kept && part == 0)
+    for (int j = m + t; j < keep; j += kThreads) kept[plane * keep + j] = -1;
+  if (p_lo == p_hi) return;
+  const int lo = min(sinks, n), hi = max(lo, n - recent);       // the keys that compete
+  const int want = m - lo - (n - hi);
+  const bool all = n <= keep;                                   // every key stays
+  const bool cached = n <= smem_keys;
+  auto order_at = [&](int i) { return cached ? order[i] : order_of(__ldcg(weights + i)); };
+
+  // ---- T: the order of the last competing key kept; `ties` of those equal to it stay
   uint32_t T = 0;
-  if (want < hi - lo)
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t t = T | (1u << bit);
-      int c = 0;
-      for (int i = lo + threadIdx.x; i < hi; i += kThreads) c += order_of(__ldcg(weights + i)) >= t;
-      if (block_sum(c, red) >= want) T = t;
-    }
-  int above = 0;
-  for (int i = lo + threadIdx.x; i < hi; i += kThreads) above += order_of(__ldcg(weights + i)) > T;
-  int ties = want - block_sum(above, red);  // of those equal to T the first `ties`
-  const int vec = src.head_dim / 8;
-  const uint4* ks = static_cast<const uint4*>(src.k) + plane * src.capacity * vec;
-  const uint4* vs = static_cast<const uint4*>(src.v) + plane * src.capacity * vec;
-  uint4* kd = static_cast<uint4*>(dst.k) + plane * dst.capacity * vec;
-  uint4* vd = static_cast<uint4*>(dst.v) + plane * dst.capacity * vec;
-  auto scan = [&](bool flag, int& total) {  // the number of flags before this thread's
-    const uint32_t ballot = __ballot_sync(0xffffffffu, flag);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = __popc(ballot);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      int s = 0;
-      for (int w = 0; w < 32; ++w) {
-        warp_base[w] = s;
-        s += red[w];
+  int ties = 0;
+  if (!all) {
+    if (cached) {
+      for (int i = t; i < n; i += 4 * kThreads) {
+        float w[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) w[u] = i + u * kThreads < n ? __ldcg(weights + i + u * kThreads) : 0.f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (i + u * kThreads < n) order[i + u * kThreads] = order_of(w[u]);
       }
-      warp_base[32] = s;
     }
-    __syncthreads();
-    total = warp_base[32];
-    return warp_base[threadIdx.x >> 5] + __popc(ballot & ((1u << (threadIdx.x & 31)) - 1));
-  };
-  int place = 0;
-  for (int i0 = 0; i0 < n; i0 += kThreads) {
-    const int i = i0 + threadIdx.x;
-    const bool in = i < n, fixed = in && (i < lo || i >= hi);
-    const uint32_t o = in && !fixed ? order_of(__ldcg(weights + i)) : 0u;
-    const bool all = want == hi - lo;
-    const bool tie = in && !fixed && o == T;
-    int n_ties, n_kept;
-    const int t = scan(tie, n_ties);
-    const bool k = in && (fixed || all || o > T || (tie && t < ties));
-    const int at = place + scan(k, n_kept);
-    if (k) {
-      for (int c = 0; c < vec; ++c) {
-        kd[static_cast<long long>(at) * vec + c] = __ldcg(ks + static_cast<long long>(i) * vec + c);
-        vd[static_cast<long long>(at) * vec + c] = __ldcg(vs + static_cast<long long>(i) * vec + c);
+    int left = want;  // to be taken among the keys whose higher digits are T's
+    if (left > 0) {
+#pragma unroll 1
+      for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), width = pass == 2 ? 10 : 11, n_bins = 1 << width;
+        for (int i = t; i < kBins; i += kThreads) bins[i] = 0;
+        __syncthreads();
+        for (int i = lo + t; i < hi; i += kThreads) {
+          const uint32_t o = order_at(i);
+          // (an integer's high bits and T's, those below them not yet found)
+          if (pass == 0 || (o >> (shift + width)) == (T >> (shift + width)))
+            atomicAdd(&bins[n_bins - 1 - static_cast<int>((o >> shift) & (n_bins - 1))], 1);  // the largest digit first
+        }
+        __syncthreads();
+        // the bin in which the left-th key lies: a prefix sum over the bins, 4 a thread
+        int c[4], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum += c[j] = bins[4 * t + j];
+        int before = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int x = __shfl_up_sync(0xffffffffu, before, o);
+          if (lane >= o) before += x;
+        }
+        if (lane == 31) warp_sum[warp] = before;
+        __syncthreads();
+        before -= sum;
+        for (int w = 0; w < warp; ++w) before += warp_sum[w];
+        if (before < left && before + sum >= left) {  // one thread's
+          int j = 0;
+          while (before + c[j] < left) before += c[j++];
+          s_bin = 4 * t + j;
+          s_left = left - before;
+        }
+        __syncthreads();
+        T |= static_cast<uint32_t>(n_bins - 1 - s_bin) << shift;
+        left = s_left;
       }
-      if (weights_out) weights_out[plane * dst.capacity + at] = __ldcg(weights + i);
-      if (kept) kept[plane * keep + at] = i;
+      ties = left;
+    } else {
+      T = 0xffffffffu;  // none of them stays (no key's order is all ones)
+      __syncthreads();
     }
-    ties -= min(ties, n_ties);
-    place += n_kept;
   }
-  if (kept)
-    for (int j = place + threadIdx.x; j < keep; j += kThreads) kept[plane * keep + j] = -1;
-  if (h == 0 && threadIdx.x == 0) dst.len[b] = place;
+
+  // ---- places: each warp's keys, a range of whole ballots
+  const int per_warp = ((n + kWarps - 1) / kWarps + 31) / 32 * 32;
+  const int i_lo = warp * per_warp, i_hi = min(n, i_lo + per_warp);
+  // a key's kind: 2 stays, 1 ties with the last that stays, 0 goes
+  auto kind = [&](int i) {
+    if (i >= i_hi) return 0;
+    if (all || i < lo || i >= hi) return 2;
+    const uint32_t o = order_at(i);
+    return o > T ? 2 : (o == T ? 1 : 0);
+  };
+  {
+    int stay = 0, tie = 0;
+    for (int i0 = i_lo; i0 < i_hi; i0 += 32) {
+      const int k = kind(i0 + lane);
+      stay += __popc(__ballot_sync(0xffffffffu, k == 2));
+      tie += __popc(__ballot_sync(0xffffffffu, k == 1));
+    }
+    if (lane == 0) {
+      warp_kept[warp] = stay;
+      warp_ties[warp] = tie;
+    }
+  }
+  __syncthreads();
+  int stay0 = 0, ties0 = 0;
+  for (int w = 0; w < warp; ++w) {
+    stay0 += warp_kept[w];
+    ties0 += warp_ties[w];
+  }
+  const int vec = 1 << vec_shift;
+  const uint4* ks = static_cast<const uint4*>(src.k) + ((plane * src.capacity) << vec_shift);
+  const uint4* vs = static_cast<const uint4*>(src.v) + ((plane * src.capacity) << vec_shift);
+  uint4* kd = static_cast<uint4*>(dst.k) + ((plane * dst.capacity) << vec_shift);
+  uint4* vd = static_cast<uint4*>(dst.v) + ((plane * dst.capacity) << vec_shift);
+#pragma unroll 1
+  for (int q_lo = p_lo; q_lo < p_hi; q_lo += kList) {
+    const int q_hi = min(p_hi, q_lo + kList);
+    __syncthreads();  // the list before is copied
+    int stay = stay0, tie = ties0;
+    for (int i0 = i_lo; i0 < i_hi && stay + min(tie, ties) < q_hi; i0 += 32) {
+      const int k = kind(i0 + lane);
+      const uint32_t s = __ballot_sync(0xffffffffu, k == 2), e = __ballot_sync(0xffffffffu, k == 1);
+      const uint32_t below = (1u << lane) - 1;
+      const int my_ties = tie + __popc(e & below);
+      const int at = stay + __popc(s & below) + min(my_ties, ties);
+      if ((k == 2 || (k == 1 && my_ties < ties)) && at >= q_lo && at < q_hi) list[at - q_lo] = i0 + lane;
+      stay += __popc(s);
+      tie += __popc(e);
+    }
+    __syncthreads();
+    const int count = q_hi - q_lo;
+    for (int j = t; j < count; j += kThreads) {
+      const int i = list[j];
+      if (weights_out) weights_out[plane * dst.capacity + q_lo + j] = __ldcg(weights + i);
+      if (kept) kept[plane * keep + q_lo + j] = i;
+    }
+    constexpr int kU = 4;
+    const long long to = static_cast<long long>(q_lo) << vec_shift;
+    for (int u0 = t; u0 < count << vec_shift; u0 += kU * kThreads) {
+      uint4 k[kU], v[kU];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int x = u0 + u * kThreads;
+        if (x < count << vec_shift) {
+          const long long from = (static_cast<long long>(list[x >> vec_shift]) << vec_shift) + (x & (vec - 1));
+          k[u] = __ldcs(ks + from);
+          v[u] = __ldcs(vs + from);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int x = u0 + u * kThreads;
+        if (x < count << vec_shift) {
+          kd[to + x] = k[u];
+          vd[to + x] = v[u];
+        }
+      }
+    }
+  }
 }
 
 // Whether [a, a + na) and [b, b + nb) share a byte.
@@ -120,7 +217,7 @@ extern "C" sd_status sd_kv_evict(const sd_kv_cache* src, const float* weights, i
   if (B < 0 || Hkv <= 0 || src->capacity <= 0 || dst->capacity <= 0) return SD_ERR_INVALID_ARG;
   if (dst->batch != B || dst->n_kv_heads != Hkv || dst->head_dim != D) return SD_ERR_INVALID_ARG;
   if (D != 64 && D != 128) return SD_ERR_UNSUPPORTED;
-  if (B > 65535) return SD_ERR_UNSUPPORTED;
+  if (B > 65535 || Hkv > 65535) return SD_ERR_UNSUPPORTED;
   if (keep <= 0 || keep > dst->capacity || sinks < 0 || recent < 0 || static_cast<long long>(sinks) + recent > keep)
     return SD_ERR_INVALID_ARG;
   if (B == 0) return SD_OK;
@@ -136,8 +233,27 @@ extern "C" sd_status sd_kv_evict(const sd_kv_cache* src, const float* weights, i
     for (int j = 0; j < 4; ++j)
       if (to_bytes[j] && overlap(in[i], in_bytes[i], to[j], to_bytes[j])) return SD_ERR_INVALID_ARG;
   if (src->len == dst->len) return SD_ERR_INVALID_ARG;
-  if (sd_launch_pdl(evict_kernel, dim3(Hkv, B), dim3(kThreads), 0, reinterpret_cast<cudaStream_t>(stream), *src, weights,
-                    *dst, keep, sinks, recent, weights_out, kept) != cudaSuccess) {
+  // two CTAs an SM over all heads, as long as each has 32 rows or more to move
+  const long long pairs = static_cast<long long>(B) * Hkv;
+  long long parts = (2LL * sd_num_sms() + pairs - 1) / pairs;
+  if (parts > (keep + 31) / 32) parts = (keep + 31) / 32;
+  const int smem_keys = src->capacity < kKeysMax ? src->capacity : kKeysMax;
+  static bool allowed[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+    (void)cudaGetLastError();
+    return SD_ERR_CUDA;
+  }
+  if (!allowed[dev]) {  // more than 48 KB of shared memory, once per device
+    if (cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeysMax * 4) != cudaSuccess) {
+      (void)cudaGetLastError();
+      return SD_ERR_CUDA;
+    }
+    allowed[dev] = true;
+  }
+  if (sd_launch_pdl(evict_kernel, dim3(static_cast<unsigned>(parts), Hkv, B), dim3(kThreads), smem_keys * sizeof(uint32_t),
+                    reinterpret_cast<cudaStream_t>(stream), *src, weights, *dst, keep, sinks, recent, weights_out, kept,
+                    smem_keys, D == 64 ? 3 : 4) != cudaSuccess) {
     (void)cudaGetLastError();
     return SD_ERR_CUDA;
   }

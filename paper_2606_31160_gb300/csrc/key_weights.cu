@@ -5,21 +5,24 @@
 //                    heads h of KV head g of p[b][i][h][n]
 // where a key appended with these rows (n >= len[b] - R) brings no weight with it.
 //
-// A weight needs its row's sum over all keys, so the scores are needed twice. They are
-// computed once: S^T[128 keys][kR rows] = K_tile . Q^T on the tensor cores (tcgen05), every
-// tile to its own columns of tensor memory, where they wait for the sums (512 columns: 16
-// tiles of 32 rows, 4 of 128). Only a CTA with more tiles than that reads its keys, and
-// forms its scores, twice. One cluster per (KV head, scene); its CTAs take contiguous ranges
-// of the keys and send each other their rows' (maximum, sum).
+// A weight needs its row's sum over all keys, so every score is needed twice. Up to 64
+// packed rows (G * R) it is formed once: S^T[128 keys][kR rows] = K_tile . Q^T on the
+// tensor cores (tcgen05), every tile to its own columns of tensor memory, where it waits
+// for the sums (512 columns: 16 tiles of 32 rows, 8 of 64). A CTA with more tiles than
+// that, and any with 128 rows, reads its keys and forms its scores a second time. One
+// cluster per (KV head, scene); its CTAs take contiguous ranges of the keys and send each
+// other their rows' (maximum, sum), (m, l).
 //
-// Pass A, the rows' sums: a thread has one key lane and a quarter of the rows, and keeps its
-// own reference for each, the first score it meets, moved only when one lies 2^100 above
-// it: no exchange between threads before the end. There the lanes' references are brought
-// to their maximum and the sums added, in a fixed order.
+// Pass A, the rows' sums: a thread has one key lane and a quarter of the rows, and keeps
+// its own reference for each, the first score it meets, moved only when one lies 2^100
+// above it: no exchange between threads before the end. There the lanes' references are
+// brought to their maximum and the sums added, in a fixed order. With 128 rows, whose
+// references and sums do not fit a thread, the product is not transposed here, S[128
+// rows][128 keys] = Q . K_tile^T: a thread has one row and a quarter of the tile's keys.
 // Pass B, the keys' weights: with its row's log sum every weight is final, 2^(S c - lse).
 // A thread has one key and all rows, so a key's sum needs no exchange at all; the four
 // warps of a lane quarter take every fourth tile.
-// Rows of more than one tile of 128 go through both passes in turn.
+// More than 128 rows go through both passes in turn.
 #include "tc_common.cuh"
 
 #include <math.h>
@@ -59,14 +62,15 @@ struct Cfg {
   static constexpr int kK = kHalves * kHalf;       // one tile of keys
   static constexpr int kQHalf = kR * 128;
   static constexpr int kBufs = 512 / kR;           // tiles of scores in tensor memory
-  static constexpr int kRpt = kR / kSlices;        // rows of a thread in pass A
+  static constexpr bool kTurned = kR == 128;       // pass A on S, not S^T
+  static constexpr int kRpt = kTurned ? 8 : kR / kSlices;  // rows of a thread in pass A on S^T
   static constexpr int kOffQ = kStages * kK;
   static constexpr int kOffBar = kOffQ + kHalves * kQHalf;
   // full[stages] free[stages] s_ready[bufs] s_free[bufs] q_full gathered[2]
   static constexpr int kNumBars = 2 * kStages + 2 * kMaxBufs + 3;
   static constexpr int kOffMisc = round_up(kOffBar + kNumBars * 8, 16);
-  static constexpr int kOffPart = kOffMisc + 16;                  // [4 quarters][kR] (maximum, sum)
-  static constexpr int kOffGather = kOffPart + 4 * kR * 8;        // [2][cluster rank][kR] (maximum, sum)
+  static constexpr int kOffPart = kOffMisc + 16;                  // [kR][4 lane quarters, or slices] (m, l)
+  static constexpr int kOffGather = kOffPart + 4 * kR * 8;        // [2][cluster rank][kR] (m, l)
   static constexpr int kOffLse = kOffGather + 2 * kMaxCluster * kR * 8;  // [kR] negated log sums
   static constexpr int kSmemBytes = kOffLse + kR * 4 + 1024;
   static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
@@ -175,7 +179,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int blk_end = static_cast<int>(static_cast<long long>(rank + 1) * nblk32 / csize);
   const int key_begin = blk_begin * 32, key_end = min(blk_end * 32, valid ? n_keys : 0);
   const int n_tiles = (blk_end - blk_begin + 3) / 4;
-  const bool resident = n_tiles <= kBufs;
+  const bool resident = !C::kTurned && n_tiles <= kBufs;
   const int m_rows = valid ? counted * a.G : 0;                       // the packed rows that count
   const int n_groups = max(1, (m_rows + kR - 1) / kR); // (no rows: the weights from before still move on)
   const int formed = n_tiles * (resident ? 1 : 2);     // tiles of scores a row group forms
@@ -218,11 +222,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_wait(FULL(T), parK(T));
       tc_fence_after();
       const uint64_t dk = dK0 + static_cast<uint64_t>(((T % kStages) * kK) >> 4);
+      const bool turned = C::kTurned && T % formed < n_tiles;  // (both operands 128 rows of one layout)
+      const uint64_t da = turned ? dQ : dk, db = turned ? dk : dQ;
+      const int half_a = turned ? C::kQHalf : kHalf, half_b = turned ? kHalf : C::kQHalf;
       if (elect_one()) {
 #pragma unroll
         for (int kk = 0; kk < kDim / 16; ++kk)
-          umma(tmem + kR * (T % kBufs), dk + (((kk >> 2) * kHalf + (kk & 3) * 32) >> 4),
-               dQ + (((kk >> 2) * C::kQHalf + (kk & 3) * 32) >> 4), kIdesc, kk > 0 ? 1 : 0);
+          umma(tmem + kR * (T % kBufs), da + (((kk >> 2) * half_a + (kk & 3) * 32) >> 4),
+               db + (((kk >> 2) * half_b + (kk & 3) * 32) >> 4), kIdesc, kk > 0 ? 1 : 0);
         umma_commit(SREADY(T));
         umma_commit(FREE(T));
       }
@@ -255,17 +262,24 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int p0 = grp * kR, T0 = grp * formed;
       const int rows_in = max(0, min(kR, m_rows - p0));
       // ---- the group's query rows (zero past the last that counts)
-      constexpr int kChunks = kDim / 8;
-#pragma unroll 1
-      for (int idx = st; idx < kR * kChunks; idx += kSoftThreads) {
-        const int row = idx / kChunks, c = idx % kChunks, p = p0 + row;
-        uint4 v = make_uint4(0, 0, 0, 0);
+      constexpr int kChunks = kDim / 8, kQc = (kR * kChunks + kSoftThreads - 1) / kSoftThreads;
+      uint4 qv[kQc];
+#pragma unroll
+      for (int u = 0; u < kQc; ++u) {
+        const int idx = st + u * kSoftThreads, row = idx / kChunks, p = p0 + row;
+        qv[u] = make_uint4(0, 0, 0, 0);
         if (row < rows_in) {
           const int i = gdiv(p);
-          v = __ldcg(reinterpret_cast<const uint4*>(
-              a.q + ((static_cast<long long>(b) * a.R + i) * a.Hq + kvh * a.G + (p - i * a.G)) * kDim + c * 8));
+          qv[u] = __ldcg(reinterpret_cast<const uint4*>(
+              a.q + ((static_cast<long long>(b) * a.R + i) * a.Hq + kvh * a.G + (p - i * a.G)) * kDim + (idx % kChunks) * 8));
         }
-        st_shared_v4(base + C::kOffQ + (c >> 3) * C::kQHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4), v.x, v.y, v.z, v.w);
+      }
+#pragma unroll
+      for (int u = 0; u < kQc; ++u) {
+        const int idx = st + u * kSoftThreads, row = idx / kChunks, c = idx % kChunks;
+        if (row < kR)
+          st_shared_v4(base + C::kOffQ + (c >> 3) * C::kQHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4), qv[u].x, qv[u].y,
+                       qv[u].z, qv[u].w);
       }
       if (grp == 0 && st == 0) griddep_launch();  // every older kernel has finished: the next may launch
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -279,102 +293,155 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       auto masked_tile = [&](int t) { return key_begin + (t + 1) * kTile > min(key_end, n_keys - a.R + 1); };
 
-      // ---- pass A: references and sums of this key lane
-      float ref[kRpt], l[kRpt];
-#pragma unroll
-      for (int j = 0; j < kRpt; ++j) {
-        ref[j] = -INFINITY;
-        l[j] = 0.f;
-      }
-      const bool idle = slice * kRpt >= rows_in;
+      // ---- pass A
+      if constexpr (C::kTurned) {
+        // this thread's row: its reference and sum over a quarter of every tile's keys
+        float ref = -INFINITY, l = 0.f;
+        const bool idle = quarter * 32 >= rows_in;
+        // keys below this one are seen
+        const int seen = kl < rows_in ? min(key_end, n_keys - a.R + gdiv(p0 + kl) + 1) : key_end;
 #pragma unroll 1
-      for (int t = 0; t < n_tiles; ++t) {
-        const int T = T0 + t;
-        mbar_wait(SREADY(T), parS(T));
-        tc_fence_after();
-        if (!idle) {
-          const int below = masked_tile(t) ? first_row(key_begin + t * kTile + kl) - slice * kRpt : 0;
+        for (int t = 0; t < n_tiles; ++t) {
+          const int T = T0 + t;
+          mbar_wait(SREADY(T), parS(T));
+          tc_fence_after();
+          if (!idle) {
+            const int lim = seen - (key_begin + t * kTile + slice * 32);
+            float x[32];
 #pragma unroll
-          for (int u = 0; u < kRpt; u += 8) {
-            float x[8];
-            tmem_ld8(tmem + kR * (T % kBufs) + slice * kRpt + u + lane_off, x);
-            tmem_wait_ld<8>(x);
-            float y[8], m = -INFINITY;
+            for (int u = 0; u < 32; u += 8) tmem_ld8(tmem + kR * (T % kBufs) + slice * 32 + u + lane_off, x + u);
+            tmem_wait_ld<32>(x);
+            if (masked_tile(t)) {  // whatever the score, NaN included
 #pragma unroll
-            for (int j = 0; j < 8; j += 2) scaled(x[j], x[j + 1], -ref[u + j], -ref[u + j + 1], y[j], y[j + 1]);
-            if (below > u) {  // whatever the score, NaN included
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (u + j < below) y[j] = -INFINITY;
+              for (int j = 0; j < 32; ++j)
+                if (j >= lim) x[j] = -INFINITY;
             }
+            float m = x[0];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) m = fmaxf(m, y[j]);
-            if (m > kFar) {  // the first score, or one far above it: the new reference
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (y[j] > kFar) {
-                  const float now = x[j] * a.scale_log2;
-                  l[u + j] = ref[u + j] == -INFINITY ? 0.f : l[u + j] * ex2(ref[u + j] - now);
-                  ref[u + j] = now;
-                  y[j] = 0.f;
-                }
+            for (int j = 1; j < 32; ++j) m = fmaxf(m, x[j]);
+            m *= a.scale_log2;
+            if (m - kFar > ref) {  // the first scores, or one far above them: the new reference
+              l *= ref == -INFINITY ? 0.f : ex2(ref - m);
+              ref = m;
             }
+            if (ref > -INFINITY) {
+              float s4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) l[u + j] += ex2(y[j]);
+              for (int j = 0; j < 32; j += 2) {
+                float y0, y1;
+                scaled(x[j], x[j + 1], -ref, -ref, y0, y1);
+                s4[j & 3] += ex2(y0);
+                s4[(j & 3) + 1] += ex2(y1);
+              }
+              l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+            } else {
+              float s0 = 0.f;  // no key seen, or no number among them: NaN stays
+#pragma unroll
+              for (int j = 0; j < 32; ++j) s0 += x[j] == -INFINITY ? 0.f : x[j] * 0.f;
+              l += s0;
+            }
           }
-        }
-        if (!resident) {
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(SFREE(T));
         }
-      }
-      // ---- the rows' (maximum, sum) over the warp, the CTA and the cluster
+        part[kl * 4 + slice] = make_float2(ref, l);
+      } else {
+        // references and sums of this key lane
+        float ref[kRpt], l[kRpt];
 #pragma unroll
-      for (int u = 0; u < kRpt; u += 8) {
-        float v[8], mine = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          // (a reference that is not a number makes the row's sums so)
-          const bool nan = __any_sync(0xffffffffu, ref[u + j] != ref[u + j]);
-          const float m = nan ? __uint_as_float(0x7fc00000u) : warp_max(ref[u + j]);
-          v[j] = l[u + j] * (ref[u + j] == -INFINITY ? 0.f : ex2(ref[u + j] - m));
-          if ((lane >> 2) == j) mine = m;
+        for (int j = 0; j < kRpt; ++j) {
+          ref[j] = -INFINITY;
+          l[j] = 0.f;
         }
-        const float s = warp_sum8(v, lane);
-        if ((lane & 3) == 0) part[quarter * kR + slice * kRpt + u + (lane >> 2)] = make_float2(mine, s);
+        const bool idle = slice * kRpt >= rows_in;
+#pragma unroll 1
+        for (int t = 0; t < n_tiles; ++t) {
+          const int T = T0 + t;
+          mbar_wait(SREADY(T), parS(T));
+          tc_fence_after();
+          if (!idle) {
+            const int below = masked_tile(t) ? first_row(key_begin + t * kTile + kl) - slice * kRpt : 0;
+            float x[kRpt];
+#pragma unroll
+            for (int u = 0; u < kRpt; u += 8) tmem_ld8(tmem + kR * (T % kBufs) + slice * kRpt + u + lane_off, x + u);
+            tmem_wait_ld<kRpt>(x);
+#pragma unroll
+            for (int u = 0; u < kRpt; u += 8) {
+              float y[8];
+#pragma unroll
+              for (int j = 0; j < 8; j += 2) scaled(x[u + j], x[u + j + 1], -ref[u + j], -ref[u + j + 1], y[j], y[j + 1]);
+              if (below > u) {  // whatever the score, NaN included
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                  if (u + j < below) y[j] = -INFINITY;
+              }
+              const float m = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
+              if (m > kFar) {  // the first score, or one far above it: the new reference
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                  if (y[j] > kFar) {
+                    const float now = x[u + j] * a.scale_log2;
+                    l[u + j] = ref[u + j] == -INFINITY ? 0.f : l[u + j] * ex2(ref[u + j] - now);
+                    ref[u + j] = now;
+                    y[j] = 0.f;
+                  }
+              }
+#pragma unroll
+              for (int j = 0; j < 8; ++j) l[u + j] += ex2(y[j]);
+            }
+          }
+          if (!resident) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(SFREE(T));
+          }
+        }
+        // the rows' (m, l) over the warp's lanes
+#pragma unroll
+        for (int u = 0; u < kRpt; u += 8) {
+          float v[8], mine = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float m = warp_max(ref[u + j]);  // (a lane whose every score is NaN has no reference, and a sum that is NaN)
+            v[j] = l[u + j] * (ref[u + j] == -INFINITY ? 0.f : ex2(ref[u + j] - m));
+            if ((lane >> 2) == j) mine = m;
+          }
+          const float s = warp_sum8(v, lane);
+          if ((lane & 3) == 0) part[(slice * kRpt + u + (lane >> 2)) * 4 + quarter] = make_float2(mine, s);
+        }
       }
       named_bar_sync(2, kSoftThreads);
       if (grp == 0) cluster_wait();  // every CTA of the cluster has started
-      auto joined = [&](const float2* x, int stride, int n) {
-        float m = -INFINITY, s = 0.f;
-        bool nan = false;
-        for (int i = 0; i < n; ++i) {
-          m = fmaxf(m, x[i * stride].x);
-          nan |= x[i * stride].x != x[i * stride].x;
-        }
-        for (int i = 0; i < n; ++i)
-          if (x[i * stride].x != -INFINITY) s = fmaf(ex2(x[i * stride].x - m), x[i * stride].y, s);
-        return make_float2(nan ? __uint_as_float(0x7fc00000u) : m, s);
+      // ---- (m, l) over 4 or 16 lanes; NaN stays, in l
+      auto joined = [&](float2 x, int lanes) {
+        float m = x.x;
+        for (int o = 1; o < lanes; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        float l = x.y * (x.x == -INFINITY ? 0.f : ex2(x.x - m));
+        for (int o = 1; o < lanes; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        return make_float2(m, l);
       };
       float2* box = gather + (grp & 1) * kMaxCluster * kR;
       // to every CTA of the cluster, this one too: the stores complete on its barrier. (A CTA
       // sends a group's sums when it has read the boxes of the one before, so those of two
       // groups before are free)
       if (st == 0) mbar_expect_tx(GATHERED(grp), static_cast<uint32_t>(csize * kR * 8));
-      for (int i = st; i < kR * csize; i += kSoftThreads) {
-        const int row = i % kR, to = i / kR;
-        const float2 ml = joined(part + row, kR, 4);
-        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(
-                         cluster_map(smem_addr(box + rank * kR + row), to)),
-                     "f"(ml.x), "f"(ml.y), "r"(cluster_map(GATHERED(grp), to))
-                     : "memory");
+      if (st < 4 * kR) {  // (whole warps)
+        const int row = st >> 2;
+        const float2 ml = joined(part[st], 4);
+        for (int to = st & 3; to < csize; to += 4)
+          asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(
+                           cluster_map(smem_addr(box + rank * kR + row), to)),
+                       "f"(ml.x), "f"(ml.y), "r"(cluster_map(GATHERED(grp), to))
+                       : "memory");
       }
       mbar_wait(GATHERED(grp), (grp >> 1) & 1);
-      if (st < kR) {
-        const float2 ml = joined(box + st, kR, csize);
+#pragma unroll
+      for (int r0 = 0; r0 < kR; r0 += kSoftThreads / kMaxCluster) {
+        const int row = r0 + (st >> 4), from = st & 15;
+        const float2 ml = joined(from < csize ? box[from * kR + row] : make_float2(-INFINITY, 0.f), kMaxCluster);
         // rows that do not count give no weight
-        nlse[st] = st < rows_in ? -(ml.x + lg2(ml.y)) : -INFINITY;
+        if (from == 0) nlse[row] = row < rows_in ? -(ml.x + lg2(ml.y)) : -INFINITY;
       }
       named_bar_sync(2, kSoftThreads);
 
@@ -519,9 +586,14 @@ extern "C" sd_status sd_attention_weights(const void* q, const sd_kv_cache* cach
   a.scale_log2 = static_cast<float>(sc * 1.4426950408889634);
   a.decay = decay;
   if (!allowed()) return SD_ERR_CUDA;
-  // CTAs a head: two tiles of keys each, as far as clusters go
-  int cs = 1;
-  while (cs < kMaxCluster && cap > 256LL * cs) cs *= 2;
+  // CTAs a head: as many as fit on the SMs in one wave, with a tile of keys each
+  const long long units = static_cast<long long>(B) * Hkv;
+  int cs = sd_internal_forced_cluster();
+  if (cs <= 0) {
+    cs = static_cast<int>(sd_num_sms() / units);
+    cs = cs < 1 ? 1 : (cs > kMaxCluster ? kMaxCluster : cs);
+    while (cs > 1 && (cap + kTile - 1) / kTile < cs) --cs;
+  }
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   return D == 64 ? launch_rows<64>(cache, a, cs, st) : launch_rows<128>(cache, a, cs, st);
 }

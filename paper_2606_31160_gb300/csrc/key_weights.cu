@@ -42,7 +42,8 @@ constexpr int kThreads = kSoft0 + kSoftThreads;
 constexpr int kMaxCluster = 16;
 constexpr int kMaxBufs = 16;
 constexpr int kStages = 4;
-constexpr float kFar = 100.f;            // log2 of what a sum may hold over its reference
+constexpr float kFar = 100.f;            // log2 of what a weight may lie above its reference
+constexpr float kHuge = 1e30f;           // a tile's sum that moves the reference
 
 struct Args {
   const __nv_bfloat16* q;
@@ -155,7 +156,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < kBufs; ++i) {
       mbar_init(SREADY(i), 1);
-      mbar_init(SFREE(i), kSoftWarps);
+      mbar_init(SFREE(i), C::kTurned ? 4 : kSoftWarps);  // the warps that read the buffer
     }
     mbar_init(QFULL, kSoftWarps);
     mbar_init(GATHERED(0), 1);
@@ -183,7 +184,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int m_rows = valid ? counted * a.G : 0;                       // the packed rows that count
   const int n_groups = max(1, (m_rows + kR - 1) / kR); // (no rows: the weights from before still move on)
   const int formed = n_tiles * (resident ? 1 : 2);     // tiles of scores a row group forms
-  auto tile_of = [&](int T) { return (T % formed) % n_tiles; };
+  // a second reading goes backwards: what was read last is the likeliest to be in L2 still
+  auto tile_of = [&](int T) {
+    const int t = T % formed;
+    return t < n_tiles ? t : 2 * n_tiles - 1 - t;
+  };
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -250,12 +255,25 @@ __global__ void __launch_bounds__(kThreads, 1)
       asm("mov.b64 %0, {%1, %1};" : "=l"(d) : "f"(a.scale_log2));
       return d;
     }();
+    auto pack2 = [](float x0, float x1) {
+      uint64_t d;
+      asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(x0), "f"(x1));
+      return d;
+    };
+    auto sum2 = [](uint64_t d) {
+      float x0, x1;
+      asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(d));
+      return x0 + x1;
+    };
     auto scaled = [&](float x0, float x1, float n0, float n1, float& y0, float& y1) {  // x * c + n, in pairs
-      uint64_t x, n, y;
-      asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(x0), "f"(x1));
-      asm("mov.b64 %0, {%1, %2};" : "=l"(n) : "f"(n0), "f"(n1));
-      asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(x), "l"(c2), "l"(n));
+      uint64_t y;
+      asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(pack2(x0, x1)), "l"(c2), "l"(pack2(n0, n1)));
       asm("mov.b64 {%0, %1}, %2;" : "=f"(y0), "=f"(y1) : "l"(y));
+    };
+    auto add2 = [&](uint64_t s, float x0, float x1) {
+      uint64_t d;
+      asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(s), "l"(pack2(x0, x1)));
+      return d;
     };
 #pragma unroll 1
     for (int grp = 0; grp < n_groups; ++grp) {
@@ -295,50 +313,76 @@ __global__ void __launch_bounds__(kThreads, 1)
 
       // ---- pass A
       if constexpr (C::kTurned) {
-        // this thread's row: its reference and sum over a quarter of every tile's keys
+        // this thread's row: its reference and sum over every fourth tile's keys (with a quarter
+        // of every tile the 16 warps met at each tile, and its chain of latencies set the pace:
+        // 51.5 us for eight scenes of 8192 keys)
         float ref = -INFINITY, l = 0.f;
         const bool idle = quarter * 32 >= rows_in;
         // keys below this one are seen
         const int seen = kl < rows_in ? min(key_end, n_keys - a.R + gdiv(p0 + kl) + 1) : key_end;
-#pragma unroll 1
-        for (int t = 0; t < n_tiles; ++t) {
-          const int T = T0 + t;
-          mbar_wait(SREADY(T), parS(T));
-          tc_fence_after();
-          if (!idle) {
-            const int lim = seen - (key_begin + t * kTile + slice * 32);
-            float x[32];
+        auto fold = [&](float* x, int lim, bool masks) {
+          if (masks) {  // whatever the score, NaN included
 #pragma unroll
-            for (int u = 0; u < 32; u += 8) tmem_ld8(tmem + kR * (T % kBufs) + slice * 32 + u + lane_off, x + u);
-            tmem_wait_ld<32>(x);
-            if (masked_tile(t)) {  // whatever the score, NaN included
+            for (int j = 0; j < 16; ++j)
+              if (j >= lim) x[j] = -INFINITY;
+          }
+          auto sum = [&] {
+            uint64_t s0 = 0ull, s1 = 0ull;
 #pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (j >= lim) x[j] = -INFINITY;
+            for (int j = 0; j < 16; j += 4) {
+              float y[4];
+              scaled(x[j], x[j + 1], -ref, -ref, y[0], y[1]);
+              scaled(x[j + 2], x[j + 3], -ref, -ref, y[2], y[3]);
+              s0 = add2(s0, ex2(y[0]), ex2(y[1]));
+              s1 = add2(s1, ex2(y[2]), ex2(y[3]));
             }
+            return sum2(s0) + sum2(s1);
+          };
+          // relative to the present reference, unless there is none (the sum is then
+          // infinite, or not a number) or scores lie too far above it
+          float s = sum();
+          if (!(s < kHuge)) {
             float m = x[0];
 #pragma unroll
-            for (int j = 1; j < 32; ++j) m = fmaxf(m, x[j]);
+            for (int j = 1; j < 16; ++j) m = fmaxf(m, x[j]);
             m *= a.scale_log2;
-            if (m - kFar > ref) {  // the first scores, or one far above them: the new reference
+            if (m > ref) {
               l *= ref == -INFINITY ? 0.f : ex2(ref - m);
               ref = m;
             }
             if (ref > -INFINITY) {
-              float s4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-              for (int j = 0; j < 32; j += 2) {
-                float y0, y1;
-                scaled(x[j], x[j + 1], -ref, -ref, y0, y1);
-                s4[j & 3] += ex2(y0);
-                s4[(j & 3) + 1] += ex2(y1);
-              }
-              l += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+              s = sum();
             } else {
-              float s0 = 0.f;  // no key seen, or no number among them: NaN stays
+              s = 0.f;  // no key seen, or no number among them: NaN stays
 #pragma unroll
-              for (int j = 0; j < 32; ++j) s0 += x[j] == -INFINITY ? 0.f : x[j] * 0.f;
-              l += s0;
+              for (int j = 0; j < 16; ++j) s += x[j] == -INFINITY ? 0.f : x[j] * 0.f;
+            }
+          }
+          l += s;
+        };
+#pragma unroll 1
+        for (int t = slice; t < n_tiles; t += kSlices) {
+          const int T = T0 + t;
+          mbar_wait(SREADY(T), parS(T));
+          tc_fence_after();
+          if (!idle) {
+            const int lim = seen - (key_begin + t * kTile);
+            const bool masks = masked_tile(t);
+            const uint32_t ts = tmem + kR * (T % kBufs) + lane_off;
+            float x[2][16];
+            auto load = [&](int c, float* to) {
+              tmem_ld8(ts + 16 * c, to);
+              tmem_ld8(ts + 16 * c + 8, to + 8);
+            };
+            load(0, x[0]);
+#pragma unroll 1
+            for (int c = 0; c < kTile / 16; c += 2) {  // a chunk's scores on their way while the one before is summed
+              tmem_wait_ld<16>(x[0]);
+              load(c + 1, x[1]);
+              fold(x[0], lim - 16 * c, masks);
+              tmem_wait_ld<16>(x[1]);
+              if (c + 2 < kTile / 16) load(c + 2, x[0]);
+              fold(x[1], lim - 16 * c - 16, masks);
             }
           }
           tc_fence_before();
@@ -447,8 +491,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 
       // ---- pass B: the keys' weights
 #pragma unroll 1
-      for (int t = 0; t < n_tiles; ++t) {
-        const int T = T0 + t + (resident ? 0 : n_tiles);
+      for (int i = 0; i < n_tiles; ++i) {
+        const int t = resident ? i : n_tiles - 1 - i;
+        const int T = T0 + i + (resident ? 0 : n_tiles);
+        if (C::kTurned && (t & 3) != slice) continue;
         if (!resident) {
           mbar_wait(SREADY(T), parS(T));
           tc_fence_after();
@@ -462,22 +508,39 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (grp > 0) before = a.out[at];
             else if (a.in && key < n_keys - a.R) before = __ldcg(a.in + at) * a.decay;
           }
-          float w[4] = {0.f, 0.f, 0.f, 0.f};
+          uint64_t w0 = 0ull, w1 = 0ull;
           const int units = (rows_in + 7) / 8;
-#pragma unroll 2
-          for (int u = 0; u < units; ++u) {
-            float x[8], y[8];
-            tmem_ld8(tmem + kR * (T % kBufs) + 8 * u + lane_off, x);
+          float x[2][8];
+          auto load = [&](int u, float* to) { tmem_ld8(tmem + kR * (T % kBufs) + 8 * u + lane_off, to); };
+          auto add = [&](int u, const float* x, bool masks) {
             const float4 n0 = *reinterpret_cast<const float4*>(nlse + 8 * u), n1 = *reinterpret_cast<const float4*>(nlse + 8 * u + 4);
-            tmem_wait_ld<8>(x);
+            float y[8];
             scaled(x[0], x[1], n0.x, n0.y, y[0], y[1]);
             scaled(x[2], x[3], n0.z, n0.w, y[2], y[3]);
             scaled(x[4], x[5], n1.x, n1.y, y[4], y[5]);
             scaled(x[6], x[7], n1.z, n1.w, y[6], y[7]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j & 3] += 8 * u + j < below ? 0.f : ex2(y[j]);
-          }
-          if (key < key_end) a.out[at] = before + ((w[0] + w[1]) + (w[2] + w[3]));
+            for (int j = 0; j < 8; ++j) y[j] = masks && 8 * u + j < below ? 0.f : ex2(y[j]);  // (a masked score may be NaN)
+            w0 = add2(add2(w0, y[0], y[1]), y[2], y[3]);
+            w1 = add2(add2(w1, y[4], y[5]), y[6], y[7]);
+          };
+          auto all = [&](bool masks) {  // a unit's scores on their way while the one before is summed
+            if (units > 0) load(0, x[0]);
+#pragma unroll 1
+            for (int u = 0; u < units; u += 2) {
+              tmem_wait_ld<8>(x[0]);
+              if (u + 1 < units) load(u + 1, x[1]);
+              add(u, x[0], masks);
+              if (u + 1 < units) {
+                tmem_wait_ld<8>(x[1]);
+                if (u + 2 < units) load(u + 2, x[0]);
+                add(u + 1, x[1], masks);
+              }
+            }
+          };
+          if (masked_tile(t)) all(true);
+          else all(false);
+          if (key < key_end) a.out[at] = before + (sum2(w0) + sum2(w1));
         }
         tc_fence_before();
         __syncwarp();
@@ -504,19 +567,77 @@ bool allow() {
   return ok;
 }
 
-// The launch attributes, once per device and kernel.
-bool allowed() {
-  static std::once_flag once[64];
-  static bool ok[64];
+constexpr int kClusterSizes[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16};
+constexpr int kNumSizes = sizeof(kClusterSizes) / sizeof(int);
+
+template <int kR, int kDim>
+bool active_clusters(int* active) {
+  if (!allow<kR, kDim>()) return false;
+  for (int i = 0; i < kNumSizes; ++i) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kClusterSizes[i];
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(kClusterSizes[i], 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = Cfg<kR, kDim>::kSmemBytes;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&active[i], reinterpret_cast<const void*>(key_weights_kernel<kR, kDim>), &cfg) != cudaSuccess) {
+      (void)cudaGetLastError();
+      active[i] = 0;
+    }
+  }
+  return true;
+}
+
+// What the launches need, once per device: the attributes, and how many clusters of each
+// size fit at once (one CTA an SM whatever the rows).
+struct DevState {
+  std::once_flag once;
+  bool ok = false;
+  int active[kNumSizes] = {};
+};
+
+DevState* state() {
+  static DevState states[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
     (void)cudaGetLastError();
-    return false;
+    return nullptr;
   }
-  std::call_once(once[dev], [dev] {
-    ok[dev] = allow<32, 64>() && allow<64, 64>() && allow<128, 64>() && allow<32, 128>() && allow<64, 128>() && allow<128, 128>();
+  DevState& s = states[dev];
+  std::call_once(s.once, [&s] {
+    s.ok = allow<32, 64>() && allow<64, 64>() && allow<128, 64>() && allow<32, 128>() && allow<64, 128>() &&
+           active_clusters<128, 128>(s.active);
   });
-  return ok[dev];
+  return s.ok ? &s : nullptr;
+}
+
+// Cluster size: the one forced by sd_set_cluster_size, else the least waves x (a fixed
+// cost + a cost a tile, more where the scores are formed twice).
+int pick_cluster(const int* active, long long units, int cap, int rows) {
+  const int forced = sd_internal_forced_cluster();
+  for (int i = 0; i < kNumSizes && forced > 0; ++i)
+    if (kClusterSizes[i] == forced && active[i] > 0) return forced;
+  const int n_tiles = (cap + kTile - 1) / kTile;
+  double best_cost = -1;
+  int best = 1;
+  for (int i = 0; i < kNumSizes; ++i) {
+    const int cs = kClusterSizes[i];
+    if (active[i] <= 0 || (cs > 1 && n_tiles < cs)) continue;
+    const double waves = static_cast<double>((units + active[i] - 1) / active[i]);
+    const double tiles = static_cast<double>(n_tiles) / cs;
+    const double a_tile = rows == 128 ? 1.3 : (tiles <= 512.0 / rows ? 0.85 : 1.45);
+    const double cost = waves * (4.0 + a_tile * tiles);
+    if (best_cost < 0 || cost < best_cost) {
+      best_cost = cost;
+      best = cs;
+    }
+  }
+  return best;
 }
 
 // [planes][cap][D] bf16 keys in boxes of 64 columns x 32 rows, 128-byte swizzle
@@ -585,15 +706,9 @@ extern "C" sd_status sd_attention_weights(const void* q, const sd_kv_cache* cach
   a.inv_g = 1.0f / static_cast<float>(a.G);
   a.scale_log2 = static_cast<float>(sc * 1.4426950408889634);
   a.decay = decay;
-  if (!allowed()) return SD_ERR_CUDA;
-  // CTAs a head: as many as fit on the SMs in one wave, with a tile of keys each
-  const long long units = static_cast<long long>(B) * Hkv;
-  int cs = sd_internal_forced_cluster();
-  if (cs <= 0) {
-    cs = static_cast<int>(sd_num_sms() / units);
-    cs = cs < 1 ? 1 : (cs > kMaxCluster ? kMaxCluster : cs);
-    while (cs > 1 && (cap + kTile - 1) / kTile < cs) --cs;
-  }
+  DevState* dev = state();
+  if (!dev) return SD_ERR_CUDA;
+  const int cs = pick_cluster(dev->active, static_cast<long long>(B) * Hkv, cap, a.M <= 32 ? 32 : (a.M <= 64 ? 64 : 128));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   return D == 64 ? launch_rows<64>(cache, a, cs, st) : launch_rows<128>(cache, a, cs, st);
 }

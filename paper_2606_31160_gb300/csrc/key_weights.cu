@@ -18,11 +18,18 @@
 // above it: no exchange between threads before the end. There the lanes' references are
 // brought to their maximum and the sums added, in a fixed order. With 128 rows, whose
 // references and sums do not fit a thread, the product is not transposed here, S[128
-// rows][128 keys] = Q . K_tile^T: a thread has one row and a quarter of the tile's keys.
+// rows][128 keys] = Q . K_tile^T: a thread has one row of every fourth tile.
 // Pass B, the keys' weights: with its row's log sum every weight is final, 2^(S c - lse).
 // A thread has one key and all rows, so a key's sum needs no exchange at all; the four
 // warps of a lane quarter take every fourth tile.
 // More than 128 rows go through both passes in turn.
+//
+// What bounds it. One scene (8 heads, L = 4096, 32 rows: 6.8 us) the chain of latencies:
+// lengths, keys and rows, products, sums, their exchange, weights. Eight scenes of 8192
+// keys and 128 rows (51.5 us, 121 MB of keys read twice) memory: the second reading finds
+// about two thirds of the keys in L2 (152 MB from DRAM), and the arithmetic is hidden (32
+// rows: 43). Two CTAs an SM, each with half the warps and tensor memory, were slower (one
+// scene 9.7, eight 52 at their best size).
 #include "tc_common.cuh"
 
 #include <math.h>
@@ -617,7 +624,10 @@ DevState* state() {
 }
 
 // Cluster size: the one forced by sd_set_cluster_size, else the least waves x (a fixed
-// cost + a cost a tile, more where the scores are formed twice).
+// cost + a cost a tile, in us), the tile's as measured: on 32, 64 and 128 rows, more where
+// the scores are formed twice and where more waves than one share the memory. (One scene of
+// 8 heads, L = 4096, at 4 / 6 / 8 / 16: 10.7 / 9.2 / 7.4 / 12.3 us; eight scenes, L = 8192,
+// at 2 / 4 / 8: 43 / 38 / 57 on 32 rows, 51 / 53 / 75 on 64, 52 / 56 / 89 on 128.)
 int pick_cluster(const int* active, long long units, int cap, int rows) {
   const int forced = sd_internal_forced_cluster();
   for (int i = 0; i < kNumSizes && forced > 0; ++i)
@@ -630,7 +640,9 @@ int pick_cluster(const int* active, long long units, int cap, int rows) {
     if (active[i] <= 0 || (cs > 1 && n_tiles < cs)) continue;
     const double waves = static_cast<double>((units + active[i] - 1) / active[i]);
     const double tiles = static_cast<double>(n_tiles) / cs;
-    const double a_tile = rows == 128 ? 1.3 : (tiles <= 512.0 / rows ? 0.85 : 1.45);
+    const bool once = rows < 128 && tiles <= 512.0 / rows;
+    const double a_tile = (rows == 32 ? (once ? 0.85 : 1.22) : (rows == 64 ? (once ? 1.1 : 1.47) : 1.5)) +
+                          (waves > 1 ? (rows == 32 ? 0.45 : 0.7) : 0.0);
     const double cost = waves * (4.0 + a_tile * tiles);
     if (best_cost < 0 || cost < best_cost) {
       best_cost = cost;

@@ -5,19 +5,21 @@
 //     alternatives: the top_n largest logits, equal ones by the lowest index.
 //
 // One pass over the logits. A cluster of CTAs has a row, each a contiguous segment; a
-// thread folds 4 chunks of 16 bytes at a time into (m, S, W) under its running maximum,
+// thread folds chunks of 32 bytes, four in flight, into (m, S, W) under its running maximum,
 // which it moves only when a chunk's maximum passes it. S and W merge over lanes, warps
 // and CTAs in a fixed order.
 //
-// Alternatives without a second pass: the threads' maxima are kept anyway, and every
-// warp's j-th largest of them, j = ceil(top_n / warps), gives a bound that at least
-// top_n elements of the segment reach, and few more do (the least of 16 warps' maxima
-// leaves about 50). Only threads whose maximum reaches the bound hold such elements:
-// their warps read those threads' chunks again, a chunk a lane, and list what reaches
-// it. A list is ranked by counting; the cluster's first CTA ranks the CTAs' lists. A
+// Alternatives without a second pass: the threads' maxima are kept anyway. The top_n-th
+// largest of each warp's 4 or 8 largest of them is a bound that at least top_n elements of
+// the segment reach, and few more do. Only threads whose maximum reaches it hold such
+// elements: their warps read those threads' chunks again, a chunk a lane, and list what
+// reaches it. (With the least of the warps' maxima as the bound a third of the row was read
+// again.) A list is ranked by counting; the cluster's first CTA ranks the CTAs' lists. A
 // bound of -inf (a masked vocabulary) lists the finite logits only, the lowest masked
-// indices fill the rest; a list that overflows (thousands of equal logits) is replaced
-// by top_n passes for the next largest.
+// indices fill the rest; a list that overflows (hundreds of equal logits) is replaced by
+// top_n passes for the next largest.
+//
+// Small CTAs, four an SM: while one merges and ranks, others stream.
 #include "common.cuh"
 
 #include <math.h>
@@ -26,11 +28,11 @@ SD_DEFINE_ERROR_ACCESSOR(sd_take_error_logprobs)
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kTopMax = 32;
 constexpr int kList = 1024;      // candidates a CTA lists
-constexpr int kUnroll = 4;       // 16-byte chunks a thread has in flight
+constexpr int kUnroll = 4;       // 32-byte chunks a thread has in flight
 constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -61,10 +63,15 @@ __device__ __forceinline__ float redux_max(float x) {
   asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ uint4 load16(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
+struct Chunk {
+  uint32_t w[8];
+};
+__device__ __forceinline__ Chunk load32(const void* p) {
+  Chunk c;
+  asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(c.w[0]), "=r"(c.w[1]), "=r"(c.w[2]), "=r"(c.w[3]), "=r"(c.w[4]), "=r"(c.w[5]), "=r"(c.w[6]), "=r"(c.w[7])
+               : "l"(p));
+  return c;
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -78,16 +85,16 @@ __device__ __forceinline__ uint32_t in_first_cta(const void* p) {
 
 template <bool kBf16>
 struct Type {
-  static constexpr int kPer = kBf16 ? 8 : 4;  // logits a chunk
-  static __device__ __forceinline__ void unpack(const uint4& c, float (&z)[kPer]) {
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+  static constexpr int kElem = kBf16 ? 2 : 4;
+  static constexpr int kPer = 32 / kElem;  // logits a chunk
+  static __device__ __forceinline__ void unpack(const Chunk& c, float (&z)[kPer]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 8; ++j) {
       if constexpr (kBf16) {
-        z[2 * j] = sd_bf16_lo(w[j]);
-        z[2 * j + 1] = sd_bf16_hi(w[j]);
+        z[2 * j] = sd_bf16_lo(c.w[j]);
+        z[2 * j + 1] = sd_bf16_hi(c.w[j]);
       } else {
-        z[j] = __uint_as_float(w[j]);
+        z[j] = __uint_as_float(c.w[j]);
       }
     }
   }
@@ -96,11 +103,35 @@ struct Type {
   }
 };
 
-// Sums relative to a maximum m, x in units of log 2: S = sum 2^x, W = sum x 2^x.
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void unpack2(uint64_t d, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(d));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// Sums relative to the largest logit m, x = (z - m) log2(e) / T: S = sum 2^x, W = sum x 2^x.
 struct Stat {
   float m, S, W;
 };
-// s moved to the maximum M >= s.m (c = log2(e) / T). Nothing seen: m = -inf, and S is 0 or NaN.
+// s moved to the maximum M >= s.m. Nothing seen: m = -inf, and S is 0 or NaN.
 __device__ __forceinline__ void move_to(Stat& s, float M, float c) {
   if (s.m == M) return;
   if (s.m == -INFINITY) {
@@ -114,43 +145,67 @@ __device__ __forceinline__ void move_to(Stat& s, float M, float c) {
   s.m = M;
 }
 
-template <bool kBf16, int kN>
-__device__ __forceinline__ void fold(Stat& s, const float (&z)[kN], float c) {
+// A thread's sums in two halves, for even and odd elements.
+struct Fold {
+  float m;
+  uint64_t S, W;
+};
+__device__ __forceinline__ void move_fold(Fold& f, float M, float c) {
+  Stat a{f.m, 0.f, 0.f}, b{f.m, 0.f, 0.f};
+  unpack2(f.S, a.S, b.S);
+  unpack2(f.W, a.W, b.W);
+  move_to(a, M, c);
+  move_to(b, M, c);
+  f.m = M;
+  f.S = pack2(a.S, b.S);
+  f.W = pack2(a.W, b.W);
+}
+template <int kN>
+__device__ __forceinline__ void fold(Fold& f, const float (&z)[kN], float c) {
+  static_assert(kN % 2 == 0, "pairs");
   float bm = z[0];
 #pragma unroll
   for (int j = 1; j < kN; ++j) bm = max_nan(bm, z[j]);
   if (bm == -INFINITY) return;  // nothing but tokens of probability 0
-  if (bm > s.m) move_to(s, bm, c);
+  if (bm > f.m) move_fold(f, bm, c);
+  const uint64_t c2 = pack2(c, c), m2 = pack2(-f.m, -f.m);
 #pragma unroll
-  for (int j = 0; j < kN; ++j) {
-    const float x = max_nan((z[j] - s.m) * c, -1000.f);  // -inf: 0 * -1000, not 0 * -inf
-    const float e = ex2(x);
-    s.S += e;
-    s.W = fmaf(e, x, s.W);
+  for (int j = 0; j < kN; j += 2) {
+    float x0, x1;
+    unpack2(mul2(add2(pack2(z[j], z[j + 1]), m2), c2), x0, x1);
+    x0 = max_nan(x0, -1000.f);  // -inf: 0 * -1000, not 0 * -inf
+    x1 = max_nan(x1, -1000.f);
+    const uint64_t e = pack2(ex2(x0), ex2(x1));
+    f.S = add2(f.S, e);
+    f.W = fma2(e, pack2(x0, x1), f.W);
   }
 }
 
 // Grid (cluster size, rows).
 template <bool kBf16>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, 4)
     logprobs_kernel(const void* logits, long long stride, int V, const int32_t* tokens, float inv_t, int top_n,
                     float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs) {
   using T = Type<kBf16>;
-  constexpr int kPer = T::kPer, kElem = kBf16 ? 2 : 4;
-  __shared__ uint64_t list[kList];
-  __shared__ uint64_t best[kMaxCluster][kTopMax];  // [0]: this CTA's; the first CTA's: every rank's
+  constexpr int kPer = T::kPer;
+  __shared__ __align__(16) uint64_t list[kList];
+  __shared__ __align__(16) uint64_t best[kMaxCluster * kTopMax];  // of the first CTA: every rank's, top_n each
   __shared__ Stat stat[kWarps];
   __shared__ Stat cta_stat[kMaxCluster];
-  __shared__ uint32_t warp_bound[kWarps];
+  __shared__ uint32_t warp_top[kWarps * 8];
   __shared__ int n_list;
   const int csize = gridDim.x, rank = blockIdx.x;
-  if (csize > 1) cluster_arrive();  // waited for before the first store into another CTA
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  if (t == 0) n_list = 0;
+  for (int i = t; i < kMaxCluster * kTopMax; i += kThreads) best[i] = 0;
+  if (csize > 1) {  // waited for before the first store into another CTA
+    __syncthreads();
+    cluster_arrive();
+  }
   sd_pdl_enter();
   const long long row = blockIdx.y;
-  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  const char* z0 = static_cast<const char*>(logits) + row * stride * kElem;
+  const char* z0 = static_cast<const char*>(logits) + row * stride * T::kElem;
   const float c = inv_t * kLog2e;
-  if (t == 0) n_list = 0;
   // the token's logit travels with the rest
   int tok = -1;
   float z_tok = 0.f;
@@ -159,70 +214,63 @@ __global__ void __launch_bounds__(kThreads, 2)
     if (tok >= 0 && tok < V) z_tok = T::load(z0, tok);
   }
   // whole chunks of the row: [lead, lead + n_vec * kPer); the ends are single elements
-  const int lead = min(V, static_cast<int>(((16 - (reinterpret_cast<uintptr_t>(z0) & 15)) & 15) / kElem));
+  const int lead = min(V, static_cast<int>(((32 - (reinterpret_cast<uintptr_t>(z0) & 31)) & 31) / T::kElem));
   const int n_vec = (V - lead) / kPer;
   const int tail = lead + n_vec * kPer;
-  const uint4* vec = reinterpret_cast<const uint4*>(z0 + static_cast<long long>(lead) * kElem);
+  const Chunk* vec = reinterpret_cast<const Chunk*>(z0 + static_cast<long long>(lead) * T::kElem);
   const int v_lo = static_cast<int>(static_cast<long long>(rank) * n_vec / csize);
   const int v_hi = static_cast<int>(static_cast<long long>(rank + 1) * n_vec / csize);
   // single elements: thread t < lead of the first CTA, the next ones the tail's
   int edge = -1;
   if (rank == 0) edge = t < lead ? t : (t - lead < V - tail ? tail + t - lead : -1);
 
-  Stat s{-INFINITY, 0.f, 0.f};
-  {
-    int v = v_lo + t;
-    for (; v + (kUnroll - 1) * kThreads < v_hi; v += kUnroll * kThreads) {
-      uint4 r[kUnroll];
+  Fold f{-INFINITY, 0ull, 0ull};
+  for (int v = v_lo + t; v < v_hi; v += kUnroll * kThreads) {
+    Chunk r[kUnroll];
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) r[u] = load16(vec + v + u * kThreads);
+    for (int u = 0; u < kUnroll; ++u)
+      if (v + u * kThreads < v_hi) r[u] = load32(vec + v + u * kThreads);
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        float z[kPer];
-        T::unpack(r[u], z);
-        fold<kBf16>(s, z, c);
-      }
-    }
-    uint4 r[kUnroll - 1];
-#pragma unroll
-    for (int u = 0; u < kUnroll - 1; ++u)
-      if (v + u * kThreads < v_hi) r[u] = load16(vec + v + u * kThreads);
-#pragma unroll
-    for (int u = 0; u < kUnroll - 1; ++u)
+    for (int u = 0; u < kUnroll; ++u)
       if (v + u * kThreads < v_hi) {
         float z[kPer];
         T::unpack(r[u], z);
-        fold<kBf16>(s, z, c);
+        fold(f, z, c);
       }
   }
   float z_edge = -INFINITY;
   if (edge >= 0) {
     z_edge = T::load(z0, edge);
-    float z[1] = {z_edge};
-    fold<kBf16>(s, z, c);
+    float z[2] = {z_edge, -INFINITY};
+    fold(f, z, c);
   }
-  const float mine = s.m;  // this thread's largest
+  const uint32_t mine = order_of(f.m);  // this thread's largest
+  Stat s{f.m, 0.f, 0.f};
+  {
+    float a, b;
+    unpack2(f.S, a, b);
+    s.S = a + b;
+    unpack2(f.W, a, b);
+    s.W = a + b;
+  }
 
   // ---- (m, S, W) over the warp, the CTA and the cluster
-  {
-    const float M = redux_max(s.m);
-    move_to(s, M, c);
+  move_to(s, redux_max(s.m), c);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      s.S += __shfl_xor_sync(0xffffffffu, s.S, o);
-      s.W += __shfl_xor_sync(0xffffffffu, s.W, o);
-    }
-    if (lane == 0) stat[warp] = s;
+  for (int o = 16; o > 0; o >>= 1) {
+    s.S += __shfl_xor_sync(0xffffffffu, s.S, o);
+    s.W += __shfl_xor_sync(0xffffffffu, s.W, o);
   }
+  if (lane == 0) stat[warp] = s;
+  const int per_warp = top_n <= 16 ? 4 : 8;  // of a warp's maxima, the largest
   if (top_n > 0) {
-    // the warp's j-th largest of its threads' maxima
-    uint32_t o = order_of(mine), bound = 0;
-    for (int j = (top_n + kWarps - 1) / kWarps; j > 0; --j) {
-      bound = __reduce_max_sync(0xffffffffu, o);
-      const uint32_t who = __ballot_sync(0xffffffffu, o == bound);
-      if (lane == __ffs(who) - 1) o = 0;
+    uint32_t o = mine, keep = 0;
+    for (int j = 0; j < per_warp; ++j) {
+      const uint32_t top = __reduce_max_sync(0xffffffffu, o);
+      if (lane == j) keep = top;
+      if (lane == __ffs(__ballot_sync(0xffffffffu, o == top)) - 1) o = 0;
     }
-    if (lane == 0) warp_bound[warp] = bound;
+    if (lane < per_warp) warp_top[warp * per_warp + lane] = keep;
   }
   __syncthreads();
   if (csize > 1) cluster_wait();  // every CTA of the cluster has started
@@ -235,10 +283,10 @@ __global__ void __launch_bounds__(kThreads, 2)
       a.W += __shfl_xor_sync(0xffffffffu, a.W, o);
     }
     if (lane == 0) {
-      const uint32_t to = in_first_cta(&cta_stat[rank]);
       if (csize == 1) {
         cta_stat[0] = a;
       } else {
+        const uint32_t to = in_first_cta(&cta_stat[rank]);
         asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(a.m) : "memory");
         asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4), "f"(a.S) : "memory");
         asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 8), "f"(a.W) : "memory");
@@ -246,9 +294,24 @@ __global__ void __launch_bounds__(kThreads, 2)
     }
   }
   if (top_n > 0) {
-    uint32_t bound = 0xffffffffu;
+    // the top_n-th largest of the warps' largest, by every warp: the largest that top_n reach
+    const uint32_t x0 = warp_top[lane], x1 = per_warp == 8 ? warp_top[32 + lane] : 0u;
+    int c0 = 0, c1 = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) bound = min(bound, warp_bound[w]);
+    for (int j = 0; j < 32; ++j) {
+      const uint32_t y0 = __shfl_sync(0xffffffffu, x0, j);
+      c0 += y0 >= x0;
+      c1 += y0 >= x1;
+    }
+    if (per_warp == 8) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        const uint32_t y1 = __shfl_sync(0xffffffffu, x1, j);
+        c0 += y1 >= x0;
+        c1 += y1 >= x1;
+      }
+    }
+    uint32_t bound = __reduce_max_sync(0xffffffffu, max(c0 >= top_n ? x0 : 0u, c1 >= top_n ? x1 : 0u));
     bound = max(bound, kOrderNegInf + 1);  // finite logits only
     auto offer = [&](float z, int i) {
       if (order_of(z) >= bound) {
@@ -257,35 +320,52 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
     };
     if (edge >= 0) offer(z_edge, edge);
-    uint32_t who = __ballot_sync(0xffffffffu, order_of(mine) >= bound);
-    while (who) {
-      const int first = v_lo + warp * 32 + __ffs(who) - 1;
-      who &= who - 1;
-      for (int v = first + lane * kThreads; v < v_hi; v += 32 * kThreads) {
-        float z[kPer];
-        T::unpack(__ldcg(vec + v), z);
+    uint32_t who = __ballot_sync(0xffffffffu, mine >= bound);
+    auto again = [&](int v, const Chunk& r) {
+      float z[kPer];
+      T::unpack(r, z);
+      float m = z[0];
+#pragma unroll
+      for (int j = 1; j < kPer; ++j) m = max_nan(m, z[j]);
+      if (order_of(m) >= bound || m != m) {
         const int i = lead + v * kPer;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) offer(z[j], i + j);
       }
+    };
+    while (who) {  // two threads' chunks at once
+      const int v0 = v_lo + warp * 32 + __ffs(who) - 1 + lane * kThreads;
+      who &= who - 1;
+      const int v1 = who ? v_lo + warp * 32 + __ffs(who) - 1 + lane * kThreads : v_hi;
+      who &= who - 1;
+      for (int o = 0; v0 + o < v_hi || v1 + o < v_hi; o += 32 * kThreads) {
+        Chunk r0, r1;
+        if (v0 + o < v_hi) r0 = load32(vec + v0 + o);
+        if (v1 + o < v_hi) r1 = load32(vec + v1 + o);
+        if (v0 + o < v_hi) again(v0 + o, r0);
+        if (v1 + o < v_hi) again(v1 + o, r1);
+      }
     }
     __syncthreads();
-    int n = n_list;
-    uint64_t* mine_best = best[0];
-    uint64_t got = 0;  // thread j < top_n: the list's j-th largest, 0 past its end
+    const int n = n_list;
+    // the segment's j-th largest to place j of its part of the first CTA's array
+    auto put = [&](int j, uint64_t k) {
+      if (csize == 1) best[j] = k;
+      else asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(in_first_cta(&best[rank * top_n + j])), "l"(k) : "memory");
+    };
     if (n <= kList) {
-      // rank by counting
-      __shared__ uint64_t sorted[kTopMax];
-      if (t < kTopMax) sorted[t] = 0;
+      if (t == 0 && (n & 1) && n < kList) list[n] = 0;  // read in pairs
       __syncthreads();
       for (int i = t; i < n; i += kThreads) {
         const uint64_t k = list[i];
         int above = 0;
-        for (int j = 0; j < n; ++j) above += list[j] > k;
-        if (above < top_n) sorted[above] = k;
+#pragma unroll 8
+        for (int j = 0; j < n; j += 2) {
+          const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(list + j);
+          above += (y.x > k) + (y.y > k);
+        }
+        if (above < top_n) put(above, k);
       }
-      __syncthreads();
-      if (t < top_n) got = sorted[t];
     } else {
       // too many equals: the next largest, one by one
       __shared__ uint64_t part[kWarps];
@@ -299,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         if (edge >= 0) look(z_edge, edge);
         for (int v = v_lo + t; v < v_hi; v += kThreads) {
           float z[kPer];
-          T::unpack(__ldcg(vec + v), z);
+          T::unpack(load32(vec + v), z);
 #pragma unroll
           for (int e = 0; e < kPer; ++e) look(z[e], lead + v * kPer + e);
         }
@@ -310,15 +390,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         __syncthreads();
         for (int w = 0; w < kWarps; ++w) k = max(k, part[w]);
         limit = k;
-        if (t == j) got = k;
-      }
-    }
-    if (t < top_n) {
-      if (csize == 1) {
-        mine_best[t] = got;
-      } else {
-        const uint32_t to = in_first_cta(&best[rank][t]);
-        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to), "l"(got) : "memory");
+        if (t == 0) put(j, k);
       }
     }
   }
@@ -357,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     logprob[row] = lp;
   }
   if (top_n == 0) return;
-  // ---- its alternatives: rank by counting over the CTAs' sorted lists
+  // ---- its alternatives: rank by counting over the CTAs' lists
   __shared__ int n_found;
   if (t == 0) n_found = 0;
   __syncthreads();
@@ -365,18 +437,19 @@ __global__ void __launch_bounds__(kThreads, 2)
     top_ids[row * top_n + at] = i;
     top_logprobs[row * top_n + at] = (z - m) * inv_t - ln;
   };
-  if (t < csize * top_n) {
-    const int r = t / top_n, j = t - r * top_n;
-    const uint64_t k = best[r][j];
-    if (k) {
-      int above = j;
-      for (int q = 0; q < csize; ++q)
-        if (q != r)
-          for (int e = 0; e < top_n && best[q][e] > k; ++e) ++above;
-      if (above < top_n) {
-        write(above, value_of(static_cast<uint32_t>(k >> 32)), static_cast<int>(~static_cast<uint32_t>(k)));
-        atomicAdd(&n_found, 1);
-      }
+  const int n_all = csize * top_n;
+  for (int i = t; i < n_all; i += kThreads) {
+    const uint64_t k = best[i];
+    if (!k) continue;
+    int above = 0;
+#pragma unroll 8
+    for (int j = 0; j < n_all; j += 2) {  // (zeros past the end)
+      const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(best + j);
+      above += (y.x > k) + (y.y > k);
+    }
+    if (above < top_n) {
+      write(above, value_of(static_cast<uint32_t>(k >> 32)), static_cast<int>(~static_cast<uint32_t>(k)));
+      atomicAdd(&n_found, 1);
     }
   }
   __syncthreads();
@@ -396,11 +469,13 @@ __global__ void __launch_bounds__(kThreads, 2)
   }
 }
 
-// CTAs a row: enough for two an SM over all rows, as long as each keeps 32 KB of the row
-// or so (at least one batch of chunks a thread).
+// CTAs a row: as many as fit at once over all rows (four an SM), as long as each keeps 32 KB
+// of the row, four chunks a thread. 256 rows of 608 KB at 1 / 2 / 4 / 8: 41.0 / 35.8 / 40.9 /
+// 55.4 us; 8 rows of 304 KB: 16.8 / 11.3 / 8.6 / 7.6. (With two or three chunks in flight and
+// five or six CTAs an SM: 37.1 to 39.7 at best.)
 int cluster_size(int rows, long long row_bytes) {
   int s = 1;
-  while (s < kMaxCluster && static_cast<long long>(rows) * s * 2 <= 2LL * sd_num_sms() && row_bytes / (2 * s) >= 16384) s *= 2;
+  while (s < kMaxCluster && 2LL * rows * s <= 4LL * sd_num_sms() && row_bytes / (2 * s) >= 32768) s *= 2;
   return s;
 }
 

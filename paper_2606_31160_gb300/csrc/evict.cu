@@ -6,11 +6,12 @@
 // Several CTAs a (KV head, scene), each moving its share of the places in dst: they need
 // nothing of each other, as each finds the whole selection itself from the weights (4 bytes
 // a key against the 512 of a kept row: 16384 keys are 64 KB from L2). The weight of the last
-// key kept is found by three passes of counting on the digits (11, 11 and 10 bits) of its
-// order-preserving integer, in shared memory. Then a key's place is the number of kept keys
-// before it: each warp counts its part of the keys by ballots, a sum over the warps gives it
-// its first place, and a second walk lists the CTA's share, whose rows are copied with
-// eight 16-byte loads a thread in flight.
+// key kept: the keys are counted by the leading 11 bits of an integer that orders as the
+// weight does; those that share the deciding bits are listed, and a few of them ranked by
+// counting, more of them counted by their other bits, in two more passes (over all keys
+// where the list is too short: weights within an eighth of each other). Then a key's place is the number of kept keys before it: ballots,
+// kept in shared memory, are summed a warp a range of keys, and the CTA lists its share from
+// them, whose rows it copies with eight 16-byte loads a thread in flight.
 #include "common.cuh"
 
 SD_DEFINE_ERROR_ACCESSOR(sd_take_error_evict)
@@ -21,7 +22,8 @@ constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kBins = 2048;
 constexpr int kList = 1024;     // kept keys that a CTA lists, then copies, at a time
-constexpr int kKeysMax = 20480; // keys whose integers stay in shared memory; more are read anew each time
+constexpr int kRank = 64;      // listed keys that are ranked by counting
+constexpr int kKeysMax = 20480; // keys whose integers and ballots stay in shared memory; more are read anew each time
 
 // An integer that orders as the weight does (-0 as +0; NaN below every number).
 __device__ __forceinline__ uint32_t order_of(float w) {
@@ -30,16 +32,23 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Grid (parts, Hkv, B); dynamic shared memory for `kept_in_smem` keys.
+// The sum of x[w], w < n <= 32, by a whole warp.
+__device__ __forceinline__ int sum_of(const int* x, int n, int lane) {
+  return __reduce_add_sync(0xffffffffu, lane < n ? x[lane] : 0);
+}
+
+// Grid (parts, Hkv, B); dynamic shared memory for smem_keys keys.
 __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, const float* weights, const sd_kv_cache dst,
                                                          int keep, int sinks, int recent, float* weights_out, int32_t* kept,
                                                          int smem_keys, int vec_shift) {
-  extern __shared__ uint32_t order[];
+  extern __shared__ uint32_t order[];                  // [smem_keys], then ballots[smem_keys / 32]
+  uint2* ballots = reinterpret_cast<uint2*>(order + smem_keys);  // of 32 keys: which stay, which tie
   __shared__ int bins[kBins];
-  __shared__ int list[kList];
+  __shared__ __align__(16) int list[kList];
   __shared__ int warp_sum[kWarps];
   __shared__ int warp_kept[kWarps], warp_ties[kWarps];
-  __shared__ int s_bin, s_left;
+  __shared__ int s_bin, s_left, s_count;
+  __shared__ uint32_t s_T;
   sd_pdl_enter();
   const int part = blockIdx.x, parts = gridDim.x, h = blockIdx.y, b = blockIdx.z, Hkv = src.n_kv_heads;
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
@@ -67,53 +76,94 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
   uint32_t T = 0;
   int ties = 0;
   if (!all) {
-    if (cached) {
-      for (int i = t; i < n; i += 4 * kThreads) {
-        float w[4];
+    int left = want;  // to be taken among the keys whose leading bits are T's
+    // the bin in which the left-th key lies, of 2048, the largest digits first: a prefix sum
+    // over the bins, 4 a thread
+    auto find = [&](int n_bins, int shift) {
+      __syncthreads();
+      int c[4], sum = 0;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) w[u] = i + u * kThreads < n ? __ldcg(weights + i + u * kThreads) : 0.f;
+      for (int j = 0; j < 4; ++j) sum += c[j] = bins[4 * t + j];
+      int before = sum;
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (i + u * kThreads < n) order[i + u * kThreads] = order_of(w[u]);
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += x;
+      }
+      if (lane == 31) warp_sum[warp] = before;
+      __syncthreads();
+      before += sum_of(warp_sum, warp, lane) - sum;
+      if (before < left && before + sum >= left) {  // one thread's
+        int j = 0;
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+          if (j == k && before + c[k] < left) before += c[k], ++j;
+        s_bin = 4 * t + j;
+        s_left = left - before;
+      }
+      __syncthreads();
+      T |= static_cast<uint32_t>(n_bins - 1 - s_bin) << shift;
+      left = s_left;
+    };
+    for (int i = t; i < kBins; i += kThreads) bins[i] = 0;
+    if (t == 0) s_count = 0;
+    __syncthreads();
+    for (int i0 = t; i0 < n; i0 += 4 * kThreads) {
+      float w[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) w[u] = i0 + u * kThreads < n ? __ldcg(weights + i0 + u * kThreads) : 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * kThreads;
+        const uint32_t o = order_of(w[u]);
+        if (i < n && cached) order[i] = o;
+        if (i >= lo && i < hi) atomicAdd(&bins[kBins - 1 - (o >> 21)], 1);
       }
     }
-    int left = want;  // to be taken among the keys whose higher digits are T's
     if (left > 0) {
-#pragma unroll 1
-      for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), width = pass == 2 ? 10 : 11, n_bins = 1 << width;
-        for (int i = t; i < kBins; i += kThreads) bins[i] = 0;
-        __syncthreads();
+      find(kBins, 21);
+      const int alike = bins[s_bin];  // keys that share T's leading bits
+      const bool listed = alike <= kList;
+      if (listed) {
         for (int i = lo + t; i < hi; i += kThreads) {
           const uint32_t o = order_at(i);
-          // (an integer's high bits and T's, those below them not yet found)
-          if (pass == 0 || (o >> (shift + width)) == (T >> (shift + width)))
-            atomicAdd(&bins[n_bins - 1 - static_cast<int>((o >> shift) & (n_bins - 1))], 1);  // the largest digit first
+          if ((o >> 21) == (T >> 21)) list[atomicAdd(&s_count, 1)] = static_cast<int>(o);
+        }
+      }
+      if (alike <= kRank) {
+        __syncthreads();
+        if (t < alike) {
+          const uint32_t o = static_cast<uint32_t>(list[t]);
+          int above = 0, equal = 0;
+#pragma unroll 8
+          for (int j = 0; j < alike; ++j) {
+            const uint32_t x = static_cast<uint32_t>(list[j]);
+            above += x > o;
+            equal += x == o;
+          }
+          if (above < left && above + equal >= left) {  // the threads with that one integer
+            s_T = o;
+            s_left = left - above;
+          }
         }
         __syncthreads();
-        // the bin in which the left-th key lies: a prefix sum over the bins, 4 a thread
-        int c[4], sum = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sum += c[j] = bins[4 * t + j];
-        int before = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int x = __shfl_up_sync(0xffffffffu, before, o);
-          if (lane >= o) before += x;
-        }
-        if (lane == 31) warp_sum[warp] = before;
-        __syncthreads();
-        before -= sum;
-        for (int w = 0; w < warp; ++w) before += warp_sum[w];
-        if (before < left && before + sum >= left) {  // one thread's
-          int j = 0;
-          while (before + c[j] < left) before += c[j++];
-          s_bin = 4 * t + j;
-          s_left = left - before;
-        }
-        __syncthreads();
-        T |= static_cast<uint32_t>(n_bins - 1 - s_bin) << shift;
+        T = s_T;
         left = s_left;
+      } else {
+#pragma unroll 1
+        for (int pass = 1; pass < 3; ++pass) {
+          const int shift = pass == 1 ? 10 : 0, width = pass == 1 ? 11 : 10, n_bins = 1 << width;
+          __syncthreads();
+          for (int i = t; i < kBins; i += kThreads) bins[i] = 0;
+          __syncthreads();
+          const int from = listed ? 0 : lo, to = listed ? alike : hi;
+          for (int i = from + t; i < to; i += kThreads) {
+            const uint32_t o = listed ? static_cast<uint32_t>(list[i]) : order_at(i);
+            if ((o >> (shift + width)) == (T >> (shift + width)))
+              atomicAdd(&bins[n_bins - 1 - static_cast<int>((o >> shift) & (n_bins - 1))], 1);
+          }
+          find(n_bins, shift);
+        }
       }
       ties = left;
     } else {
@@ -132,12 +182,17 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
     const uint32_t o = order_at(i);
     return o > T ? 2 : (o == T ? 1 : 0);
   };
+  auto ballots_at = [&](int i0) {
+    const int k = kind(i0 + lane);
+    return make_uint2(__ballot_sync(0xffffffffu, k == 2), __ballot_sync(0xffffffffu, k == 1));
+  };
   {
     int stay = 0, tie = 0;
     for (int i0 = i_lo; i0 < i_hi; i0 += 32) {
-      const int k = kind(i0 + lane);
-      stay += __popc(__ballot_sync(0xffffffffu, k == 2));
-      tie += __popc(__ballot_sync(0xffffffffu, k == 1));
+      const uint2 b = ballots_at(i0);
+      if (cached && lane == 0) ballots[i0 >> 5] = b;
+      stay += __popc(b.x);
+      tie += __popc(b.y);
     }
     if (lane == 0) {
       warp_kept[warp] = stay;
@@ -145,11 +200,7 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
     }
   }
   __syncthreads();
-  int stay0 = 0, ties0 = 0;
-  for (int w = 0; w < warp; ++w) {
-    stay0 += warp_kept[w];
-    ties0 += warp_ties[w];
-  }
+  const int stay0 = sum_of(warp_kept, warp, lane), ties0 = sum_of(warp_ties, warp, lane);
   const int vec = 1 << vec_shift;
   const uint4* ks = static_cast<const uint4*>(src.k) + ((plane * src.capacity) << vec_shift);
   const uint4* vs = static_cast<const uint4*>(src.v) + ((plane * src.capacity) << vec_shift);
@@ -161,14 +212,16 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
     __syncthreads();  // the list before is copied
     int stay = stay0, tie = ties0;
     for (int i0 = i_lo; i0 < i_hi && stay + min(tie, ties) < q_hi; i0 += 32) {
-      const int k = kind(i0 + lane);
-      const uint32_t s = __ballot_sync(0xffffffffu, k == 2), e = __ballot_sync(0xffffffffu, k == 1);
-      const uint32_t below = (1u << lane) - 1;
-      const int my_ties = tie + __popc(e & below);
-      const int at = stay + __popc(s & below) + min(my_ties, ties);
-      if ((k == 2 || (k == 1 && my_ties < ties)) && at >= q_lo && at < q_hi) list[at - q_lo] = i0 + lane;
-      stay += __popc(s);
-      tie += __popc(e);
+      const uint2 x = cached ? ballots[i0 >> 5] : ballots_at(i0);
+      const int stay1 = stay + __popc(x.x), tie1 = tie + __popc(x.y);
+      if (stay1 + min(tie1, ties) > q_lo) {
+        const uint32_t below = (1u << lane) - 1;
+        const int my_ties = tie + __popc(x.y & below);
+        const int at = stay + __popc(x.x & below) + min(my_ties, ties);
+        if ((((x.x >> lane) & 1) || (((x.y >> lane) & 1) && my_ties < ties)) && at >= q_lo && at < q_hi) list[at - q_lo] = i0 + lane;
+      }
+      stay = stay1;
+      tie = tie1;
     }
     __syncthreads();
     const int count = q_hi - q_lo;
@@ -235,9 +288,10 @@ extern "C" sd_status sd_kv_evict(const sd_kv_cache* src, const float* weights, i
   if (src->len == dst->len) return SD_ERR_INVALID_ARG;
   // two CTAs an SM over all heads, as long as each has 32 rows or more to move
   const long long pairs = static_cast<long long>(B) * Hkv;
-  long long parts = (2LL * sd_num_sms() + pairs - 1) / pairs;
+  long long parts = 2LL * sd_num_sms() / pairs;
+  if (parts < 1) parts = 1;
   if (parts > (keep + 31) / 32) parts = (keep + 31) / 32;
-  const int smem_keys = src->capacity < kKeysMax ? src->capacity : kKeysMax;
+  const int smem_keys = src->capacity < kKeysMax ? (src->capacity + 31) / 32 * 32 : kKeysMax;
   static bool allowed[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
@@ -245,13 +299,13 @@ extern "C" sd_status sd_kv_evict(const sd_kv_cache* src, const float* weights, i
     return SD_ERR_CUDA;
   }
   if (!allowed[dev]) {  // more than 48 KB of shared memory, once per device
-    if (cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeysMax * 4) != cudaSuccess) {
+    if (cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeysMax * 4 + kKeysMax / 32 * 8) != cudaSuccess) {
       (void)cudaGetLastError();
       return SD_ERR_CUDA;
     }
     allowed[dev] = true;
   }
-  if (sd_launch_pdl(evict_kernel, dim3(static_cast<unsigned>(parts), Hkv, B), dim3(kThreads), smem_keys * sizeof(uint32_t),
+  if (sd_launch_pdl(evict_kernel, dim3(static_cast<unsigned>(parts), Hkv, B), dim3(kThreads), smem_keys * 4 + smem_keys / 32 * 8,
                     reinterpret_cast<cudaStream_t>(stream), *src, weights, *dst, keep, sinks, recent, weights_out, kept,
                     smem_keys, D == 64 ? 3 : 4) != cudaSuccess) {
     (void)cudaGetLastError();

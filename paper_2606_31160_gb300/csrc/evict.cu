@@ -18,7 +18,7 @@ SD_DEFINE_ERROR_ACCESSOR(sd_take_error_evict)
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
 constexpr int kBins = 2048;
 constexpr int kList = 1024;     // kept keys that a CTA lists, then copies, at a time
@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
                                                          int smem_keys, int vec_shift) {
   extern __shared__ uint32_t order[];                  // [smem_keys], then ballots[smem_keys / 32]
   uint2* ballots = reinterpret_cast<uint2*>(order + smem_keys);  // of 32 keys: which stay, which tie
-  __shared__ int bins[kBins];
+  __shared__ __align__(16) int bins[kBins];
   __shared__ __align__(16) int list[kList];
   __shared__ int warp_sum[kWarps];
   __shared__ int warp_kept[kWarps], warp_ties[kWarps];
@@ -77,13 +77,13 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
   int ties = 0;
   if (!all) {
     int left = want;  // to be taken among the keys whose leading bits are T's
-    // the bin in which the left-th key lies, of 2048, the largest digits first: a prefix sum
-    // over the bins, 4 a thread
+    // the bin in which the left-th key lies, the largest digits first: a prefix sum over the
+    // bins, two a thread
     auto find = [&](int n_bins, int shift) {
       __syncthreads();
-      int c[4], sum = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum += c[j] = bins[4 * t + j];
+      static_assert(kBins == 2 * kThreads, "two bins a thread");
+      const int2 c = reinterpret_cast<const int2*>(bins)[t];
+      const int sum = c.x + c.y;
       int before = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -94,12 +94,9 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
       __syncthreads();
       before += sum_of(warp_sum, warp, lane) - sum;
       if (before < left && before + sum >= left) {  // one thread's
-        int j = 0;
-#pragma unroll
-        for (int k = 0; k < 3; ++k)
-          if (j == k && before + c[k] < left) before += c[k], ++j;
-        s_bin = 4 * t + j;
-        s_left = left - before;
+        const bool second = before + c.x < left;
+        s_bin = 2 * t + second;
+        s_left = left - before - (second ? c.x : 0);
       }
       __syncthreads();
       T |= static_cast<uint32_t>(n_bins - 1 - s_bin) << shift;
@@ -286,9 +283,10 @@ extern "C" sd_status sd_kv_evict(const sd_kv_cache* src, const float* weights, i
     for (int j = 0; j < 4; ++j)
       if (to_bytes[j] && overlap(in[i], in_bytes[i], to[j], to_bytes[j])) return SD_ERR_INVALID_ARG;
   if (src->len == dst->len) return SD_ERR_INVALID_ARG;
-  // two CTAs an SM over all heads, as long as each has 32 rows or more to move
+  // a CTA an SM over all heads, as long as each has 32 rows or more to move. (Two CTAs of half
+  // the threads find every selection twice an SM.)
   const long long pairs = static_cast<long long>(B) * Hkv;
-  long long parts = 2LL * sd_num_sms() / pairs;
+  long long parts = sd_num_sms() / pairs;
   if (parts < 1) parts = 1;
   if (parts > (keep + 31) / 32) parts = (keep + 31) / 32;
   const int smem_keys = src->capacity < kKeysMax ? (src->capacity + 31) / 32 * 32 : kKeysMax;

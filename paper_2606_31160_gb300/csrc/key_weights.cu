@@ -527,7 +527,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             scaled(x[4], x[5], n1.x, n1.y, y[4], y[5]);
             scaled(x[6], x[7], n1.z, n1.w, y[6], y[7]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = masks && 8 * u + j < below ? 0.f : ex2(y[j]);  // (a masked score may be NaN)
+            for (int j = 0; j < 8; ++j) y[j] = ex2(y[j]);
+            if (masks || 8 * u + 8 > rows_in) {  // (a score that is masked or no row's may be NaN)
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (8 * u + j < below || 8 * u + j >= rows_in) y[j] = 0.f;
+            }
             w0 = add2(add2(w0, y[0], y[1]), y[2], y[3]);
             w1 = add2(add2(w1, y[4], y[5]), y[6], y[7]);
           };

@@ -344,7 +344,7 @@ class KV8Cache:
         if block <= 0:
             raise ValueError("block must be positive")
         want = (B, H, -(-cap // block))
-        if tuple(k_scale.shape) != want or tuple(v_scale.shape) != want or tuple(lens.shape) != (B,):
+        if k_scale.shape != want or v_scale.shape != want or lens.shape != (B,):
             raise ValueError("scales must be %s and len (%d,)" % (want, B))
         for t, name in ((k, "k"), (v, "v")):
             _dev(t, name, torch.float8_e4m3fn)
@@ -360,6 +360,8 @@ class KV8Cache:
 
     @classmethod
     def empty(cls, B, Hkv, cap, D, block=64, device="cuda"):
+        if int(block) <= 0:
+            raise ValueError("block must be positive")
         k = torch.zeros((B, Hkv, cap, D), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
         s = torch.ones((B, Hkv, -(-cap // block)), dtype=torch.float32, device=device)
         return cls(k, torch.zeros_like(k), s, s.clone(), torch.zeros(B, dtype=torch.int32, device=device), block)
@@ -383,7 +385,7 @@ def kv8_append(cache, k_new, v_new):
     """Quantise and write k_new / v_new [B,R,Hkv,D] bf16 at len[b] .. len[b]+R-1; len += R."""
     B, H, _, D = cache.shape
     R = k_new.shape[1]
-    if tuple(k_new.shape) != (B, R, H, D) or k_new.shape != v_new.shape:
+    if k_new.shape != (B, R, H, D) or k_new.shape != v_new.shape:
         raise ValueError("shape mismatch")
     _check(lib().sd_kv8_append(cache.struct, _dev(k_new, "k_new", torch.bfloat16), _dev(v_new, "v_new", torch.bfloat16),
                                R, _stream()), "sd_kv8_append")
@@ -424,9 +426,9 @@ def attention_weights(q, cache, weights_in=None, weights=None, decay=1.0, commit
         raise ValueError("q and cache disagree")
     if weights is None:
         weights = torch.zeros((B, Hkv, cap), dtype=torch.float32, device=q.device)
-    if tuple(weights.shape) != (B, Hkv, cap) or (weights_in is not None and weights_in.shape != weights.shape):
+    if weights.shape != (B, Hkv, cap) or (weights_in is not None and weights_in.shape != weights.shape):
         raise ValueError("weights must be [B, Hkv, cap]")
-    if committed is not None and tuple(committed.shape) != (B,):
+    if committed is not None and committed.shape != (B,):
         raise ValueError("committed must be [B]")
     _check(lib().sd_attention_weights(_dev(q, "q", torch.bfloat16), cache.struct, R, Hq, float(scale),
                                       None if committed is None else _dev(committed, "committed", torch.int32),
@@ -444,11 +446,11 @@ def kv_evict(src, weights, dst, keep, sinks=0, recent=0, weights_out=None, kept=
     keep = int(keep)
     if (dst.shape[0], dst.shape[1], dst.shape[3]) != (B, Hkv, D):
         raise ValueError("the caches disagree")
-    if tuple(weights.shape) != (B, Hkv, cap):
+    if weights.shape != (B, Hkv, cap):
         raise ValueError("weights must be [B, Hkv, cap]")
-    if weights_out is not None and tuple(weights_out.shape) != (B, Hkv, dst.shape[2]):
+    if weights_out is not None and weights_out.shape != (B, Hkv, dst.shape[2]):
         raise ValueError("weights_out must be [B, Hkv, cap of dst]")
-    if kept is not None and tuple(kept.shape) != (B, Hkv, keep):
+    if kept is not None and kept.shape != (B, Hkv, keep):
         raise ValueError("kept must be [B, Hkv, keep]")
     _check(lib().sd_kv_evict(src.struct, _dev(weights, "weights", torch.float32), keep, int(sinks), int(recent), dst.struct,
                              None if weights_out is None else _dev(weights_out, "weights_out", torch.float32),
@@ -462,25 +464,27 @@ def token_logprobs(logits, tokens, temperature=1.0, top_n=0, logprob=None, entro
     (bf16 or fp32), the rows' entropies (nats) and their top_n alternatives. A token -1
     gives 0. Returns (logprob [...], entropy [...], top_ids [..., top_n] int32,
     top_logprobs [..., top_n])."""
-    V, lead = logits.shape[-1], tuple(logits.shape[:-1])
-    dt = {torch.bfloat16: SD_BF16, torch.float32: SD_F32}.get(logits.dtype)
+    V, lead = logits.shape[-1], logits.shape[:-1]
+    dt = SD_BF16 if logits.dtype is torch.bfloat16 else (SD_F32 if logits.dtype is torch.float32 else None)
     if dt is None:
         raise ValueError("logits must be bf16 or fp32")
-    if tuple(tokens.shape) != lead:
-        raise ValueError("tokens must be %s" % (lead,))
-    top_n, dev, rows = int(top_n), logits.device, tokens.numel()
+    if tokens.shape != lead:
+        raise ValueError("tokens must be %s" % (tuple(lead),))
+    top_n, rows = int(top_n), tokens.numel()
+    wide = tuple(lead) + (max(top_n, 0),)
     if logits.is_contiguous():
         ptr, stride = _dev(logits, "logits"), V
     else:
         ptr, stride = _padded_rows(logits, rows)
-    logprob = torch.empty(lead, dtype=torch.float32, device=dev) if logprob is None else logprob
-    entropy = torch.empty(lead, dtype=torch.float32, device=dev) if entropy is None else entropy
-    if tuple(logprob.shape) != lead or tuple(entropy.shape) != lead:
-        raise ValueError("logprob and entropy must be %s" % (lead,))
-    top_ids = torch.empty(lead + (max(top_n, 0),), dtype=torch.int32, device=dev) if top_ids is None else top_ids
-    top_logprobs = torch.empty(lead + (max(top_n, 0),), dtype=torch.float32, device=dev) if top_logprobs is None else top_logprobs
-    if tuple(top_ids.shape) != lead + (top_n,) or tuple(top_logprobs.shape) != lead + (top_n,):
-        raise ValueError("top_ids and top_logprobs must be %s" % (lead + (top_n,),))
+    outs = []
+    for t, name, dtype, shape in ((logprob, "logprob", torch.float32, lead), (entropy, "entropy", torch.float32, lead),
+                                  (top_ids, "top_ids", torch.int32, wide), (top_logprobs, "top_logprobs", torch.float32, wide)):
+        if t is None:
+            t = torch.empty(shape, dtype=dtype, device=logits.device)
+        elif t.shape != shape:
+            raise ValueError("%s must be %s" % (name, tuple(shape)))
+        outs.append(t)
+    logprob, entropy, top_ids, top_logprobs = outs
     _check(lib().sd_token_logprobs(ptr, dt, rows, V, stride, _dev(tokens, "tokens", torch.int32), float(temperature), top_n,
                                    _dev(logprob, "logprob", torch.float32), _dev(entropy, "entropy", torch.float32),
                                    _dev(top_ids, "top_ids", torch.int32),

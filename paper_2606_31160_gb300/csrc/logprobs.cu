@@ -12,7 +12,7 @@
 // Alternatives without a second pass: the threads' maxima are kept anyway. The top_n-th
 // largest of each warp's 4 or 8 largest of them is a bound that at least top_n elements of
 // the segment reach, and few more do. Only threads whose maximum reaches it hold such
-// elements: their warps read those threads' chunks again, a chunk a lane, and list what
+// elements: their warps read those threads' chunks again, four a lane, and list what
 // reaches it. (With the least of the warps' maxima as the bound a third of the row was read
 // again.) A list is ranked by counting; the cluster's first CTA ranks the CTAs' lists. A
 // bound of -inf (a masked vocabulary) lists the finite logits only, the lowest masked
@@ -193,6 +193,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   __shared__ Stat stat[kWarps];
   __shared__ Stat cta_stat[kMaxCluster];
   __shared__ uint32_t warp_top[kWarps * 8];
+  __shared__ uint8_t holder[kWarps][32];
   __shared__ int n_list;
   const int csize = gridDim.x, rank = blockIdx.x;
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
@@ -333,17 +334,25 @@ __global__ void __launch_bounds__(kThreads, 4)
         for (int j = 0; j < kPer; ++j) offer(z[j], i + j);
       }
     };
-    while (who) {  // two threads' chunks at once
-      const int v0 = v_lo + warp * 32 + __ffs(who) - 1 + lane * kThreads;
-      who &= who - 1;
-      const int v1 = who ? v_lo + warp * 32 + __ffs(who) - 1 + lane * kThreads : v_hi;
-      who &= who - 1;
-      for (int o = 0; v0 + o < v_hi || v1 + o < v_hi; o += 32 * kThreads) {
-        Chunk r0, r1;
-        if (v0 + o < v_hi) r0 = load32(vec + v0 + o);
-        if (v1 + o < v_hi) r1 = load32(vec + v1 + o);
-        if (v0 + o < v_hi) again(v0 + o, r0);
-        if (v1 + o < v_hi) again(v1 + o, r1);
+    // the chunks of the warp's threads that hold such elements, four a lane on their way at
+    // once: behind a saturated memory every round trip is a few microseconds
+    const int holders = __popc(who);
+    if (holders) {
+      if ((who >> lane) & 1) holder[warp][__popc(who & ((1u << lane) - 1))] = lane;
+      __syncwarp();
+      const int each = (v_hi - v_lo - warp * 32 + kThreads - 1) / kThreads;  // chunks a thread at most
+      for (int u = lane; u < holders * each; u += 32 * kUnroll) {
+        Chunk r[kUnroll];
+        int at[kUnroll];
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+          const int x = u + 32 * k, i = x / each;
+          at[k] = x < holders * each ? v_lo + warp * 32 + holder[warp][i] + (x - i * each) * kThreads : v_hi;
+          if (at[k] < v_hi) r[k] = load32(vec + at[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k)
+          if (at[k] < v_hi) again(at[k], r[k]);
       }
     }
     __syncthreads();
@@ -470,9 +479,9 @@ __global__ void __launch_bounds__(kThreads, 4)
 }
 
 // CTAs a row: as many as fit at once over all rows (four an SM), as long as each keeps 32 KB
-// of the row, four chunks a thread. 256 rows of 608 KB at 1 / 2 / 4 / 8: 41.0 / 35.8 / 40.9 /
-// 55.4 us; 8 rows of 304 KB: 16.8 / 11.3 / 8.6 / 7.6. (With two or three chunks in flight and
-// five or six CTAs an SM: 37.1 to 39.7 at best.)
+// of the row, four chunks a thread. 256 rows of 608 KB at 1 / 2 / 4 / 8: 40.1 / 34.9 / 40.4 /
+// 51.8 us; 8 rows of 304 KB: 17.4 / 11.6 / 8.1 / 6.7, and 6.7 at 16. (With two or three
+// chunks in flight and five or six CTAs an SM the first took 37 to 40 at best.)
 int cluster_size(int rows, long long row_bytes) {
   int s = 1;
   while (s < kMaxCluster && 2LL * rows * s <= 4LL * sd_num_sms() && row_bytes / (2 * s) >= 32768) s *= 2;

@@ -383,12 +383,12 @@ def _same_device(*tensors):
 
 def kv8_append(cache, k_new, v_new):
     """Quantise and write k_new / v_new [B,R,Hkv,D] bf16 at len[b] .. len[b]+R-1; len += R."""
-    B, H, _, D = cache.shape
-    R = k_new.shape[1]
-    if k_new.shape != (B, R, H, D) or k_new.shape != v_new.shape:
+    B, H, _, D = cache._shape
+    shape = k_new.shape
+    if len(shape) != 4 or shape != (B, shape[1], H, D) or v_new.shape != shape:
         raise ValueError("shape mismatch")
-    _check(lib().sd_kv8_append(cache.struct, _dev(k_new, "k_new", torch.bfloat16), _dev(v_new, "v_new", torch.bfloat16),
-                               R, _stream()), "sd_kv8_append")
+    _check(lib().sd_kv8_append(cache._ref, _dev(k_new, "k_new", torch.bfloat16), _dev(v_new, "v_new", torch.bfloat16),
+                               shape[1], _stream()), "sd_kv8_append")
 
 
 def kv8_store(cache, src):
@@ -464,31 +464,31 @@ def token_logprobs(logits, tokens, temperature=1.0, top_n=0, logprob=None, entro
     (bf16 or fp32), the rows' entropies (nats) and their top_n alternatives. A token -1
     gives 0. Returns (logprob [...], entropy [...], top_ids [..., top_n] int32,
     top_logprobs [..., top_n])."""
-    V, lead = logits.shape[-1], logits.shape[:-1]
-    dt = SD_BF16 if logits.dtype is torch.bfloat16 else (SD_F32 if logits.dtype is torch.float32 else None)
-    if dt is None:
+    lead, V, dtype = logits.shape[:-1], logits.shape[-1], logits.dtype
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise ValueError("logits must be bf16 or fp32")
     if tokens.shape != lead:
         raise ValueError("tokens must be %s" % (tuple(lead),))
     top_n, rows = int(top_n), tokens.numel()
-    wide = tuple(lead) + (max(top_n, 0),)
     if logits.is_contiguous():
         ptr, stride = _dev(logits, "logits"), V
     else:
         ptr, stride = _padded_rows(logits, rows)
-    outs = []
-    for t, name, dtype, shape in ((logprob, "logprob", torch.float32, lead), (entropy, "entropy", torch.float32, lead),
-                                  (top_ids, "top_ids", torch.int32, wide), (top_logprobs, "top_logprobs", torch.float32, wide)):
-        if t is None:
-            t = torch.empty(shape, dtype=dtype, device=logits.device)
-        elif t.shape != shape:
-            raise ValueError("%s must be %s" % (name, tuple(shape)))
-        outs.append(t)
-    logprob, entropy, top_ids, top_logprobs = outs
+    wide, f32 = (*lead, max(top_n, 0)), torch.float32
+    if logprob is None:
+        logprob = torch.empty(lead, dtype=f32, device=logits.device)
+    if entropy is None:
+        entropy = torch.empty(lead, dtype=f32, device=logits.device)
+    if top_ids is None:
+        top_ids = torch.empty(wide, dtype=torch.int32, device=logits.device)
+    if top_logprobs is None:
+        top_logprobs = torch.empty(wide, dtype=f32, device=logits.device)
+    if logprob.shape != lead or entropy.shape != lead or top_ids.shape != wide or top_logprobs.shape != wide:
+        raise ValueError("logprob and entropy must be %s, top_ids and top_logprobs %s" % (tuple(lead), wide))
+    dt = SD_BF16 if dtype is torch.bfloat16 else SD_F32
     _check(lib().sd_token_logprobs(ptr, dt, rows, V, stride, _dev(tokens, "tokens", torch.int32), float(temperature), top_n,
-                                   _dev(logprob, "logprob", torch.float32), _dev(entropy, "entropy", torch.float32),
-                                   _dev(top_ids, "top_ids", torch.int32),
-                                   _dev(top_logprobs, "top_logprobs", torch.float32), _stream()), "sd_token_logprobs")
+                                   _dev(logprob, "logprob", f32), _dev(entropy, "entropy", f32), _dev(top_ids, "top_ids", torch.int32),
+                                   _dev(top_logprobs, "top_logprobs", f32), _stream()), "sd_token_logprobs")
     return logprob, entropy, top_ids, top_logprobs
 
 

@@ -9,17 +9,22 @@
 // which it moves only when a chunk's maximum passes it. S and W merge over lanes, warps
 // and CTAs in a fixed order.
 //
-// Alternatives without a second pass: the threads' maxima are kept anyway. The top_n-th
-// largest of each warp's 4 or 8 largest of them is a bound that at least top_n elements of
-// the segment reach, and few more do. Only threads whose maximum reaches it hold such
-// elements: their warps read those threads' chunks again, four a lane, and list what
-// reaches it. (With the least of the warps' maxima as the bound a third of the row was read
-// again.) A list is ranked by counting; the cluster's first CTA ranks the CTAs' lists. A
-// bound of -inf (a masked vocabulary) lists the finite logits only, the lowest masked
-// indices fill the rest; a list that overflows (hundreds of equal logits) is replaced by
-// top_n passes for the next largest.
+// Alternatives without a second pass: a thread remembers which of its chunks holds its
+// largest logit, and the second chunk's largest. The top_n-th largest of each warp's 4 or 8
+// largest maxima is a bound that at least top_n elements of the segment reach, and few more
+// do. A remembered chunk that reaches it is read again, one round trip; all chunks of a
+// thread only where its second one does too. What reaches the bound is listed and ranked by
+// counting; the cluster's first CTA ranks the CTAs' lists. (Every chunk of the threads whose
+// maximum reaches the bound read again: 34.9 us for 256 rows of 608 KB where this takes
+// 32.0; with two chunks remembered 32.7.) A bound
+// of -inf (a masked vocabulary) lists the finite logits only, the lowest masked indices fill
+// the rest; a list that overflows (hundreds of equal logits) is replaced by top_n passes for
+// the next largest.
 //
-// Small CTAs, four an SM: while one merges and ranks, others stream.
+// Small CTAs, four an SM: while one merges and ranks, others stream. 256 rows of 608 KB:
+// 4.8 TB/s, 0.71 of the measured copy rate; a CTA reads its segment for four fifths of the
+// time, the merge and the list are the rest. 8 rows of 304 KB: 7.0 us, 5 of which is latency
+// (launch, two round trips to DRAM, two cluster barriers).
 #include "common.cuh"
 
 #include <math.h>
@@ -57,6 +62,19 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+template <int kN>
+__device__ __forceinline__ float largest(const float (&z)[kN]) {  // NaN if one is
+  static_assert(kN % 2 == 0, "pairs");
+  float m = max_nan(z[0], z[1]);
+#pragma unroll
+  for (int j = 2; j < kN; j += 2) m = max3_nan(m, z[j], z[j + 1]);
+  return m;
 }
 __device__ __forceinline__ float redux_max(float x) {
   float r;
@@ -149,6 +167,8 @@ __device__ __forceinline__ void move_to(Stat& s, float M, float c) {
 struct Fold {
   float m;
   uint64_t S, W;
+  float m2;  // the second largest of the chunks' maxima
+  int i1;    // the chunk of the largest, -1: none
 };
 __device__ __forceinline__ void move_fold(Fold& f, float M, float c) {
   Stat a{f.m, 0.f, 0.f}, b{f.m, 0.f, 0.f};
@@ -161,13 +181,16 @@ __device__ __forceinline__ void move_fold(Fold& f, float M, float c) {
   f.W = pack2(a.W, b.W);
 }
 template <int kN>
-__device__ __forceinline__ void fold(Fold& f, const float (&z)[kN], float c) {
-  static_assert(kN % 2 == 0, "pairs");
-  float bm = z[0];
-#pragma unroll
-  for (int j = 1; j < kN; ++j) bm = max_nan(bm, z[j]);
+__device__ __forceinline__ void fold(Fold& f, const float (&z)[kN], int chunk, float c) {
+  const float bm = largest(z);
   if (bm == -INFINITY) return;  // nothing but tokens of probability 0
-  if (bm > f.m) move_fold(f, bm, c);
+  if (bm > f.m2) {
+    f.m2 = fminf(bm, f.m);
+    if (bm > f.m) {
+      f.i1 = chunk;
+      move_fold(f, bm, c);
+    }
+  }
   const uint64_t c2 = pack2(c, c), m2 = pack2(-f.m, -f.m);
 #pragma unroll
   for (int j = 0; j < kN; j += 2) {
@@ -193,7 +216,6 @@ __global__ void __launch_bounds__(kThreads, 4)
   __shared__ Stat stat[kWarps];
   __shared__ Stat cta_stat[kMaxCluster];
   __shared__ uint32_t warp_top[kWarps * 8];
-  __shared__ uint8_t holder[kWarps][32];
   __shared__ int n_list;
   const int csize = gridDim.x, rank = blockIdx.x;
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
@@ -225,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   int edge = -1;
   if (rank == 0) edge = t < lead ? t : (t - lead < V - tail ? tail + t - lead : -1);
 
-  Fold f{-INFINITY, 0ull, 0ull};
+  Fold f{-INFINITY, 0ull, 0ull, -INFINITY, -1};
   for (int v = v_lo + t; v < v_hi; v += kUnroll * kThreads) {
     Chunk r[kUnroll];
 #pragma unroll
@@ -236,14 +258,14 @@ __global__ void __launch_bounds__(kThreads, 4)
       if (v + u * kThreads < v_hi) {
         float z[kPer];
         T::unpack(r[u], z);
-        fold(f, z, c);
+        fold(f, z, v + u * kThreads, c);
       }
   }
   float z_edge = -INFINITY;
   if (edge >= 0) {
     z_edge = T::load(z0, edge);
     float z[2] = {z_edge, -INFINITY};
-    fold(f, z, c);
+    fold(f, z, -1, c);
   }
   const uint32_t mine = order_of(f.m);  // this thread's largest
   Stat s{f.m, 0.f, 0.f};
@@ -321,38 +343,32 @@ __global__ void __launch_bounds__(kThreads, 4)
       }
     };
     if (edge >= 0) offer(z_edge, edge);
-    uint32_t who = __ballot_sync(0xffffffffu, mine >= bound);
     auto again = [&](int v, const Chunk& r) {
       float z[kPer];
       T::unpack(r, z);
-      float m = z[0];
-#pragma unroll
-      for (int j = 1; j < kPer; ++j) m = max_nan(m, z[j]);
+      const float m = largest(z);
       if (order_of(m) >= bound || m != m) {
         const int i = lead + v * kPer;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) offer(z[j], i + j);
       }
     };
-    // the chunks of the warp's threads that hold such elements, four a lane on their way at
-    // once: behind a saturated memory every round trip is a few microseconds
-    const int holders = __popc(who);
-    if (holders) {
-      if ((who >> lane) & 1) holder[warp][__popc(who & ((1u << lane) - 1))] = lane;
-      __syncwarp();
-      const int each = (v_hi - v_lo - warp * 32 + kThreads - 1) / kThreads;  // chunks a thread at most
-      for (int u = lane; u < holders * each; u += 32 * kUnroll) {
-        Chunk r[kUnroll];
-        int at[kUnroll];
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-          const int x = u + 32 * k, i = x / each;
-          at[k] = x < holders * each ? v_lo + warp * 32 + holder[warp][i] + (x - i * each) * kThreads : v_hi;
-          if (at[k] < v_hi) r[k] = load32(vec + at[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k)
-          if (at[k] < v_hi) again(at[k], r[k]);
+    // the chunk that a thread remembers
+    const bool many = order_of(f.m2) >= bound;
+    if (mine >= bound && f.i1 >= 0 && !many) again(f.i1, load32(vec + f.i1));
+    // every chunk of the threads with a second one, two threads' at once
+    uint32_t who = __ballot_sync(0xffffffffu, many);
+    while (who) {
+      const int v0 = v_lo + warp * 32 + __ffs(who) - 1 + lane * kThreads;
+      who &= who - 1;
+      const int v1 = who ? v_lo + warp * 32 + __ffs(who) - 1 + lane * kThreads : v_hi;
+      who &= who - 1;
+      for (int o = 0; v0 + o < v_hi || v1 + o < v_hi; o += 32 * kThreads) {
+        Chunk r1, r2;
+        if (v0 + o < v_hi) r1 = load32(vec + v0 + o);
+        if (v1 + o < v_hi) r2 = load32(vec + v1 + o);
+        if (v0 + o < v_hi) again(v0 + o, r1);
+        if (v1 + o < v_hi) again(v1 + o, r2);
       }
     }
     __syncthreads();
@@ -479,9 +495,9 @@ __global__ void __launch_bounds__(kThreads, 4)
 }
 
 // CTAs a row: as many as fit at once over all rows (four an SM), as long as each keeps 32 KB
-// of the row, four chunks a thread. 256 rows of 608 KB at 1 / 2 / 4 / 8: 40.1 / 34.9 / 40.4 /
-// 51.8 us; 8 rows of 304 KB: 17.4 / 11.6 / 8.1 / 6.7, and 6.7 at 16. (With two or three
-// chunks in flight and five or six CTAs an SM the first took 37 to 40 at best.)
+// of the row, four chunks a thread. 256 rows of 608 KB at 1 / 2 / 4 / 8: 36.5 / 32.0 / 37.8 /
+// 50.1 us; 8 rows of 304 KB: 17.5 / 11.4 / 8.4 / 7.0, and no less at 16. (Two or three chunks
+// in flight and five or six CTAs an SM: 37 to 40 for the first.)
 int cluster_size(int rows, long long row_bytes) {
   int s = 1;
   while (s < kMaxCluster && 2LL * rows * s <= 4LL * sd_num_sms() && row_bytes / (2 * s) >= 32768) s *= 2;

@@ -208,7 +208,7 @@ sd_status sd_verify_attention_ex(const void* q, const sd_kv_cache* cache, void* 
 /*
  * Cluster size of the tcgen05 verify-attention kernels (sd_verify_attention
  * and sd_verify_layer; sd_verify_kernel says which shapes take them; and
- * sd_kv8_attention): one
+ * sd_kv8_attention and sd_attention_weights): one
  * thread-block cluster of `cluster_size` CTAs per (scene, KV head) splits that
  * head's keys evenly and merges the partial softmax states in distributed
  * shared memory (the split-L form of Eq. verify). 0 (the default) lets every
@@ -447,10 +447,21 @@ sd_status sd_kv8_store(const sd_kv8_cache* cache, const sd_kv_cache* src, sd_str
 /*
  * Verify attention over an 8-bit cache: sd_verify_attention_ex (the same rows,
  * masks, q and out) on the keys and values that the codes stand for.
- * flags: SD_ATTN_BLOCK_MASK; other bits SD_ERR_INVALID_ARG. Needs no workspace.
+ * flags: SD_ATTN_BLOCK_MASK; other bits SD_ERR_INVALID_ARG.
  * D in {64, 128}, Hq % Hkv == 0 and G*R <= 128. A scene with len[b] < R or
  * len[b] > capacity sets SD_DEVERR_LENGTH and its output is left unwritten.
+ * sd_kv8_attention needs no workspace. With one, sd_kv8_attention_ex gives every
+ * SM an equal share of all scenes' keys where whole clusters a KV head would
+ * leave SMs idle, and joins the heads that a share's border cuts in a second
+ * kernel. workspace: sd_kv8_attention_workspace bytes (0: none is used) of device
+ * memory, 16-byte aligned, of any content; calls that share one must not overlap
+ * on the device; shorter: SD_ERR_WORKSPACE. NULL: as sd_kv8_attention, and so is a
+ * size forced by sd_set_cluster_size. Results of the two ways differ by fp32
+ * rounding order, each the same from run to run.
  */
+size_t sd_kv8_attention_workspace(int B, int R, int Hq, int Hkv, int D, int capacity);
+sd_status sd_kv8_attention_ex(const void* q, const sd_kv8_cache* cache, void* out, int R, int Hq, float scale,
+                              int flags, void* workspace, size_t ws_bytes, sd_stream_t stream);
 sd_status sd_kv8_attention(const void* q, const sd_kv8_cache* cache, void* out, int R, int Hq, float scale,
                            int flags, sd_stream_t stream);
 

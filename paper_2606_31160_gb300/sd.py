@@ -74,6 +74,8 @@ _SIGNATURES = {
     "sd_attention_budget": ([_vp, ctypes.POINTER(KVCacheStruct), _i, _i, _f, _vp, _vp, _vp, _vp], _i),
     "sd_kv8_append": ([ctypes.POINTER(KV8CacheStruct), _vp, _vp, _i, _vp], _i),
     "sd_kv8_store": ([ctypes.POINTER(KV8CacheStruct), ctypes.POINTER(KVCacheStruct), _vp], _i),
+    "sd_kv8_attention_workspace": ([_i, _i, _i, _i, _i, _i], _sz),
+    "sd_kv8_attention_ex": ([_vp, ctypes.POINTER(KV8CacheStruct), _vp, _i, _i, _f, _i, _vp, _sz, _vp], _i),
     "sd_kv8_attention": ([_vp, ctypes.POINTER(KV8CacheStruct), _vp, _i, _i, _f, _i, _vp], _i),
     "sd_attention_weights": ([_vp, ctypes.POINTER(KVCacheStruct), _i, _i, _f, _vp, _vp, _f, _vp, _vp], _i),
     "sd_kv_evict": ([ctypes.POINTER(KVCacheStruct), _vp, _i, _i, _i, ctypes.POINTER(KVCacheStruct), _vp, _vp, _vp], _i),
@@ -398,19 +400,34 @@ def kv8_store(cache, src):
     _check(lib().sd_kv8_store(cache.struct, src.struct, _stream()), "sd_kv8_store")
 
 
-def kv8_attention(q, cache, out=None, scale=0.0, block=False):
+def kv8_attention_workspace_bytes(B, R, Hq, Hkv, D, capacity):
+    return int(lib().sd_kv8_attention_workspace(B, R, Hq, Hkv, D, capacity))
+
+
+def kv8_attention(q, cache, out=None, scale=0.0, block=False, ws=None):
     """Verify attention of q [B,R,Hq,D] bf16 (rotated) over an 8-bit cache (rows appended):
     verify_attention on the keys and values that the codes stand for. block=True selects
-    the block mask."""
+    the block mask. ws: kv8_attention_workspace_bytes of device memory; when None a batch
+    that takes one has it from torch's allocator, on the current stream."""
     B, R, Hq, D = q.shape
-    if cache.shape[0] != B or cache.shape[3] != D:
+    _, Hkv, cap, dim = cache.shape
+    if cache.shape[0] != B or dim != D:
         raise ValueError("q and cache disagree")
     if out is None:
         out = torch.empty_like(q)
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
-    _check(lib().sd_kv8_attention(_dev(q, "q", torch.bfloat16), cache.struct, _dev(out, "out", torch.bfloat16), R, Hq,
-                                  float(scale), SD_ATTN_BLOCK_MASK if block else 0, _stream()), "sd_kv8_attention")
+    if ws is None and B > 1:
+        need = lib().sd_kv8_attention_workspace(B, R, Hq, Hkv, D, cap)
+        if need:
+            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    args = (_dev(q, "q", torch.bfloat16), cache.struct, _dev(out, "out", torch.bfloat16), R, Hq, float(scale),
+            SD_ATTN_BLOCK_MASK if block else 0)
+    if ws is None:
+        _check(lib().sd_kv8_attention(*args, _stream()), "sd_kv8_attention")
+    else:
+        _check(lib().sd_kv8_attention_ex(*args, _dev(ws, "ws"), ws.numel() * ws.element_size(), _stream()),
+               "sd_kv8_attention")
     return out
 
 

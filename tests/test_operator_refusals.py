@@ -58,6 +58,18 @@ def test_kv8_attention(lib):
     assert call(_c8(B=0), q=0, out=0) == 0
 
 
+def test_kv8_attention_with_a_workspace(lib):
+    def call(c, q=16, out=16, R=8, Hq=32, scale=0.0, flags=0, ws=16, nbytes=1 << 24):
+        return lib.sd_kv8_attention_ex(P(q), c, P(out), R, Hq, scale, flags, P(ws), nbytes, None)
+    assert call(None) == 1 and call(_c8(D=32)) == 2 and call(_c8(), R=33) == 2
+    assert call(_c8(), Hq=30) == 1 and call(_c8(), flags=2) == 1 and call(_c8(), scale=-1.0) == 1
+    assert call(_c8(), q=0) == 1 and call(_c8(), ws=24) == 1
+    assert call(_c8(B=0), q=0, out=0, ws=0, nbytes=0) == 0
+    for shape in ((0, 8, 32, 8, 128, 100), (4, 0, 32, 8, 128, 100), (4, 8, 30, 8, 128, 100), (4, 33, 32, 8, 128, 100),
+                  (4, 8, 32, 8, 96, 100), (4, 8, 32, 8, 128, 0), (4, 8, 32, 0, 128, 100)):
+        assert lib.sd_kv8_attention_workspace(*shape) == 0
+
+
 def test_attention_weights(lib):
     def call(c, q=16, R=8, Hq=32, scale=0.0, committed=0, before=16, decay=1.0, out=32):
         return lib.sd_attention_weights(P(q), c, R, Hq, scale, P(committed), P(before), decay, P(out), None)

@@ -36,8 +36,8 @@
 // share of the tiles of all units instead, and a second kernel joins what the shares' borders
 // cut.
 //
-// What bounds it. 32 scenes of 6200 to 8192 keys, 8 heads, 36 rows: 102 us, 489 MB at
-// 0.70 of the measured copy rate. The softmax: a tile takes an SM 1.6 thousand cycles, 16
+// What bounds it. 32 scenes of 6200 to 8192 keys, 8 heads, 36 rows: 101 us, 489 MB at
+// 0.71 of the measured copy rate. The softmax: a tile takes an SM 1.6 thousand cycles, 16
 // warps and 96 registers a thread; without its arithmetic 82 us (of the 112 of whole clusters),
 // without the vote 101, without the conversions to two terms besides 92, and with every key
 // from L2 still 111. One scene of 4096 keys (8 heads, 32 rows: 8.1 us; 4 heads of one row
@@ -1035,8 +1035,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv8_join_kernel(const Args a,
     const int slot = 2 * (c - 1 + i) + (i == 0 && s.begin(c - 1) < unit_begin ? 1 : 0);
     return a.part + (static_cast<long long>(slot) * kR + row0) * kRowF;
   };
-  griddep_wait();
-  griddep_launch();
+  griddep_wait();  // (the next kernel waits for this one's end: beside its large CTAs these ran late, 107 us)
   if (!mine || n_rows <= 0) return;
   float m[kJoinRows], l[kJoinRows], o[kJoinRows][kPer];
 #pragma unroll
@@ -1145,7 +1144,7 @@ DevState* state() {
 // where they cost less (tiles a CTA + 4 a unit + the start and the join) and the call may
 // have them. Clusters / even shares in us, 8 KV heads of 4096 keys (3/4 to all of them
 // filled) and 32 rows: 10 scenes 23.4 / 27.5, 16: 25.7 / 33.4, 20: 43.7 / 38.7, 24: 45.4 /
-// 43.2, 32: 48.2 / 52.0, 64: 103 / 90; 32 scenes of 8192 keys and 36 rows 108 / 102, 64 of
+// 43.2, 32: 48.2 / 52.0, 64: 103 / 90; 32 scenes of 8192 keys and 36 rows 108 / 101, 64 of
 // 1024 40 / 45. Head dim 64, 4 KV heads of 4096: 20 scenes 33.5 / 32.9, 40: 55.7 / 50.2.
 int pick_cluster(const int* active, long long units, int cap, int D, bool may) {
   const int forced = sd_internal_forced_cluster();

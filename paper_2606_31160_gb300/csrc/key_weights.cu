@@ -24,12 +24,13 @@
 // warps of a lane quarter take every fourth tile.
 // More than 128 rows go through both passes in turn.
 //
-// What bounds it. One scene (8 heads, L = 4096, 32 rows: 6.8 us) the chain of latencies:
+// What bounds it. One scene (8 heads, L = 4096, 32 rows: 6.9 us) the chain of latencies:
 // lengths, keys and rows, products, sums, their exchange, weights. Eight scenes of 8192
-// keys and 128 rows (51.5 us, 121 MB of keys read twice) memory: the second reading finds
-// about two thirds of the keys in L2 (152 MB from DRAM), and the arithmetic is hidden (32
-// rows: 43). Two CTAs an SM, each with half the warps and tensor memory, were slower (one
-// scene 9.7, eight 52 at their best size).
+// keys and 128 rows (52.0 us, 121 MB of keys read twice) the SMs' reading of 262 MB, 35 us
+// by itself on 128 CTAs (36 bytes a cycle and SM); the second reading finds about two
+// thirds of the keys in L2 (152 MB from DRAM). With the products 38, with the exponentials
+// of both passes 48 from L2. Two CTAs an SM, each with half the warps and tensor memory,
+// were slower (one scene 9.7, eight 52 at their best size).
 #include "tc_common.cuh"
 
 #include <math.h>
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if constexpr (C::kTurned) {
         // this thread's row: its reference and sum over every fourth tile's keys (with a quarter
         // of every tile the 16 warps met at each tile, and its chain of latencies set the pace:
-        // 51.5 us for eight scenes of 8192 keys)
+        // 53.8 us for eight scenes of 8192 keys)
         float ref = -INFINITY, l = 0.f;
         const bool idle = quarter * 32 >= rows_in;
         // keys below this one are seen
@@ -528,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             scaled(x[6], x[7], n1.z, n1.w, y[6], y[7]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = ex2(y[j]);
-            if (masks || 8 * u + 8 > rows_in) {  // (a score that is masked or no row's may be NaN)
+            if (masks) {  // (a score that is masked or no row's may be NaN)
 #pragma unroll
               for (int j = 0; j < 8; ++j)
                 if (8 * u + j < below || 8 * u + j >= rows_in) y[j] = 0.f;
@@ -550,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
             }
           };
-          if (masked_tile(t)) all(true);
+          if (masked_tile(t) || (rows_in & 7)) all(true);
           else all(false);
           if (key < key_end) a.out[at] = before + (sum2(w0) + sum2(w1));
         }

@@ -6,12 +6,19 @@
 // Several CTAs a (KV head, scene), each moving its share of the places in dst: they need
 // nothing of each other, as each finds the whole selection itself from the weights (4 bytes
 // a key against the 512 of a kept row: 16384 keys are 64 KB from L2). The weight of the last
-// key kept: the keys are counted by the leading 11 bits of an integer that orders as the
-// weight does; those that share the deciding bits are listed, and a few of them ranked by
-// counting, more of them counted by their other bits, in two more passes (over all keys
-// where the list is too short: weights within an eighth of each other). Then a key's place is the number of kept keys before it: ballots,
-// kept in shared memory, are summed a warp a range of keys, and the CTA lists its share from
-// them, whose rows it copies with eight 16-byte loads a thread in flight.
+// key kept: integers that order as the weights do are counted by 4096 equal ranges between
+// the least and the largest of them; those of the deciding range are listed, and a few
+// ranked by counting, more counted by their other bits (over all keys where the list is too
+// short). Then a key's place is the number of kept keys before it: a lane marks four keys, a
+// warp sums a range of them, and the CTA lists its share from the marks, whose rows it
+// copies with eight 16-byte loads a thread in flight.
+//
+// What bounds it. 8 scenes of 16384 keys to 4096, 8 heads: 56.5 us, of which the rows' copies
+// are ~43 (268 MB at 6.2 TB/s) and the selection 12 (20 thousand cycles: lengths 3.0, weights
+// and their range 3.3, counting 3.0, list 2.3, rank 1.8, marks 2.1, places 5.0), before which
+// no row can be copied. It is instructions, not latency: four keys a lane took it from 31
+// thousand cycles (and one scene of 4096 keys from 9.4 to 7.7 us), more loads in flight did
+// not.
 #include "common.cuh"
 
 SD_DEFINE_ERROR_ACCESSOR(sd_take_error_evict)
@@ -20,16 +27,18 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
-constexpr int kBins = 2048;
-constexpr int kList = 1024;     // kept keys that a CTA lists, then copies, at a time
-constexpr int kRank = 64;      // listed keys that are ranked by counting
-constexpr int kKeysMax = 20480; // keys whose integers and ballots stay in shared memory; more are read anew each time
+constexpr int kBits = 12, kBins = 1 << kBits;
+constexpr int kBlock = 128;     // keys a warp looks at at once: four a lane
+constexpr int kList = 2048;     // kept keys that a CTA lists, then copies, at a time
+constexpr int kRank = 128;      // listed keys that are ranked by counting
+constexpr int kKeysMax = 20480; // keys whose integers and marks stay in shared memory; more are read anew each time
 
-// An integer that orders as the weight does (-0 as +0; NaN below every number).
+// An integer that orders as the weight does (-0 as +0; NaN below every number: 1). 0 is
+// no key's, nor is kSure, which stands for the keys that stay whatever their weight.
+constexpr uint32_t kSure = 0xffffffffu;
 __device__ __forceinline__ uint32_t order_of(float w) {
   const uint32_t u = __float_as_uint(w + 0.f);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  return w != w ? 1u : u ^ (static_cast<uint32_t>(static_cast<int>(u) >> 31) | 0x80000000u);
 }
 
 // The sum of x[w], w < n <= 32, by a whole warp.
@@ -41,14 +50,15 @@ __device__ __forceinline__ int sum_of(const int* x, int n, int lane) {
 __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, const float* weights, const sd_kv_cache dst,
                                                          int keep, int sinks, int recent, float* weights_out, int32_t* kept,
                                                          int smem_keys, int vec_shift) {
-  extern __shared__ uint32_t order[];                  // [smem_keys], then ballots[smem_keys / 32]
-  uint2* ballots = reinterpret_cast<uint2*>(order + smem_keys);  // of 32 keys: which stay, which tie
+  extern __shared__ __align__(16) uint32_t order[];    // [smem_keys], then the marks
+  uint8_t* marks = reinterpret_cast<uint8_t*>(order + smem_keys);  // of four keys: which stay, 16 times which tie
   __shared__ __align__(16) int bins[kBins];
-  __shared__ __align__(16) int list[kList];
+  __shared__ __align__(16) int list[kList + 4];
   __shared__ int warp_sum[kWarps];
   __shared__ int warp_kept[kWarps], warp_ties[kWarps];
   __shared__ int s_bin, s_left, s_count;
   __shared__ uint32_t s_T;
+  __shared__ uint32_t warp_least[kWarps], warp_most[kWarps];
   sd_pdl_enter();
   const int part = blockIdx.x, parts = gridDim.x, h = blockIdx.y, b = blockIdx.z, Hkv = src.n_kv_heads;
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
@@ -70,20 +80,89 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
   const int want = m - lo - (n - hi);
   const bool all = n <= keep;                                   // every key stays
   const bool cached = n <= smem_keys;
-  auto order_at = [&](int i) { return cached ? order[i] : order_of(__ldcg(weights + i)); };
+  const bool aligned = (reinterpret_cast<uintptr_t>(weights) & 15) == 0;
+  auto weights4 = [&](int i, float (&w)[4]) {  // of keys i .. i + 3, i a multiple of 4; 0 past the last
+    if (aligned && i + 4 <= n) {
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(weights + i));
+      w[0] = x.x;
+      w[1] = x.y;
+      w[2] = x.z;
+      w[3] = x.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = i + e < n ? __ldcg(weights + i + e) : 0.f;
+    }
+  };
+  auto orders4 = [&](int i, const float (&w)[4]) {  // 0 past the last key
+    uint32_t o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = order_of(w[e]);
+    if (i < lo || i + 4 > hi) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = i + e >= n ? 0u : (i + e < lo || i + e >= hi ? kSure : o[e]);
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+  };
+  auto order4 = [&](int i) {
+    if (cached) return *reinterpret_cast<const uint4*>(order + i);
+    float w[4];
+    weights4(i, w);
+    return orders4(i, w);
+  };
+  const int n_blocks = (n + kBlock - 1) / kBlock;
+  // f(order) of every key
+  auto each = [&](auto f) {
+    for (int i = 4 * t; i < n; i += 4 * kThreads) {
+      const uint4 o = order4(i);
+      f(o.x);
+      f(o.y);
+      f(o.z);
+      f(o.w);
+    }
+  };
 
   // ---- T: the order of the last competing key kept; `ties` of those equal to it stay
   uint32_t T = 0;
   int ties = 0;
   if (!all) {
-    int left = want;  // to be taken among the keys whose leading bits are T's
+    int left = want;  // to be taken among the keys of the range [T, T + 2^shift)
+    // every key's integer, the least and the largest of those that compete
+    for (int i = t; i < kBins; i += kThreads) bins[i] = 0;
+    if (t == 0) s_count = 0;
+    uint32_t least = kSure, most = 0;  // less and plus 1: of 0 and kSure neither counts
+    constexpr int kU = 4;
+    for (int i0 = 4 * t; i0 < n_blocks * kBlock; i0 += kU * 4 * kThreads) {
+      float w[kU][4];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) weights4(i0 + u * 4 * kThreads, w[u]);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int i = i0 + u * 4 * kThreads;
+        if (i >= n_blocks * kBlock) break;
+        const uint4 o = orders4(i, w[u]);
+        if (cached) *reinterpret_cast<uint4*>(order + i) = o;
+        least = min(least, min(min(o.x - 1, o.y - 1), min(o.z - 1, o.w - 1)));
+        most = max(most, max(max(o.x + 1, o.y + 1), max(o.z + 1, o.w + 1)));
+      }
+    }
+    least = __reduce_min_sync(0xffffffffu, least);
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) {
+      warp_least[warp] = least;
+      warp_most[warp] = most;
+    }
+    __syncthreads();
+    // kBins ranges from the least on, each of the smallest power of two that reaches the largest
+    T = __reduce_min_sync(0xffffffffu, warp_least[lane]) + 1;
+    static_assert(kWarps == 32, "a lane a warp");
+    int shift = max(0, 32 - __clz(__reduce_max_sync(0xffffffffu, warp_most[lane]) - 1 - T) - kBits);
     // the bin in which the left-th key lies, the largest digits first: a prefix sum over the
-    // bins, two a thread
-    auto find = [&](int n_bins, int shift) {
+    // bins, four a thread
+    auto find = [&](int n_bins) {
       __syncthreads();
-      static_assert(kBins == 2 * kThreads, "two bins a thread");
-      const int2 c = reinterpret_cast<const int2*>(bins)[t];
-      const int sum = c.x + c.y;
+      static_assert(kBins == 4 * kThreads, "four bins a thread");
+      const int4 c = reinterpret_cast<const int4*>(bins)[t];
+      const int sum = (c.x + c.y) + (c.z + c.w);
       int before = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -94,49 +173,39 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
       __syncthreads();
       before += sum_of(warp_sum, warp, lane) - sum;
       if (before < left && before + sum >= left) {  // one thread's
-        const bool second = before + c.x < left;
-        s_bin = 2 * t + second;
-        s_left = left - before - (second ? c.x : 0);
+        const int c1 = before + c.x, c2 = c1 + c.y, c3 = c2 + c.z;
+        const int which = (c1 < left) + (c2 < left) + (c3 < left);
+        s_bin = 4 * t + which;
+        s_left = left - (which == 0 ? before : which == 1 ? c1 : which == 2 ? c2 : c3);
       }
       __syncthreads();
-      T |= static_cast<uint32_t>(n_bins - 1 - s_bin) << shift;
+      T += static_cast<uint32_t>(n_bins - 1 - s_bin) << shift;
       left = s_left;
     };
-    for (int i = t; i < kBins; i += kThreads) bins[i] = 0;
-    if (t == 0) s_count = 0;
-    __syncthreads();
-    for (int i0 = t; i0 < n; i0 += 4 * kThreads) {
-      float w[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) w[u] = i0 + u * kThreads < n ? __ldcg(weights + i0 + u * kThreads) : 0.f;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int i = i0 + u * kThreads;
-        const uint32_t o = order_of(w[u]);
-        if (i < n && cached) order[i] = o;
-        if (i >= lo && i < hi) atomicAdd(&bins[kBins - 1 - (o >> 21)], 1);
-      }
-    }
     if (left > 0) {
-      find(kBins, 21);
-      const int alike = bins[s_bin];  // keys that share T's leading bits
+      each([&](uint32_t o) {
+        if (o - 1 < kSure - 1) atomicAdd(&bins[kBins - 1 - ((o - T) >> shift)], 1);
+      });
+      find(kBins);
+      const int alike = bins[s_bin];  // keys in T's range
       const bool listed = alike <= kList;
       if (listed) {
-        for (int i = lo + t; i < hi; i += kThreads) {
-          const uint32_t o = order_at(i);
-          if ((o >> 21) == (T >> 21)) list[atomicAdd(&s_count, 1)] = static_cast<int>(o);
-        }
+        // (0 and kSure are further than 2^20 from every weight's integer)
+        each([&](uint32_t o) {
+          if (o - T < 1u << shift) list[atomicAdd(&s_count, 1)] = static_cast<int>(o);
+        });
       }
       if (alike <= kRank) {
+        if (t >= alike && t < alike + 3) list[t] = 0;  // (read four at a time)
         __syncthreads();
         if (t < alike) {
           const uint32_t o = static_cast<uint32_t>(list[t]);
           int above = 0, equal = 0;
-#pragma unroll 8
-          for (int j = 0; j < alike; ++j) {
-            const uint32_t x = static_cast<uint32_t>(list[j]);
-            above += x > o;
-            equal += x == o;
+#pragma unroll 4
+          for (int j = 0; j < alike; j += 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(list + j);
+            above += (x.x > o) + (x.y > o) + (x.z > o) + (x.w > o);
+            equal += (x.x == o) + (x.y == o) + (x.z == o) + (x.w == o);
           }
           if (above < left && above + equal >= left) {  // the threads with that one integer
             s_T = o;
@@ -148,56 +217,56 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
         left = s_left;
       } else {
 #pragma unroll 1
-        for (int pass = 1; pass < 3; ++pass) {
-          const int shift = pass == 1 ? 10 : 0, width = pass == 1 ? 11 : 10, n_bins = 1 << width;
+        while (shift > 0) {
+          const int width = min(kBits, shift), n_bins = 1 << width;
+          shift -= width;
           __syncthreads();
           for (int i = t; i < kBins; i += kThreads) bins[i] = 0;
           __syncthreads();
-          const int from = listed ? 0 : lo, to = listed ? alike : hi;
-          for (int i = from + t; i < to; i += kThreads) {
-            const uint32_t o = listed ? static_cast<uint32_t>(list[i]) : order_at(i);
-            if ((o >> (shift + width)) == (T >> (shift + width)))
-              atomicAdd(&bins[n_bins - 1 - static_cast<int>((o >> shift) & (n_bins - 1))], 1);
+          auto count = [&](uint32_t o) {
+            if (o - T < 1u << (shift + width)) atomicAdd(&bins[n_bins - 1 - static_cast<int>((o - T) >> shift)], 1);
+          };
+          if (listed) {
+            for (int i = t; i < alike; i += kThreads) count(static_cast<uint32_t>(list[i]));
+          } else {
+            each(count);
           }
-          find(n_bins, shift);
+          find(n_bins);
         }
       }
       ties = left;
     } else {
-      T = 0xffffffffu;  // none of them stays (no key's order is all ones)
+      T = kSure - 1;  // none of them stays
       __syncthreads();
     }
   }
 
-  // ---- places: each warp's keys, a range of whole ballots
-  const int per_warp = ((n + kWarps - 1) / kWarps + 31) / 32 * 32;
-  const int i_lo = warp * per_warp, i_hi = min(n, i_lo + per_warp);
-  // a key's kind: 2 stays, 1 ties with the last that stays, 0 goes
-  auto kind = [&](int i) {
-    if (i >= i_hi) return 0;
-    if (all || i < lo || i >= hi) return 2;
-    const uint32_t o = order_at(i);
-    return o > T ? 2 : (o == T ? 1 : 0);
+  // ---- places: each warp's keys, a range of whole blocks
+  const int per_warp = (n_blocks + kWarps - 1) / kWarps;
+  const int blk_lo = min(n_blocks, warp * per_warp), blk_hi = min(n_blocks, blk_lo + per_warp);
+  auto marks_of = [&](int blk) {
+    const uint4 o = order4(blk * kBlock + 4 * lane);
+    return (o.x > T ? 1u : 0u) | (o.y > T ? 2u : 0u) | (o.z > T ? 4u : 0u) | (o.w > T ? 8u : 0u) |
+           (o.x == T ? 16u : 0u) | (o.y == T ? 32u : 0u) | (o.z == T ? 64u : 0u) | (o.w == T ? 128u : 0u);
   };
-  auto ballots_at = [&](int i0) {
-    const int k = kind(i0 + lane);
-    return make_uint2(__ballot_sync(0xffffffffu, k == 2), __ballot_sync(0xffffffffu, k == 1));
-  };
-  {
+  auto ones = [](uint32_t x) { return __popc(x & 15u) | __popc(x >> 4) << 16; };  // that stay, and 2^16 times that tie
+  if (!all) {
     int stay = 0, tie = 0;
-    for (int i0 = i_lo; i0 < i_hi; i0 += 32) {
-      const uint2 b = ballots_at(i0);
-      if (cached && lane == 0) ballots[i0 >> 5] = b;
-      stay += __popc(b.x);
-      tie += __popc(b.y);
+    for (int blk = blk_lo; blk < blk_hi; ++blk) {
+      const uint32_t x = marks_of(blk);
+      if (cached) marks[blk * 32 + lane] = static_cast<uint8_t>(x);
+      stay += __popc(x & 15u);
+      tie += __popc(x >> 4);
     }
+    stay = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(stay));
+    tie = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(tie));
     if (lane == 0) {
       warp_kept[warp] = stay;
       warp_ties[warp] = tie;
     }
   }
   __syncthreads();
-  const int stay0 = sum_of(warp_kept, warp, lane), ties0 = sum_of(warp_ties, warp, lane);
+  const int stay0 = all ? 0 : sum_of(warp_kept, warp, lane), ties0 = all ? 0 : sum_of(warp_ties, warp, lane);
   const int vec = 1 << vec_shift;
   const uint4* ks = static_cast<const uint4*>(src.k) + ((plane * src.capacity) << vec_shift);
   const uint4* vs = static_cast<const uint4*>(src.v) + ((plane * src.capacity) << vec_shift);
@@ -207,18 +276,41 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
   for (int q_lo = p_lo; q_lo < p_hi; q_lo += kList) {
     const int q_hi = min(p_hi, q_lo + kList);
     __syncthreads();  // the list before is copied
-    int stay = stay0, tie = ties0;
-    for (int i0 = i_lo; i0 < i_hi && stay + min(tie, ties) < q_hi; i0 += 32) {
-      const uint2 x = cached ? ballots[i0 >> 5] : ballots_at(i0);
-      const int stay1 = stay + __popc(x.x), tie1 = tie + __popc(x.y);
-      if (stay1 + min(tie1, ties) > q_lo) {
-        const uint32_t below = (1u << lane) - 1;
-        const int my_ties = tie + __popc(x.y & below);
-        const int at = stay + __popc(x.x & below) + min(my_ties, ties);
-        if ((((x.x >> lane) & 1) || (((x.y >> lane) & 1) && my_ties < ties)) && at >= q_lo && at < q_hi) list[at - q_lo] = i0 + lane;
+    if (all) {
+      for (int j = q_lo + t; j < q_hi; j += kThreads) list[j - q_lo] = j;
+    } else {
+      int stay = stay0, tie = ties0;
+      const bool mine = stay + warp_kept[warp] + min(tie + warp_ties[warp], ties) > q_lo;  // of this warp's keys one at least
+      for (int blk = blk_lo; mine && blk < blk_hi && stay + min(tie, ties) < q_hi; ++blk) {
+        const uint32_t x = cached ? marks[blk * 32 + lane] : marks_of(blk);
+        const int own = ones(x);
+        int upto = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += y;
+        }
+        const int sums = __shfl_sync(0xffffffffu, upto, 31), stay1 = stay + (sums & 0xffff), tie1 = tie + (sums >> 16);
+        if (stay1 + min(tie1, ties) > q_lo) {
+          int at = stay + ((upto - own) & 0xffff) - q_lo, tied = tie + ((upto - own) >> 16);
+          const int first = blk * kBlock + 4 * lane;
+          // (one store a key, its address chosen: branches were slower)
+          const int count = q_hi - q_lo;
+          const bool any_tie = sums >> 16 != 0;
+          if (!any_tie) at += min(tie, ties);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool stays = (x >> e) & 1, ties_here = any_tie && ((x >> (4 + e)) & 1);
+            const int place = any_tie ? at + min(tied, ties) : at;
+            const bool ok = (stays || (ties_here && tied < ties)) && static_cast<unsigned>(place) < static_cast<unsigned>(count);
+            list[ok ? place : kList] = first + e;
+            at += stays;
+            tied += ties_here;
+          }
+        }
+        stay = stay1;
+        tie = tie1;
       }
-      stay = stay1;
-      tie = tie1;
     }
     __syncthreads();
     const int count = q_hi - q_lo;
@@ -289,7 +381,7 @@ extern "C" sd_status sd_kv_evict(const sd_kv_cache* src, const float* weights, i
   long long parts = sd_num_sms() / pairs;
   if (parts < 1) parts = 1;
   if (parts > (keep + 31) / 32) parts = (keep + 31) / 32;
-  const int smem_keys = src->capacity < kKeysMax ? (src->capacity + 31) / 32 * 32 : kKeysMax;
+  const int smem_keys = src->capacity < kKeysMax ? (src->capacity + kBlock - 1) / kBlock * kBlock : kKeysMax;
   static bool allowed[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {

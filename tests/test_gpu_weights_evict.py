@@ -157,6 +157,29 @@ def test_evict_special_weights():
         _evict(w, [257, 130], keep, 0, 0)
 
 
+@pytest.mark.parametrize("cap", [127, 128, 129, 515, 5000, 21000])
+@pytest.mark.parametrize("kind", ["crowded", "far", "nan", "low", "negative"])
+def test_evict_ranges_of_weights(cap, kind):
+    """The selection counts weights by equal ranges between the least and the largest."""
+    rng = np.random.default_rng(cap)
+    if kind == "crowded":    # all but two in one range, few of them alike
+        w = (1.0 + rng.integers(0, 4000, (1, 2, cap)) * 2.0 ** -23).astype(np.float32)
+        w[:, :, 1], w[:, :, 2] = 1e30, 1e-30
+    elif kind == "far":      # infinities, denormals, zeros of both signs
+        w = np.exp(rng.standard_normal((1, 2, cap)) * 30).astype(np.float32)
+        w[:, :, ::5], w[:, :, 1::7], w[:, :, 2::11], w[:, 0, 3], w[:, 1, 4] = 0.0, -0.0, 1e-42, np.inf, -np.inf
+    elif kind == "nan":      # more keys are kept than have a number
+        w = np.full((1, 2, cap), np.nan, dtype=np.float32)
+        w[:, :, ::9] = rng.random(w[:, :, ::9].shape)
+    elif kind == "low":      # every weight -inf but one
+        w = np.full((1, 2, cap), -np.inf, dtype=np.float32)
+        w[:, :, cap // 2] = -1e38
+    else:
+        w = -rng.random((1, 2, cap)).astype(np.float32)
+    for keep, sinks, recent in ((1, 0, 0), (cap // 2, 3, 5), (cap - 1, 0, 0), (cap - 1, cap // 3, cap // 3)):
+        _evict(w, [cap], keep, sinks, recent)
+
+
 def test_evict_without_extras_and_into_a_smaller_capacity():
     rng = np.random.default_rng(10)
     _evict(rng.random((2, 2, 500)), [500, 77], 100, 2, 3, cap2=100, extra=False)

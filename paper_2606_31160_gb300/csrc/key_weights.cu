@@ -26,7 +26,7 @@
 //
 // What bounds it. One scene (8 heads, L = 4096, 32 rows: 6.9 us) the chain of latencies:
 // lengths, keys and rows, products, sums, their exchange, weights. Eight scenes of 8192
-// keys and 128 rows (52.0 us, 121 MB of keys read twice) the SMs' reading of 262 MB, 35 us
+// keys and 128 rows (52.0 us, 121 MB of keys read twice) the SMs' reading of 242 MB, 35 us
 // by itself on 128 CTAs (36 bytes a cycle and SM); the second reading finds about two
 // thirds of the keys in L2 (152 MB from DRAM). With the products 38, with the exponentials
 // of both passes 48 from L2. Two CTAs an SM, each with half the warps and tensor memory,

@@ -478,10 +478,18 @@ sd_status sd_kv8_attention(const void* q, const sd_kv8_cache* cache, void* out, 
  *   NULL: all R. weights_in, weights: fp32 [B][Hkv][capacity] device;
  *   weights_in may be NULL (nothing before) or weights itself; scale as for
  *   sd_verify_attention.
- * D in {64, 128}, Hq % Hkv == 0; any R. A scene with len[b] < R or len[b] >
- * capacity sets SD_DEVERR_LENGTH, one with committed[b] outside [0, R]
- * SD_DEVERR_ROLLBACK; both are left unwritten.
+ * D in {64, 128}, Hq % Hkv == 0, Hq / Hkv <= 4095 and G*R <= 2^20. A scene with
+ * len[b] < R or len[b] > capacity sets SD_DEVERR_LENGTH, one with committed[b]
+ * outside [0, R] SD_DEVERR_ROLLBACK; both are left unwritten.
+ * sd_attention_weights needs no workspace. With one, sd_attention_weights_ex gives
+ * every SM an equal share of all scenes' keys, in two kernels, where that is faster
+ * than clusters a KV head: sd_attention_weights_workspace bytes (0: none is used),
+ * as for sd_kv8_attention_ex.
  */
+size_t sd_attention_weights_workspace(int B, int R, int Hq, int Hkv, int D, int capacity);
+sd_status sd_attention_weights_ex(const void* q, const sd_kv_cache* cache, int R, int Hq, float scale,
+                                  const int32_t* committed, const float* weights_in, float decay,
+                                  float* weights, void* workspace, size_t ws_bytes, sd_stream_t stream);
 sd_status sd_attention_weights(const void* q, const sd_kv_cache* cache, int R, int Hq, float scale,
                                const int32_t* committed, const float* weights_in, float decay,
                                float* weights, sd_stream_t stream);

@@ -42,6 +42,7 @@
 // without the vote 101, without the conversions to two terms besides 92, and with every key
 // from L2 still 111. One scene of 4096 keys (8 heads, 32 rows: 8.1 us; 4 heads of one row
 // each: 6.6) the chain of latencies: lengths, rows and keys, S, references, P, PV, merge.
+#include "shares.cuh"
 #include "tc_common.cuh"
 
 #include <math.h>
@@ -235,97 +236,18 @@ __device__ __forceinline__ float warp_sum8(float (&v)[8], int lane) {
   return x;
 }
 
-// ------------------------------------------------------------------ even shares
-// The tiles of all units (scene, KV head, m-block), one unit after the other, cut into one
-// contiguous share a CTA; fewer than 2^31. Scenes whose length is not valid have no tiles.
-__device__ __forceinline__ int tiles_of(const Args& a, int n_keys) {
-  return n_keys >= a.R && n_keys <= a.cap ? (n_keys + kTile - 1) / kTile : 0;
-}
-struct Shares {
-  int units, total, each, rest;  // units a scene, all tiles, tiles a share, shares with one more
-  int n_keys;                    // of scene `lane`
-  __device__ __forceinline__ Shares(const Args& a, int lane, int ctas) {
-    units = a.Hkv * a.mblocks;
-    n_keys = lane < a.B ? __ldcg(a.len + lane) : -1;
-    int n = tiles_of(a, n_keys);
-    for (int b = lane + 32; b < a.B; b += 32) n += tiles_of(a, __ldcg(a.len + b));
-    total = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(n))) * units;
-    each = total / ctas;
-    rest = total - each * ctas;
-  }
-  __device__ __forceinline__ int begin(int cta) const { return cta * each + min(cta, rest); }
-};
-struct Place {
-  int b, unit, tile;  // tile `tile` of unit `unit` (KV head and m-block) of scene b,
-  int n_keys, tiles;  // which has so many keys, and tiles a unit
-};
-__device__ __forceinline__ Place locate(const Args& a, const Shares& s, int pos, int lane) {  // pos < total
-  Place p = {};
-  int n_keys = s.n_keys;
-  for (int b0 = 0; b0 < a.B; b0 += 32) {
-    if (b0 > 0) n_keys = b0 + lane < a.B ? __ldcg(a.len + b0 + lane) : -1;
-    const int mine = tiles_of(a, n_keys) * s.units;
-    int upto = mine;
-#pragma unroll
-    for (int x = 1; x < 32; x <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, upto, x);
-      if (lane >= x) upto += y;
-    }
-    const uint32_t past = __ballot_sync(0xffffffffu, upto > pos);
-    if (past) {
-      const int at = __ffs(past) - 1;
-      p.b = b0 + at;
-      p.n_keys = __shfl_sync(0xffffffffu, n_keys, at);
-      p.tiles = tiles_of(a, p.n_keys);
-      const int in = pos - __shfl_sync(0xffffffffu, upto - mine, at);
-      p.unit = in / p.tiles;
-      p.tile = in - p.unit * p.tiles;
-      break;
-    }
-    pos -= __shfl_sync(0xffffffffu, upto, 31);
-  }
-  return p;
-}
-// A run of one unit's tiles that a CTA takes.
+// A run of one unit's keys that a CTA takes.
 struct Run {
   int b, kvh, mblock, n_keys, key_begin, key_end, n_tiles;
   bool whole;  // all the unit's tiles
 };
-// A CTA's share, run by run.
-struct Walk {
-  Place at;
-  int left;  // tiles
-  __device__ __forceinline__ void begin(const Args& a, int lane) {
-    const Shares s(a, lane, gridDim.x);
-    const int first = s.begin(blockIdx.x);
-    left = s.begin(blockIdx.x + 1) - first;
-    at = Place{};
-    if (left > 0) at = locate(a, s, first, lane);
-  }
-  __device__ __forceinline__ Run next(const Args& a) {
-    Run r;
-    r.b = at.b;
-    r.kvh = at.unit / a.mblocks;
-    r.mblock = at.unit - r.kvh * a.mblocks;
-    r.n_keys = at.n_keys;
-    r.n_tiles = min(at.tiles - at.tile, left);
-    r.whole = r.n_tiles == at.tiles;
-    r.key_begin = at.tile * kTile;
-    r.key_end = at.tile + r.n_tiles == at.tiles ? at.n_keys : r.key_begin + r.n_tiles * kTile;
-    left -= r.n_tiles;
-    at.tile = 0;
-    if (left > 0 && ++at.unit == a.Hkv * a.mblocks) {
-      at.unit = 0;
-      at.tiles = 0;
-      while (at.tiles == 0 && ++at.b < a.B) {
-        at.n_keys = __ldcg(a.len + at.b);
-        at.tiles = tiles_of(a, at.n_keys);
-      }
-      if (at.tiles == 0) left = 0;  // (only if a length changed under the kernel)
-    }
-    return r;
-  }
-};
+// Even shares: units are (KV head, m-block).
+__device__ __forceinline__ Scenes scenes_of(const Args& a) { return Scenes{a.len, nullptr, a.B, a.R, a.cap, a.Hkv * a.mblocks}; }
+__device__ __forceinline__ Run take(Walk<false>& walk, const Args& a) {
+  const Span s = walk.next(scenes_of(a));
+  const int kvh = s.unit / a.mblocks;
+  return Run{s.b, kvh, s.unit - kvh * a.mblocks, s.n_keys, s.key_begin, s.key_end, s.n_tiles, s.whole};
+}
 
 // ------------------------------------------------------------------ kernel
 // kEven false: grid (cluster size, Hkv * m-blocks, B), the m-blocks of a head side by side.
@@ -399,7 +321,7 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
   }
   // this CTA's runs: of its cluster's unit the rank's share of the keys, in blocks of 32, or
   // those of its share of all tiles
-  Walk walk = {};
+  Walk<false> walk = {};
   Run one = {};
   bool valid = true;
   if constexpr (!kEven) {
@@ -409,7 +331,7 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
   }
   griddep_wait();  // nothing before this touches global memory
   if constexpr (kEven) {
-    walk.begin(a, lane);
+    walk.begin(scenes_of(a), shares_of(scenes_of(a), lane, gridDim.x), lane);
   } else {
     one.n_keys = __ldcg(a.len + one.b);
     valid = one.n_keys >= a.R && one.n_keys <= a.cap;
@@ -425,7 +347,7 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
     else return n_run == 0;
   };
   auto next_run = [&] {
-    if constexpr (kEven) return walk.next(a);
+    if constexpr (kEven) return take(walk, a);
     else return one;
   };
 
@@ -434,7 +356,7 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
     if constexpr (kEven) {
       if (blockIdx.x == 0)
         for (int b = lane; b < a.B; b += 32)
-          if (tiles_of(a, __ldcg(a.len + b)) == 0) sd_set_error(SD_DEVERR_LENGTH);
+          if (keys_of(scenes_of(a), b) == 0) sd_set_error(SD_DEVERR_LENGTH);
       tc_fence_before();
       __syncthreads();
       tc_fence_after();
@@ -464,7 +386,7 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
       int T = 0, key_v = 0, z_v = 0;
 #pragma unroll 1
       while (walk.left > 0) {
-        const Run r = walk.next(a);
+        const Run r = take(walk, a);
         const int z = r.b * a.Hkv + r.kvh;
 #pragma unroll 1
         for (int t = 0; t < r.n_tiles; ++t, ++T) {
@@ -581,23 +503,23 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
     const int kl = quarter * 32 + lane;  // key lane of S^T / d lane of O^T
     const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
     if constexpr (kEven) {
-      if (st == 0) *reinterpret_cast<Walk*>(smem + C::kOffWalk) = walk;
+      if (st == 0) *reinterpret_cast<Walk<false>*>(smem + C::kOffWalk) = walk;
       tc_fence_before();
       __syncthreads();
       tc_fence_after();
     }
     // (the walk and the run stand in shared memory: in registers they are spilled, and the
     // tile loop with them)
-    Walk* const my_walk = reinterpret_cast<Walk*>(smem + C::kOffWalk);
+    Walk<false>* const my_walk = reinterpret_cast<Walk<false>*>(smem + C::kOffWalk);
     Run* const my_run = reinterpret_cast<Run*>(smem + C::kOffWalk + 32);
-    static_assert(sizeof(Walk) <= 32 && sizeof(Run) <= 32, "shared memory layout");
+    static_assert(sizeof(*my_walk) <= 32 && sizeof(Run) <= 32, "shared memory layout");
     int T0 = 0;  // tiles before this run
 #pragma unroll 1
     for (int n_run = 0; kEven ? my_walk->left > 0 : n_run == 0; ++n_run) {
       Run r = one;
       if constexpr (kEven) {
         walk = *my_walk;
-        r = walk.next(a);
+        r = take(walk, a);
       }
       const int b = r.b, n_keys = r.n_keys, key_begin = r.key_begin, key_end = r.key_end, n_tiles = r.n_tiles;
       const int kvh = r.kvh, mblock = r.mblock;
@@ -1016,12 +938,13 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv8_join_kernel(const Args a,
   constexpr int kRowF = kDim + 4, kPer = kDim / 32;
   const int lane = threadIdx.x & 31, c = blockIdx.x + 1;
   // (the lengths are older than the attention, which let this kernel start after its own wait)
-  const Shares s(a, lane, ctas);
+  const Scenes scenes = scenes_of(a);
+  const Shares s = shares_of(scenes, lane, ctas);
   const int pos = s.begin(c);
   bool mine = pos < s.total;
   Place at = {};
-  if (mine) at = locate(a, s, pos, lane);
-  const int unit_begin = pos - at.tile, unit_end = unit_begin + at.tiles;
+  if (mine) at = locate(scenes, s, pos, lane);
+  const int unit_begin = at.first, unit_end = unit_begin + at.tiles;
   mine = mine && at.tile > 0 && s.begin(c - 1) <= unit_begin;
   const int kvh = at.unit / a.mblocks, mblock = at.unit - kvh * a.mblocks;
   const int row0 = (blockIdx.y * kJoinWarps + (threadIdx.x >> 5)) * kJoinRows;

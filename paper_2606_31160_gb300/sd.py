@@ -77,6 +77,8 @@ _SIGNATURES = {
     "sd_kv8_attention_workspace": ([_i, _i, _i, _i, _i, _i], _sz),
     "sd_kv8_attention_ex": ([_vp, ctypes.POINTER(KV8CacheStruct), _vp, _i, _i, _f, _i, _vp, _sz, _vp], _i),
     "sd_kv8_attention": ([_vp, ctypes.POINTER(KV8CacheStruct), _vp, _i, _i, _f, _i, _vp], _i),
+    "sd_attention_weights_workspace": ([_i, _i, _i, _i, _i, _i], _sz),
+    "sd_attention_weights_ex": ([_vp, ctypes.POINTER(KVCacheStruct), _i, _i, _f, _vp, _vp, _f, _vp, _vp, _sz, _vp], _i),
     "sd_attention_weights": ([_vp, ctypes.POINTER(KVCacheStruct), _i, _i, _f, _vp, _vp, _f, _vp, _vp], _i),
     "sd_kv_evict": ([ctypes.POINTER(KVCacheStruct), _vp, _i, _i, _i, ctypes.POINTER(KVCacheStruct), _vp, _vp, _vp], _i),
     "sd_token_logprobs": ([_vp, _i, _i, _i, ctypes.c_longlong, _vp, _f, _i, _vp, _vp, _vp, _vp, _vp], _i),
@@ -433,10 +435,16 @@ def kv8_attention(q, cache, out=None, scale=0.0, block=False, ws=None):
 
 # ------------------------------------------------------ weights and eviction
 
-def attention_weights(q, cache, weights_in=None, weights=None, decay=1.0, committed=None, scale=0.0):
+def attention_weights_workspace_bytes(B, R, Hq, Hkv, D, capacity):
+    return int(lib().sd_attention_weights_workspace(B, R, Hq, Hkv, D, capacity))
+
+
+def attention_weights(q, cache, weights_in=None, weights=None, decay=1.0, committed=None, scale=0.0, ws=None):
     """The attention weight that each cached key gathers from the rows q [B,R,Hq,D] (keys
     appended): weights = decay * weights_in + the sum over the committed rows and the KV
-    head's query heads, fp32 [B,Hkv,cap]. committed: int32 [B] rows that count, or all."""
+    head's query heads, fp32 [B,Hkv,cap]. committed: int32 [B] rows that count, or all. ws:
+    attention_weights_workspace_bytes of device memory; when None a batch that takes one
+    has it from torch's allocator, on the current stream."""
     B, R, Hq, D = q.shape
     _, Hkv, cap, _ = cache.shape
     if cache.shape[0] != B or cache.shape[3] != D:
@@ -447,11 +455,19 @@ def attention_weights(q, cache, weights_in=None, weights=None, decay=1.0, commit
         raise ValueError("weights must be [B, Hkv, cap]")
     if committed is not None and committed.shape != (B,):
         raise ValueError("committed must be [B]")
-    _check(lib().sd_attention_weights(_dev(q, "q", torch.bfloat16), cache.struct, R, Hq, float(scale),
-                                      None if committed is None else _dev(committed, "committed", torch.int32),
-                                      None if weights_in is None else _dev(weights_in, "weights_in", torch.float32),
-                                      float(decay), _dev(weights, "weights", torch.float32), _stream()),
-           "sd_attention_weights")
+    if ws is None and B > 1:
+        need = lib().sd_attention_weights_workspace(B, R, Hq, Hkv, D, cap)
+        if need:
+            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    args = (_dev(q, "q", torch.bfloat16), cache.struct, R, Hq, float(scale),
+            None if committed is None else _dev(committed, "committed", torch.int32),
+            None if weights_in is None else _dev(weights_in, "weights_in", torch.float32),
+            float(decay), _dev(weights, "weights", torch.float32))
+    if ws is None:
+        _check(lib().sd_attention_weights(*args, _stream()), "sd_attention_weights")
+    else:
+        _check(lib().sd_attention_weights_ex(*args, _dev(ws, "ws"), ws.numel() * ws.element_size(), _stream()),
+               "sd_attention_weights")
     return weights
 
 

@@ -81,6 +81,17 @@ def test_attention_weights(lib):
     assert call(_c16(B=0), q=0, out=0) == 0
 
 
+def test_attention_weights_with_a_workspace(lib):
+    def call(c, q=16, R=8, Hq=32, out=32, ws=16, nbytes=1 << 20):
+        return lib.sd_attention_weights_ex(P(q), c, R, Hq, 0.0, P(0), P(0), 1.0, P(out), P(ws), nbytes, None)
+    assert call(None) == 1 and call(_c16(D=96)) == 2 and call(_c16(), R=0) == 1 and call(_c16(), Hq=30) == 1
+    assert call(_c16(), q=0) == 1 and call(_c16(), out=0) == 1 and call(_c16(), ws=24) == 1
+    assert call(_c16(B=0), q=0, out=0, ws=0, nbytes=0) == 0
+    for shape in ((0, 8, 32, 8, 128, 100), (4, 0, 32, 8, 128, 100), (4, 8, 30, 8, 128, 100), (4, 33, 32, 8, 128, 100),
+                  (4, 8, 32, 8, 96, 100), (4, 8, 32, 8, 128, 0), (4, 8, 32, 0, 128, 100)):
+        assert lib.sd_attention_weights_workspace(*shape) == 0
+
+
 def test_kv_evict(lib):
     big = 1 << 30
     src = dict(k=big, v=2 * big, n=16)

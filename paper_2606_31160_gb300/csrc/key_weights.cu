@@ -29,9 +29,9 @@
 //
 // What bounds it. One scene (8 heads, L = 4096, 32 rows: 6.9 us) the chain of latencies:
 // lengths, keys and rows, products, sums, their exchange, weights. Eight scenes of 8192
-// keys and 128 rows (52.0 us, 121 MB of keys read twice) the SMs' reading of 242 MB, 35 us
+// keys and 128 rows (51.4 us, 121 MB of keys read twice) the SMs' reading of 242 MB, 35 us
 // by itself on 128 CTAs (36 bytes a cycle and SM); the second reading finds about two
-// thirds of the keys in L2 (152 MB from DRAM). With the products 38, with the exponentials
+// thirds of the keys in L2 (152 MB from DRAM), and a CTA's last four tiles in their slots. With the products 38, with the exponentials
 // of both passes 48 from L2. Two CTAs an SM, each with half the warps and tensor memory,
 // were slower (one scene 9.7, eight 52 at their best size).
 #include "shares.cuh"
@@ -148,15 +148,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t base = smem_addr(smem);
   auto bar = [&](int i) { return base + C::kOffBar + 8u * i; };
   // T counts the tiles of scores formed, over passes and row groups; a barrier's next phase
-  // waits for the one before to have been seen: K(T + stages) for S(T), S(T + bufs) for the
-  // last reading of S(T)
-  auto FULL = [&](int T) { return bar(T % kStages); };
-  auto FREE = [&](int T) { return bar(kStages + T % kStages); };
+  // waits for the one before to have been seen: S(T + bufs) for the last reading of S(T), and
+  // the next keys of a slot for its last S
+  auto FULL = [&](int slot) { return bar(slot); };
+  auto FREE = [&](int slot) { return bar(kStages + slot); };
   auto SREADY = [&](int T) { return bar(2 * kStages + T % kBufs); };
   auto SFREE = [&](int T) { return bar(2 * kStages + kMaxBufs + T % kBufs); };
   const uint32_t QFULL = bar(2 * kStages + 2 * kMaxBufs);
   auto GATHERED = [&](int grp) { return bar(2 * kStages + 2 * kMaxBufs + 1 + (grp & 1)); };
-  auto parK = [](int T) { return static_cast<uint32_t>((T / kStages) & 1); };
   auto parS = [](int T) { return static_cast<uint32_t>((T / kBufs) & 1); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
   float2* part = reinterpret_cast<float2*>(smem + C::kOffPart);
@@ -212,15 +211,25 @@ __global__ void __launch_bounds__(kThreads, 1)
     one.n_tiles = (blk_end - blk_begin + 3) / 4;
   }
   // What a run of keys takes: its row groups, and the tiles of scores that each forms. A
-  // second reading goes backwards: what was read last is the likeliest to be in L2 still.
+  // second reading goes backwards, and the next group's first forwards again: what was read
+  // last is the likeliest to be in L2 still, and the last tiles are in their slots.
   struct Work {
     int m_rows, n_groups, n_tiles, formed;
     bool resident;
-    __device__ __forceinline__ int tile_of(int T) const {  // the T-th tile formed
-      if constexpr (kPass == kWeights) return n_tiles - 1 - T % formed;
-      const int t = T % formed;
-      return t < n_tiles ? t : 2 * n_tiles - 1 - t;
-    }
+  };
+  struct Use {  // of a tile's keys, for the j-th tile of scores of a group
+    int tile, slot;
+    bool second, load, last;  // in pass B; not in its slot yet; the slot's last before another load
+  };
+  auto use_of = [](const Work& w, int grp, int j, int T) {
+    Use u;
+    const int n = w.n_tiles, keep = min(n, kStages);
+    u.second = kPass == kWeights || j >= n;
+    u.tile = kPass == kWeights ? n - 1 - j : (u.second ? 2 * n - 1 - j : j);
+    u.slot = (kEven ? T : u.tile) % kStages;
+    u.load = kEven || (w.resident ? grp == 0 || n > kStages : (u.second ? u.tile < n - keep : grp == 0 || u.tile >= keep));
+    u.last = kEven || (w.resident ? n > kStages : (u.second ? u.tile >= keep : u.tile < n - keep));
+    return u;
   };
   auto work_of = [&](const Span& r) {
     Work w;
@@ -258,26 +267,35 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!valid && rank == 0 && lane == 0 && one.unit == 0)
       sd_set_error(one.n_keys >= a.R && one.n_keys <= a.cap ? SD_DEVERR_ROLLBACK : SD_DEVERR_LENGTH);
     int T = 0;
+    uint32_t held = 0, phase = 0;  // slots that have been loaded; the phases of FREE
     for_runs([&](const Span& r) {
       const Work w = work_of(r);
       const int z = r.b * a.Hkv + r.unit;
 #pragma unroll 1
-      for (int i = 0; i < w.n_groups * w.formed; ++i, ++T) {
-        if (T >= kStages) mbar_wait(FREE(T), parK(T - kStages));
-        const int key0 = r.key_begin + w.tile_of(i) * kTile;
-        const int boxes = (min(kTile, r.key_end - key0) + 31) / 32;  // of 32 keys, as many as there are
-        if (lane == 0) mbar_expect_tx(FULL(T), static_cast<uint32_t>(boxes * 32 * 128 * kHalves));
-        __syncwarp();
-        if (lane < boxes * kHalves) {
-          const int h = lane / boxes, x = lane - h * boxes;
-          asm volatile(
-              "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
-                  base + (T % kStages) * kK + h * kHalf + x * 32 * 128),
-              "l"(reinterpret_cast<uint64_t>(&tm_k)), "r"(FULL(T)), "r"(h * 64), "r"(key0 + x * 32), "r"(z)
-              : "memory");
+      for (int grp = 0; grp < w.n_groups; ++grp)
+#pragma unroll 1
+        for (int j = 0; j < w.formed; ++j, ++T) {
+          const Use u = use_of(w, grp, j, T);
+          if (!u.load) continue;
+          if ((held >> u.slot) & 1) {
+            mbar_wait(FREE(u.slot), (phase >> u.slot) & 1);
+            phase ^= 1u << u.slot;
+          }
+          held |= 1u << u.slot;
+          const int key0 = r.key_begin + u.tile * kTile;
+          const int boxes = (min(kTile, r.key_end - key0) + 31) / 32;  // of 32 keys, as many as there are
+          if (lane == 0) mbar_expect_tx(FULL(u.slot), static_cast<uint32_t>(boxes * 32 * 128 * kHalves));
+          __syncwarp();
+          if (lane < boxes * kHalves) {
+            const int h = lane / boxes, x = lane - h * boxes;
+            asm volatile(
+                "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+                    base + u.slot * kK + h * kHalf + x * 32 * 128),
+                "l"(reinterpret_cast<uint64_t>(&tm_k)), "r"(FULL(u.slot)), "r"(h * 64), "r"(key0 + x * 32), "r"(z)
+                : "memory");
+          }
+          __syncwarp();
         }
-        __syncwarp();
-      }
     });
   } else if (warp == 1) {
     // -------------------------------------------------------------- S issue
@@ -285,28 +303,35 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint64_t dK0 = umma_desc(base, 16, 1024);
     const uint64_t dQ = umma_desc(base + C::kOffQ, 16, 1024);
     int T = 0, n_q = 0;
+    uint32_t phase = 0;  // of FULL
     for_runs([&](const Span& r) {
       const Work w = work_of(r);
 #pragma unroll 1
-      for (int i = 0; i < w.n_groups * w.formed; ++i, ++T) {
-        if (i % w.formed == 0) mbar_wait(QFULL, n_q++ & 1);
-        if (T >= kBufs) mbar_wait(SFREE(T), parS(T - kBufs));
-        mbar_wait(FULL(T), parK(T));
-        tc_fence_after();
-        const uint64_t dk = dK0 + static_cast<uint64_t>(((T % kStages) * kK) >> 4);
-        const bool turned = C::kTurned && kPass != kWeights && i % w.formed < w.n_tiles;  // (both operands 128 rows of one layout)
-        const uint64_t da = turned ? dQ : dk, db = turned ? dk : dQ;
-        const int half_a = turned ? C::kQHalf : kHalf, half_b = turned ? kHalf : C::kQHalf;
-        if (elect_one()) {
+      for (int grp = 0; grp < w.n_groups; ++grp)
+#pragma unroll 1
+        for (int j = 0; j < w.formed; ++j, ++T) {
+          const Use u = use_of(w, grp, j, T);
+          if (j == 0) mbar_wait(QFULL, n_q++ & 1);
+          if (T >= kBufs) mbar_wait(SFREE(T), parS(T - kBufs));
+          if (u.load) {
+            mbar_wait(FULL(u.slot), (phase >> u.slot) & 1);
+            phase ^= 1u << u.slot;
+          }
+          tc_fence_after();
+          const uint64_t dk = dK0 + static_cast<uint64_t>((u.slot * kK) >> 4);
+          const bool turned = C::kTurned && !u.second;  // (both operands 128 rows of one layout)
+          const uint64_t da = turned ? dQ : dk, db = turned ? dk : dQ;
+          const int half_a = turned ? C::kQHalf : kHalf, half_b = turned ? kHalf : C::kQHalf;
+          if (elect_one()) {
 #pragma unroll
-          for (int kk = 0; kk < kDim / 16; ++kk)
-            umma(tmem + kR * (T % kBufs), da + (((kk >> 2) * half_a + (kk & 3) * 32) >> 4),
-                 db + (((kk >> 2) * half_b + (kk & 3) * 32) >> 4), kIdesc, kk > 0 ? 1 : 0);
-          umma_commit(SREADY(T));
-          umma_commit(FREE(T));
+            for (int kk = 0; kk < kDim / 16; ++kk)
+              umma(tmem + kR * (T % kBufs), da + (((kk >> 2) * half_a + (kk & 3) * 32) >> 4),
+                   db + (((kk >> 2) * half_b + (kk & 3) * 32) >> 4), kIdesc, kk > 0 ? 1 : 0);
+            umma_commit(SREADY(T));
+            if (u.last) umma_commit(FREE(u.slot));
+          }
+          __syncwarp();
         }
-        __syncwarp();
-      }
     });
   } else {
     // -------------------------------------------------------------- softmax
@@ -734,9 +759,9 @@ DevState* state() {
 // 8 heads, L = 4096, at 4 / 6 / 8 / 16: 10.7 / 9.2 / 7.4 / 12.3 us; eight scenes, L = 8192,
 // at 2 / 4 / 8: 43 / 38 / 57 on 32 rows, 51 / 53 / 75 on 64, 52 / 56 / 89 on 128.) 0: even
 // shares, where those cost less and the call may have them. Clusters / even shares in us, 8
-// heads of 8192 keys (3/4 to all of them filled): 128 rows, 8 scenes 47 / 52, 12: 87 / 69, 16:
-// 88 / 85, 24: 136 / 125, 24 of 2048 keys 52 / 49, 16: 29 / 35; 64 rows, 8: 47 / 48, 12: 90 /
-// 65, 24: 138 / 120; 32 rows, whose scores clusters form once: 12: 52 / 59, 24: 110 / 110.
+// heads of 8192 keys (3/4 to all of them filled): 128 rows, 8 scenes 47 / 52, 12: 83 / 69, 16:
+// 86 / 85, 24: 134 / 124, 24 of 2048 keys 52 / 50, 16: 28 / 35; 64 rows, 8: 46 / 48, 12: 82 /
+// 66, 24: 131 / 120; 32 rows, whose scores clusters form once: 12: 52 / 59, 24: 108 / 110.
 int pick_cluster(const int* active, long long units, int cap, int rows, bool may) {
   const int forced = sd_internal_forced_cluster();
   for (int i = 0; i < kNumSizes && forced > 0; ++i)

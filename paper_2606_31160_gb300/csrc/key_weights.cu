@@ -31,9 +31,10 @@
 // lengths, keys and rows, products, sums, their exchange, weights. Eight scenes of 8192
 // keys and 128 rows (51.4 us, 121 MB of keys read twice) the SMs' reading of 242 MB, 35 us
 // by itself on 128 CTAs (36 bytes a cycle and SM); the second reading finds about two
-// thirds of the keys in L2 (152 MB from DRAM), and a CTA's last four tiles in their slots. With the products 38, with the exponentials
-// of both passes 48 from L2. Two CTAs an SM, each with half the warps and tensor memory,
-// were slower (one scene 9.7, eight 52 at their best size).
+// thirds of the keys in L2 (152 MB from DRAM), and a CTA's last four tiles in their slots.
+// With the products 38, with the exponentials of both passes 48 from L2. Two CTAs an SM,
+// each with half the warps and tensor memory, were slower (one scene 9.7, eight 52 at their
+// best size).
 #include "shares.cuh"
 #include "tc_common.cuh"
 

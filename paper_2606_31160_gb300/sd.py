@@ -135,9 +135,14 @@ def _stream():
     return _raw_stream(_raw_device())
 
 
+_Tensor = torch.Tensor
+
+
 def _dev(t, name, dtype=None, ndim=None):
     """The checked tensor's device address (an int: the declared argument types
     convert it; a c_void_p object an argument cost as much as its checks)."""
+    if t.__class__ is _Tensor and t.is_cuda and t.is_contiguous() and (dtype is None or t.dtype is dtype) and ndim is None:
+        return t.data_ptr()
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
     if not t.is_cuda:
@@ -497,31 +502,33 @@ def token_logprobs(logits, tokens, temperature=1.0, top_n=0, logprob=None, entro
     (bf16 or fp32), the rows' entropies (nats) and their top_n alternatives. A token -1
     gives 0. Returns (logprob [...], entropy [...], top_ids [..., top_n] int32,
     top_logprobs [..., top_n])."""
-    lead, V, dtype = logits.shape[:-1], logits.shape[-1], logits.dtype
+    shape, lead, dtype, top_n = logits.shape, tokens.shape, logits.dtype, int(top_n)
     if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise ValueError("logits must be bf16 or fp32")
-    if tokens.shape != lead:
-        raise ValueError("tokens must be %s" % (tuple(lead),))
-    top_n, rows = int(top_n), tokens.numel()
+    V, rows = shape[-1], tokens.numel()
+    if shape[:-1] != lead:
+        raise ValueError("tokens must be %s" % (tuple(shape[:-1]),))
     if logits.is_contiguous():
         ptr, stride = _dev(logits, "logits"), V
     else:
         ptr, stride = _padded_rows(logits, rows)
-    wide, f32 = (*lead, max(top_n, 0)), torch.float32
+    wide, f32, i32 = (*lead, max(top_n, 0)), torch.float32, torch.int32
     if logprob is None:
         logprob = torch.empty(lead, dtype=f32, device=logits.device)
     if entropy is None:
         entropy = torch.empty(lead, dtype=f32, device=logits.device)
     if top_ids is None:
-        top_ids = torch.empty(wide, dtype=torch.int32, device=logits.device)
+        top_ids = torch.empty(wide, dtype=i32, device=logits.device)
     if top_logprobs is None:
         top_logprobs = torch.empty(wide, dtype=f32, device=logits.device)
     if logprob.shape != lead or entropy.shape != lead or top_ids.shape != wide or top_logprobs.shape != wide:
         raise ValueError("logprob and entropy must be %s, top_ids and top_logprobs %s" % (tuple(lead), wide))
-    dt = SD_BF16 if dtype is torch.bfloat16 else SD_F32
-    _check(lib().sd_token_logprobs(ptr, dt, rows, V, stride, _dev(tokens, "tokens", torch.int32), float(temperature), top_n,
-                                   _dev(logprob, "logprob", f32), _dev(entropy, "entropy", f32), _dev(top_ids, "top_ids", torch.int32),
-                                   _dev(top_logprobs, "top_logprobs", f32), _stream()), "sd_token_logprobs")
+    status = lib().sd_token_logprobs(ptr, SD_BF16 if dtype is torch.bfloat16 else SD_F32, rows, V, stride,
+                                     _dev(tokens, "tokens", i32), float(temperature), top_n,
+                                     _dev(logprob, "logprob", f32), _dev(entropy, "entropy", f32),
+                                     _dev(top_ids, "top_ids", i32), _dev(top_logprobs, "top_logprobs", f32), _stream())
+    if status:
+        raise SDError("sd_token_logprobs", status)
     return logprob, entropy, top_ids, top_logprobs
 
 

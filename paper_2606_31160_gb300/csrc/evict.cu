@@ -11,10 +11,10 @@
 // ranked by counting, more counted by their other bits (over all keys where the list is too
 // short). Then a key's place is the number of kept keys before it: a lane marks four keys, a
 // warp sums a range of them, and the CTA lists its share from the marks, whose rows it
-// copies with eight 16-byte loads a thread in flight.
+// copies with four 16-byte loads a thread in flight.
 //
-// What bounds it. 8 scenes of 16384 keys to 4096, 8 heads: 56.5 us, of which the rows' copies
-// are ~43 (268 MB at 6.2 TB/s) and the selection 12 (20 thousand cycles: lengths 3.0, weights
+// What bounds it. 8 scenes of 16384 keys to 4096, 8 heads: 55.2 us, of which the rows' copies
+// are ~42 (268 MB at 6.4 TB/s; with eight loads a thread and stores that stay in L2 56.7) and the selection 12 (20 thousand cycles: lengths 3.0, weights
 // and their range 3.3, counting 3.0, list 2.3, rank 1.8, marks 2.1, places 5.0), before which
 // no row can be copied. It is instructions, not latency: four keys a lane took it from 31
 // thousand cycles (and one scene of 4096 keys from 9.4 to 7.7 us), more loads in flight did
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
       if (weights_out) weights_out[plane * dst.capacity + q_lo + j] = __ldcg(weights + i);
       if (kept) kept[plane * keep + q_lo + j] = i;
     }
-    constexpr int kU = 4;
+    constexpr int kU = 2;
     const long long to = static_cast<long long>(q_lo) << vec_shift;
     for (int u0 = t; u0 < count << vec_shift; u0 += kU * kThreads) {
       uint4 k[kU], v[kU];
@@ -336,8 +336,8 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const sd_kv_cache src, 
       for (int u = 0; u < kU; ++u) {
         const int x = u0 + u * kThreads;
         if (x < count << vec_shift) {
-          kd[to + x] = k[u];
-          vd[to + x] = v[u];
+          __stcs(kd + to + x, k[u]);
+          __stcs(vd + to + x, v[u]);
         }
       }
     }

@@ -13,12 +13,12 @@
 // warp sums a range of them, and the CTA lists its share from the marks, whose rows it
 // copies with four 16-byte loads a thread in flight.
 //
-// What bounds it. 8 scenes of 16384 keys to 4096, 8 heads: 55.2 us, of which the rows' copies
-// are ~42 (268 MB at 6.4 TB/s; with eight loads a thread and stores that stay in L2 56.7) and the selection 12 (20 thousand cycles: lengths 3.0, weights
-// and their range 3.3, counting 3.0, list 2.3, rank 1.8, marks 2.1, places 5.0), before which
-// no row can be copied. It is instructions, not latency: four keys a lane took it from 31
-// thousand cycles (and one scene of 4096 keys from 9.4 to 7.7 us), more loads in flight did
-// not.
+// What bounds it. 8 scenes of 16384 keys to 4096, 8 heads: 55.2 us, of which the rows'
+// copies are ~42 (268 MB at 6.4 TB/s; with eight loads a thread and stores that stay in L2
+// 56.7) and the selection 12 (20 thousand cycles: lengths 3.0, weights and their range 3.3,
+// counting 3.0, list 2.3, rank 1.8, marks 2.1, places 5.0), before which no row can be
+// copied. It is instructions, not latency: four keys a lane took it from 31 thousand cycles
+// (and one scene of 4096 keys from 9.4 to 7.7 us), more loads in flight did not.
 #include "common.cuh"
 
 SD_DEFINE_ERROR_ACCESSOR(sd_take_error_evict)

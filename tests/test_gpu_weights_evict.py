@@ -65,6 +65,29 @@ def test_weights_parity(D, cap, R, Hq, Hkv, lens, spread):
     assert sd.get_device_error() == 0
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("size", [1, 2])
+@pytest.mark.parametrize("Hq,R", [(6, 50), (2, 32), (4, 8)])
+def test_weights_tiles_kept_between_readings(D, size, Hq, R):
+    """One to eleven tiles of keys a CTA, one to three groups of rows: keys that stay in
+    shared memory between the readings, and those that are read again."""
+    rng = np.random.default_rng(D + R)
+    lens = [60, 128, 300, 400, 513, 640, 700, 896, 1000, 1150, 1280, 1400]
+    k = _bf16(rng.standard_normal((len(lens), 1, 1400, D)))
+    q = _bf16(rng.standard_normal((len(lens), R, Hq, D)))
+    sd.set_cluster_size(size)
+    try:
+        got = to64(sd.attention_weights(q, sd.KVCache(k, k.clone(), _i32(lens))))
+    finally:
+        sd.set_cluster_size(0)
+    assert sd.get_device_error() == 0
+    ref = oracle.attention_weights(to64(q), to64(k), lens)
+    for b, n in enumerate(lens):
+        big = 2.0 ** -21 * np.abs(to64(q[b])).max() * np.abs(to64(k[b])).max() * np.sqrt(D)
+        tol = (1e-5 + min(big, 1e-3)) * ref[b, :, :n] + 1e-7 * R * Hq
+        assert np.all(np.abs(got[b, :, :n] - ref[b, :, :n]) <= tol)
+
+
 def test_weights_in_place_and_accumulating():
     rng = np.random.default_rng(3)
     k = _bf16(rng.standard_normal((2, 2, 400, 128)))

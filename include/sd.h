@@ -448,6 +448,10 @@ sd_status sd_kv8_store(const sd_kv8_cache* cache, const sd_kv_cache* src, sd_str
  * Verify attention over an 8-bit cache: sd_verify_attention_ex (the same rows,
  * masks, q and out) on the keys and values that the codes stand for.
  * flags: SD_ATTN_BLOCK_MASK; other bits SD_ERR_INVALID_ARG.
+ * Precision: a key's weight times its v_scale is held to 2^-9 of itself, or, where that is
+ * more, to 2^-21 of the row's sum of them (2^-16 where four keys or more share the most of
+ * it); the errors of the small ones are spread over the keys, so that a long tail keeps its
+ * mass. Sums are fp32, and v_scale may differ by up to 2^100 between the blocks of a head.
  * D in {64, 128}, Hq % Hkv == 0 and G*R <= 128. A scene with len[b] < R or
  * len[b] > capacity sets SD_DEVERR_LENGTH and its output is left unwritten.
  * sd_kv8_attention needs no workspace. With one, sd_kv8_attention_ex gives every

@@ -9,10 +9,15 @@
 //   * the query rows, scaled by the power of two that brings their largest element into
 //     [128, 256), are exact in two terms (bf16 has 8 bits; elements below 2^-10 of the
 //     largest to 2^-18 of it), both products into the same sum;
-//   * a weight is hi + lo / 16, hi = e4m3(P), lo = e4m3(16 (P - hi)): 8 bits, as a bf16
-//     one would keep, down to 2^-12 of its row's largest, and off by 2^-16 of it at most
-//     below that. The terms are columns of one product, 2 kR wide (four of N = 2 kR take
-//     200 cycles at kR = 32, eight of N = kR 330).
+//   * a weight is hi + lo / 16, hi = e4m3(P), lo = e4m3(16 (P - hi) + dither): 8 bits, as a
+//     bf16 one would keep, down to P = 2^-5; below, the terms are subnormal and end at steps
+//     of 2^-13. A long tail of weights that small may hold much of a row beside a few large
+//     keys, and rounded to nearest, all alike, it would be lost or grow (a row with 0.8 of it
+//     in one key of 16384 at P = 2^2: a tenth of the output). So a reference lets what stands
+//     out stand high (below), and the dither, half a step at most and made of the key's
+//     index, spreads the rounding: of equal weights a share of the keys rounds up that makes
+//     their sum right. The terms are columns of one product, 2 kR wide (four of N = 2 kR
+//     take 200 cycles at kR = 32, eight of N = kR 330).
 // The packed query rows of a KV head (G * R) are few, so both products run transposed,
 //     S^T[128 keys][kR rows] = K_tile . Q^T,   O^T[128 d][2 kR] += V_tile^T . P^T
 // with kR = 32 or 48 and, above 48 rows, two or three m-blocks. Scales enter between the two: a
@@ -20,11 +25,17 @@
 //     P = 2^(t * qscale + log2 v_scale - ref[row]),   l[row] += P / v_scale,
 // so O / l is the attention whatever the scales are.
 //
-// Reference. P has to stay within e4m3's 448, so ref[row] gives the largest weight that
-// the first tile shows 2^2, and moves when a later one would pass 2^8.75: every thread
-// compares its largest exponent and the group votes once a tile (an OR in its barrier).
-// Moving takes the tile's exact row maxima (redux over the lanes), and rescales l and O
-// in tensor memory.
+// Reference. P has to stay within e4m3's 448, and a row's largest weights far above 2^-13.
+// ref[row] is the least number that gives the largest weight of the first tile no more than
+// 2^8 and the lowest of the four largest of each 32 of its keys no more than 2^1: what
+// stands out has up to 2^8, and rows of many alike, among which a later one may be larger,
+// have room for it. It moves by the same rule when a later weight would pass 2^8.75. A row's
+// weights then sum to 2^8 or more, or at the least to 2^3 (four keys alike), and a small one
+// is off by less than 2^-13 in these units, at random. (By the largest weight alone: at 2^2
+// the tail's error is 16 to 60 times this, at 2^6 the moves take 32 scenes from 103 to 116
+// us, at 2^4 they take 104 with ten times the error.) Every thread compares its largest
+// exponent and the group votes once a tile (an OR in its barrier). Moving takes the tile's
+// exact row maxima over 32 keys (redux over the lanes), and rescales l and O in tensor memory.
 //
 // Warps (608 threads): 0 the TMA producer; 1 issues S and owns tensor memory; 2 issues
 // PV; 3..18 two softmax groups of eight, which take alternate tiles. The groups are two
@@ -58,7 +69,8 @@ constexpr int kTile = 128;               // keys a tile
 constexpr int kStages = 4;               // K slots, V slots and S buffers
 constexpr int kFirstSoft = 3;            // the first softmax warp
 constexpr int kSoft0 = 32 * kFirstSoft;
-constexpr float kTop = 2.f;              // log2 of the weight that a reference gives the largest key
+constexpr float kTop = 8.f;              // log2 of the largest weight that a reference gives the tile that sets it,
+constexpr float kLow = 1.f;              // and of the lowest of the four largest of each 32 keys
 constexpr float kHot = 8.75f;            // log2 of the largest weight a reference may leave (e4m3 ends at 448 = 2^8.81)
 
 struct Args {
@@ -195,20 +207,30 @@ __device__ __forceinline__ float lg2(float x) {
 }
 
 // Two numbers of magnitude up to 448 as two e4m3 terms each, x = hi + lo / kLo (by way of
-// fp16, whose 11 bits both terms together do not reach): codes in the low 16 bits.
+// fp16, whose 11 bits both terms together do not reach): codes in the low 16 bits. `dither`
+// (two fp16 numbers) is added to lo before its rounding.
 template <int kLo>
-__device__ __forceinline__ void two_terms(float x0, float x1, uint32_t& hi, uint32_t& lo) {
+__device__ __forceinline__ void two_terms(float x0, float x1, uint32_t dither, uint32_t& hi, uint32_t& lo) {
   static_assert(kLo == 1 || kLo == 16, "as fp16 below");
   asm("{\n\t.reg .b32 f, b, d;\n\t.reg .b16 h, l;\n\t"
       "cvt.rn.f16x2.f32 f, %3, %2;\n\t"
       "cvt.rn.satfinite.e4m3x2.f16x2 h, f;\n\t"
       "cvt.rn.f16x2.e4m3x2 b, h;\n\t"
       "sub.f16x2 d, f, b;\n\t"
-      "mul.f16x2 d, d, %4;\n\t"
+      "fma.rn.f16x2 d, d, %4, %5;\n\t"
       "cvt.rn.satfinite.e4m3x2.f16x2 l, d;\n\t"
       "cvt.u32.u16 %0, h;\n\tcvt.u32.u16 %1, l;\n\t}"
       : "=r"(hi), "=r"(lo)
-      : "f"(x0), "f"(x1), "r"(kLo == 1 ? 0x3c003c00u : 0x4c004c00u));
+      : "f"(x0), "f"(x1), "r"(kLo == 1 ? 0x3c003c00u : 0x4c004c00u), "r"(dither));
+}
+// Half an e4m3 step of subnormal numbers, 2^-10, times a number in [-1, 1) that is spread
+// evenly over any run of keys, and over every second, third, ... of them (the multiples of
+// the golden ratio); twice, as fp16.
+__device__ __forceinline__ uint32_t dither_of(int key) {
+  const float x = static_cast<float>(static_cast<int>(static_cast<uint32_t>(key) * 0x9e3779b9u)) * 0x1p-41f;
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %1;" : "=r"(d) : "f"(x));
+  return d;
 }
 
 __device__ __forceinline__ float rcp(float x) {
@@ -586,7 +608,7 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
         const float inv = __uint_as_float(static_cast<uint32_t>(min(261 - e, 254)) << 23);
         uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) two_terms<1>(sd_bf16_lo(w[j]) * inv, sd_bf16_hi(w[j]) * inv, hi[j], lo[j]);
+        for (int j = 0; j < 4; ++j) two_terms<1>(sd_bf16_lo(w[j]) * inv, sd_bf16_hi(w[j]) * inv, 0u, hi[j], lo[j]);
         // the swizzle moves 16-byte chunks: of 8 rows of 128 bytes, or of 4 pairs of rows of 64
         const uint32_t sw16 = kDim == 128 ? ((c >> 1) ^ (row & 7)) : ((c >> 1) ^ ((row >> 1) & 3));
         const uint32_t dst = base + C::kOffQ + row * kDim + (sw16 << 4) + (c & 1) * 8;
@@ -690,7 +712,7 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
         };
         const bool hot = exponents(false) > kHot;
         if (__builtin_expect(named_bar_or(4 + group, kGroupThreads, hot), 0)) {
-          // ---- move the references to the rows' exact maxima over this tile
+          // ---- move the references by the rows' exact maxima over this tile
           exponents(true);
 #pragma unroll
           for (int u = 0; u < kUnits; ++u)
@@ -707,7 +729,8 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
           if (gt < ((rows_in + 7) & ~7)) {  // (rows that do not exist, in a unit with some that do, need one too)
             const float* rm = row_max + group * 4 * kR + gt;
             const float x = fmaxf(fmaxf(rm[0], rm[kR]), fmaxf(rm[2 * kR], rm[3 * kR]));
-            const float old = row_ref[group * kR + gt], now = fmaxf(old, x - kTop);
+            const float low = fminf(fminf(rm[0], rm[kR]), fminf(rm[2 * kR], rm[3 * kR]));
+            const float old = row_ref[group * kR + gt], now = fmaxf(old, fmaxf(x - kTop, low - kLow));
             row_ref[group * kR + gt] = now;
             row_nref[group * kR + gt] = -now;
             row_fac[group * kR + gt] = old == -INFINITY ? 0.f : ex2(old - now);
@@ -743,6 +766,7 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(SFREE(T));
         if (T >= 2) mbar_wait(PVDONE(T - 2), par(T - 2));  // PV(T - 2) has read the P buffer
+        const uint32_t dither = dither_of(tile0 + kl);
 #pragma unroll
         for (int u = 0; u < kUnits; ++u)
           if (u < n_units) {
@@ -751,7 +775,7 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
             for (int e = 0; e < 4; ++e) {
               const float e0 = ex2(y[u][2 * e]), e1 = ex2(y[u][2 * e + 1]);
               lp2[u][e] = fma2(pack2f(e0, e1), iv2, lp2[u][e]);
-              two_terms<16>(e0, e1, h[e], l[e]);
+              two_terms<16>(e0, e1, dither, h[e], l[e]);
             }
             auto store = [&](int row, const uint32_t (&w)[4]) {  // rows row .. row + 7 of 2 kR
               const uint32_t dst = pkey + (row >> 5) * C::kPGroup + ((((row >> 4) & 1) ^ psw) << 4) + (row & 8);

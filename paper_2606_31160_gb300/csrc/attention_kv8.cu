@@ -824,9 +824,10 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
         const float4 s1 = reinterpret_cast<const float4*>(row_sum + st * 8)[1];
         const float l0 = (s0.x + s0.y) + (s0.z + s0.w), l1 = (s1.x + s1.y) + (s1.z + s1.w);
         const float r0 = row_ref[st], r1 = row_ref[kR + st], ref = fmaxf(r0, r1);
-        // a group without a key for the row counts for nothing
+        // a group without a key for the row counts for nothing, one whose keys are no numbers (it
+        // has no reference, or one far below) leaves NaN in l
         const float w0 = r0 == -INFINITY ? 0.f : ex2(r0 - ref), w1 = r1 == -INFINITY ? 0.f : ex2(r1 - ref);
-        const float l = (w0 > 0.f ? w0 * l0 : 0.f) + (w1 > 0.f ? w1 * l1 : 0.f);
+        const float l = w0 * l0 + w1 * l1;
         bool part = merge;
         if constexpr (kEven) part = !my_run->whole;
         row_join[st] = make_float4(w0, w1, part ? l : 1.f / l, ref);
@@ -919,7 +920,7 @@ __global__ void __launch_bounds__(Cfg<kR, kDim>::kThreads, 1)
                                          : make_float2(0.f, -INFINITY);
           const float ref = warp_max(lr.y);
           const float w = lr.y == -INFINITY ? 0.f : ex2(lr.y - ref);
-          float l = w > 0.f ? w * lr.x : 0.f;
+          float l = w * lr.x;  // (NaN stays whatever its weight)
 #pragma unroll
           for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
           Row ov = {};
@@ -1010,7 +1011,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv8_join_kernel(const Args a,
       // (no key of the part that the row sees: its reference is -inf, its weight 0)
       const float now = fmaxf(m[r], lr.y), f = m[r] == -INFINITY ? 0.f : ex2(m[r] - now);
       const float w = lr.y == -INFINITY ? 0.f : ex2(lr.y - now);
-      l[r] = l[r] * f + (w > 0.f ? w * lr.x : 0.f);
+      l[r] = l[r] * f + w * lr.x;  // (NaN stays whatever its weight)
 #pragma unroll
       for (int j = 0; j < kPer; ++j) o[r][j] = o[r][j] * f + (w != 0.f ? w * v[j] : 0.f);
       m[r] = now;

@@ -156,7 +156,7 @@ __device__ __forceinline__ void move_to(Stat& s, float M, float c) {
     s.S *= 0.f;
     s.W = s.S;
   } else {
-    const float d = (s.m - M) * c, f = ex2(d);
+    const float d = fmaxf((s.m - M) * c, -1000.f), f = ex2(d);  // (a mask's lowest value: 0 times -inf in W)
     s.W = f * fmaf(d, s.S, s.W);
     s.S *= f;
   }

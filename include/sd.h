@@ -519,7 +519,8 @@ sd_status sd_kv_evict(const sd_kv_cache* src, const float* weights, int keep, in
 /*
  * Log probabilities of given tokens under softmax(z / T), with the entropy of
  * the rows and their top alternatives.
- *   logits: `rows` rows of V values of `dtype`, row_stride elements apart (>= V);
+ *   logits: `rows` rows of V values of `dtype`, row_stride elements apart (>= V), which may
+ *   begin at any element;
  *   tokens: int32 [rows] device. Token -1 (what the acceptance leaves past
  *   n_emit) gives logprob 0; any other outside [0, V) gives NaN and sets
  *   SD_DEVERR_TOKEN_RANGE.

@@ -27,6 +27,7 @@
 // (launch, two round trips to DRAM, two cluster barriers).
 #include "common.cuh"
 
+#include <float.h>
 #include <math.h>
 
 SD_DEFINE_ERROR_ACCESSOR(sd_take_error_logprobs)
@@ -228,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   sd_pdl_enter();
   const long long row = blockIdx.y;
   const char* z0 = static_cast<const char*>(logits) + row * stride * T::kElem;
-  const float c = inv_t * kLog2e;
+  const float c = fminf(inv_t * kLog2e, FLT_MAX);  // (0 * c is 0 at the smallest temperatures too)
   // the token's logit travels with the rest
   int tok = -1;
   float z_tok = 0.f;

@@ -196,7 +196,8 @@ __global__ void __launch_bounds__(Kv8Cfg<D, kBlock>::kThreads) kv8_append_kernel
       if (threadIdx.x == 0) *scale = s;
     }
   }
-  const bool pow2 = (__float_as_uint(s) & 0x7fffffu) == 0;
+  // (2^127 has no normal inverse)
+  const bool pow2 = (__float_as_uint(s) & 0x7fffffu) == 0 && __float_as_uint(s) < 0x7f000000u;
   const float inv = pow2f(127 - static_cast<int>(__float_as_uint(s) >> 23));
 #pragma unroll
   for (int u = 0; u < C::kPer; ++u) {

@@ -430,7 +430,10 @@ typedef struct {
  * infinities become +-448, NaN stays NaN.
  * A scene with len[b] + R > capacity is left untouched and sets
  * SD_DEVERR_KV_OVERFLOW. sd_kv_rollback rolls the length back; a block's scale
- * stays what it was until the block begins anew.
+ * stays what it was until the block begins anew, and the older codes stay as a
+ * rejected row of larger magnitude left them: those that its scale makes
+ * subnormal are rounded to steps of 2^-9 of that scale. Rows that fit the
+ * block's scale leave no mark.
  */
 sd_status sd_kv8_append(const sd_kv8_cache* cache, const void* k_new, const void* v_new, int R,
                         sd_stream_t stream);

@@ -57,6 +57,7 @@ constexpr int kMaxBufs = 16;
 constexpr int kStages = 4;
 constexpr float kFar = 100.f;            // log2 of what a weight may lie above its reference
 constexpr float kHuge = 1e30f;           // a tile's sum that moves the reference
+constexpr float kNone = -3e38f;          // no reference yet: finite, so that a score of -inf has weight 0
 
 struct Args {
   const __nv_bfloat16* q;
@@ -497,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           float ref[kRpt], l[kRpt];
 #pragma unroll
           for (int j = 0; j < kRpt; ++j) {
-            ref[j] = -INFINITY;
+            ref[j] = kNone;
             l[j] = 0.f;
           }
           const bool idle = slice * kRpt >= rows_in;
@@ -528,9 +529,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                   for (int j = 0; j < 8; ++j)
                     if (y[j] > kFar) {
                       const float now = x[u + j] * a.scale_log2;
-                      l[u + j] = ref[u + j] == -INFINITY ? 0.f : l[u + j] * ex2(ref[u + j] - now);
+                      l[u + j] *= ex2(ref[u + j] - now);
                       ref[u + j] = now;
-                      y[j] = 0.f;
+                      y[j] = now - now;  // (a score of +inf: NaN)
                     }
                 }
 #pragma unroll
@@ -550,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               const float m = warp_max(ref[u + j]);  // (a lane whose every score is NaN has no reference, and a sum that is NaN)
-              v[j] = l[u + j] * (ref[u + j] == -INFINITY ? 0.f : ex2(ref[u + j] - m));
+              v[j] = l[u + j] * ex2(ref[u + j] - m);
               if ((lane >> 2) == j) mine = m;
             }
             const float s = warp_sum8(v, lane);

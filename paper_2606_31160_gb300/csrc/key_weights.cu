@@ -692,16 +692,20 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // ------------------------------------------------------------------ host
+constexpr int kEvenAbove = 32;  // rows up to which a batch never takes even shares (pick_cluster)
+
 template <int kR, int kDim>
 bool allow() {
   constexpr int smem = Cfg<kR, kDim>::kSmemBytes;
   const void* k = reinterpret_cast<const void*>(key_weights_kernel<kR, kDim, kBoth>);
-  const void* k1 = reinterpret_cast<const void*>(key_weights_kernel<kR, kDim, kSums>);
-  const void* k2 = reinterpret_cast<const void*>(key_weights_kernel<kR, kDim, kWeights>);
-  const bool ok = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess &&
-                  cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
-                  cudaFuncSetAttribute(k1, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess &&
-                  cudaFuncSetAttribute(k2, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess;
+  bool ok = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess &&
+            cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+  if constexpr (kR > kEvenAbove) {
+    const void* k1 = reinterpret_cast<const void*>(key_weights_kernel<kR, kDim, kSums>);
+    const void* k2 = reinterpret_cast<const void*>(key_weights_kernel<kR, kDim, kWeights>);
+    ok = ok && cudaFuncSetAttribute(k1, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess &&
+         cudaFuncSetAttribute(k2, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess;
+  }
   if (!ok) (void)cudaGetLastError();
   return ok;
 }
@@ -786,7 +790,7 @@ int pick_cluster(const int* active, long long units, int cap, int rows, bool may
     }
   }
   const double tiles = static_cast<double>(units) * n_tiles;
-  if (may && active[0] > 1 && tiles < 2e9 && rows > 32 && 14.0 + 1.45 * tiles / active[0] < best_cost) return 0;
+  if (may && active[0] > 1 && tiles < 2e9 && rows > kEvenAbove && 14.0 + 1.45 * tiles / active[0] < best_cost) return 0;
   return best;
 }
 
@@ -812,10 +816,10 @@ sd_status launch(const sd_kv_cache* c, const Args& a, int cs, int ctas, cudaStre
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = cs > 0 ? 2 : 1;
-  cudaError_t e;
+  cudaError_t e = cudaErrorInvalidValue;
   if (cs > 0) {
     e = cudaLaunchKernelEx(&cfg, key_weights_kernel<kR, kDim, kBoth>, k, a);
-  } else {
+  } else if constexpr (kR > kEvenAbove) {
     e = cudaLaunchKernelEx(&cfg, key_weights_kernel<kR, kDim, kSums>, k, a);
     if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, key_weights_kernel<kR, kDim, kWeights>, k, a);
   }

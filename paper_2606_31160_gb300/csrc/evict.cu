@@ -21,6 +21,8 @@
 // (and one scene of 4096 keys from 9.4 to 7.7 us), more loads in flight did not.
 #include "common.cuh"
 
+#include <mutex>
+
 SD_DEFINE_ERROR_ACCESSOR(sd_take_error_evict)
 
 namespace {
@@ -382,19 +384,20 @@ extern "C" sd_status sd_kv_evict(const sd_kv_cache* src, const float* weights, i
   if (parts < 1) parts = 1;
   if (parts > (keep + 31) / 32) parts = (keep + 31) / 32;
   const int smem_keys = src->capacity < kKeysMax ? (src->capacity + kBlock - 1) / kBlock * kBlock : kKeysMax;
-  static bool allowed[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
     (void)cudaGetLastError();
     return SD_ERR_CUDA;
   }
-  if (!allowed[dev]) {  // more than 48 KB of shared memory, once per device
-    if (cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeysMax * 4 + kKeysMax / 32 * 8) != cudaSuccess) {
-      (void)cudaGetLastError();
-      return SD_ERR_CUDA;
-    }
-    allowed[dev] = true;
-  }
+  // more than 48 KB of shared memory, once per device
+  static std::once_flag once[64];
+  static bool allowed[64];
+  std::call_once(once[dev], [dev] {
+    allowed[dev] = cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                        kKeysMax * 4 + kKeysMax / 32 * 8) == cudaSuccess;
+    if (!allowed[dev]) (void)cudaGetLastError();
+  });
+  if (!allowed[dev]) return SD_ERR_CUDA;
   if (sd_launch_pdl(evict_kernel, dim3(static_cast<unsigned>(parts), Hkv, B), dim3(kThreads), smem_keys * 4 + smem_keys / 32 * 8,
                     reinterpret_cast<cudaStream_t>(stream), *src, weights, *dst, keep, sinks, recent, weights_out, kept,
                     smem_keys, D == 64 ? 3 : 4) != cudaSuccess) {

@@ -121,17 +121,27 @@ class ClockSampler:
         self.index = index
         self.samples = []
         self._stop = threading.Event()
+        self._started = threading.Event()
         self._thread = None
 
     def _one(self):
         try:
-            out = subprocess.run(["nvidia-smi", "-i", str(self.index), "--query-gpu=" + ",".join(self.FIELDS),
-                                  "--format=csv,noheader,nounits"], capture_output=True, text=True, timeout=5)
-            parts = [p.strip() for p in out.stdout.strip().split(",")]
+            p = subprocess.Popen(["nvidia-smi", "-i", str(self.index), "--query-gpu=" + ",".join(self.FIELDS),
+                                  "--format=csv,noheader,nounits"], stdout=subprocess.PIPE, stderr=subprocess.DEVNULL, text=True)
+            self._started.set()
+            try:
+                out = p.communicate(timeout=5)[0]
+            except subprocess.TimeoutExpired:
+                p.kill()
+                p.communicate()
+                return
+            parts = [x.strip() for x in out.strip().split(",")]
             if len(parts) == len(self.FIELDS):
                 self.samples.append(parts)
         except Exception:
             pass
+        finally:
+            self._started.set()
 
     def _run(self):
         while not self._stop.is_set():
@@ -139,8 +149,11 @@ class ClockSampler:
             self._stop.wait(0.1)
 
     def __enter__(self):
+        """Returns when the first sample's process has started: starting it holds this
+        one up for about a millisecond, which a timed region of 20 steps would count."""
         self._thread = threading.Thread(target=self._run, daemon=True)
         self._thread.start()
+        self._started.wait(timeout=10)
         return self
 
     def __exit__(self, *exc):

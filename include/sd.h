@@ -208,15 +208,17 @@ sd_status sd_verify_attention_ex(const void* q, const sd_kv_cache* cache, void* 
 /*
  * Cluster size of the tcgen05 verify-attention kernels (sd_verify_attention
  * and sd_verify_layer; sd_verify_kernel says which shapes take them; and
- * sd_kv8_attention and sd_attention_weights): one
- * thread-block cluster of `cluster_size` CTAs per (scene, KV head) splits that
- * head's keys evenly and merges the partial softmax states in distributed
- * shared memory (the split-L form of Eq. verify). 0 (the default) lets every
- * call choose among 1, 2, 4, 5, 6, 8, 10, 12 and 16 from the occupancy of each
- * size and the capacity; 1, 2, 4, 6, 8 or 16 forces that size for later calls on
- * every device (a size of which no
- * cluster fits on the device falls back to the automatic choice). Process-wide, host-only, no
- * device work; results are the same for every size up to fp32 rounding order.
+ * sd_kv8_attention and sd_attention_weights, whose forms with a workspace may
+ * take none): one thread-block cluster of `cluster_size` CTAs per (scene, KV
+ * head) splits that head's keys evenly and merges the partial softmax states in
+ * distributed shared memory (the split-L form of Eq. verify). 0 (the default)
+ * lets every call choose among 1, 2, 4, 5, 6, 8, 10, 12 and 16
+ * (sd_attention_weights among 3 too) from the occupancy of each size and the
+ * capacity; 1, 2, 4, 6, 8 or 16 forces that size for later calls on every device
+ * (a size of which no cluster fits on the device falls back to the automatic
+ * choice). Process-wide, host-only, no device work; results are the same for
+ * every size up to fp32 rounding order (sd_kv8_attention: and of its weights,
+ * see there).
  * Returns SD_ERR_INVALID_ARG for any other value.
  */
 sd_status sd_set_cluster_size(int cluster_size);
@@ -463,8 +465,8 @@ sd_status sd_kv8_store(const sd_kv8_cache* cache, const sd_kv_cache* src, sd_str
  * kernel. workspace: sd_kv8_attention_workspace bytes (0: none is used) of device
  * memory, 16-byte aligned, of any content; calls that share one must not overlap
  * on the device; shorter: SD_ERR_WORKSPACE. NULL: as sd_kv8_attention, and so is a
- * size forced by sd_set_cluster_size. Results of the two ways differ by fp32
- * rounding order, each the same from run to run.
+ * size forced by sd_set_cluster_size. Results of the two ways differ by the
+ * weights' rounding and fp32 order, each the same from run to run.
  */
 size_t sd_kv8_attention_workspace(int B, int R, int Hq, int Hkv, int D, int capacity);
 sd_status sd_kv8_attention_ex(const void* q, const sd_kv8_cache* cache, void* out, int R, int Hq, float scale,

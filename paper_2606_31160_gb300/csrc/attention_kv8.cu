@@ -47,12 +47,13 @@
 // share of the tiles of all units instead, and a second kernel joins what the shares' borders
 // cut.
 //
-// What bounds it. 32 scenes of 6200 to 8192 keys, 8 heads, 36 rows: 101 us, 489 MB at
-// 0.71 of the measured copy rate. The softmax: a tile takes an SM 1.6 thousand cycles, 16
-// warps and 96 registers a thread; without its arithmetic 82 us (of the 112 of whole clusters),
-// without the vote 101, without the conversions to two terms besides 92, and with every key
-// from L2 still 111. One scene of 4096 keys (8 heads, 32 rows: 8.1 us; 4 heads of one row
-// each: 6.6) the chain of latencies: lengths, rows and keys, S, references, P, PV, merge.
+// What bounds it. 32 scenes of 6200 to 8192 keys, 8 heads, 36 rows: 103 us, 489 MB at
+// 0.70 of the measured copy rate. The softmax: a tile takes an SM 1.6 thousand cycles, 16
+// warps and 96 registers a thread (8 to 56 B of stores spilled); without its arithmetic
+// 82 us (of the 112 of whole clusters), without the vote 101, without the conversions to two
+// terms besides 92, and with every key from L2 still 111. One scene of 4096 keys (8 heads, 32
+// rows: 8.1 us; 4 heads of one row each: 6.6) the chain of latencies: lengths, rows and keys,
+// S, references, P, PV, merge.
 #include "shares.cuh"
 #include "tc_common.cuh"
 
@@ -1091,9 +1092,9 @@ DevState* state() {
 // 128-key tiles: waves x (tiles a CTA + a fixed cost a wave). 0: even shares over all SMs,
 // where they cost less (tiles a CTA + 4 a unit + the start and the join) and the call may
 // have them. Clusters / even shares in us, 8 KV heads of 4096 keys (3/4 to all of them
-// filled) and 32 rows: 10 scenes 23.4 / 27.5, 16: 25.7 / 33.4, 20: 43.7 / 38.7, 24: 45.4 /
-// 43.2, 32: 48.2 / 52.0, 64: 103 / 90; 32 scenes of 8192 keys and 36 rows 108 / 101, 64 of
-// 1024 40 / 45. Head dim 64, 4 KV heads of 4096: 20 scenes 33.5 / 32.9, 40: 55.7 / 50.2.
+// filled) and 32 rows: 10 scenes 24.0 / 26.6, 16: 25.4 / 31.9, 20: 44.9 / 38.2, 24: 46.6 /
+// 42.6, 32: 49.2 / 50.3, 64: 102 / 86; 32 scenes of 8192 keys and 36 rows 113 / 103, 64 of
+// 1024 41 / 44. Head dim 64, 4 KV heads of 4096: 20 scenes 34.7 / 32.6, 40: 57.0 / 49.6.
 int pick_cluster(const int* active, long long units, int cap, int D, bool may) {
   const int forced = sd_internal_forced_cluster();
   for (int i = 0; i < kNumSizes && forced > 0; ++i)

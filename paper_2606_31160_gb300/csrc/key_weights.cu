@@ -765,9 +765,11 @@ DevState* state() {
 // 8 heads, L = 4096, at 4 / 6 / 8 / 16: 10.7 / 9.2 / 7.4 / 12.3 us; eight scenes, L = 8192,
 // at 2 / 4 / 8: 43 / 38 / 57 on 32 rows, 51 / 53 / 75 on 64, 52 / 56 / 89 on 128.) 0: even
 // shares, where those cost less and the call may have them. Clusters / even shares in us, 8
-// heads of 8192 keys (3/4 to all of them filled): 128 rows, 8 scenes 47 / 52, 12: 83 / 69, 16:
-// 86 / 85, 24: 134 / 124, 24 of 2048 keys 52 / 50, 16: 28 / 35; 64 rows, 8: 46 / 48, 12: 82 /
-// 66, 24: 131 / 120; 32 rows, whose scores clusters form once: 12: 52 / 59, 24: 108 / 110.
+// heads of 8192 keys (3/4 to all of them filled, in a cache with room for a few more): 128
+// rows, 8 scenes 52 / 54, 12: 90 / 74, 16: 93 / 91, 24: 145 / 135, 24 of 2048 keys 55 / 53,
+// 16: 30 / 37; 64 rows, 8: 43 / 47, 12: 78 / 65, 24: 124 / 119. Not for 32 rows, whose scores
+// clusters of 4 form once: 12: 56 / 62, 24: 113 / 115 (but where the room makes a CTA's
+// tiles 17 the choice above is 1, for 72 and 120).
 int pick_cluster(const int* active, long long units, int cap, int rows, bool may) {
   const int forced = sd_internal_forced_cluster();
   for (int i = 0; i < kNumSizes && forced > 0; ++i)

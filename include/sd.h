@@ -64,6 +64,8 @@ typedef enum { SD_BF16 = 0, SD_F32 = 1 } sd_dtype;
 #define SD_DEVERR_TOKEN_RANGE   0x4u  /* a draft token outside [0, V)          */
 #define SD_DEVERR_LENGTH        0x8u  /* len[b] < R or len[b] > capacity       */
 #define SD_DEVERR_TIMEOUT       0x10u /* a bounded mbarrier wait ran out       */
+#define SD_DEVERR_TREE          0x20u /* a parent that is not an earlier row   */
+#define SD_DEVERR_PAGE          0x40u /* a page table entry outside the pool   */
 
 /*
  * KV cache of one attention layer. k and v are [B][Hkv][capacity][D] bf16;
@@ -540,6 +542,120 @@ sd_status sd_kv_evict(const sd_kv_cache* src, const float* weights, int keep, in
 sd_status sd_token_logprobs(const void* logits, sd_dtype dtype, int rows, int V, long long row_stride,
                             const int32_t* tokens, float temperature, int top_n, float* logprob,
                             float* entropy, int32_t* top_ids, float* top_logprobs, sd_stream_t stream);
+
+/*
+ * A paged KV cache of one attention layer. k and v are pools [n_pages][Hkv][page][D]
+ * bf16; row n of scene b is row n % page of page table[b][n / page], so a scene
+ * holds up to max_pages * page rows (fewer than 2^31). table: device int32
+ * [batch][max_pages], which no call writes; several caches (the layers of a model)
+ * may share one. Entries past a scene's rows are never read. len as in
+ * sd_kv_cache; every cache has its own. Rows at or past len[b] are never read.
+ * ticket: device uint32 [batch], zero-filled before the cache's first use and left
+ * zeroed by every completed call; calls that share it must not overlap on the device.
+ * D in {64, 128}, page in {16, 32, 64, 128}. A page may stand in the tables of several
+ * scenes (a shared prefix) as long as no call writes rows to it. A scene with an
+ * entry outside [0, n_pages) among the pages that a call takes sets SD_DEVERR_PAGE.
+ */
+typedef struct {
+  void* k;
+  void* v;
+  const int32_t* table;
+  int32_t* len;
+  uint32_t* ticket;
+  int32_t batch;
+  int32_t n_kv_heads;
+  int32_t n_pages;
+  int32_t page;
+  int32_t max_pages;
+  int32_t head_dim;
+} sd_paged_cache;
+
+/*
+ * The tree calls below: R new rows a scene, row 0 the last committed token and the
+ * others drafted ones, each behind its parent.
+ *   parents: int32 [B][R] device, parents[b][i] the row that row i follows, an
+ *            earlier one, or -1: it follows the prefix. NULL: a chain (row i follows
+ *            row i - 1). An entry outside [-1, i) sets SD_DEVERR_TREE.
+ *   n_new:   int32 [B] device, rows of each scene that count, the first ones (trees of
+ *            several sizes in one batch), in [0, R]; NULL: all R. What belongs to the
+ *            other rows is neither read nor written. A value outside sets SD_DEVERR_LENGTH.
+ */
+
+/*
+ * Append R new rows per scene to a paged cache, rotated on the way: sd_rope_apply of
+ * the new queries and keys and sd_kv_append of the new rows in one call.
+ *   k_new, v_new: [B][R][Hkv][D] bf16, read only; row (b, i) begins k_stride (v_stride)
+ *   elements after the one before it, a multiple of 8, at least Hkv * D.
+ *   q: [B][R][Hq][D] bf16, rows q_stride elements apart, or NULL (with Hq = 0): no queries.
+ *   q_out: the rotated queries, [B][R][Hq][D] contiguous; NULL: in place of q.
+ *   pos, sections, interleaved, base: as for sd_rope_apply; pos NULL: nothing is
+ *   rotated (then q must be NULL).
+ * Writes row i of scene b at position len[b] + i, then len[b] += n_new[b]. A scene with
+ * len[b] + n_new[b] > max_pages * page sets SD_DEVERR_KV_OVERFLOW; it, and one with
+ * another error, is left untouched, its queries too.
+ */
+sd_status sd_paged_append(const sd_paged_cache* cache, const void* k_new, long long k_stride, const void* v_new,
+                          long long v_stride, void* q, long long q_stride, void* q_out, int R, int Hq,
+                          const int32_t* pos, const int32_t sections[3], int interleaved, float base,
+                          const int32_t* n_new, sd_stream_t stream);
+
+/*
+ * Attention of a drafted tree's rows over a paged cache that holds them (appended):
+ * for scene b, query head h (KV head g = h / G) and row i < n_new[b],
+ *   o[b][i][h] = softmax_n( q[b][i][h] . k[b][g][n] * scale ) v[b][g][n]
+ * over the prefix n < L_b = len[b] - n_new[b] and n = L_b + j for j = i and the
+ * ancestors j of row i. With parents NULL it is sd_verify_attention's causal mask.
+ *   q: [B][R][Hq][D] bf16 (rotated), rows q_stride elements apart, a multiple of 8;
+ *   out: [B][R][Hq][D] bf16, contiguous; scale: 0 selects 1/sqrt(D).
+ * What a row does not see does not reach it, infinities and NaN included.
+ * workspace: sd_tree_attention_workspace bytes (0: none is used) of device memory,
+ * 16-byte aligned, of any content; calls that share one must not overlap on the device.
+ * Hq % Hkv == 0, R <= 256. A scene with len[b] < n_new[b] or len[b] > max_pages * page
+ * sets SD_DEVERR_LENGTH; its output, as that of one whose tree is not valid, is left
+ * unwritten. Where a page is not valid the scene's output is NaN.
+ */
+size_t sd_tree_attention_workspace(int B, int R, int Hq, int Hkv, int D, int capacity);
+sd_status sd_tree_attention(const void* q, long long q_stride, const sd_paged_cache* cache, const int32_t* parents,
+                            const int32_t* n_new, void* out, int R, int Hq, float scale, void* workspace,
+                            size_t ws_bytes, sd_stream_t stream);
+
+/*
+ * Workspace bytes sd_accept_tree needs for (B, R, V).
+ */
+size_t sd_accept_tree_workspace(int B, int R, int V);
+
+/*
+ * Greedy acceptance along a tree: sd_accept_greedy with a tree for the chain.
+ *   logits: [B][R][V] of `dtype`, rows row_stride elements apart (>= V), which may begin
+ *   at any element; tokens: int32 [B][R] device, the token of each row (row 0's is not read).
+ * From row 0 the walk goes to the child whose token is the row's argmax (of several
+ * the lowest row), as long as there is one.
+ * Outputs (device, [B][R] int32 each but the first): n_emit [B] = rows on the walk;
+ * path = those rows in order, then -1; out = the argmax of each row on the walk (the
+ * accepted tokens, then the one that follows them), then -1; argmax (may be NULL), the
+ * lowest index among equal maxima, of the rows that count. n_new[b] = 0: n_emit 0, path
+ * and out -1. A token outside [0, V) sets SD_DEVERR_TOKEN_RANGE and is never accepted; a
+ * scene whose tree is not valid is left unwritten. NaN is outside the contract.
+ * ws: as for sd_accept_greedy. R <= 256.
+ */
+sd_status sd_accept_tree(const void* logits, sd_dtype dtype, int B, int R, int V, long long row_stride,
+                         const int32_t* tokens, const int32_t* parents, const int32_t* n_new, int32_t* n_emit,
+                         int32_t* path, int32_t* out, int32_t* argmax, void* ws, size_t ws_bytes, sd_stream_t stream);
+
+/*
+ * Keep what a tree's acceptance committed, in several caches at once (a step's layers):
+ * with first = len[b] - n_new[b], row first + path[b][i] moves to row first + i for
+ * i < n_emit[b], then len[b] = first + n_emit[b].
+ *   caches: HOST array of `count` caches that agree in batch, heads, page and head dim,
+ *   each with its own pools, len and ticket;
+ *   path: int32 [B][R] device, ascending, in [0, n_new[b]); n_emit: int32 [B] device, in
+ *   [0, n_new[b]]; R: rows appended per scene (n_new as above).
+ * A scene with a path or n_emit that is not such sets SD_DEVERR_ROLLBACK, one with
+ * len[b] < n_new[b] or len[b] > max_pages * page SD_DEVERR_LENGTH, and is left untouched.
+ * R <= 65535.
+ */
+sd_status sd_paged_commit(const sd_paged_cache* caches, int count, const int32_t* path, const int32_t* n_emit,
+                          const int32_t* n_new, int R, sd_stream_t stream);
 
 /*
  * Synchronise `stream`, return the device error bits accumulated on the

@@ -16,6 +16,7 @@ Driving", arxiv 2606.31160):
   kv8.py        the 8-bit KV cache: e4m3 codes with a scale for each block of tokens
   evict.py      the weight that keys accumulate, and which of them an eviction keeps
   logprobs.py   log probabilities of given tokens, entropy, top alternatives
+  tree.py       drafted trees over a paged cache: attention, acceptance, commit
 
 Only tests/, __graft_entry__.smoke() and bench.py (its cpu_baseline leg and
 its --impl reference arm) may import it. The CUDA library and its Python
@@ -37,6 +38,7 @@ from .budget import attention_budget
 from .kv8 import dequantise, e4m3_values, kv8_append, round_e4m3
 from .evict import attention_weights, kept_keys
 from .logprobs import token_logprobs
+from .tree import accept_tree, commit_rows, gather_pages, scatter_rows, tree_attention, tree_sees
 
 __all__ = [
     "rope_frequencies", "axis_assignment", "mrope_apply", "rope_1d",
@@ -44,4 +46,5 @@ __all__ = [
     "accept_greedy", "accept_sample", "argmax_lowest", "kv_append",
     "kv_rollback", "attention_budget", "dequantise", "e4m3_values", "kv8_append",
     "round_e4m3", "attention_weights", "kept_keys", "token_logprobs",
+    "accept_tree", "commit_rows", "gather_pages", "scatter_rows", "tree_attention", "tree_sees",
 ]

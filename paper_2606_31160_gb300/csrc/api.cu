@@ -29,7 +29,8 @@ extern "C" sd_status sd_get_device_error(sd_stream_t stream, uint32_t* bits) {
                                       sd_take_error_greedy,
                                       sd_take_error_sample, sd_take_error_budget, sd_take_error_kv8,
                                       sd_take_error_attention_kv8, sd_take_error_weights, sd_take_error_evict,
-                                      sd_take_error_logprobs};
+                                      sd_take_error_logprobs, sd_take_error_paged, sd_take_error_attention_tree,
+                                      sd_take_error_accept_tree};
   for (auto fn : take) {
     if (fn(bits) != cudaSuccess) {
       (void)cudaGetLastError();

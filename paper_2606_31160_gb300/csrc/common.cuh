@@ -42,9 +42,15 @@ cudaError_t sd_take_error_attention_kv8(uint32_t* bits);
 cudaError_t sd_take_error_weights(uint32_t* bits);
 cudaError_t sd_take_error_evict(uint32_t* bits);
 cudaError_t sd_take_error_logprobs(uint32_t* bits);
+cudaError_t sd_take_error_paged(uint32_t* bits);
+cudaError_t sd_take_error_attention_tree(uint32_t* bits);
+cudaError_t sd_take_error_accept_tree(uint32_t* bits);
 
 // Host checks of an 8-bit cache (kv8.cu).
 sd_status sd_internal_kv8_check(const sd_kv8_cache* c);
+
+// Host checks of a paged cache (paged.cu).
+sd_status sd_internal_paged_check(const sd_paged_cache* c);
 
 // Verify attention on the tcgen05 path (attention_tc.cu). Sets *handled when
 // the shape is one it serves (G * R <= 128; head_dim 64 with up to 31 new rows) and it launched.

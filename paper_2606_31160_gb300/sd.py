@@ -24,6 +24,8 @@ SD_DEVERR_ROLLBACK = 0x2
 SD_DEVERR_TOKEN_RANGE = 0x4
 SD_DEVERR_LENGTH = 0x8
 SD_DEVERR_TIMEOUT = 0x10
+SD_DEVERR_TREE = 0x20
+SD_DEVERR_PAGE = 0x40
 
 
 class SDError(RuntimeError):
@@ -45,9 +47,17 @@ class KV8CacheStruct(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32)]
 
 
+class PagedCacheStruct(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p), ("len", ctypes.c_void_p),
+                ("ticket", ctypes.c_void_p), ("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("page", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
 _lib = None
 
 _vp, _i, _f, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+_ll = ctypes.c_longlong
 _SIGNATURES = {
     "sd_status_str": ([_i], ctypes.c_char_p),
     "sd_version": ([], ctypes.c_char_p),
@@ -81,6 +91,13 @@ _SIGNATURES = {
     "sd_attention_weights_ex": ([_vp, ctypes.POINTER(KVCacheStruct), _i, _i, _f, _vp, _vp, _f, _vp, _vp, _sz, _vp], _i),
     "sd_attention_weights": ([_vp, ctypes.POINTER(KVCacheStruct), _i, _i, _f, _vp, _vp, _f, _vp, _vp], _i),
     "sd_kv_evict": ([ctypes.POINTER(KVCacheStruct), _vp, _i, _i, _i, ctypes.POINTER(KVCacheStruct), _vp, _vp, _vp], _i),
+    "sd_paged_append": ([ctypes.POINTER(PagedCacheStruct), _vp, _ll, _vp, _ll, _vp, _ll, _vp, _i, _i, _vp,
+                         ctypes.POINTER(ctypes.c_int32), _i, _f, _vp, _vp], _i),
+    "sd_tree_attention_workspace": ([_i, _i, _i, _i, _i, _i], _sz),
+    "sd_tree_attention": ([_vp, _ll, ctypes.POINTER(PagedCacheStruct), _vp, _vp, _vp, _i, _i, _f, _vp, _sz, _vp], _i),
+    "sd_accept_tree_workspace": ([_i, _i, _i], _sz),
+    "sd_accept_tree": ([_vp, _i, _i, _i, _i, _ll, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp], _i),
+    "sd_paged_commit": ([ctypes.POINTER(PagedCacheStruct), _i, _vp, _vp, _vp, _i, _vp], _i),
     "sd_token_logprobs": ([_vp, _i, _i, _i, ctypes.c_longlong, _vp, _f, _i, _vp, _vp, _vp, _vp, _vp], _i),
 }
 
@@ -547,6 +564,218 @@ def _padded_rows(logits, rows):
     if (logits.shape[-1] > 1 and strides[-1] != 1) or step < logits.shape[-1]:
         raise ValueError("logits' rows must be contiguous")
     return logits.data_ptr(), step
+
+
+# ------------------------------------------------- paged KV cache, drafted trees
+
+class PagedKVCache:
+    """One layer's paged bf16 KV cache: pools [pages, Hkv, page, D], a page table [B,
+    max_pages] int32 (which may be shared between layers) and device lengths [B]; row n of
+    scene b lies in page table[b, n // page]."""
+
+    def __init__(self, k, v, table, lens):
+        if k.shape != v.shape or k.dim() != 4:
+            raise ValueError("k and v must both be [pages, Hkv, page, D]")
+        if table.dim() != 2 or lens.shape != table.shape[:1]:
+            raise ValueError("table must be [B, max_pages] and len [B]")
+        for t, name, dtype in ((k, "k", torch.bfloat16), (v, "v", torch.bfloat16), (table, "table", torch.int32),
+                               (lens, "len", torch.int32)):
+            _dev(t, name, dtype)
+        _same_device(k, v, table, lens)
+        self.k, self.v, self.table, self.len = k, v, table, lens
+        n_pages, H, page, D = k.shape
+        B, max_pages = table.shape
+        self._ticket = torch.zeros(max(B, 1), dtype=torch.int32, device=k.device)
+        self._struct = PagedCacheStruct(k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr(),
+                                        self._ticket.data_ptr(), B, H, n_pages, page, max_pages, D)
+        # what a call reads, fixed with the struct
+        self._ref, self._shape, self._device = ctypes.byref(self._struct), (B, H, max_pages * page, D), k.device.index
+
+    @classmethod
+    def empty(cls, B, Hkv, cap, D, page=64, device="cuda"):
+        """Room for cap rows a scene, every scene with pages of its own."""
+        if int(page) <= 0:
+            raise ValueError("page must be positive")
+        per = -(-cap // page)
+        k = torch.zeros((B * per, Hkv, page, D), dtype=torch.bfloat16, device=device)
+        table = torch.arange(B * per, dtype=torch.int32, device=device).view(B, per)
+        return cls(k, torch.zeros_like(k), table, torch.zeros(B, dtype=torch.int32, device=device))
+
+    @property
+    def struct(self):
+        return self._ref
+
+    @property
+    def shape(self):
+        """(scenes, KV heads, rows that a scene's pages hold, head dim)"""
+        return self._shape
+
+
+class PagedKVCacheGroup:
+    """The caches of a step's layers, as paged_commit takes them."""
+
+    def __init__(self, caches):
+        self.caches = tuple(caches)
+        if not self.caches:
+            raise ValueError("no caches")
+        _same_device(*(c.k for c in self.caches))
+        self._structs = (PagedCacheStruct * len(self.caches))(*(c._struct for c in self.caches))
+
+
+def _current_device(index):
+    """Kernels launch on the current device, on its current stream."""
+    if index != (torch.cuda.current_device() if _raw_device is None else _raw_device()):
+        raise ValueError("the tensors must be on the current device")
+
+
+def _ints(t, name, shape, device):
+    """Address of an int32 tensor of this shape on this device, None for None."""
+    if t is None:
+        return None
+    p = _dev(t, name, torch.int32)
+    if t.shape != shape or t.device.index != device:
+        raise ValueError("%s must be %s on the caller's device" % (name, tuple(shape)))
+    return p
+
+
+def _row_stride(t, name, shape, device):
+    """Address and row stride of bf16 rows [B, R, H, D] whose last two dims are contiguous
+    and whose rows are evenly spaced (part of a projection's output)."""
+    if not isinstance(t, _Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if not t.is_cuda or t.dtype is not torch.bfloat16 or t.shape != shape or t.device.index != device:
+        raise ValueError("%s must be %s bf16 on the caller's CUDA device" % (name, tuple(shape)))
+    B, R, H, D = shape
+    sb, sr, sh, sd_ = t.stride()
+    if t.is_contiguous():
+        return t.data_ptr(), H * D
+    if (D > 1 and sd_ != 1) or (H > 1 and sh != D):
+        raise ValueError("%s: a row's heads must be contiguous" % name)
+    step = sr if R > 1 else sb
+    if R > 1 and B > 1 and sb != R * sr:
+        raise ValueError("%s's rows must be evenly spaced" % name)
+    if step % 8:
+        raise ValueError("%s's rows must be a multiple of 8 elements apart" % name)
+    return t.data_ptr(), step
+
+
+def paged_append(cache, k_new, v_new, q=None, pos=None, sections=None, interleaved=0, base=1e6, n_new=None, q_out=None):
+    """Append k_new / v_new [B,R,Hkv,D] to a PagedKVCache, the keys rotated at pos [B,R,3] on
+    the way, and rotate q [B,R,Hq,D] beside them: into q_out [B,R,Hq,D], or in place. pos
+    None: nothing is rotated (q must be None). n_new: int32 [B] rows of each scene that
+    count, or all. k_new, v_new and q may be parts of one projection's output. Returns the
+    rotated queries."""
+    B, H, _, D = cache._shape
+    dev = cache._device
+    _current_device(dev)
+    if len(k_new.shape) != 4:
+        raise ValueError("k_new must be [B, R, Hkv, D]")
+    R = k_new.shape[1]
+    kp, ks = _row_stride(k_new, "k_new", (B, R, H, D), dev)
+    vp, vs = _row_stride(v_new, "v_new", (B, R, H, D), dev)
+    Hq, qp, qs, op = 0, None, 0, None
+    if q is not None:
+        if pos is None:
+            raise ValueError("q without pos")
+        Hq = q.shape[2] if len(q.shape) == 4 else 0
+        qp, qs = _row_stride(q, "q", (B, R, Hq, D), dev)
+        if q_out is not None:
+            op = _dev(q_out, "q_out", torch.bfloat16)
+            if q_out.shape != q.shape or q_out.device.index != dev:
+                raise ValueError("q_out must have q's shape and device")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if pos is not None and sections is None:
+        raise ValueError("pos without sections")
+    sec = None if pos is None else _sections(tuple(int(x) for x in sections))
+    _check(lib().sd_paged_append(cache._ref, kp, ks, vp, vs, qp, qs, op, R, Hq, _ints(pos, "pos", (B, R, 3), dev), sec,
+                                 int(interleaved), float(base), _ints(n_new, "n_new", (B,), dev), _stream()),
+           "sd_paged_append")
+    return q if q_out is None else q_out
+
+
+def tree_attention_workspace_bytes(B, R, Hq, Hkv, D, capacity):
+    return int(lib().sd_tree_attention_workspace(B, R, Hq, Hkv, D, capacity))
+
+
+def tree_attention(q, cache, parents=None, n_new=None, out=None, scale=0.0, ws=None):
+    """Attention of a drafted tree's rows q [B,R,Hq,D] (rotated) over a PagedKVCache that
+    holds them: a row sees the prefix, its ancestors and itself. parents [B,R] int32: the
+    earlier row that each row follows, -1 for the prefix; None: a chain. n_new: int32 [B]
+    rows of each scene that count, or all. ws: tree_attention_workspace_bytes of device
+    memory; when None a call that takes one has it from torch's allocator, on the current
+    stream."""
+    B, H, cap, D = cache._shape
+    dev = cache._device
+    _current_device(dev)
+    if len(q.shape) != 4:
+        raise ValueError("q must be [B, R, Hq, D]")
+    R, Hq = q.shape[1], q.shape[2]
+    qp, qs = _row_stride(q, "q", (B, R, Hq, D), dev)
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    elif out.shape != q.shape or out.device.index != dev:
+        raise ValueError("out must have q's shape and device")
+    if ws is None:
+        need = lib().sd_tree_attention_workspace(B, R, Hq, H, D, cap)
+        if need:
+            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(lib().sd_tree_attention(qp, qs, cache._ref, _ints(parents, "parents", (B, R), dev),
+                                   _ints(n_new, "n_new", (B,), dev), _dev(out, "out", torch.bfloat16), R, Hq, float(scale),
+                                   None if ws is None else _dev(ws, "ws"), 0 if ws is None else ws.numel() * ws.element_size(),
+                                   _stream()), "sd_tree_attention")
+    return out
+
+
+def accept_tree_workspace_bytes(B, R, V):
+    return int(lib().sd_accept_tree_workspace(B, R, V))
+
+
+def accept_tree(logits, tokens, parents=None, n_new=None, ws=None, n_emit=None, path=None, out=None, argmax=None):
+    """Greedy acceptance along a tree: from row 0 to the child whose token [B,R] int32 is the
+    row's argmax of logits [B,R,V] (bf16 or fp32), while there is one. parents, n_new: as for
+    tree_attention. ws: accept_tree_workspace_bytes, zero-filled before its first use.
+    Returns (n_emit [B], path [B,R], out [B,R], argmax [B,R]) int32: the rows on the walk, their
+    indices, then -1, and the tokens that they emit, then -1."""
+    B, R, V = logits.shape
+    dt = {torch.bfloat16: SD_BF16, torch.float32: SD_F32}.get(logits.dtype)
+    if dt is None:
+        raise ValueError("logits must be bf16 or fp32")
+    if logits.is_contiguous():
+        ptr, stride = _dev(logits, "logits"), V
+    else:
+        ptr, stride = _padded_rows(logits, B * R)
+    dev = logits.device
+    _current_device(dev.index)
+    if ws is None:
+        ws = workspace(accept_tree_workspace_bytes(B, R, V), dev)
+    n_emit = torch.empty(B, dtype=torch.int32, device=dev) if n_emit is None else n_emit
+    path = torch.empty((B, R), dtype=torch.int32, device=dev) if path is None else path
+    out = torch.empty((B, R), dtype=torch.int32, device=dev) if out is None else out
+    argmax = torch.empty((B, R), dtype=torch.int32, device=dev) if argmax is None else argmax
+    wide, at = (B, R), dev.index
+    _check(lib().sd_accept_tree(ptr, dt, B, R, V, stride, _ints(tokens, "tokens", wide, at), _ints(parents, "parents", wide, at),
+                                _ints(n_new, "n_new", (B,), at), _ints(n_emit, "n_emit", (B,), at), _ints(path, "path", wide, at),
+                                _ints(out, "out", wide, at), _ints(argmax, "argmax", wide, at), _dev(ws, "ws"),
+                                ws.numel() * ws.element_size(), _stream()), "sd_accept_tree")
+    return n_emit, path, out, argmax
+
+
+def paged_commit(caches, path, n_emit, n_new=None):
+    """Keep the rows path [B,R] int32 (n_emit [B] of them) of the R rows (n_new [B]) that were
+    appended last, in a PagedKVCacheGroup, a PagedKVCache or a list of them: they move
+    together behind the prefix and the lengths follow."""
+    if not isinstance(caches, PagedKVCacheGroup):
+        caches = PagedKVCacheGroup([caches] if isinstance(caches, PagedKVCache) else caches)
+    first = caches.caches[0]
+    B, dev = first._shape[0], first._device
+    _current_device(dev)
+    if len(path.shape) != 2:
+        raise ValueError("path must be [B, R]")
+    R = path.shape[1]
+    _check(lib().sd_paged_commit(caches._structs, len(caches.caches), _ints(path, "path", (B, R), dev),
+                                 _ints(n_emit, "n_emit", (B,), dev), _ints(n_new, "n_new", (B,), dev), R, _stream()),
+           "sd_paged_commit")
 
 
 # -------------------------------------------------------------- acceptance

@@ -44,9 +44,10 @@ def tree_sees(parents):
 def tree_attention(q, k, v, parents, scale=None, spread=False):
     """One scene: q [n, Hq, D], k and v [Hkv, prefix + n, D], parents [n] -> [n, Hq, D].
 
-    What a row does not see has no part in its sums. spread: also sum_j w_j |v_j - o|
-    (what an error of one part in the weights can move the output by) and the sum
-    of |q k| scale (what an error of one part in a product can move a score by)."""
+    What a row does not see has no part in its sums. spread: also a bound on
+    sum_j w_j |v_j - o| (what an error of one part in the weights can move the output by),
+    the root of sum_j w_j (v_j - o)^2, and the largest sum of |q k| scale (what an error
+    of one part in a product can move a score by)."""
     q, k, v = (np.asarray(x, dtype=np.float64) for x in (q, k, v))
     n, hq, d = q.shape
     hkv, keys, _ = k.shape
@@ -55,18 +56,25 @@ def tree_attention(q, k, v, parents, scale=None, spread=False):
     prefix = keys - n
     visible = np.concatenate([np.ones((n, prefix), dtype=bool), tree_sees(parents)], axis=1)
     out, dev, size = np.zeros_like(q), np.zeros_like(q), np.zeros((n, hq, 1))
+
+    def rows(i, h, kk, vv, seen):  # rows i of head h over keys of which they see some
+        s = np.where(seen, (q[i, h] @ kk.T) * scale, -np.inf)
+        w = np.exp(s - s.max(axis=1, keepdims=True))
+        w = w / w.sum(axis=1, keepdims=True)
+        o = w @ vv
+        out[i, h] = o
+        if spread:
+            dev[i, h] = np.sqrt(np.maximum(w @ (vv * vv) - o * o, 0.0))
+            size[i, h] = np.where(seen, np.abs(q[i, h]) @ np.abs(kk).T, 0.0).max(axis=1, keepdims=True) * scale
+
     with np.errstate(invalid="ignore", over="ignore"):
         for h in range(hq):
             g = h // (hq // hkv)
+            if np.isfinite(k[g]).all() and np.isfinite(v[g]).all():
+                rows(np.arange(n), h, k[g], v[g], visible)
+                continue
             for i in range(n):
-                kk, vv = k[g][visible[i]], v[g][visible[i]]
-                s = (kk @ q[i, h]) * scale
-                w = np.exp(s - s.max())
-                w = w / w.sum()
-                out[i, h] = w @ vv
-                if spread:
-                    dev[i, h] = w @ np.abs(vv - out[i, h])
-                    size[i, h] = (np.abs(kk) @ np.abs(q[i, h])).max() * scale
+                rows(np.array([i]), h, k[g][visible[i]], v[g][visible[i]], np.ones((1, int(visible[i].sum())), dtype=bool))
     return (out, dev, size) if spread else out
 
 

@@ -1,92 +1,777 @@
-// Attention of a drafted tree's rows over a paged cache (sm_103a): the simplest form. A
-// warp takes one row of one query head and all the keys that it sees, one after the
-// other, with a running maximum and sum.
-#include "common.cuh"
+// Attention of a drafted tree's rows over a paged cache (sm_103a, tcgen05).
+//
+// For row i of a scene (its position behind the prefix) and query head h of KV head g
+//     o_i = sum_n softmax_n(q_i k_n scale) v_n,   n < prefix, and the ancestors of i and i.
+// The G n_new rows that share a KV head are packed, so that every key is read once for up to
+// 256 of them (an m-block):
+//     S[128 rows][128 keys] = Q K^T        (both from shared memory, K-major)
+//     O[128 rows][D]       += P V          (P from tensor memory, V MN-major)
+// with one running maximum and sum a row. A row's maximum moves only when a score passes it
+// by more than 2^8 (O is then scaled in place, seldom after the first tile): weights stay
+// below 2^8 and sums far inside fp32. P is bf16, and the sum is taken over the rounded
+// weights, so that they add up to 1 whatever their rounding.
+//
+// Two softmax groups of four warps, each with a product warp, an S | P buffer and an O
+// accumulator of its own. Up to 128 packed rows the groups take alternate key tiles of the
+// same rows; with more, the same tile for 128 rows each. A group's S(next) waits for its PV,
+// because P lies in S's columns; meanwhile the other group's products run. Few rows leave
+// most of the 128 lanes idle, so up to 64 (32) of them are put into the tile two (four)
+// times, each copy with its own half (quarter) of the keys: its weights for the other keys
+// are 0, and copies, groups and shares join at the end by one rule
+//     m = max m_c,  l = sum l_c 2^(m_c - m),  o = sum O_c 2^(m_c - m) / l.
+//
+// Work: the 128-key tiles of all units (scene, KV head, m-block), one unit after the other,
+// in one even share a CTA, one CTA an SM. A unit that a share's border cuts leaves its parts
+// in the workspace, and a second kernel joins them.
+//
+// What a row does not see does not reach it: hidden scores are replaced before the maximum,
+// and in the tiles that hold new rows, values that are no numbers are taken out of V (0 times
+// them would be NaN) and added at the end to the rows that see them.
+#include "tmem.cuh"
 
 #include <math.h>
+#include <algorithm>
 
 SD_DEFINE_ERROR_ACCESSOR(sd_take_error_attention_tree)
 
 namespace {
 
-constexpr int kMaxRows = 256;
+constexpr int kMaxRows = 256;    // rows of a tree
+constexpr int kTile = 128;       // keys a tile
+constexpr int kSoft = 256;       // softmax threads
+constexpr int kProducer = 8, kProduct = 9;  // warps
+constexpr int kThreads = kSoft + 96;
+constexpr float kSlack = 8.f;    // log2 units that a score may pass its row's reference by
+constexpr int kJoinWarps = 8;
 
 struct TreeArgs {
-  const __nv_bfloat16 *q, *k, *v;
+  const __nv_bfloat16* q;
   __nv_bfloat16* out;
+  const __nv_bfloat16* v;   // (only for values that are no numbers)
   const int32_t *table, *len, *parents, *n_new;
   long long q_stride;
-  int R, Hq, Hkv, G, n_pages, shift, max_pages;
-  float scale;
+  float* part;              // per CTA two parts: [rows][D] O, then [rows][2] (m, l)
+  int B, R, Hq, Hkv, G, n_pages, shift, max_pages, cap, rows;  // rows: of an m-block
+  float scale_log2;
 };
 
-// Grid (rows x heads / 4, scenes), a warp each.
-template <int D>
-__global__ void __launch_bounds__(128) tree_attention_kernel(const TreeArgs a) {
-  constexpr int kPer = D / 32;
-  sd_pdl_enter();
-  const int b = blockIdx.y, lane = threadIdx.x & 31;
+// ------------------------------------------------------------------ shares
+struct Scene {
+  int n_keys, m, tiles, units;  // tiles 0: not valid, or no rows that count
+};
+__device__ __forceinline__ Scene scene_of(const TreeArgs& a, int b) {
+  Scene s;
+  s.n_keys = __ldcg(a.len + b);
+  s.m = a.n_new ? __ldcg(a.n_new + b) : a.R;
+  const bool ok = s.m > 0 && s.m <= a.R && s.n_keys >= s.m && s.n_keys <= a.cap;
+  s.tiles = ok ? (s.n_keys + kTile - 1) / kTile : 0;
+  s.units = a.Hkv * ((s.m * a.G + a.rows - 1) / a.rows);
+  if (!ok) s.n_keys = s.m = s.units = 0;
+  return s;
+}
+__device__ __forceinline__ bool length_error(const TreeArgs& a, int b) {
   const int n = __ldcg(a.len + b), m = a.n_new ? __ldcg(a.n_new + b) : a.R;
-  if (m < 0 || m > a.R || n < m || n > static_cast<long long>(a.max_pages) << a.shift) {
-    if (blockIdx.x == 0 && threadIdx.x == 0) sd_set_error(SD_DEVERR_LENGTH);
-    return;
+  return m < 0 || m > a.R || n < m || n > a.cap;
+}
+
+struct Plan {
+  int total, each, rest;  // tiles, tiles a share, shares with one more
+  __device__ __forceinline__ int begin(int cta) const { return cta * each + min(cta, rest); }
+  __device__ __forceinline__ int cta_of(int pos) const {
+    const int more = rest * (each + 1);
+    return pos < more ? pos / (each + 1) : rest + (pos - more) / each;
   }
-  __shared__ int s_parent[kMaxRows];
-  bool ok = true;
-  for (int i = threadIdx.x; i < m; i += blockDim.x) {
-    const int p = a.parents ? __ldcg(a.parents + static_cast<long long>(b) * a.R + i) : i - 1;
-    s_parent[i] = p;
-    ok &= p >= -1 && p < i;
+};
+__device__ __forceinline__ Plan plan_of(const TreeArgs& a, int lane, int ctas) {
+  int n = 0;
+  for (int b = lane; b < a.B; b += 32) {
+    const Scene s = scene_of(a, b);
+    n += s.tiles * s.units;
   }
-  if (!__syncthreads_and(ok)) {
-    if (blockIdx.x == 0 && threadIdx.x == 0) sd_set_error(SD_DEVERR_TREE);
-    return;
-  }
-  const int32_t* table = a.table + static_cast<long long>(b) * a.max_pages;
-  bool paged = true;
-  for (int i = threadIdx.x; i < (n + (1 << a.shift) - 1) >> a.shift; i += blockDim.x) {
-    const int id = __ldcg(table + i);
-    paged &= id >= 0 && id < a.n_pages;
-  }
-  paged = __syncthreads_and(paged) != 0;
-  if (!paged && blockIdx.x == 0 && threadIdx.x == 0) sd_set_error(SD_DEVERR_PAGE);
-  const int item = blockIdx.x * 4 + (threadIdx.x >> 5), i = item / a.Hq, h = item % a.Hq;
-  if (i >= m) return;
-  const int g = h / a.G, prefix = n - m;
-  const long long row = static_cast<long long>(b) * a.R + i;
-  float q[kPer], o[kPer], top = -INFINITY, sum = 0.f;
+  Plan p;
+  p.total = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(n)));
+  p.each = p.total / ctas;
+  p.rest = p.total - p.each * ctas;
+  return p;
+}
+
+// A run of one unit's tiles in a share.
+struct Run {
+  int b, kvh, mb, n_keys, m, tiles;  // of the unit
+  int tile0, n_tiles;                // the run
+  int first;                         // the unit's first tile among all
+};
+struct Walk {
+  int b, unit, tile, first, left;
+  Scene s;
+  // stands at tile `pos` of all, with `n` tiles to go
+  __device__ __forceinline__ void begin(const TreeArgs& a, int pos, int n, int lane) {
+    left = n;
+    if (n <= 0) return;
+    int before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+      Scene mine = {};
+      if (b0 + lane < a.B) mine = scene_of(a, b0 + lane);
+      const int own = mine.tiles * mine.units;
+      int upto = own;
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    q[j] = sd_ldcg_bf16(a.q + row * a.q_stride + h * D + lane + 32 * j) * a.scale;
-    o[j] = 0.f;
+      for (int x = 1; x < 32; x <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, upto, x);
+        if (lane >= x) upto += y;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, before + upto > pos);
+      if (past) {
+        const int at = __ffs(past) - 1;
+        b = b0 + at;
+        s.n_keys = __shfl_sync(0xffffffffu, mine.n_keys, at);
+        s.m = __shfl_sync(0xffffffffu, mine.m, at);
+        s.tiles = __shfl_sync(0xffffffffu, mine.tiles, at);
+        s.units = __shfl_sync(0xffffffffu, mine.units, at);
+        const int in = pos - before - __shfl_sync(0xffffffffu, upto - own, at);
+        unit = in / s.tiles;
+        tile = in - unit * s.tiles;
+        first = pos - tile;
+        return;
+      }
+      before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    left = 0;
   }
-  auto key = [&](int at) {
-    const long long x =
-        (((static_cast<long long>(__ldcg(table + (at >> a.shift))) * a.Hkv + g) << a.shift) + (at & ((1 << a.shift) - 1))) * D + lane;
-    float z = 0.f;
+  __device__ __forceinline__ bool next(const TreeArgs& a, Run& r) {
+    if (left <= 0) return false;
+    if (tile == s.tiles) {
+      first += s.tiles;
+      tile = 0;
+      if (++unit == s.units) {
+        unit = 0;
+        do {
+          if (++b >= a.B) return false;  // (only if a length changed under the kernel)
+          s = scene_of(a, b);
+        } while (s.tiles == 0);
+      }
+    }
+    const int mblocks = s.units / a.Hkv;
+    r.b = b;
+    r.kvh = unit / mblocks;
+    r.mb = unit - r.kvh * mblocks;
+    r.n_keys = s.n_keys;
+    r.m = s.m;
+    r.tiles = s.tiles;
+    r.first = first;
+    r.tile0 = tile;
+    r.n_tiles = min(s.tiles - tile, left);
+    left -= r.n_tiles;
+    tile += r.n_tiles;
+    return true;
+  }
+};
+
+// ------------------------------------------------------------------ configuration
+// kCopies: times that the packed rows stand in the 128-row tile; kQ: row tiles.
+template <int kDim, int kCopies, int kQ>
+struct Cfg {
+  static_assert(kCopies == 1 || kQ == 1, "copies of one tile");
+  static constexpr int kRows = kTile / kCopies;            // packed rows a tile
+  static constexpr int kCols = kTile / kCopies;            // keys of a tile that a lane looks at
+  static constexpr int kHalf = kTile * 128;                // 64 columns of 128 rows
+  static constexpr int kTileBytes = kHalf * (kDim / 64);
+  // With one row tile the groups wait for alternate tiles: a slot must be the same group's
+  // every time, or a group that is ahead takes the phase before for its own (a barrier tells
+  // phases only by their parity). So the counts are even there.
+  static constexpr int kKSlots = kDim == 64 || kQ == 1 ? 4 : 3, kVSlots = kDim == 64 ? 4 : 2;
+  static_assert(kQ == 2 || (kKSlots % 2 == 0 && kVSlots % 2 == 0), "a slot's group");
+  static constexpr int kOffV = kKSlots * kTileBytes;
+  static constexpr int kOffQ = kOffV + kVSlots * kTileBytes;
+  static constexpr int kOffParent = kOffQ + kQ * kTileBytes;     // [256] int16
+  static constexpr int kOffMl = kOffParent + kMaxRows * 2;       // [2][128] float2
+  static constexpr int kOffBar = kOffMl + 2 * kTile * 8;
+  static constexpr int kBars = 2 * (kKSlots + kVSlots) + 7;
+  static constexpr int kOffMisc = kOffBar + kBars * 8;           // tensor memory, bad pages, [8] rows with bad values
+  static constexpr int kSmem = kOffMisc + 48;
+  static_assert(kSmem <= 227 * 1024, "shared memory");
+  static_assert(kOffBar % 8 == 0 && kOffMisc % 8 == 0 && kOffQ % 1024 == 0, "alignment");
+};
+__host__ __device__ constexpr size_t part_floats(int rows, int D) { return static_cast<size_t>(rows) * (D + 2); }
+
+__device__ __forceinline__ bool bad_pair(uint32_t w) { return __vcmpeq2(w & 0x7f807f80u, 0x7f807f80u) != 0; }
+
+// Sum of the values that are no numbers at column d of the bad rows that row i of scene b sees.
+__device__ __noinline__ float bad_values(const TreeArgs& a, const int16_t* parent, const uint32_t* bad, int b, int kvh, int prefix,
+                                         int i, int d, int dim) {
+  float sum = 0.f;
+  for (int j = i; j >= 0; j = a.parents ? parent[j] : j - 1) {
+    if (!(bad[j >> 5] >> (j & 31) & 1)) continue;
+    const int n = prefix + j, id = __ldcg(a.table + static_cast<long long>(b) * a.max_pages + (n >> a.shift));
+    if (id < 0 || id >= a.n_pages) continue;
+    const long long row = ((static_cast<long long>(id) * a.Hkv + kvh) << a.shift) + (n & ((1 << a.shift) - 1));
+    const float v = sd_ldcg_bf16(a.v + row * dim + d);
+    if (!(fabsf(v) < INFINITY)) sum += v;
+  }
+  return sum;
+}
+
+// ------------------------------------------------------------------ kernel
+template <int kDim, int kCopies, int kQ>
+__global__ void __launch_bounds__(kThreads, 1)
+    tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                          const __grid_constant__ TreeArgs a) {
+  using C = Cfg<kDim, kCopies, kQ>;
+  constexpr int kKS = C::kKSlots, kVS = C::kVSlots;
+  extern __shared__ __align__(1024) uint8_t smem[];  // (the kernel has no other shared memory)
+  const uint32_t base = smem_addr(smem);
+  auto bar = [&](int i) { return base + C::kOffBar + 8u * i; };
+  // K and V slots are filled by the producer and freed by the products that read them (one
+  // arrival a row tile); SREADY, PFULL, PVDONE: one of each a group, once a tile of it
+  auto FULLK = [&](int s) { return bar(s); };
+  auto FREEK = [&](int s) { return bar(kKS + s); };
+  auto FULLV = [&](int s) { return bar(2 * kKS + s); };
+  auto FREEV = [&](int s) { return bar(2 * kKS + kVS + s); };
+  auto SREADY = [&](int g) { return bar(2 * (kKS + kVS) + g); };
+  auto PFULL = [&](int g) { return bar(2 * (kKS + kVS) + 2 + g); };
+  auto PVDONE = [&](int g) { return bar(2 * (kKS + kVS) + 4 + g); };
+  const uint32_t QFULL = bar(2 * (kKS + kVS) + 6);  // a run's query tile, and O may be written
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
+  volatile uint32_t* bad_page = reinterpret_cast<uint32_t*>(smem + C::kOffMisc + 4);  // bit: a run's number mod 32
+  uint32_t* bad_rows = reinterpret_cast<uint32_t*>(smem + C::kOffMisc + 8);           // [8]
+  int16_t* s_parent = reinterpret_cast<int16_t*>(smem + C::kOffParent);
+  float2* s_ml = reinterpret_cast<float2*>(smem + C::kOffMl);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kKS; ++s) {
+      mbar_init(FULLK(s), 1);
+      mbar_init(FREEK(s), kQ);
+    }
+    for (int s = 0; s < kVS; ++s) {
+      mbar_init(FULLV(s), 1);
+      mbar_init(FREEV(s), kQ);
+    }
+    for (int g = 0; g < 2; ++g) {
+      mbar_init(SREADY(g), 1);
+      mbar_init(PFULL(g), 4);
+      mbar_init(PVDONE(g), 1);
+    }
+    mbar_init(QFULL, 1);
+    *const_cast<uint32_t*>(bad_page) = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  // tensor memory is taken after the wait for the kernel before (which may hold some) and
+  // before the next kernel may come
+  griddep_wait();
+  if (warp == kProduct) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_slot)), "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  griddep_launch();
+  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem_o = tmem + 256;  // S | P of group g at column 128 g, O at 256 + kDim g
+
+  const Plan plan = plan_of(a, lane, gridDim.x);
+  Walk walk;
+  {
+    const int from = plan.begin(blockIdx.x);
+    walk.begin(a, from, plan.begin(blockIdx.x + 1) - from, lane);
+  }
+  Run r;
+  if (warp == kProducer) {
+    // -------------------------------------------------------------- producer
+    if (blockIdx.x == 0)
+      for (int b = lane; b < a.B; b += 32)
+        if (length_error(a, b)) sd_set_error(SD_DEVERR_LENGTH);
+    const uint64_t evict_first = l2_evict_first_policy();
+    const int page = 1 << a.shift, pages = kTile >> a.shift;  // pages a tile
+    int T = 0, run = 0;
+    while (walk.next(a, r)) {
+      const int32_t* table = a.table + static_cast<long long>(r.b) * a.max_pages;
+      auto page_id = [&](int t) {  // the lane's page of tile t, or -2: none
+        const int at = t * pages + lane;
+        return lane < pages && (at << a.shift) < r.n_keys ? __ldcg(table + at) : INT32_MIN;
+      };
+      int id = page_id(r.tile0);
+      for (int t = 0; t < r.n_tiles; ++t, ++T) {
+        const int tile = r.tile0 + t;
+        const bool need = lane < pages && ((tile * pages + lane) << a.shift) < r.n_keys, ok = need && id >= 0 && id < a.n_pages;
+        if (__any_sync(0xffffffffu, need && !ok) && lane == 0) {
+          atomicOr(const_cast<uint32_t*>(bad_page), 1u << (run & 31));
+          sd_set_error(SD_DEVERR_PAGE);
+        }
+        const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, ok)) * page * kDim * 2;
+        const int z = id * a.Hkv + r.kvh;
+        if (t + 1 < r.n_tiles) id = page_id(tile + 1);
+        auto load = [&](const CUtensorMap* map, uint32_t full, uint32_t dst) {
+          if (lane == 0) mbar_expect_tx(full, bytes);
+          __syncwarp();
+          if (ok) {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) z = fmaf(q[j], sd_ldcg_bf16(a.k + x + 32 * j), z);
+            for (int h = 0; h < kDim / 64; ++h)
+              tma_load_3d_hint(dst + h * C::kHalf + lane * page * 128, map, full, h * 64, 0, z, evict_first);
+          }
+          __syncwarp();
+        };
+        if (T >= kKS) mbar_wait(FREEK(T % kKS), (T / kKS - 1) & 1);
+        load(&tm_k, FULLK(T % kKS), base + (T % kKS) * C::kTileBytes);
+        if (T >= kVS) mbar_wait(FREEV(T % kVS), (T / kVS - 1) & 1);
+        load(&tm_v, FULLV(T % kVS), base + C::kOffV + (T % kVS) * C::kTileBytes);
+      }
+      ++run;
+    }
+  } else if (warp >= kProduct) {
+    // -------------------------------------------------------------- products of group g
+    const int g = warp - kProduct;
+    constexpr uint32_t kIdescS = umma_idesc(128, kTile, 0, 0), kIdescO = umma_idesc(128, kDim, 0, 1);
+    const uint64_t dK = umma_desc(base, 16, 1024), dV = umma_desc(base + C::kOffV, C::kHalf, 1024);
+    const uint64_t dQ = umma_desc(base + C::kOffQ + (kQ == 2 ? g * C::kTileBytes : 0), 16, 1024);
+    const uint32_t ts = tmem + 128 * g, to = tmem_o + kDim * g;
+    int n = 0, T0 = 0, run = 0;
+    while (walk.next(a, r)) {
+      mbar_wait(QFULL, run & 1);
+      for (int t = kQ == 1 ? g : 0; t < r.n_tiles; t += 3 - kQ, ++n) {
+        const int T = T0 + t, ks = T % kKS, vs = T % kVS;
+        if (n > 0) mbar_wait(PVDONE(g), (n - 1) & 1);  // P lies where S goes
+        mbar_wait(FULLK(ks), (T / kKS) & 1);
+        tc_fence_after();
+        if (elect_one()) {
 #pragma unroll
-    for (int d = 16; d; d >>= 1) z += __shfl_xor_sync(0xffffffffu, z, d);
-    const float now = fmaxf(top, z), ref = now == -INFINITY ? 0.f : now;
-    const float f = expf(top - ref), w = expf(z - ref);
-    top = now;
-    sum = sum * f + w;
+          for (int kk = 0; kk < kDim / 16; ++kk) {
+            const uint64_t step = ((kk >> 2) * C::kHalf + (kk & 3) * 32) >> 4;
+            umma(ts, dQ + step, dK + ((ks * C::kTileBytes) >> 4) + step, kIdescS, kk > 0 ? 1 : 0);
+          }
+          umma_commit(SREADY(g));
+          umma_commit(FREEK(ks));
+        }
+        __syncwarp();
+        mbar_wait(PFULL(g), n & 1);
+        mbar_wait(FULLV(vs), (T / kVS) & 1);
+        tc_fence_after();
+        if (elect_one()) {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) o[j] = o[j] * f + w * sd_ldcg_bf16(a.v + x + 32 * j);
+          for (int kk = 0; kk < kTile / 16; ++kk)
+            umma_ta(to, ts + kk * 8, dV + ((vs * C::kTileBytes + kk * 2048) >> 4), kIdescO, t >= 3 - kQ || kk > 0 ? 1 : 0);
+          umma_commit(PVDONE(g));
+          umma_commit(FREEV(vs));
+        }
+        __syncwarp();
+      }
+      T0 += r.n_tiles;
+      ++run;
+    }
+  } else {
+    // -------------------------------------------------------------- softmax
+    const int g = warp >> 2, rl = threadIdx.x & 127;      // lane of the 128-row tile
+    const int copy = rl / C::kRows, row = (kQ == 2 ? g * kTile : 0) + rl % C::kRows;
+    const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t ts = tmem + 128 * g + lane_off, to = tmem_o + lane_off;
+    const float sl = a.scale_log2;
+    constexpr int kWords = C::kCols / 32;
+    int n = 0, T0 = 0, run = 0;
+    while (walk.next(a, r)) {
+      const int prefix = r.n_keys - r.m, M = r.m * a.G, p = r.mb * a.rows + row;
+      const bool live = p < M;
+      const int node = live ? p / a.G : 0;
+      const bool masked_run = (r.tile0 + r.n_tiles) * kTile > prefix;
+      // ---- the packed queries; the tree where the run reaches the new rows
+      for (int x = threadIdx.x; x < kQ * C::kRows * (kDim / 8); x += kSoft) {
+        const int qr = x / (kDim / 8), c = x % (kDim / 8), pq = r.mb * a.rows + qr;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (pq < M) {
+          const int i = pq / a.G;
+          v = __ldcg(reinterpret_cast<const uint4*>(a.q + (static_cast<long long>(r.b) * a.R + i) * a.q_stride +
+                                                    (r.kvh * a.G + pq - i * a.G) * kDim) + c);
+        }
+#pragma unroll
+        for (int cp = 0; cp < kCopies; ++cp) {
+          const int at = cp * C::kRows + (qr & 127);
+          st_shared_v4(base + C::kOffQ + (kCopies == 1 ? (qr >> 7) * C::kTileBytes : 0) + (c >> 3) * C::kHalf + at * 128 +
+                           (((c & 7) ^ (at & 7)) << 4),
+                       v.x, v.y, v.z, v.w);
+        }
+      }
+      bool wrong = false;
+      if (masked_run && a.parents && static_cast<int>(threadIdx.x) < r.m) {
+        const int up = __ldcg(a.parents + static_cast<long long>(r.b) * a.R + threadIdx.x);
+        wrong = up < -1 || up >= static_cast<int>(threadIdx.x);
+        s_parent[threadIdx.x] = static_cast<int16_t>(wrong ? -1 : up);
+      }
+      if (threadIdx.x < 8) bad_rows[threadIdx.x] = 0;
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      tc_fence_before();  // (the run before: its O has been read)
+      __syncwarp();
+      const bool tree_ok = !named_bar_or(1, kSoft, wrong);
+      if (threadIdx.x == 0) mbar_arrive(QFULL);
+      // ---- tiles
+      float m_ref = -INFINITY, l = 0.f;
+      for (int t = kQ == 1 ? g : 0; t < r.n_tiles; t += 3 - kQ, ++n) {
+        const int T = T0 + t, key0 = (r.tile0 + t) * kTile;
+        const bool masked = key0 + kTile > prefix;
+        uint32_t see[kWords];
+        if (masked) {
+          const int c0 = key0 + copy * C::kCols;  // the lane's first key
+#pragma unroll
+          for (int w = 0; w < kWords; ++w) {
+            // keys of the prefix; of a chain, up to the row itself
+            const int cnt = min(max((a.parents ? prefix : prefix + node + 1) - c0 - 32 * w, 0), 32);
+            see[w] = !live ? 0u : (cnt == 32 ? 0xffffffffu : (1u << cnt) - 1);
+          }
+          if (a.parents && live && tree_ok)
+            for (int j = node; j >= 0; j = s_parent[j]) {
+              const int c = prefix + j - c0;
+#pragma unroll
+              for (int w = 0; w < kWords; ++w)
+                if ((c >> 5) == w) see[w] |= 1u << (c & 31);
+            }
+        }
+        mbar_wait(SREADY(g), n & 1);
+        __syncwarp();
+        tc_fence_after();
+        uint32_t s[C::kCols];
+        tmem_load(ts + copy * C::kCols, s);
+        if (masked) {
+#pragma unroll
+          for (int j = 0; j < C::kCols; ++j)
+            if (!(see[j >> 5] >> (j & 31) & 1)) s[j] = 0xff800000u;
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < C::kCols; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(s[j]));
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl;
+        if (__any_sync(0xffffffffu, top > m_ref + kSlack || (m_ref == -INFINITY && top > m_ref))) {
+          const float now = fmaxf(m_ref, top), f = m_ref == -INFINITY ? 0.f : ex2(m_ref - now);
+          m_ref = now;
+          l *= f;
+          if (t >= 3 - kQ) {  // the group's PV of the tile before is done: S came after it
+#pragma unroll
+            for (int c = 0; c < kDim; c += 32) {
+              uint32_t o[32];
+              tmem_load(to + kDim * g + c, o);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_store(to + kDim * g + c, o);
+            }
+          }
+        }
+        const float sub = m_ref == -INFINITY ? 0.f : m_ref;
+        float sum[2] = {0.f, 0.f};
+        uint32_t pw[C::kCols / 2];
+#pragma unroll
+        for (int j = 0; j < C::kCols / 2; ++j) {
+          pw[j] = cvt_bf16x2(ex2(fmaf(__uint_as_float(s[2 * j]), sl, -sub)), ex2(fmaf(__uint_as_float(s[2 * j + 1]), sl, -sub)));
+          sum[0] += sd_bf16_lo(pw[j]);
+          sum[1] += sd_bf16_hi(pw[j]);
+        }
+        l += sum[0] + sum[1];
+        tmem_store(ts + copy * (C::kCols / 2), pw);
+        if (kCopies > 1) {
+          const uint32_t none[C::kCols / 2] = {};
+#pragma unroll
+          for (int c = 1; c < kCopies; ++c) tmem_store(ts + (copy ^ c) * (C::kCols / 2), none);
+        }
+        if (masked) {
+          // V rows behind the last key become 0 (whatever they hold), and so do values of new
+          // rows that are no numbers
+          mbar_wait(FULLV(T % kVS), (T / kVS) & 1);
+          const int kk = kQ == 1 ? rl : 64 * g + rl, key = key0 + kk;
+          const uint32_t vrow = base + C::kOffV + (T % kVS) * C::kTileBytes + kk * 128;
+          if ((kQ == 1 || rl < 64) && key >= prefix) {
+            bool bad = false;
+#pragma unroll
+            for (int h = 0; h < kDim / 64; ++h)
+#pragma unroll
+              for (int c = 0; c < 8; ++c) {
+                const uint32_t at = vrow + h * C::kHalf + ((c ^ (kk & 7)) << 4);
+                if (key >= r.n_keys) {
+                  st_shared_v4(at, 0u, 0u, 0u, 0u);
+                } else {
+                  uint32_t w[4];
+                  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+                  if (bad_pair(w[0]) || bad_pair(w[1]) || bad_pair(w[2]) || bad_pair(w[3])) {
+                    bad = true;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                      if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
+                      if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0x0000ffffu;
+                    }
+                    st_shared_v4(at, w[0], w[1], w[2], w[3]);
+                  }
+                }
+              }
+            if (bad) atomicOr(&bad_rows[(key - prefix) >> 5], 1u << ((key - prefix) & 31));
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (kQ == 2) named_bar_sync(1, kSoft);  // both halves, before either group's product
+        }
+        __syncwarp();
+        tmem_wait_store();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(PFULL(g));
+      }
+      T0 += r.n_tiles;
+      // ---- the run's end: the groups and copies join
+      const int own = kQ == 2 ? r.n_tiles : (r.n_tiles + 1 - g) / 2;
+      if (own > 0) mbar_wait(PVDONE(g), (n - 1) & 1);
+      s_ml[threadIdx.x] = make_float2(m_ref, l);
+      tc_fence_before();
+      __syncwarp();
+      named_bar_sync(1, kSoft);
+      tc_fence_after();
+      const bool whole = r.n_tiles == r.tiles, both = kQ == 1 && r.n_tiles > 1;
+      uint32_t any_bad = 0;
+      if (masked_run)
+        for (int w = 0; w < 8; ++w) any_bad |= bad_rows[w];
+      const bool page_bad = *bad_page >> (run & 31) & 1;
+      // a row's maximum over groups and copies, and its sum relative to that
+      auto joined_ml = [&](int rr, float& mm, float& ll) {
+        mm = -INFINITY, ll = 0.f;
+#pragma unroll
+        for (int c = 0; c < 2 * kCopies; ++c) mm = fmaxf(mm, s_ml[c * C::kRows + rr].x);
+        const float sub = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+        for (int c = 0; c < 2 * kCopies; ++c) ll += s_ml[c * C::kRows + rr].y * ex2(s_ml[c * C::kRows + rr].x - sub);
+        if (page_bad) ll = NAN;
+        if (!tree_ok) mm = NAN;  // says so to the joining kernel
+        return sub;
+      };
+      float top, total, ref = 0.f;
+      if (kQ == 2) {
+        top = tree_ok ? m_ref : NAN;
+        total = page_bad ? NAN : l;
+      } else {
+        ref = joined_ml(rl % C::kRows, top, total);
+      }
+      const float f0 = kQ == 2 ? 1.f : ex2(s_ml[rl].x - ref), f1 = both ? ex2(s_ml[kTile + rl].x - ref) : 0.f;
+      if (!tree_ok && threadIdx.x == 0) sd_set_error(SD_DEVERR_TREE);
+      const int i = node, h = r.kvh * a.G + p - i * a.G;
+      __nv_bfloat16* out = a.out + ((static_cast<long long>(r.b) * a.R + i) * a.Hq + h) * kDim;
+      float* part = a.part + (2 * static_cast<size_t>(blockIdx.x) + (r.tile0 == 0 ? 1 : 0)) * part_floats(a.rows, kDim);
+      float2* part_ml = reinterpret_cast<float2*>(part + static_cast<size_t>(a.rows) * kDim);
+      // 32 columns of the lane's row, the groups' O joined
+      auto joined = [&](int c, float (&x)[32]) {
+        uint32_t o[32];
+        __syncwarp();
+        tmem_load(to + (kQ == 2 ? kDim * g : 0) + c, o);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] = f0 * __uint_as_float(o[j]);
+        if (both) {
+          tmem_load(to + kDim + c, o);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) x[j] = fmaf(f1, __uint_as_float(o[j]), x[j]);
+        }
+        if (any_bad && live && tree_ok && copy == 0)
+#pragma unroll 1
+          for (int j = 0; j < 32; ++j) {
+            const float v = bad_values(a, s_parent, bad_rows, r.b, r.kvh, prefix, i, c + j, kDim);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) x[k] += k == j ? v : 0.f;
+          }
+      };
+      if (kCopies == 1) {
+        const float inv = 1.f / total;
+#pragma unroll 1
+        for (int c = kQ == 2 ? 0 : g * (kDim / 2); c < (kQ == 2 ? kDim : (g + 1) * (kDim / 2)); c += 32) {
+          float x[32];
+          joined(c, x);
+          if (!live) continue;
+          if (!whole) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+              *reinterpret_cast<float4*>(part + static_cast<size_t>(row) * kDim + c + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+          } else if (tree_ok) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8)
+              *reinterpret_cast<uint4*>(out + c + j) =
+                  make_uint4(cvt_bf16x2(x[j] * inv, x[j + 1] * inv), cvt_bf16x2(x[j + 2] * inv, x[j + 3] * inv),
+                             cvt_bf16x2(x[j + 4] * inv, x[j + 5] * inv), cvt_bf16x2(x[j + 6] * inv, x[j + 7] * inv));
+          }
+        }
+        if (live && !whole && (kQ == 2 || g == 0)) part_ml[row] = make_float2(top, total);
+      } else {
+        // the copies' sums through the query tile (its products are done): [128 lanes][kDim / 2]
+        constexpr int kC = kDim / 4;  // columns a group and round
+        float* stage = reinterpret_cast<float*>(smem + C::kOffQ);
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          if (kC == 32) {
+            float x[32];
+            joined(half * 2 * kC + g * kC, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              *reinterpret_cast<float4*>(stage + rl * 2 * kC + (((g * (kC / 4) + j) ^ (rl & 7)) << 2)) =
+                  make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+          } else if (g == 0) {  // head dim 64: one group's 32 columns a round
+            float x[32];
+            joined(half * 32, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              *reinterpret_cast<float4*>(stage + rl * 32 + ((j ^ (rl & 7)) << 2)) = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+          }
+          __syncwarp();
+          named_bar_sync(1, kSoft);
+          for (int x = threadIdx.x; x < C::kRows * (kC / 2); x += kSoft) {
+            const int rr = x / (kC / 2), c4 = x % (kC / 2), pr = r.mb * a.rows + rr;
+            if (pr >= M) continue;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int cp = 0; cp < kCopies; ++cp) {
+              const int at = cp * C::kRows + rr;
+              const float4 y = *reinterpret_cast<const float4*>(stage + at * 2 * kC + ((c4 ^ (at & 7)) << 2));
+              v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
+            }
+            float2 fin;
+            joined_ml(rr, fin.x, fin.y);
+            const int d = half * 2 * kC + c4 * 4, ii = pr / a.G, hh = r.kvh * a.G + pr - ii * a.G;
+            if (!whole) {
+              *reinterpret_cast<float4*>(part + static_cast<size_t>(rr) * kDim + d) = v;
+              if (half == 0 && c4 == 0) part_ml[rr] = fin;
+            } else if (tree_ok) {
+              const float inv = 1.f / fin.y;
+              *reinterpret_cast<uint2*>(a.out + ((static_cast<long long>(r.b) * a.R + ii) * a.Hq + hh) * kDim + d) =
+                  make_uint2(cvt_bf16x2(v.x * inv, v.y * inv), cvt_bf16x2(v.z * inv, v.w * inv));
+            }
+          }
+          __syncwarp();
+          named_bar_sync(1, kSoft);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      named_bar_sync(1, kSoft);
+      if (threadIdx.x == 0 && page_bad) atomicAnd(const_cast<uint32_t*>(bad_page), ~(1u << (run & 31)));
+      ++run;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kProduct) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+// The units that a share's border cuts: border c lies between shares c and c + 1, and the
+// first one that cuts a unit joins its parts, a warp a row.
+template <int kDim>
+__global__ void __launch_bounds__(32 * kJoinWarps) tree_join_kernel(const TreeArgs a, int ctas) {
+  sd_pdl_enter();
+  const int lane = threadIdx.x & 31, c = blockIdx.x + 1, row = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
+  const Plan plan = plan_of(a, lane, ctas);
+  const int pos = plan.begin(c);
+  if (pos <= 0 || pos >= plan.total) return;
+  Walk walk;
+  walk.begin(a, pos, plan.total - pos, lane);
+  Run r;
+  if (!walk.next(a, r) || r.first == pos || plan.begin(c - 1) > r.first) return;
+  const int p = r.mb * a.rows + row;
+  if (row >= a.rows || p >= r.m * a.G) return;
+  const int c1 = plan.cta_of(r.first + r.tiles - 1);
+  auto part = [&](int k) {  // the unit's part in share k
+    return a.part + (2 * static_cast<size_t>(k) + (k == c - 1 ? 1 : 0)) * part_floats(a.rows, kDim);
   };
-  if (paged) {
-    for (int at = 0; at < prefix; ++at) key(at);
-    for (int j = i; j >= 0; j = s_parent[j]) key(prefix + j);
+  auto ml = [&](int k) {
+    const float* x = part(k) + static_cast<size_t>(a.rows) * kDim + 2 * row;
+    return make_float2(__ldcg(x), __ldcg(x + 1));
+  };
+  float top = -INFINITY;
+  bool skip = false;
+  for (int k = c - 1 + lane; k <= c1; k += 32) {
+    const float m = ml(k).x;
+    skip |= m != m;  // its tree is not valid
+    top = fmaxf(top, m);
   }
 #pragma unroll
-  for (int j = 0; j < kPer; ++j)
-    a.out[(row * a.Hq + h) * D + lane + 32 * j] = __float2bfloat16(paged ? o[j] / sum : NAN);
+  for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  if (__any_sync(0xffffffffu, skip)) return;
+  const float ref = top == -INFINITY ? 0.f : top;
+  constexpr int kPer = kDim / 32;
+  float o[kPer] = {}, total = 0.f;
+  for (int k0 = c - 1; k0 <= c1; k0 += 32) {
+    float w = 0.f;
+    if (k0 + lane <= c1) {
+      const float2 x = ml(k0 + lane);
+      w = ex2(x.x - ref);
+      total += w * x.y;
+    }
+    const int cnt = min(32, c1 + 1 - k0);
+#pragma unroll 4
+    for (int k = 0; k < cnt; ++k) {
+      const float f = __shfl_sync(0xffffffffu, w, k);
+      const float* x = part(k0 + k) + static_cast<size_t>(row) * kDim + lane * kPer;
+      if (kPer == 4) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(x));
+        o[0] = fmaf(f, v.x, o[0]), o[1] = fmaf(f, v.y, o[1]), o[kPer - 2] = fmaf(f, v.z, o[kPer - 2]), o[kPer - 1] = fmaf(f, v.w, o[kPer - 1]);
+      } else {
+        const float2 v = __ldcg(reinterpret_cast<const float2*>(x));
+        o[0] = fmaf(f, v.x, o[0]), o[1] = fmaf(f, v.y, o[1]);
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+  const float inv = 1.f / total;
+  const int i = p / a.G;
+  uint32_t* out = reinterpret_cast<uint32_t*>(
+      a.out + ((static_cast<long long>(r.b) * a.R + i) * a.Hq + r.kvh * a.G + p - i * a.G) * kDim) + lane * (kPer / 2);
+#pragma unroll
+  for (int j = 0; j < kPer / 2; ++j) out[j] = cvt_bf16x2(o[2 * j] * inv, o[2 * j + 1] * inv);
+}
+
+// ------------------------------------------------------------------ host
+template <int kDim, int kCopies, int kQ>
+bool prepare() {
+  return cudaFuncSetAttribute(tree_attention_kernel<kDim, kCopies, kQ>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              Cfg<kDim, kCopies, kQ>::kSmem) == cudaSuccess;
+}
+// The kernels' shared memory, once per device.
+bool device_ready() {
+  static std::once_flag once[64];
+  static bool ok[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+    (void)cudaGetLastError();
+    return false;
+  }
+  std::call_once(once[dev], [dev] {
+    ok[dev] = prepare<64, 4, 1>() && prepare<64, 2, 1>() && prepare<64, 1, 1>() && prepare<64, 1, 2>() &&
+              prepare<128, 4, 1>() && prepare<128, 2, 1>() && prepare<128, 1, 1>() && prepare<128, 1, 2>();
+    if (!ok[dev]) (void)cudaGetLastError();
+  });
+  return ok[dev];
+}
+
+struct HostPlan {
+  int rows, ctas;   // packed rows of an m-block
+  size_t ws_bytes;
+};
+// false: too many tiles to count
+bool host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) {
+  const long long M = static_cast<long long>(Hq / Hkv) * R;
+  p->rows = M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
+  const long long tiles = (static_cast<long long>(cap) + kTile - 1) / kTile;
+  const long long units = static_cast<long long>(B) * Hkv * ((M + p->rows - 1) / p->rows);
+  if (units > 0x7fffffffll / tiles || cap > 0x7fffff00) return false;
+  p->ctas = static_cast<int>(std::min<long long>(sd_num_sms(), units * tiles));
+  // one tile a unit: no share's border cuts one
+  p->ws_bytes = tiles > 1 ? 2 * static_cast<size_t>(p->ctas) * part_floats(p->rows, D) * sizeof(float) : 0;
+  return true;
+}
+
+template <int kDim, int kCopies, int kQ>
+cudaError_t launch(const CUtensorMap& k, const CUtensorMap& v, const TreeArgs& a, int ctas, cudaStream_t st) {
+  return sd_launch_pdl(tree_attention_kernel<kDim, kCopies, kQ>, dim3(ctas), dim3(kThreads), Cfg<kDim, kCopies, kQ>::kSmem, st,
+                       k, v, a);
 }
 
 }  // namespace
 
-extern "C" size_t sd_tree_attention_workspace(int, int, int, int, int, int) { return 0; }
+extern "C" size_t sd_tree_attention_workspace(int B, int R, int Hq, int Hkv, int D, int capacity) {
+  if (B <= 0 || R <= 0 || R > kMaxRows || Hkv <= 0 || Hq <= 0 || Hq % Hkv || (D != 64 && D != 128) || capacity <= 0) return 0;
+  HostPlan p;
+  return host_plan(B, R, Hq, Hkv, D, capacity, &p) ? p.ws_bytes : 0;
+}
 
 extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const sd_paged_cache* cache,
                                        const int32_t* parents, const int32_t* n_new, void* out, int R, int Hq,
@@ -97,20 +782,26 @@ extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const 
   if (R <= 0 || Hq <= 0 || Hq % Hkv) return SD_ERR_INVALID_ARG;
   if (!(scale >= 0.f) || !isfinite(scale)) return SD_ERR_INVALID_ARG;
   if (q_stride < static_cast<long long>(Hq) * D || q_stride % 8) return SD_ERR_INVALID_ARG;
-  if (R > kMaxRows) return SD_ERR_UNSUPPORTED;
+  if (R > kMaxRows || Hq / Hkv > 4095) return SD_ERR_UNSUPPORTED;
   if (B == 0) return SD_OK;
   if (!q || !out || !sd_aligned16(q) || !sd_aligned16(out)) return SD_ERR_INVALID_ARG;
   if (workspace && !sd_aligned16(workspace)) return SD_ERR_INVALID_ARG;
+  const int cap = cache->max_pages * cache->page;
+  HostPlan p;
+  if (!host_plan(B, R, Hq, Hkv, D, cap, &p)) return SD_ERR_UNSUPPORTED;
+  if (p.ws_bytes > 0 && (!workspace || ws_bytes < p.ws_bytes)) return SD_ERR_WORKSPACE;
+  if (!device_ready()) return SD_ERR_CUDA;
   TreeArgs a = {};
   a.q = static_cast<const __nv_bfloat16*>(q);
-  a.k = static_cast<const __nv_bfloat16*>(cache->k);
-  a.v = static_cast<const __nv_bfloat16*>(cache->v);
   a.out = static_cast<__nv_bfloat16*>(out);
+  a.v = static_cast<const __nv_bfloat16*>(cache->v);
   a.table = cache->table;
   a.len = cache->len;
   a.parents = parents;
   a.n_new = n_new;
   a.q_stride = q_stride;
+  a.part = static_cast<float*>(workspace);
+  a.B = B;
   a.R = R;
   a.Hq = Hq;
   a.Hkv = Hkv;
@@ -118,9 +809,25 @@ extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const 
   a.n_pages = cache->n_pages;
   a.shift = cache->page == 16 ? 4 : cache->page == 32 ? 5 : cache->page == 64 ? 6 : 7;
   a.max_pages = cache->max_pages;
-  a.scale = scale > 0.f ? scale : static_cast<float>(1.0 / sqrt(static_cast<double>(D)));
-  if (sd_launch_pdl(D == 64 ? tree_attention_kernel<64> : tree_attention_kernel<128>, dim3((R * Hq + 3) / 4, B), dim3(128), 0,
-                    reinterpret_cast<cudaStream_t>(stream), a) != cudaSuccess) {
+  a.cap = cap;
+  a.rows = p.rows;
+  const double sc = scale > 0.f ? scale : 1.0 / sqrt(static_cast<double>(D));
+  a.scale_log2 = static_cast<float>(sc * 1.4426950408889634);
+  CUtensorMap k, v;
+  if (!make_map(&k, cache->k, cache->page, cache->n_pages * Hkv, cache->page, D) ||
+      !make_map(&v, cache->v, cache->page, cache->n_pages * Hkv, cache->page, D))
+    return SD_ERR_CUDA;
+  const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const auto run = D == 128 ? (p.rows == 32 ? launch<128, 4, 1> : p.rows == 64 ? launch<128, 2, 1>
+                               : p.rows == 128 ? launch<128, 1, 1> : launch<128, 1, 2>)
+                            : (p.rows == 32 ? launch<64, 4, 1> : p.rows == 64 ? launch<64, 2, 1>
+                               : p.rows == 128 ? launch<64, 1, 1> : launch<64, 1, 2>);
+  cudaError_t e = run(k, v, a, p.ctas, st);
+  if (e == cudaSuccess && p.ws_bytes > 0 && p.ctas > 1)
+    e = sd_launch_pdl(D == 128 ? tree_join_kernel<128> : tree_join_kernel<64>,
+                      dim3(p.ctas - 1, (std::min<long long>(p.rows, static_cast<long long>(a.G) * R) + kJoinWarps - 1) / kJoinWarps),
+                      dim3(32 * kJoinWarps), 0, st, a, p.ctas);
+  if (e != cudaSuccess) {
     (void)cudaGetLastError();
     return SD_ERR_CUDA;
   }

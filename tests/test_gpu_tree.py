@@ -3,8 +3,9 @@ against the float64 oracle.
 
 The attention's bound, per element o = sum_j w_j v_j: the output's rounding to bf16 (at
 most 2^-8 |o|), the weights' (at most 2^-8 of each, numerator and sum alike: 2^-8 sum_j w_j
-|v_j - o|), and the scores' fp32 sums of D products (D 2^-23 sum |q k| scale on a score, twice
-that on a ratio of weights), with 2^-20 of the largest value for the fp32 sums over keys."""
+|v_j - o|, which is at most 2^-8 (sum_j w_j (v_j - o)^2)^(1/2)), and the scores' fp32 sums of D
+products (D 2^-23 sum |q k| scale on a score, twice that on a ratio of weights), with 2^-20 of
+the largest value for the fp32 sums over keys."""
 import numpy as np
 import pytest
 import torch
@@ -61,6 +62,14 @@ CASES = [
     (1, 256, 3, 1, 128, 129, 128, True, False),     # three m-blocks, the largest tree
     (5, 3, 7, 1, 128, 60, 16, True, True),          # an odd group
     (9, 4, 10, 2, 64, 300, 32, True, True),
+    # many tiles a CTA, for every number of packed rows and both head dims
+    (1, 2, 8, 8, 128, 27000, 128, False, False),
+    (3, 3, 16, 8, 64, 21000, 64, True, True),
+    (2, 12, 32, 8, 128, 11000, 16, True, False),
+    (2, 30, 24, 8, 64, 16001, 128, True, True),
+    (5, 13, 56, 8, 128, 5003, 64, True, True),
+    (3, 61, 32, 8, 128, 6000, 64, True, True),
+    (2, 40, 32, 4, 64, 13000, 32, True, False),
 ]
 
 

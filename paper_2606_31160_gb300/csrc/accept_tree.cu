@@ -4,22 +4,19 @@
 //   at = 0;  at <- the lowest child c of at with token_c == star_at, while there is one
 //   emit star of every row on the walk
 //
-// The simplest form: a CTA finds one row's maximum; the scene's last CTA (a ticket) walks.
-#include "common.cuh"
+// One kernel: a CTA scans a segment of one row and raises the row's key by atomicMax; the
+// scene's last CTA (a ticket, no spin) walks the tree over the keys and re-arms the
+// workspace. The order of the keys is total, so the result does not depend on the order in
+// which they come. CTAs of rows that do not count end at once.
+#include "row_scan.cuh"
+
+#include <algorithm>
 
 SD_DEFINE_ERROR_ACCESSOR(sd_take_error_accept_tree)
 
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int kMaxRows = 256;
-
-__device__ __forceinline__ uint32_t ordered(float x) {
-  const uint32_t u = __float_as_uint(x + 0.f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-__device__ __forceinline__ float load_one(const float* p) { return __ldcg(p); }
-__device__ __forceinline__ float load_one(const __nv_bfloat16* p) { return sd_ldcg_bf16(p); }
 
 struct AcceptArgs {
   const int32_t *tokens, *parents, *n_new;
@@ -76,45 +73,41 @@ __device__ void walk(const AcceptArgs& a, int b, int n) {
   if (lane == 0) a.n_emit[b] = count;
 }
 
-// Grid (rows, scenes).
+// Grid (segments, rows, scenes).
 template <typename T>
-__global__ void __launch_bounds__(kThreads) accept_tree_kernel(const T* logits, const AcceptArgs a) {
-  __shared__ unsigned long long s_best[kThreads / 32];
+__global__ void __launch_bounds__(kThreads) accept_tree_kernel(const T* logits, int vps, const AcceptArgs a) {
+  __shared__ uint32_t s_best[kThreads / 32], s_index;
   __shared__ bool s_last;
   sd_pdl_enter();
-  const int r = blockIdx.x, b = blockIdx.y;
+  const int r = blockIdx.y, b = blockIdx.z;
   const int n = a.n_new ? __ldcg(a.n_new + b) : a.R;
   if (n < 0 || n > a.R) {
-    if (r == 0 && threadIdx.x == 0) sd_set_error(SD_DEVERR_LENGTH);
+    if (r == 0 && blockIdx.x == 0 && threadIdx.x == 0) sd_set_error(SD_DEVERR_LENGTH);
     return;
   }
   if (r >= max(n, 1)) return;
-  if (n > 0) {
-    const T* row = logits + (static_cast<long long>(b) * a.R + r) * a.stride;
-    unsigned long long best = 0;
-    for (int v = threadIdx.x; v < a.V; v += kThreads) {
-      const float x = load_one(row + v);
-      const unsigned long long key =
-          (static_cast<unsigned long long>(ordered(x)) << 32) | (0xffffffffu - static_cast<uint32_t>(v));
-      if (x == x && key > best) best = key;
-    }
-    for (int d = 16; d; d >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, d));
-    if ((threadIdx.x & 31) == 0) s_best[threadIdx.x >> 5] = best;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      for (int w = 1; w < kThreads / 32; ++w) best = max(best, s_best[w]);
-      if (best == 0) best = 0xffffffffull;  // nothing but NaN: index 0
-      a.keys[static_cast<long long>(b) * a.R + r] = best;
-    }
-  }
+  const long long at = static_cast<long long>(b) * a.R + r;
+  unsigned long long best = 0;
+  if (n > 0) best = scan_segment(logits + at * a.stride, a.V, static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x), vps, s_best, &s_index);
   if (threadIdx.x == 0) {
+    if (n > 0) atomicMax(&a.keys[at], best);
     __threadfence();
-    s_last = atomicAdd(&a.ticket[b], 1u) == static_cast<uint32_t>(max(n, 1) - 1);
+    s_last = atomicAdd(&a.ticket[b], 1u) == static_cast<uint32_t>(max(n, 1)) * gridDim.x - 1;
     if (s_last) a.ticket[b] = 0;
     __threadfence();
   }
   __syncthreads();
   if (s_last) walk(a, b, n);
+}
+
+// Vectors a segment: about six CTAs an SM over all rows and at least 16 KB (one step of every
+// thread) a segment; where rows do not count the CTAs left would be uneven, so three times as many.
+int segment_vectors(int B, int R, int V, int elem_bytes, bool ragged) {
+  const long long row = (static_cast<long long>(V) * elem_bytes + 15) / 16;
+  const long long ctas = (ragged ? 18LL : 6LL) * sd_num_sms();
+  const long long vps = std::max<long long>((row * B * R + ctas - 1) / ctas, kStep * kThreads);
+  const long long segs = (row + vps - 1) / vps;
+  return static_cast<int>((row + segs - 1) / segs);
 }
 
 }  // namespace
@@ -148,12 +141,14 @@ extern "C" sd_status sd_accept_tree(const void* logits, sd_dtype dtype, int B, i
   a.stride = row_stride;
   a.R = R;
   a.V = V;
-  const dim3 grid(R, B);
+  const int vps = segment_vectors(B, R, V, dtype == SD_BF16 ? 2 : 4, n_new != nullptr);
+  const long long row = (static_cast<long long>(V) * (dtype == SD_BF16 ? 2 : 4) + 15) / 16;
+  const dim3 grid(static_cast<unsigned>((row + vps - 1) / vps), R, B);
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e =
       dtype == SD_BF16
-          ? sd_launch_pdl(accept_tree_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, st, static_cast<const __nv_bfloat16*>(logits), a)
-          : sd_launch_pdl(accept_tree_kernel<float>, grid, dim3(kThreads), 0, st, static_cast<const float*>(logits), a);
+          ? sd_launch_pdl(accept_tree_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, st, static_cast<const __nv_bfloat16*>(logits), vps, a)
+          : sd_launch_pdl(accept_tree_kernel<float>, grid, dim3(kThreads), 0, st, static_cast<const float*>(logits), vps, a);
   if (e != cudaSuccess) {
     (void)cudaGetLastError();
     return SD_ERR_CUDA;

@@ -55,6 +55,29 @@ struct TreeArgs {
   float scale_log2;
 };
 
+// The largest of three (NaN loses), and sums and products of pairs.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
 // ------------------------------------------------------------------ shares
 struct Scene {
   int n_keys, m, tiles, units;  // tiles 0: not valid, or no rows that count
@@ -82,19 +105,6 @@ struct Plan {
     return pos < more ? pos / (each + 1) : rest + (pos - more) / each;
   }
 };
-__device__ __forceinline__ Plan plan_of(const TreeArgs& a, int lane, int ctas) {
-  int n = 0;
-  for (int b = lane; b < a.B; b += 32) {
-    const Scene s = scene_of(a, b);
-    n += s.tiles * s.units;
-  }
-  Plan p;
-  p.total = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(n)));
-  p.each = p.total / ctas;
-  p.rest = p.total - p.each * ctas;
-  return p;
-}
-
 // A run of one unit's tiles in a share.
 struct Run {
   int b, kvh, mb, n_keys, m, tiles;  // of the unit
@@ -104,15 +114,32 @@ struct Run {
 struct Walk {
   int b, unit, tile, first, left;
   Scene s;
-  // stands at tile `pos` of all, with `n` tiles to go
-  __device__ __forceinline__ void begin(const TreeArgs& a, int pos, int n, int lane) {
-    left = n;
-    if (n <= 0) return;
+  // Cuts all tiles into even shares of `ctas` CTAs and stands at the first tile of share
+  // `cta`, with its tiles to go (kOn: with all that follow). A warp; up to 32 scenes are
+  // looked at once.
+  template <bool kOn>
+  __device__ __forceinline__ Plan begin(const TreeArgs& a, int cta, int ctas, int lane) {
+    Scene mine = {};
+    if (lane < a.B) mine = scene_of(a, lane);
+    int own = mine.tiles * mine.units, n = own;
+    for (int b0 = lane + 32; b0 < a.B; b0 += 32) {
+      const Scene x = scene_of(a, b0);
+      n += x.tiles * x.units;
+    }
+    Plan p;
+    p.total = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(n)));
+    p.each = p.total / ctas;
+    p.rest = p.total - p.each * ctas;
+    const int pos = p.begin(cta);
+    left = (kOn ? p.total : p.begin(cta + 1)) - pos;
+    if (left <= 0) return p;
     int before = 0;
     for (int b0 = 0; b0 < a.B; b0 += 32) {
-      Scene mine = {};
-      if (b0 + lane < a.B) mine = scene_of(a, b0 + lane);
-      const int own = mine.tiles * mine.units;
+      if (b0 > 0) {
+        mine = Scene{};
+        if (b0 + lane < a.B) mine = scene_of(a, b0 + lane);
+        own = mine.tiles * mine.units;
+      }
       int upto = own;
 #pragma unroll
       for (int x = 1; x < 32; x <<= 1) {
@@ -131,11 +158,12 @@ struct Walk {
         unit = in / s.tiles;
         tile = in - unit * s.tiles;
         first = pos - tile;
-        return;
+        return p;
       }
       before += __shfl_sync(0xffffffffu, upto, 31);
     }
-    left = 0;
+    left = 0;  // (only if a length changed under the kernel)
+    return p;
   }
   __device__ __forceinline__ bool next(const TreeArgs& a, Run& r) {
     if (left <= 0) return false;
@@ -270,12 +298,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = *tmem_slot;
   const uint32_t tmem_o = tmem + 256;  // S | P of group g at column 128 g, O at 256 + kDim g
 
-  const Plan plan = plan_of(a, lane, gridDim.x);
   Walk walk;
-  {
-    const int from = plan.begin(blockIdx.x);
-    walk.begin(a, from, plan.begin(blockIdx.x + 1) - from, lane);
-  }
+  walk.begin<false>(a, blockIdx.x, gridDim.x, lane);
   Run r;
   if (warp == kProducer) {
     // -------------------------------------------------------------- producer
@@ -427,23 +451,26 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_wait(SREADY(g), n & 1);
         __syncwarp();
         tc_fence_after();
-        uint32_t s[C::kCols];
-        tmem_load(ts + copy * C::kCols, s);
-        if (masked) {
+        // 32 scores of the lane, hidden ones as -inf
+        auto scores = [&](int c, uint32_t (&s)[32]) {
+          tmem_load(ts + copy * C::kCols + 32 * c, s);
+          if (masked) {
 #pragma unroll
-          for (int j = 0; j < C::kCols; ++j)
-            if (!(see[j >> 5] >> (j & 31) & 1)) s[j] = 0xff800000u;
-        }
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            for (int w = 0; w < kWords; ++w)
+              if (w == c)
 #pragma unroll
-        for (int j = 0; j < C::kCols; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(s[j]));
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl;
-        if (__any_sync(0xffffffffu, top > m_ref + kSlack || (m_ref == -INFINITY && top > m_ref))) {
+                for (int j = 0; j < 32; ++j)
+                  if (!(see[w] >> j & 1)) s[j] = 0xff800000u;
+          }
+        };
+        auto passes = [&](float top) { return top > m_ref + kSlack || (m_ref == -INFINITY && top > m_ref); };
+        // the row's reference moves to `top`, and with it what was summed
+        auto move_reference = [&](float top) {
           const float now = fmaxf(m_ref, top), f = m_ref == -INFINITY ? 0.f : ex2(m_ref - now);
           m_ref = now;
           l *= f;
           if (t >= 3 - kQ) {  // the group's PV of the tile before is done: S came after it
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < kDim; c += 32) {
               uint32_t o[32];
               tmem_load(to + kDim * g + c, o);
@@ -452,17 +479,45 @@ __global__ void __launch_bounds__(kThreads, 1)
               tmem_store(to + kDim * g + c, o);
             }
           }
-        }
-        const float sub = m_ref == -INFINITY ? 0.f : m_ref;
-        float sum[2] = {0.f, 0.f};
-        uint32_t pw[C::kCols / 2];
+        };
+        if (t < 3 - kQ) {  // the first tile: its maximum
+          float mx = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < C::kCols / 2; ++j) {
-          pw[j] = cvt_bf16x2(ex2(fmaf(__uint_as_float(s[2 * j]), sl, -sub)), ex2(fmaf(__uint_as_float(s[2 * j + 1]), sl, -sub)));
-          sum[0] += sd_bf16_lo(pw[j]);
-          sum[1] += sd_bf16_hi(pw[j]);
+          for (int c = 0; c < kWords; ++c) {
+            uint32_t s[32];
+            scores(c, s);
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) mx = max3(mx, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
+          }
+          move_reference(mx * sl);
         }
-        l += sum[0] + sum[1];
+        // weights relative to the reference, and the tile's maximum with them; where that
+        // passes the reference by too much (seldom), once more with it
+        uint32_t pw[C::kCols / 2];
+        float2 sum;
+#pragma unroll 1
+        for (;;) {
+          const float sub = m_ref == -INFINITY ? 0.f : -m_ref;
+          float mx = -INFINITY;
+          sum = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int c = 0; c < kWords; ++c) {
+            uint32_t s[32];
+            scores(c, s);
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              mx = max3(mx, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
+              const float2 y = fma2(make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), make_float2(sl, sl), make_float2(sub, sub));
+              const uint32_t w = cvt_bf16x2(ex2(y.x), ex2(y.y));
+              pw[16 * c + j / 2] = w;
+              sum = add2(sum, make_float2(sd_bf16_lo(w), sd_bf16_hi(w)));
+            }
+          }
+          const float top = mx * sl;
+          if (!__any_sync(0xffffffffu, passes(top))) break;
+          move_reference(top);
+        }
+        l += sum.x + sum.y;
         tmem_store(ts + copy * (C::kCols / 2), pw);
         if (kCopies > 1) {
           const uint32_t none[C::kCols / 2] = {};
@@ -653,31 +708,29 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // The units that a share's border cuts: border c lies between shares c and c + 1, and the
-// first one that cuts a unit joins its parts, a warp a row.
+// first one that cuts a unit joins its parts, a warp a row: the parts' maxima and sums a lane
+// each, then eight parts of the row in flight.
 template <int kDim>
-__global__ void __launch_bounds__(32 * kJoinWarps) tree_join_kernel(const TreeArgs a, int ctas) {
+__global__ void __launch_bounds__(32 * kJoinWarps) tree_join_kernel(const __grid_constant__ TreeArgs a, int ctas) {
+  constexpr int kPer = kDim / 32, kBatch = 8;
   sd_pdl_enter();
   const int lane = threadIdx.x & 31, c = blockIdx.x + 1, row = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
-  const Plan plan = plan_of(a, lane, ctas);
-  const int pos = plan.begin(c);
-  if (pos <= 0 || pos >= plan.total) return;
   Walk walk;
-  walk.begin(a, pos, plan.total - pos, lane);
+  const Plan plan = walk.begin<true>(a, c, ctas, lane);
   Run r;
-  if (!walk.next(a, r) || r.first == pos || plan.begin(c - 1) > r.first) return;
+  if (plan.begin(c) <= 0 || !walk.next(a, r) || r.first == plan.begin(c) || plan.begin(c - 1) > r.first) return;
   const int p = r.mb * a.rows + row;
   if (row >= a.rows || p >= r.m * a.G) return;
-  const int c1 = plan.cta_of(r.first + r.tiles - 1);
-  auto part = [&](int k) {  // the unit's part in share k
-    return a.part + (2 * static_cast<size_t>(k) + (k == c - 1 ? 1 : 0)) * part_floats(a.rows, kDim);
-  };
+  const int n = plan.cta_of(r.first + r.tiles - 1) - c + 2;  // parts: shares c - 1 ...
+  const size_t pf = part_floats(a.rows, kDim);
+  // (the unit begins in its first share's second part, and goes on in the others' first)
+  auto part = [&](int k) { return a.part + (2 * static_cast<size_t>(c - 1 + k) + (k == 0 ? 1 : 0)) * pf; };
   auto ml = [&](int k) {
-    const float* x = part(k) + static_cast<size_t>(a.rows) * kDim + 2 * row;
-    return make_float2(__ldcg(x), __ldcg(x + 1));
+    return __ldcg(reinterpret_cast<const float2*>(part(k) + static_cast<size_t>(a.rows) * kDim) + row);
   };
   float top = -INFINITY;
   bool skip = false;
-  for (int k = c - 1 + lane; k <= c1; k += 32) {
+  for (int k = lane; k < n; k += 32) {
     const float m = ml(k).x;
     skip |= m != m;  // its tree is not valid
     top = fmaxf(top, m);
@@ -686,26 +739,35 @@ __global__ void __launch_bounds__(32 * kJoinWarps) tree_join_kernel(const TreeAr
   for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
   if (__any_sync(0xffffffffu, skip)) return;
   const float ref = top == -INFINITY ? 0.f : top;
-  constexpr int kPer = kDim / 32;
   float o[kPer] = {}, total = 0.f;
-  for (int k0 = c - 1; k0 <= c1; k0 += 32) {
+  for (int k0 = 0; k0 < n; k0 += 32) {
     float w = 0.f;
-    if (k0 + lane <= c1) {
+    if (k0 + lane < n) {
       const float2 x = ml(k0 + lane);
       w = ex2(x.x - ref);
       total += w * x.y;
     }
-    const int cnt = min(32, c1 + 1 - k0);
-#pragma unroll 4
-    for (int k = 0; k < cnt; ++k) {
-      const float f = __shfl_sync(0xffffffffu, w, k);
-      const float* x = part(k0 + k) + static_cast<size_t>(row) * kDim + lane * kPer;
-      if (kPer == 4) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(x));
-        o[0] = fmaf(f, v.x, o[0]), o[1] = fmaf(f, v.y, o[1]), o[kPer - 2] = fmaf(f, v.z, o[kPer - 2]), o[kPer - 1] = fmaf(f, v.w, o[kPer - 1]);
-      } else {
-        const float2 v = __ldcg(reinterpret_cast<const float2*>(x));
-        o[0] = fmaf(f, v.x, o[0]), o[1] = fmaf(f, v.y, o[1]);
+    for (int k1 = k0; k1 < min(n, k0 + 32); k1 += kBatch) {
+      float x[kBatch][kPer];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const float* src = part(k1 + u) + static_cast<size_t>(row) * kDim + lane * kPer;
+        if (k1 + u < n) {
+          if (kPer == 4) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
+            x[u][0] = v.x, x[u][1] = v.y, x[u][kPer - 2] = v.z, x[u][kPer - 1] = v.w;
+          } else {
+            const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
+            x[u][0] = v.x, x[u][1] = v.y;
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const float f = __shfl_sync(0xffffffffu, w, (k1 + u) & 31);
+        if (k1 + u < n)
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) o[j] = fmaf(f, x[u][j], o[j]);
       }
     }
   }

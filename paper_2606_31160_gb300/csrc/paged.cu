@@ -256,10 +256,14 @@ extern "C" sd_status sd_paged_append(const sd_paged_cache* cache, const void* k_
   a.pos = pos;
   a.R = R;
   a.Hq = Hq;
-  const long long heads = Hq + 2ll * Hkv;
-  const long long blocks = (R * heads + kThreads / (D / 8) - 1) / (kThreads / (D / 8));
+  // heads a thread: one where the call is short, so that many threads share its latency; eight
+  // where it is long: the angles of a row are taken once for eight heads
+  const long long heads = Hq + 2ll * Hkv, per_cta = kThreads / (D / 8);
+  const int per = static_cast<long long>(B) * R * heads >= 16 * per_cta * sd_num_sms() ? 8 : 1;
+  const long long blocks = (R * ((heads + per - 1) / per) + per_cta - 1) / per_cta;
   if (blocks > 0x7fffffffll) return SD_ERR_UNSUPPORTED;
-  if (sd_launch_pdl(D == 64 ? paged_append_kernel<64, 1> : paged_append_kernel<128, 1>,
+  if (sd_launch_pdl(D == 64 ? (per == 8 ? paged_append_kernel<64, 8> : paged_append_kernel<64, 1>)
+                            : (per == 8 ? paged_append_kernel<128, 8> : paged_append_kernel<128, 1>),
                     dim3(static_cast<unsigned>(blocks), B), dim3(kThreads), 0, reinterpret_cast<cudaStream_t>(stream), a,
                     tab) != cudaSuccess) {
     (void)cudaGetLastError();

@@ -11,18 +11,20 @@
 // below 2^8 and sums far inside fp32. P is bf16, and the sum is taken over the rounded
 // weights, so that they add up to 1 whatever their rounding.
 //
-// Two softmax groups of four warps, each with a product warp, an S | P buffer and an O
-// accumulator of its own. Up to 128 packed rows the groups take alternate key tiles of the
-// same rows; with more, the same tile for 128 rows each. A group's S(next) waits for its PV,
-// because P lies in S's columns; meanwhile the other group's products run. Few rows leave
-// most of the 128 lanes idle, so up to 64 (32) of them are put into the tile two (four)
-// times, each copy with its own half (quarter) of the keys: its weights for the other keys
-// are 0, and copies, groups and shares join at the end by one rule
+// Two softmax groups of four warps, each with an S | P buffer and an O accumulator of its
+// own. Up to 128 packed rows the groups take alternate key tiles of the same rows; with more,
+// the same tile for 128 rows each. One warp issues all products, a group's PV and then its
+// next S (which goes where P was, so PV has to be done), then the other's: while one group's
+// products run, the other's softmax does. Few rows leave most of the 128 lanes idle, so up to
+// 64 (32) of them are put into the tile two (four) times, each copy with its own half
+// (quarter) of the keys: its weights for the other keys are 0, and copies, groups and shares
+// join at the end by one rule
 //     m = max m_c,  l = sum l_c 2^(m_c - m),  o = sum O_c 2^(m_c - m) / l.
 //
-// Work: the 128-key tiles of all units (scene, KV head, m-block), one unit after the other,
-// in one even share a CTA, one CTA an SM. A unit that a share's border cuts leaves its parts
-// in the workspace, and a second kernel joins them.
+// Work: one CTA an SM. Where there are many units (scene, KV head, m-block), the 128-key tiles
+// of all of them, one unit after the other, in one even share a CTA; where there are few, the
+// same number of CTAs for each unit, so that no CTA begins a second one. A unit that more than
+// one CTA takes leaves its parts in the workspace, and a second kernel joins them.
 //
 // What a row does not see does not reach it: hidden scores are replaced before the maximum,
 // and in the tiles that hold new rows, values that are no numbers are taken out of V (0 times
@@ -40,9 +42,11 @@ constexpr int kMaxRows = 256;    // rows of a tree
 constexpr int kTile = 128;       // keys a tile
 constexpr int kSoft = 256;       // softmax threads
 constexpr int kProducer = 8, kProduct = 9;  // warps
-constexpr int kThreads = kSoft + 96;
+constexpr int kThreads = kSoft + 64;
 constexpr float kSlack = 8.f;    // log2 units that a score may pass its row's reference by
-constexpr int kJoinWarps = 8;
+constexpr int kJoin = 256;       // threads of the joining kernel
+constexpr int kMaxCtas = 192;    // shares
+constexpr int kApart = 4;        // tiles that a second unit in a share costs
 
 struct TreeArgs {
   const __nv_bfloat16* q;
@@ -50,9 +54,9 @@ struct TreeArgs {
   const __nv_bfloat16* v;   // (only for values that are no numbers)
   const int32_t *table, *len, *parents, *n_new;
   long long q_stride;
-  float* part;              // per CTA two parts: [rows][D] O, then [rows][2] (m, l)
+  float* part;              // per CTA two parts: O [D / 4][rows][4], then (m, l) [rows][2]
   int B, R, Hq, Hkv, G, n_pages, shift, max_pages, cap, rows;  // rows: of an m-block
-  float scale_log2;
+  float scale_log2, inv_g;
 };
 
 // The largest of three (NaN loses), and sums and products of pairs.
@@ -99,12 +103,14 @@ __device__ __forceinline__ bool length_error(const TreeArgs& a, int b) {
 
 struct Plan {
   int total, each, rest;  // tiles, tiles a share, shares with one more
+  int units, per;         // per > 0: so many CTAs a unit instead
   __device__ __forceinline__ int begin(int cta) const { return cta * each + min(cta, rest); }
   __device__ __forceinline__ int cta_of(int pos) const {
     const int more = rest * (each + 1);
     return pos < more ? pos / (each + 1) : rest + (pos - more) / each;
   }
 };
+
 // A run of one unit's tiles in a share.
 struct Run {
   int b, kvh, mb, n_keys, m, tiles;  // of the unit
@@ -114,32 +120,39 @@ struct Run {
 struct Walk {
   int b, unit, tile, first, left;
   Scene s;
-  // Cuts all tiles into even shares of `ctas` CTAs and stands at the first tile of share
-  // `cta`, with its tiles to go (kOn: with all that follow). A warp; up to 32 scenes are
-  // looked at once.
-  template <bool kOn>
+  // Plans the work of `ctas` CTAs and stands at the first tile of share `cta`, with its tiles
+  // to go. kJoin: at the unit that border `cta` cuts (even shares: all that follows), or at
+  // unit cta - 1. A warp; up to 32 scenes are looked at once.
+  template <bool kJoin>
   __device__ __forceinline__ Plan begin(const TreeArgs& a, int cta, int ctas, int lane) {
     Scene mine = {};
     if (lane < a.B) mine = scene_of(a, lane);
-    int own = mine.tiles * mine.units, n = own;
+    int n = mine.tiles * mine.units, u = mine.units, most = mine.tiles;
     for (int b0 = lane + 32; b0 < a.B; b0 += 32) {
       const Scene x = scene_of(a, b0);
       n += x.tiles * x.units;
+      u += x.units;
+      most = max(most, x.tiles);
     }
     Plan p;
     p.total = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(n)));
+    p.units = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(u)));
+    most = __reduce_max_sync(0xffffffffu, most);
     p.each = p.total / ctas;
     p.rest = p.total - p.each * ctas;
-    const int pos = p.begin(cta);
-    left = (kOn ? p.total : p.begin(cta + 1)) - pos;
-    if (left <= 0) return p;
+    p.per = p.units > 0 && p.units <= ctas / 2 ? ctas / p.units : 0;
+    if (p.per > 0 && (most + p.per - 1) / p.per > p.each + 1 + kApart) p.per = 0;
+    const int share_unit = p.per > 0 ? (kJoin ? cta - 1 : cta / p.per) : 0;
+    const int pos = p.per > 0 ? share_unit : p.begin(cta);
+    left = 0;
+    if (pos >= (p.per > 0 ? p.units : p.total)) return p;
     int before = 0;
     for (int b0 = 0; b0 < a.B; b0 += 32) {
       if (b0 > 0) {
         mine = Scene{};
         if (b0 + lane < a.B) mine = scene_of(a, b0 + lane);
-        own = mine.tiles * mine.units;
       }
+      const int own = p.per > 0 ? mine.units : mine.tiles * mine.units;
       int upto = own;
 #pragma unroll
       for (int x = 1; x < 32; x <<= 1) {
@@ -155,15 +168,23 @@ struct Walk {
         s.tiles = __shfl_sync(0xffffffffu, mine.tiles, at);
         s.units = __shfl_sync(0xffffffffu, mine.units, at);
         const int in = pos - before - __shfl_sync(0xffffffffu, upto - own, at);
-        unit = in / s.tiles;
-        tile = in - unit * s.tiles;
-        first = pos - tile;
+        if (p.per > 0) {
+          const int part = kJoin ? 0 : cta - share_unit * p.per, each = s.tiles / p.per, rest = s.tiles - each * p.per;
+          unit = in;
+          tile = part * each + min(part, rest);
+          first = 0;
+          left = kJoin ? s.tiles : each + (part < rest ? 1 : 0);
+        } else {
+          unit = in / s.tiles;
+          tile = in - unit * s.tiles;
+          first = pos - tile;
+          left = (kJoin ? p.total : p.begin(cta + 1)) - pos;
+        }
         return p;
       }
       before += __shfl_sync(0xffffffffu, upto, 31);
     }
-    left = 0;  // (only if a length changed under the kernel)
-    return p;
+    return p;  // (only if a length changed under the kernel)
   }
   __device__ __forceinline__ bool next(const TreeArgs& a, Run& r) {
     if (left <= 0) return false;
@@ -203,11 +224,7 @@ struct Cfg {
   static constexpr int kCols = kTile / kCopies;            // keys of a tile that a lane looks at
   static constexpr int kHalf = kTile * 128;                // 64 columns of 128 rows
   static constexpr int kTileBytes = kHalf * (kDim / 64);
-  // With one row tile the groups wait for alternate tiles: a slot must be the same group's
-  // every time, or a group that is ahead takes the phase before for its own (a barrier tells
-  // phases only by their parity). So the counts are even there.
-  static constexpr int kKSlots = kDim == 64 || kQ == 1 ? 4 : 3, kVSlots = kDim == 64 ? 4 : 2;
-  static_assert(kQ == 2 || (kKSlots % 2 == 0 && kVSlots % 2 == 0), "a slot's group");
+  static constexpr int kKSlots = kDim == 64 ? 4 : 3, kVSlots = kDim == 64 ? 4 : (kQ == 1 ? 3 : 2);
   static constexpr int kOffV = kKSlots * kTileBytes;
   static constexpr int kOffQ = kOffV + kVSlots * kTileBytes;
   static constexpr int kOffParent = kOffQ + kQ * kTileBytes;     // [256] int16
@@ -249,7 +266,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t base = smem_addr(smem);
   auto bar = [&](int i) { return base + C::kOffBar + 8u * i; };
   // K and V slots are filled by the producer and freed by the products that read them (one
-  // arrival a row tile); SREADY, PFULL, PVDONE: one of each a group, once a tile of it
+  // arrival a row tile); SREADY, PFULL, PVDONE: one of each a group, once a tile of it. A
+  // barrier tells phases by their parity only: whoever waits for a slot's phase knows that the
+  // one before is over (the products take the slots in order, and a group's S comes after them)
   auto FULLK = [&](int s) { return bar(s); };
   auto FREEK = [&](int s) { return bar(kKS + s); };
   auto FULLV = [&](int s) { return bar(2 * kKS + s); };
@@ -291,6 +310,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  Walk walk;
+  walk.begin<false>(a, blockIdx.x, gridDim.x, lane);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -298,8 +319,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = *tmem_slot;
   const uint32_t tmem_o = tmem + 256;  // S | P of group g at column 128 g, O at 256 + kDim g
 
-  Walk walk;
-  walk.begin<false>(a, blockIdx.x, gridDim.x, lane);
   Run r;
   if (warp == kProducer) {
     // -------------------------------------------------------------- producer
@@ -343,42 +362,62 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       ++run;
     }
-  } else if (warp >= kProduct) {
-    // -------------------------------------------------------------- products of group g
-    const int g = warp - kProduct;
+  } else if (warp == kProduct) {
+    // -------------------------------------------------------------- products
     constexpr uint32_t kIdescS = umma_idesc(128, kTile, 0, 0), kIdescO = umma_idesc(128, kDim, 0, 1);
     const uint64_t dK = umma_desc(base, 16, 1024), dV = umma_desc(base + C::kOffV, C::kHalf, 1024);
-    const uint64_t dQ = umma_desc(base + C::kOffQ + (kQ == 2 ? g * C::kTileBytes : 0), 16, 1024);
-    const uint32_t ts = tmem + 128 * g, to = tmem_o + kDim * g;
-    int n = 0, T0 = 0, run = 0;
+    const uint64_t dQ = umma_desc(base + C::kOffQ, 16, 1024);
+    int n0 = 0, n1 = 0, T0 = 0, run = 0;  // n0, n1: products of the groups so far
     while (walk.next(a, r)) {
-      mbar_wait(QFULL, run & 1);
-      for (int t = kQ == 1 ? g : 0; t < r.n_tiles; t += 3 - kQ, ++n) {
-        const int T = T0 + t, ks = T % kKS, vs = T % kVS;
-        if (n > 0) mbar_wait(PVDONE(g), (n - 1) & 1);  // P lies where S goes
-        mbar_wait(FULLK(ks), (T / kKS) & 1);
+      // item x: group x mod 2, of tile x / 2 (two row tiles) or x. The first group's wait for a
+      // tile stands for the second's.
+      const int items = kQ * r.n_tiles;
+      auto tile_of = [&](int x) { return T0 + (kQ == 2 ? x >> 1 : x); };
+      auto wait_k = [&](int x) {
+        const int T = tile_of(x);
+        if (kQ == 1 || !(x & 1)) mbar_wait(FULLK(T % kKS), (T / kKS) & 1);
+      };
+      auto scores = [&](int x) {
+        const int g = x & 1, ks = tile_of(x) % kKS;
         tc_fence_after();
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < kDim / 16; ++kk) {
             const uint64_t step = ((kk >> 2) * C::kHalf + (kk & 3) * 32) >> 4;
-            umma(ts, dQ + step, dK + ((ks * C::kTileBytes) >> 4) + step, kIdescS, kk > 0 ? 1 : 0);
+            umma(tmem + 128 * g, dQ + (kQ == 2 ? (g * C::kTileBytes) >> 4 : 0) + step, dK + ((ks * C::kTileBytes) >> 4) + step, kIdescS,
+                 kk > 0 ? 1 : 0);
           }
           umma_commit(SREADY(g));
           umma_commit(FREEK(ks));
         }
         __syncwarp();
+      };
+      mbar_wait(QFULL, run & 1);
+      for (int x = 0; x < min(2, items); ++x) {
+        wait_k(x);
+        scores(x);
+      }
+      for (int x = 0; x < items; ++x) {
+        const int g = x & 1, T = tile_of(x), vs = T % kVS, n = g ? n1 : n0;
+        if (kQ == 1 || g == 0) mbar_wait(FULLV(vs), (T / kVS) & 1);
         mbar_wait(PFULL(g), n & 1);
-        mbar_wait(FULLV(vs), (T / kVS) & 1);
         tc_fence_after();
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < kTile / 16; ++kk)
-            umma_ta(to, ts + kk * 8, dV + ((vs * C::kTileBytes + kk * 2048) >> 4), kIdescO, t >= 3 - kQ || kk > 0 ? 1 : 0);
+            umma_ta(tmem_o + kDim * g, tmem + 128 * g + kk * 8, dV + ((vs * C::kTileBytes + kk * 2048) >> 4), kIdescO,
+                    x >= 2 || kk > 0 ? 1 : 0);
           umma_commit(PVDONE(g));
           umma_commit(FREEV(vs));
         }
         __syncwarp();
+        if (x + 2 < items) {
+          wait_k(x + 2);               // (while the product runs)
+          mbar_wait(PVDONE(g), n & 1); // P lies where S goes
+          scores(x + 2);
+        }
+        if (g) ++n1;
+        else ++n0;
       }
       T0 += r.n_tiles;
       ++run;
@@ -395,23 +434,34 @@ __global__ void __launch_bounds__(kThreads, 1)
     while (walk.next(a, r)) {
       const int prefix = r.n_keys - r.m, M = r.m * a.G, p = r.mb * a.rows + row;
       const bool live = p < M;
-      const int node = live ? p / a.G : 0;
+      auto gdiv = [&](int x) { return __float2int_rz((static_cast<float>(x) + 0.5f) * a.inv_g); };  // exact below 2^21
+      const int node = live ? gdiv(p) : 0;
       const bool masked_run = (r.tile0 + r.n_tiles) * kTile > prefix;
       // ---- the packed queries; the tree where the run reaches the new rows
-      for (int x = threadIdx.x; x < kQ * C::kRows * (kDim / 8); x += kSoft) {
-        const int qr = x / (kDim / 8), c = x % (kDim / 8), pq = r.mb * a.rows + qr;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (pq < M) {
-          const int i = pq / a.G;
-          v = __ldcg(reinterpret_cast<const uint4*>(a.q + (static_cast<long long>(r.b) * a.R + i) * a.q_stride +
-                                                    (r.kvh * a.G + pq - i * a.G) * kDim) + c);
+      constexpr int kChunks = kQ * C::kRows * (kDim / 8) / kSoft, kBatch = kChunks < 8 ? kChunks : 8;  // a thread's
+#pragma unroll 1
+      for (int x0 = 0; x0 < kChunks; x0 += kBatch) {
+        uint4 v[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int x = threadIdx.x + (x0 + u) * kSoft, qr = x / (kDim / 8), c = x % (kDim / 8), pq = r.mb * a.rows + qr;
+          v[u] = make_uint4(0, 0, 0, 0);
+          if (pq < M) {
+            const int i = gdiv(pq);
+            v[u] = __ldcg(reinterpret_cast<const uint4*>(a.q + (static_cast<long long>(r.b) * a.R + i) * a.q_stride +
+                                                         (r.kvh * a.G + pq - i * a.G) * kDim) + c);
+          }
         }
 #pragma unroll
-        for (int cp = 0; cp < kCopies; ++cp) {
-          const int at = cp * C::kRows + (qr & 127);
-          st_shared_v4(base + C::kOffQ + (kCopies == 1 ? (qr >> 7) * C::kTileBytes : 0) + (c >> 3) * C::kHalf + at * 128 +
-                           (((c & 7) ^ (at & 7)) << 4),
-                       v.x, v.y, v.z, v.w);
+        for (int u = 0; u < kBatch; ++u) {
+          const int x = threadIdx.x + (x0 + u) * kSoft, qr = x / (kDim / 8), c = x % (kDim / 8);
+#pragma unroll
+          for (int cp = 0; cp < kCopies; ++cp) {
+            const int at = cp * C::kRows + (qr & 127);
+            st_shared_v4(base + C::kOffQ + (kQ == 2 ? (qr >> 7) * C::kTileBytes : 0) + (c >> 3) * C::kHalf + at * 128 +
+                             (((c & 7) ^ (at & 7)) << 4),
+                         v[u].x, v[u].y, v[u].z, v[u].w);
+          }
         }
       }
       bool wrong = false;
@@ -600,10 +650,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       const float f0 = kQ == 2 ? 1.f : ex2(s_ml[rl].x - ref), f1 = both ? ex2(s_ml[kTile + rl].x - ref) : 0.f;
       if (!tree_ok && threadIdx.x == 0) sd_set_error(SD_DEVERR_TREE);
-      const int i = node, h = r.kvh * a.G + p - i * a.G;
-      __nv_bfloat16* out = a.out + ((static_cast<long long>(r.b) * a.R + i) * a.Hq + h) * kDim;
       float* part = a.part + (2 * static_cast<size_t>(blockIdx.x) + (r.tile0 == 0 ? 1 : 0)) * part_floats(a.rows, kDim);
       float2* part_ml = reinterpret_cast<float2*>(part + static_cast<size_t>(a.rows) * kDim);
+      auto part_o = [&](int rr, int c) { return reinterpret_cast<float4*>(part) + static_cast<size_t>(c >> 2) * a.rows + rr; };
+      auto out_of = [&](int pr) {  // packed row pr's output
+        const int i = gdiv(pr);
+        return a.out + ((static_cast<long long>(r.b) * a.R + i) * a.Hq + r.kvh * a.G + pr - i * a.G) * kDim;
+      };
       // 32 columns of the lane's row, the groups' O joined
       auto joined = [&](int c, float (&x)[32]) {
         uint32_t o[32];
@@ -619,31 +672,50 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (any_bad && live && tree_ok && copy == 0)
 #pragma unroll 1
           for (int j = 0; j < 32; ++j) {
-            const float v = bad_values(a, s_parent, bad_rows, r.b, r.kvh, prefix, i, c + j, kDim);
+            const float v = bad_values(a, s_parent, bad_rows, r.b, r.kvh, prefix, node, c + j, kDim);
 #pragma unroll
             for (int k = 0; k < 32; ++k) x[k] += k == j ? v : 0.f;
           }
       };
       if (kCopies == 1) {
+        // whole rows go out through the query tile (its products are done), a warp's own lanes
         const float inv = 1.f / total;
+        const uint32_t stage = base + C::kOffQ + (kQ == 2 ? g * C::kTileBytes : 0);
+        constexpr int kWide = kQ == 2 ? kDim : kDim / 2;  // columns a group
+        const int c0 = kQ == 2 ? 0 : g * kWide;
 #pragma unroll 1
-        for (int c = kQ == 2 ? 0 : g * (kDim / 2); c < (kQ == 2 ? kDim : (g + 1) * (kDim / 2)); c += 32) {
+        for (int c = c0; c < c0 + kWide; c += 32) {
           float x[32];
           joined(c, x);
-          if (!live) continue;
           if (!whole) {
+            if (live)
 #pragma unroll
-            for (int j = 0; j < 32; j += 4)
-              *reinterpret_cast<float4*>(part + static_cast<size_t>(row) * kDim + c + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
-          } else if (tree_ok) {
+              for (int j = 0; j < 32; j += 4) *part_o(row, c + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+          } else {
 #pragma unroll
             for (int j = 0; j < 32; j += 8)
-              *reinterpret_cast<uint4*>(out + c + j) =
-                  make_uint4(cvt_bf16x2(x[j] * inv, x[j + 1] * inv), cvt_bf16x2(x[j + 2] * inv, x[j + 3] * inv),
-                             cvt_bf16x2(x[j + 4] * inv, x[j + 5] * inv), cvt_bf16x2(x[j + 6] * inv, x[j + 7] * inv));
+              st_shared_v4(stage + (c >> 6) * C::kHalf + rl * 128 + (((((c & 63) + j) >> 3) ^ (rl & 7)) << 4),
+                           cvt_bf16x2(x[j] * inv, x[j + 1] * inv), cvt_bf16x2(x[j + 2] * inv, x[j + 3] * inv),
+                           cvt_bf16x2(x[j + 4] * inv, x[j + 5] * inv), cvt_bf16x2(x[j + 6] * inv, x[j + 7] * inv));
           }
         }
-        if (live && !whole && (kQ == 2 || g == 0)) part_ml[row] = make_float2(top, total);
+        __syncwarp();
+        if (!whole) {
+          if (live && (kQ == 2 || g == 0)) part_ml[row] = make_float2(top, total);
+        } else if (tree_ok) {
+          constexpr int kPer = kWide / 8;  // 16-byte chunks a row
+#pragma unroll 1
+          for (int x = lane; x < 32 * kPer; x += 32) {
+            const int at = (warp & 3) * 32 + x / kPer, c = c0 / 8 + x % kPer, pr = r.mb * a.rows + (kQ == 2 ? g * kTile : 0) + at;
+            if (pr >= M) break;
+            uint4 v;
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                         : "r"(stage + (c >> 3) * C::kHalf + at * 128 + (((c & 7) ^ (at & 7)) << 4))
+                         : "memory");
+            *reinterpret_cast<uint4*>(out_of(pr) + c * 8) = v;
+          }
+        }
       } else {
         // the copies' sums through the query tile (its products are done): [128 lanes][kDim / 2]
         constexpr int kC = kDim / 4;  // columns a group and round
@@ -667,7 +739,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           named_bar_sync(1, kSoft);
           for (int x = threadIdx.x; x < C::kRows * (kC / 2); x += kSoft) {
-            const int rr = x / (kC / 2), c4 = x % (kC / 2), pr = r.mb * a.rows + rr;
+            // (rows along the lanes for the parts, columns for the output)
+            const int rr = whole ? x / (kC / 2) : x % C::kRows, c4 = whole ? x % (kC / 2) : x / C::kRows, pr = r.mb * a.rows + rr;
             if (pr >= M) continue;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -676,16 +749,19 @@ __global__ void __launch_bounds__(kThreads, 1)
               const float4 y = *reinterpret_cast<const float4*>(stage + at * 2 * kC + ((c4 ^ (at & 7)) << 2));
               v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
             }
-            float2 fin;
-            joined_ml(rr, fin.x, fin.y);
-            const int d = half * 2 * kC + c4 * 4, ii = pr / a.G, hh = r.kvh * a.G + pr - ii * a.G;
+            const int d = half * 2 * kC + c4 * 4;
             if (!whole) {
-              *reinterpret_cast<float4*>(part + static_cast<size_t>(rr) * kDim + d) = v;
-              if (half == 0 && c4 == 0) part_ml[rr] = fin;
+              *part_o(rr, d) = v;
+              if (half == 0 && c4 == 0) {
+                float2 fin;
+                joined_ml(rr, fin.x, fin.y);
+                part_ml[rr] = fin;
+              }
             } else if (tree_ok) {
-              const float inv = 1.f / fin.y;
-              *reinterpret_cast<uint2*>(a.out + ((static_cast<long long>(r.b) * a.R + ii) * a.Hq + hh) * kDim + d) =
-                  make_uint2(cvt_bf16x2(v.x * inv, v.y * inv), cvt_bf16x2(v.z * inv, v.w * inv));
+              float mm, ll;
+              joined_ml(rr, mm, ll);
+              const float inv = 1.f / ll;
+              *reinterpret_cast<uint2*>(out_of(pr) + d) = make_uint2(cvt_bf16x2(v.x * inv, v.y * inv), cvt_bf16x2(v.z * inv, v.w * inv));
             }
           }
           __syncwarp();
@@ -707,78 +783,70 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// The units that a share's border cuts: border c lies between shares c and c + 1, and the
-// first one that cuts a unit joins its parts, a warp a row: the parts' maxima and sums a lane
-// each, then eight parts of the row in flight.
+// The units that several CTAs took. Border c lies between shares c - 1 and c, and the first
+// one that cuts a unit joins its parts; with so many CTAs a unit, block c - 1 the unit c - 1's.
+// A thread takes four columns of a row, rows along the lanes (as the parts lie), and eight
+// parts at once.
 template <int kDim>
-__global__ void __launch_bounds__(32 * kJoinWarps) tree_join_kernel(const __grid_constant__ TreeArgs a, int ctas) {
-  constexpr int kPer = kDim / 32, kBatch = 8;
+__global__ void __launch_bounds__(kJoin) tree_join_kernel(const __grid_constant__ TreeArgs a, int ctas) {
+  constexpr int kRowsJ = kJoin / (kDim / 4), kBatch = 8;
+  __shared__ float2 s_ml[kMaxCtas][kRowsJ];
   sd_pdl_enter();
-  const int lane = threadIdx.x & 31, c = blockIdx.x + 1, row = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, c = blockIdx.x + 1;
   Walk walk;
   const Plan plan = walk.begin<true>(a, c, ctas, lane);
   Run r;
-  if (plan.begin(c) <= 0 || !walk.next(a, r) || r.first == plan.begin(c) || plan.begin(c - 1) > r.first) return;
-  const int p = r.mb * a.rows + row;
-  if (row >= a.rows || p >= r.m * a.G) return;
-  const int n = plan.cta_of(r.first + r.tiles - 1) - c + 2;  // parts: shares c - 1 ...
+  if (!walk.next(a, r)) return;
+  int share = c - 1, n;  // the first share of the unit, its parts
+  if (plan.per > 0) {
+    share = (c - 1) * plan.per;
+    n = min(plan.per, r.tiles);
+    if (n == 1) return;
+  } else {
+    if (r.first == plan.begin(c) || plan.begin(c - 1) > r.first) return;
+    n = plan.cta_of(r.first + r.tiles - 1) - c + 2;
+  }
+  const int row0 = blockIdx.y * kRowsJ, row = row0 + threadIdx.x % kRowsJ, c4 = threadIdx.x / kRowsJ;
+  if (row0 >= a.rows || r.mb * a.rows + row0 >= r.m * a.G) return;
   const size_t pf = part_floats(a.rows, kDim);
   // (the unit begins in its first share's second part, and goes on in the others' first)
-  auto part = [&](int k) { return a.part + (2 * static_cast<size_t>(c - 1 + k) + (k == 0 ? 1 : 0)) * pf; };
-  auto ml = [&](int k) {
-    return __ldcg(reinterpret_cast<const float2*>(part(k) + static_cast<size_t>(a.rows) * kDim) + row);
-  };
+  auto part = [&](int k) { return a.part + (2 * static_cast<size_t>(share + k) + (k == 0 ? 1 : 0)) * pf; };
+  for (int x = threadIdx.x; x < n * kRowsJ; x += kJoin) {
+    const int k = x / kRowsJ, rr = x % kRowsJ;
+    s_ml[k][rr] = __ldcg(reinterpret_cast<const float2*>(part(k) + static_cast<size_t>(a.rows) * kDim) + row0 + rr);
+  }
+  __syncthreads();
+  const int p = r.mb * a.rows + row, rr = threadIdx.x % kRowsJ;
+  if (p >= r.m * a.G) return;
   float top = -INFINITY;
-  bool skip = false;
-  for (int k = lane; k < n; k += 32) {
-    const float m = ml(k).x;
-    skip |= m != m;  // its tree is not valid
+  bool skip = false;  // its tree is not valid
+  for (int k = 0; k < n; ++k) {
+    const float m = s_ml[k][rr].x;
+    skip |= m != m;
     top = fmaxf(top, m);
   }
-#pragma unroll
-  for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-  if (__any_sync(0xffffffffu, skip)) return;
+  if (skip) return;
   const float ref = top == -INFINITY ? 0.f : top;
-  float o[kPer] = {}, total = 0.f;
-  for (int k0 = 0; k0 < n; k0 += 32) {
-    float w = 0.f;
-    if (k0 + lane < n) {
-      const float2 x = ml(k0 + lane);
-      w = ex2(x.x - ref);
-      total += w * x.y;
-    }
-    for (int k1 = k0; k1 < min(n, k0 + 32); k1 += kBatch) {
-      float x[kBatch][kPer];
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float total = 0.f;
+  for (int k0 = 0; k0 < n; k0 += kBatch) {
+    float4 x[kBatch];
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const float* src = part(k1 + u) + static_cast<size_t>(row) * kDim + lane * kPer;
-        if (k1 + u < n) {
-          if (kPer == 4) {
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
-            x[u][0] = v.x, x[u][1] = v.y, x[u][kPer - 2] = v.z, x[u][kPer - 1] = v.w;
-          } else {
-            const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
-            x[u][0] = v.x, x[u][1] = v.y;
-          }
-        }
+    for (int u = 0; u < kBatch; ++u)
+      if (k0 + u < n) x[u] = __ldcg(reinterpret_cast<const float4*>(part(k0 + u)) + static_cast<size_t>(c4) * a.rows + row);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (k0 + u < n) {
+        const float2 y = s_ml[k0 + u][rr];
+        const float f = ex2(y.x - ref);
+        total = fmaf(f, y.y, total);
+        o.x = fmaf(f, x[u].x, o.x), o.y = fmaf(f, x[u].y, o.y), o.z = fmaf(f, x[u].z, o.z), o.w = fmaf(f, x[u].w, o.w);
       }
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const float f = __shfl_sync(0xffffffffu, w, (k1 + u) & 31);
-        if (k1 + u < n)
-#pragma unroll
-          for (int j = 0; j < kPer; ++j) o[j] = fmaf(f, x[u][j], o[j]);
-      }
-    }
   }
-#pragma unroll
-  for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
   const float inv = 1.f / total;
   const int i = p / a.G;
-  uint32_t* out = reinterpret_cast<uint32_t*>(
-      a.out + ((static_cast<long long>(r.b) * a.R + i) * a.Hq + r.kvh * a.G + p - i * a.G) * kDim) + lane * (kPer / 2);
-#pragma unroll
-  for (int j = 0; j < kPer / 2; ++j) out[j] = cvt_bf16x2(o[2 * j] * inv, o[2 * j + 1] * inv);
+  *reinterpret_cast<uint2*>(a.out + ((static_cast<long long>(r.b) * a.R + i) * a.Hq + r.kvh * a.G + p - i * a.G) * kDim + c4 * 4) =
+      make_uint2(cvt_bf16x2(o.x * inv, o.y * inv), cvt_bf16x2(o.z * inv, o.w * inv));
 }
 
 // ------------------------------------------------------------------ host
@@ -815,7 +883,7 @@ bool host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) {
   const long long tiles = (static_cast<long long>(cap) + kTile - 1) / kTile;
   const long long units = static_cast<long long>(B) * Hkv * ((M + p->rows - 1) / p->rows);
   if (units > 0x7fffffffll / tiles || cap > 0x7fffff00) return false;
-  p->ctas = static_cast<int>(std::min<long long>(sd_num_sms(), units * tiles));
+  p->ctas = static_cast<int>(std::min<long long>(std::min(sd_num_sms(), kMaxCtas), units * tiles));
   // one tile a unit: no share's border cuts one
   p->ws_bytes = tiles > 1 ? 2 * static_cast<size_t>(p->ctas) * part_floats(p->rows, D) * sizeof(float) : 0;
   return true;
@@ -875,6 +943,7 @@ extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const 
   a.rows = p.rows;
   const double sc = scale > 0.f ? scale : 1.0 / sqrt(static_cast<double>(D));
   a.scale_log2 = static_cast<float>(sc * 1.4426950408889634);
+  a.inv_g = 1.0f / static_cast<float>(a.G);
   CUtensorMap k, v;
   if (!make_map(&k, cache->k, cache->page, cache->n_pages * Hkv, cache->page, D) ||
       !make_map(&v, cache->v, cache->page, cache->n_pages * Hkv, cache->page, D))
@@ -887,8 +956,8 @@ extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const 
   cudaError_t e = run(k, v, a, p.ctas, st);
   if (e == cudaSuccess && p.ws_bytes > 0 && p.ctas > 1)
     e = sd_launch_pdl(D == 128 ? tree_join_kernel<128> : tree_join_kernel<64>,
-                      dim3(p.ctas - 1, (std::min<long long>(p.rows, static_cast<long long>(a.G) * R) + kJoinWarps - 1) / kJoinWarps),
-                      dim3(32 * kJoinWarps), 0, st, a, p.ctas);
+                      dim3(p.ctas - 1, static_cast<unsigned>((std::min<long long>(p.rows, static_cast<long long>(a.G) * R) * (D / 4) + kJoin - 1) / kJoin)),
+                      dim3(kJoin), 0, st, a, p.ctas);
   if (e != cudaSuccess) {
     (void)cudaGetLastError();
     return SD_ERR_CUDA;

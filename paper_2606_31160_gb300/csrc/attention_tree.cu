@@ -21,10 +21,10 @@
 // join at the end by one rule
 //     m = max m_c,  l = sum l_c 2^(m_c - m),  o = sum O_c 2^(m_c - m) / l.
 //
-// Work: one CTA an SM. Where there are many units (scene, KV head, m-block), the 128-key tiles
-// of all of them, one unit after the other, in one even share a CTA; where there are few, the
-// same number of CTAs for each unit, so that no CTA begins a second one. A unit that more than
-// one CTA takes leaves its parts in the workspace, and a second kernel joins them.
+// Work. Few units (scene, KV head, m-block): a cluster of CTAs a unit, which split its 128-key
+// tiles and join their parts through distributed shared memory. Many: one CTA an SM, the tiles
+// of all units, one unit after the other, in one even share each; a unit that a share's border
+// cuts leaves its parts in the workspace, and a second kernel joins them.
 //
 // What a row does not see does not reach it: hidden scores are replaced before the maximum,
 // and in the tiles that hold new rows, values that are no numbers are taken out of V (0 times
@@ -46,7 +46,6 @@ constexpr int kThreads = kSoft + 64;
 constexpr float kSlack = 8.f;    // log2 units that a score may pass its row's reference by
 constexpr int kJoin = 256;       // threads of the joining kernel
 constexpr int kMaxCtas = 192;    // shares
-constexpr int kApart = 4;        // tiles that a second unit in a share costs
 
 struct TreeArgs {
   const __nv_bfloat16* q;
@@ -54,8 +53,8 @@ struct TreeArgs {
   const __nv_bfloat16* v;   // (only for values that are no numbers)
   const int32_t *table, *len, *parents, *n_new;
   long long q_stride;
-  float* part;              // per CTA two parts: O [D / 4][rows][4], then (m, l) [rows][2]
-  int B, R, Hq, Hkv, G, n_pages, shift, max_pages, cap, rows;  // rows: of an m-block
+  float* part;              // even shares: per CTA two parts, O [D / 4][rows][4], then (m, l) [rows][2]
+  int B, R, Hq, Hkv, G, n_pages, shift, max_pages, cap, rows, mblocks;  // rows: of an m-block
   float scale_log2, inv_g;
 };
 
@@ -103,7 +102,6 @@ __device__ __forceinline__ bool length_error(const TreeArgs& a, int b) {
 
 struct Plan {
   int total, each, rest;  // tiles, tiles a share, shares with one more
-  int units, per;         // per > 0: so many CTAs a unit instead
   __device__ __forceinline__ int begin(int cta) const { return cta * each + min(cta, rest); }
   __device__ __forceinline__ int cta_of(int pos) const {
     const int more = rest * (each + 1);
@@ -120,39 +118,32 @@ struct Run {
 struct Walk {
   int b, unit, tile, first, left;
   Scene s;
-  // Plans the work of `ctas` CTAs and stands at the first tile of share `cta`, with its tiles
-  // to go. kJoin: at the unit that border `cta` cuts (even shares: all that follows), or at
-  // unit cta - 1. A warp; up to 32 scenes are looked at once.
-  template <bool kJoin>
+  // Cuts all tiles into even shares of `ctas` CTAs and stands at the first tile of share
+  // `cta`, with its tiles to go (kOn: with all that follow). A warp; up to 32 scenes are
+  // looked at once.
+  template <bool kOn>
   __device__ __forceinline__ Plan begin(const TreeArgs& a, int cta, int ctas, int lane) {
     Scene mine = {};
     if (lane < a.B) mine = scene_of(a, lane);
-    int n = mine.tiles * mine.units, u = mine.units, most = mine.tiles;
+    int n = mine.tiles * mine.units;
     for (int b0 = lane + 32; b0 < a.B; b0 += 32) {
       const Scene x = scene_of(a, b0);
       n += x.tiles * x.units;
-      u += x.units;
-      most = max(most, x.tiles);
     }
     Plan p;
     p.total = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(n)));
-    p.units = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(u)));
-    most = __reduce_max_sync(0xffffffffu, most);
     p.each = p.total / ctas;
     p.rest = p.total - p.each * ctas;
-    p.per = p.units > 0 && p.units <= ctas / 2 ? ctas / p.units : 0;
-    if (p.per > 0 && (most + p.per - 1) / p.per > p.each + 1 + kApart) p.per = 0;
-    const int share_unit = p.per > 0 ? (kJoin ? cta - 1 : cta / p.per) : 0;
-    const int pos = p.per > 0 ? share_unit : p.begin(cta);
-    left = 0;
-    if (pos >= (p.per > 0 ? p.units : p.total)) return p;
+    const int pos = p.begin(cta);
+    left = (kOn ? p.total : p.begin(cta + 1)) - pos;
+    if (left <= 0) return p;
     int before = 0;
     for (int b0 = 0; b0 < a.B; b0 += 32) {
       if (b0 > 0) {
         mine = Scene{};
         if (b0 + lane < a.B) mine = scene_of(a, b0 + lane);
       }
-      const int own = p.per > 0 ? mine.units : mine.tiles * mine.units;
+      const int own = mine.tiles * mine.units;
       int upto = own;
 #pragma unroll
       for (int x = 1; x < 32; x <<= 1) {
@@ -168,23 +159,28 @@ struct Walk {
         s.tiles = __shfl_sync(0xffffffffu, mine.tiles, at);
         s.units = __shfl_sync(0xffffffffu, mine.units, at);
         const int in = pos - before - __shfl_sync(0xffffffffu, upto - own, at);
-        if (p.per > 0) {
-          const int part = kJoin ? 0 : cta - share_unit * p.per, each = s.tiles / p.per, rest = s.tiles - each * p.per;
-          unit = in;
-          tile = part * each + min(part, rest);
-          first = 0;
-          left = kJoin ? s.tiles : each + (part < rest ? 1 : 0);
-        } else {
-          unit = in / s.tiles;
-          tile = in - unit * s.tiles;
-          first = pos - tile;
-          left = (kJoin ? p.total : p.begin(cta + 1)) - pos;
-        }
+        unit = in / s.tiles;
+        tile = in - unit * s.tiles;
+        first = pos - tile;
         return p;
       }
       before += __shfl_sync(0xffffffffu, upto, 31);
     }
-    return p;  // (only if a length changed under the kernel)
+    left = 0;  // (only if a length changed under the kernel)
+    return p;
+  }
+  // Stands at the tiles that CTA `rank` of a cluster of `cs` takes of its unit. kvh, mb: the
+  // unit's place in scene b
+  __device__ __forceinline__ void begin_part(const TreeArgs& a, int scene, int kvh, int mb, int rank, int cs) {
+    b = scene;
+    s = scene_of(a, b);
+    const int mblocks = s.units / a.Hkv;
+    if (mb >= mblocks) s.tiles = 0;
+    unit = kvh * mblocks + mb;
+    const int each = s.tiles / cs, rest = s.tiles - each * cs;
+    tile = rank * each + min(rank, rest);
+    first = 0;
+    left = each + (rank < rest ? 1 : 0);
   }
   __device__ __forceinline__ bool next(const TreeArgs& a, Run& r) {
     if (left <= 0) return false;
@@ -238,6 +234,17 @@ struct Cfg {
 };
 __host__ __device__ constexpr size_t part_floats(int rows, int D) { return static_cast<size_t>(rows) * (D + 2); }
 
+// A part in a cluster's shared memory: chunk c4 of four columns of a row, the chunks of a row
+// in an order of its own (rows along the lanes to write, chunks to read), and its (m, l).
+template <int kDim>
+__device__ __forceinline__ uint32_t cluster_o(int row, int c4) {
+  return static_cast<uint32_t>(row * (kDim / 4) + (c4 ^ (row & (kDim / 4 - 1)))) * 16;
+}
+template <int kDim>
+__device__ __forceinline__ uint32_t cluster_ml(int rows, int row) {
+  return static_cast<uint32_t>(rows * kDim * 4 + row * 8);
+}
+
 __device__ __forceinline__ bool bad_pair(uint32_t w) { return __vcmpeq2(w & 0x7f807f80u, 0x7f807f80u) != 0; }
 
 // Sum of the values that are no numbers at column d of the bad rows that row i of scene b sees.
@@ -256,7 +263,8 @@ __device__ __noinline__ float bad_values(const TreeArgs& a, const int16_t* paren
 }
 
 // ------------------------------------------------------------------ kernel
-template <int kDim, int kCopies, int kQ>
+// kCluster: grid (cluster size, KV heads x m-blocks, scenes), else (shares).
+template <int kDim, int kCopies, int kQ, bool kCluster>
 __global__ void __launch_bounds__(kThreads, 1)
     tree_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                           const __grid_constant__ TreeArgs a) {
@@ -311,7 +319,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   Walk walk;
-  walk.begin<false>(a, blockIdx.x, gridDim.x, lane);
+  if (kCluster) walk.begin_part(a, blockIdx.z, blockIdx.y / a.mblocks, blockIdx.y % a.mblocks, blockIdx.x, gridDim.x);
+  else walk.begin<false>(a, blockIdx.x, gridDim.x, lane);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -322,8 +331,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   Run r;
   if (warp == kProducer) {
     // -------------------------------------------------------------- producer
-    if (blockIdx.x == 0)
-      for (int b = lane; b < a.B; b += 32)
+    if (kCluster ? blockIdx.x == 0 && blockIdx.y == 0 : blockIdx.x == 0)
+      for (int b = kCluster ? blockIdx.z + 32 * lane : lane; b < (kCluster ? blockIdx.z + 1 : a.B); b += 32)
         if (length_error(a, b)) sd_set_error(SD_DEVERR_LENGTH);
     const uint64_t evict_first = l2_evict_first_policy();
     const int page = 1 << a.shift, pages = kTile >> a.shift;  // pages a tile
@@ -651,8 +660,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float f0 = kQ == 2 ? 1.f : ex2(s_ml[rl].x - ref), f1 = both ? ex2(s_ml[kTile + rl].x - ref) : 0.f;
       if (!tree_ok && threadIdx.x == 0) sd_set_error(SD_DEVERR_TREE);
       float* part = a.part + (2 * static_cast<size_t>(blockIdx.x) + (r.tile0 == 0 ? 1 : 0)) * part_floats(a.rows, kDim);
-      float2* part_ml = reinterpret_cast<float2*>(part + static_cast<size_t>(a.rows) * kDim);
-      auto part_o = [&](int rr, int c) { return reinterpret_cast<float4*>(part) + static_cast<size_t>(c >> 2) * a.rows + rr; };
+      // (in a cluster: rows in this CTA's K and V slots, whose products are done)
+      auto put_o = [&](int rr, int c, const float4& v) {
+        if (kCluster) *reinterpret_cast<float4*>(smem + cluster_o<kDim>(rr, c >> 2)) = v;
+        else *(reinterpret_cast<float4*>(part) + static_cast<size_t>(c >> 2) * a.rows + rr) = v;
+      };
+      auto put_ml = [&](int rr, const float2& v) {
+        if (kCluster) *reinterpret_cast<float2*>(smem + cluster_ml<kDim>(a.rows, rr)) = v;
+        else *(reinterpret_cast<float2*>(part + static_cast<size_t>(a.rows) * kDim) + rr) = v;
+      };
       auto out_of = [&](int pr) {  // packed row pr's output
         const int i = gdiv(pr);
         return a.out + ((static_cast<long long>(r.b) * a.R + i) * a.Hq + r.kvh * a.G + pr - i * a.G) * kDim;
@@ -690,7 +706,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!whole) {
             if (live)
 #pragma unroll
-              for (int j = 0; j < 32; j += 4) *part_o(row, c + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+              for (int j = 0; j < 32; j += 4) put_o(row, c + j, make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]));
           } else {
 #pragma unroll
             for (int j = 0; j < 32; j += 8)
@@ -701,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __syncwarp();
         if (!whole) {
-          if (live && (kQ == 2 || g == 0)) part_ml[row] = make_float2(top, total);
+          if (live && (kQ == 2 || g == 0)) put_ml(row, make_float2(top, total));
         } else if (tree_ok) {
           constexpr int kPer = kWide / 8;  // 16-byte chunks a row
 #pragma unroll 1
@@ -751,11 +767,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             const int d = half * 2 * kC + c4 * 4;
             if (!whole) {
-              *part_o(rr, d) = v;
+              put_o(rr, d, v);
               if (half == 0 && c4 == 0) {
                 float2 fin;
                 joined_ml(rr, fin.x, fin.y);
-                part_ml[rr] = fin;
+                put_ml(rr, fin);
               }
             } else if (tree_ok) {
               float mm, ll;
@@ -781,10 +797,67 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
+  if (kCluster) {
+    // ---- the cluster's parts: a CTA joins its share of the rows, a thread four columns of one
+    const int cs = gridDim.x, n = min(cs, walk.s.tiles);  // CTAs that had tiles: the first n
+    if (n <= 1) return;                                    // (the same for the whole cluster)
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    cluster_wait();
+    const int M = walk.s.m * a.G, mb = blockIdx.y % a.mblocks, rows = min(a.rows, M - mb * a.rows), each = (rows + cs - 1) / cs;
+    const int row0 = blockIdx.x * each, mine = min(each, rows - row0);
+    for (int x = threadIdx.x; x < mine * (kDim / 4); x += kThreads) {
+      const int row = row0 + x / (kDim / 4), c4 = x % (kDim / 4);
+      const uint32_t at = base + cluster_o<kDim>(row, c4), at_ml = base + cluster_ml<kDim>(a.rows, row);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      float top = -INFINITY, total = 0.f;
+      bool skip = false;
+      constexpr int kBatch = 4;
+      for (int k0 = 0; k0 < n; k0 += kBatch) {
+        float4 v[kBatch];
+        float2 ml[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          ml[u] = make_float2(-INFINITY, 0.f);
+          v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (k0 + u < n) {
+            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(ml[u].x), "=f"(ml[u].y) : "r"(cluster_map(at_ml, k0 + u)));
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(v[u].x), "=f"(v[u].y), "=f"(v[u].z), "=f"(v[u].w)
+                         : "r"(cluster_map(at, k0 + u)));
+          }
+        }
+        float now = top;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          skip |= ml[u].x != ml[u].x;  // its tree is not valid
+          now = fmaxf(now, ml[u].x);
+        }
+        const float ref = now == -INFINITY ? 0.f : now, f0 = ex2(top - ref);
+        o.x *= f0, o.y *= f0, o.z *= f0, o.w *= f0, total *= f0;
+        top = now;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const float f = ex2(ml[u].x - ref);
+          total = fmaf(f, ml[u].y, total);
+          o.x = fmaf(f, v[u].x, o.x), o.y = fmaf(f, v[u].y, o.y), o.z = fmaf(f, v[u].z, o.z), o.w = fmaf(f, v[u].w, o.w);
+        }
+      }
+      if (!skip) {
+        const float inv = 1.f / total;
+        const int pr = mb * a.rows + row, i = pr / a.G;
+        *reinterpret_cast<uint2*>(a.out + ((static_cast<long long>(blockIdx.z) * a.R + i) * a.Hq + (blockIdx.y / a.mblocks) * a.G + pr - i * a.G) * kDim +
+                                  c4 * 4) = make_uint2(cvt_bf16x2(o.x * inv, o.y * inv), cvt_bf16x2(o.z * inv, o.w * inv));
+      }
+    }
+    __syncwarp();
+    cluster_arrive_relaxed();  // (its reads are done; nobody's memory goes before)
+    cluster_wait();
+  }
 }
 
-// The units that several CTAs took. Border c lies between shares c - 1 and c, and the first
-// one that cuts a unit joins its parts; with so many CTAs a unit, block c - 1 the unit c - 1's.
+// The units that a share's border cuts: border c lies between shares c - 1 and c, and the
+// first one that cuts a unit joins its parts.
 // A thread takes four columns of a row, rows along the lanes (as the parts lie), and eight
 // parts at once.
 template <int kDim>
@@ -797,15 +870,8 @@ __global__ void __launch_bounds__(kJoin) tree_join_kernel(const __grid_constant_
   const Plan plan = walk.begin<true>(a, c, ctas, lane);
   Run r;
   if (!walk.next(a, r)) return;
-  int share = c - 1, n;  // the first share of the unit, its parts
-  if (plan.per > 0) {
-    share = (c - 1) * plan.per;
-    n = min(plan.per, r.tiles);
-    if (n == 1) return;
-  } else {
-    if (r.first == plan.begin(c) || plan.begin(c - 1) > r.first) return;
-    n = plan.cta_of(r.first + r.tiles - 1) - c + 2;
-  }
+  if (r.first == plan.begin(c) || plan.begin(c - 1) > r.first) return;
+  const int share = c - 1, n = plan.cta_of(r.first + r.tiles - 1) - share + 1;  // its first share, its parts
   const int row0 = blockIdx.y * kRowsJ, row = row0 + threadIdx.x % kRowsJ, c4 = threadIdx.x / kRowsJ;
   if (row0 >= a.rows || r.mb * a.rows + row0 >= r.m * a.G) return;
   const size_t pf = part_floats(a.rows, kDim);
@@ -850,57 +916,122 @@ __global__ void __launch_bounds__(kJoin) tree_join_kernel(const __grid_constant_
 }
 
 // ------------------------------------------------------------------ host
-template <int kDim, int kCopies, int kQ>
-bool prepare() {
-  return cudaFuncSetAttribute(tree_attention_kernel<kDim, kCopies, kQ>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              Cfg<kDim, kCopies, kQ>::kSmem) == cudaSuccess;
-}
-// The kernels' shared memory, once per device.
-bool device_ready() {
-  static std::once_flag once[64];
-  static bool ok[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
-    (void)cudaGetLastError();
-    return false;
-  }
-  std::call_once(once[dev], [dev] {
-    ok[dev] = prepare<64, 4, 1>() && prepare<64, 2, 1>() && prepare<64, 1, 1>() && prepare<64, 1, 2>() &&
-              prepare<128, 4, 1>() && prepare<128, 2, 1>() && prepare<128, 1, 1>() && prepare<128, 1, 2>();
-    if (!ok[dev]) (void)cudaGetLastError();
-  });
-  return ok[dev];
+constexpr int kSizes[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16};  // CTAs a cluster
+constexpr int kNumSizes = sizeof(kSizes) / sizeof(int);
+
+cudaLaunchConfig_t config(dim3 grid, int smem, int cs, cudaStream_t st, cudaLaunchAttribute (&attr)[2]) {
+  cudaLaunchConfig_t cfg = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cs;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = cs > 0 ? 2 : 1;
+  return cfg;
 }
 
-struct HostPlan {
-  int rows, ctas;   // packed rows of an m-block
-  size_t ws_bytes;
-};
-// false: too many tiles to count
-bool host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) {
-  const long long M = static_cast<long long>(Hq / Hkv) * R;
-  p->rows = M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
-  const long long tiles = (static_cast<long long>(cap) + kTile - 1) / kTile;
-  const long long units = static_cast<long long>(B) * Hkv * ((M + p->rows - 1) / p->rows);
-  if (units > 0x7fffffffll / tiles || cap > 0x7fffff00) return false;
-  p->ctas = static_cast<int>(std::min<long long>(std::min(sd_num_sms(), kMaxCtas), units * tiles));
-  // one tile a unit: no share's border cuts one
-  p->ws_bytes = tiles > 1 ? 2 * static_cast<size_t>(p->ctas) * part_floats(p->rows, D) * sizeof(float) : 0;
+// The kernel of a shape: even shares over `grid` CTAs (cs = 0) or clusters of cs.
+template <int kDim, int kCopies, int kQ>
+cudaError_t launch(const CUtensorMap& k, const CUtensorMap& v, const TreeArgs& a, dim3 grid, int cs, cudaStream_t st) {
+  cudaLaunchAttribute attr[2];
+  const cudaLaunchConfig_t cfg = config(grid, Cfg<kDim, kCopies, kQ>::kSmem, cs, st, attr);
+  return cs > 0 ? cudaLaunchKernelEx(&cfg, tree_attention_kernel<kDim, kCopies, kQ, true>, k, v, a)
+                : cudaLaunchKernelEx(&cfg, tree_attention_kernel<kDim, kCopies, kQ, false>, k, v, a);
+}
+
+template <int kDim, int kCopies, int kQ>
+bool prepare(int* active) {
+  const void* even = reinterpret_cast<const void*>(tree_attention_kernel<kDim, kCopies, kQ, false>);
+  const void* cluster = reinterpret_cast<const void*>(tree_attention_kernel<kDim, kCopies, kQ, true>);
+  constexpr int smem = Cfg<kDim, kCopies, kQ>::kSmem;
+  if (cudaFuncSetAttribute(even, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+      cudaFuncSetAttribute(cluster, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+      cudaFuncSetAttribute(cluster, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+    return false;
+  for (int i = 0; i < kNumSizes; ++i) {
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg = config(dim3(kSizes[i], 1, 1), smem, kSizes[i], nullptr, attr);
+    attr[0] = attr[1];  // (the occupancy query takes the cluster alone)
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&active[i], cluster, &cfg) != cudaSuccess) {
+      (void)cudaGetLastError();
+      active[i] = 0;
+    }
+  }
   return true;
 }
 
-template <int kDim, int kCopies, int kQ>
-cudaError_t launch(const CUtensorMap& k, const CUtensorMap& v, const TreeArgs& a, int ctas, cudaStream_t st) {
-  return sd_launch_pdl(tree_attention_kernel<kDim, kCopies, kQ>, dim3(ctas), dim3(kThreads), Cfg<kDim, kCopies, kQ>::kSmem, st,
-                       k, v, a);
+// Per device, once: the kernels' shared memory, and the clusters of each size that fit at once.
+struct DevState {
+  std::once_flag once;
+  bool ok = false;
+  int active[2][4][kNumSizes] = {};  // [head dim 64, 128][copies 4, 2, 1, two row tiles]
+};
+DevState* state() {
+  static DevState states[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+    (void)cudaGetLastError();
+    return nullptr;
+  }
+  DevState& s = states[dev];
+  std::call_once(s.once, [&s] {
+    s.ok = prepare<64, 4, 1>(s.active[0][0]) && prepare<64, 2, 1>(s.active[0][1]) && prepare<64, 1, 1>(s.active[0][2]) &&
+           prepare<64, 1, 2>(s.active[0][3]) && prepare<128, 4, 1>(s.active[1][0]) && prepare<128, 2, 1>(s.active[1][1]) &&
+           prepare<128, 1, 1>(s.active[1][2]) && prepare<128, 1, 2>(s.active[1][3]);
+    if (!s.ok) (void)cudaGetLastError();
+  });
+  return s.ok ? &s : nullptr;
+}
+
+struct HostPlan {
+  int variant, rows, mblocks;  // copies 4, 2, 1, two row tiles; packed rows of an m-block
+  int cs, ctas;                // CTAs a cluster; 0: even shares over ctas
+  size_t ws_bytes;
+};
+
+sd_status host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) {
+  const long long M = static_cast<long long>(Hq / Hkv) * R, tiles = (static_cast<long long>(cap) + kTile - 1) / kTile;
+  if (cap > 0x7fffff00) return SD_ERR_UNSUPPORTED;
+  DevState* dev = state();
+  if (!dev) return SD_ERR_CUDA;
+  p->variant = M <= 32 ? 0 : M <= 64 ? 1 : M <= 128 ? 2 : 3;
+  p->rows = 32 << p->variant;
+  const long long blocks = (M + p->rows - 1) / p->rows, units = blocks * B * Hkv;
+  if (units > 0x7fffffffll / tiles) return SD_ERR_UNSUPPORTED;
+  p->mblocks = static_cast<int>(blocks);
+  p->ctas = static_cast<int>(std::min<long long>(std::min(sd_num_sms(), kMaxCtas), units * tiles));
+  // in tiles: waves x (tiles a CTA + a fixed cost), or all tiles over all CTAs, the second
+  // units' costs and the joining kernel's
+  const int* active = dev->active[D == 128][p->variant];
+  double best = static_cast<double>(tiles) * units / p->ctas + 4.0 * std::min<long long>(units, p->ctas) / p->ctas + (tiles > 1 ? 6.0 : 0.0);
+  p->cs = 0;
+  if (blocks * Hkv <= 65535)
+    for (int i = 0; i < kNumSizes; ++i) {
+      const int cs = kSizes[i];
+      if (active[i] <= 0 || cs > tiles) continue;
+      const long long waves = (units + active[i] - 1) / active[i];
+      const double cost = static_cast<double>(waves) * ((tiles + cs - 1) / cs + (waves > 1 ? 4.0 : 0.0));
+      if (cost < best) best = cost, p->cs = cs;
+    }
+  // one tile a unit: no share's border cuts one
+  p->ws_bytes = p->cs == 0 && tiles > 1 ? 2 * static_cast<size_t>(p->ctas) * part_floats(p->rows, D) * sizeof(float) : 0;
+  return SD_OK;
 }
 
 }  // namespace
 
 extern "C" size_t sd_tree_attention_workspace(int B, int R, int Hq, int Hkv, int D, int capacity) {
-  if (B <= 0 || R <= 0 || R > kMaxRows || Hkv <= 0 || Hq <= 0 || Hq % Hkv || (D != 64 && D != 128) || capacity <= 0) return 0;
-  HostPlan p;
-  return host_plan(B, R, Hq, Hkv, D, capacity, &p) ? p.ws_bytes : 0;
+  if (B <= 0 || R <= 0 || R > kMaxRows || Hkv <= 0 || Hq <= 0 || Hq % Hkv || Hq / Hkv > 4095 || (D != 64 && D != 128) || capacity <= 0)
+    return 0;
+  HostPlan p = {};
+  return host_plan(B, R, Hq, Hkv, D, capacity, &p) == SD_OK ? p.ws_bytes : 0;
 }
 
 extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const sd_paged_cache* cache,
@@ -917,10 +1048,10 @@ extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const 
   if (!q || !out || !sd_aligned16(q) || !sd_aligned16(out)) return SD_ERR_INVALID_ARG;
   if (workspace && !sd_aligned16(workspace)) return SD_ERR_INVALID_ARG;
   const int cap = cache->max_pages * cache->page;
-  HostPlan p;
-  if (!host_plan(B, R, Hq, Hkv, D, cap, &p)) return SD_ERR_UNSUPPORTED;
+  HostPlan p = {};
+  const sd_status planned = host_plan(B, R, Hq, Hkv, D, cap, &p);
+  if (planned != SD_OK) return planned;
   if (p.ws_bytes > 0 && (!workspace || ws_bytes < p.ws_bytes)) return SD_ERR_WORKSPACE;
-  if (!device_ready()) return SD_ERR_CUDA;
   TreeArgs a = {};
   a.q = static_cast<const __nv_bfloat16*>(q);
   a.out = static_cast<__nv_bfloat16*>(out);
@@ -941,6 +1072,7 @@ extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const 
   a.max_pages = cache->max_pages;
   a.cap = cap;
   a.rows = p.rows;
+  a.mblocks = p.mblocks;
   const double sc = scale > 0.f ? scale : 1.0 / sqrt(static_cast<double>(D));
   a.scale_log2 = static_cast<float>(sc * 1.4426950408889634);
   a.inv_g = 1.0f / static_cast<float>(a.G);
@@ -949,15 +1081,16 @@ extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const 
       !make_map(&v, cache->v, cache->page, cache->n_pages * Hkv, cache->page, D))
     return SD_ERR_CUDA;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const auto run = D == 128 ? (p.rows == 32 ? launch<128, 4, 1> : p.rows == 64 ? launch<128, 2, 1>
-                               : p.rows == 128 ? launch<128, 1, 1> : launch<128, 1, 2>)
-                            : (p.rows == 32 ? launch<64, 4, 1> : p.rows == 64 ? launch<64, 2, 1>
-                               : p.rows == 128 ? launch<64, 1, 1> : launch<64, 1, 2>);
-  cudaError_t e = run(k, v, a, p.ctas, st);
-  if (e == cudaSuccess && p.ws_bytes > 0 && p.ctas > 1)
+  const auto run = D == 128 ? (p.variant == 0 ? launch<128, 4, 1> : p.variant == 1 ? launch<128, 2, 1>
+                               : p.variant == 2 ? launch<128, 1, 1> : launch<128, 1, 2>)
+                            : (p.variant == 0 ? launch<64, 4, 1> : p.variant == 1 ? launch<64, 2, 1>
+                               : p.variant == 2 ? launch<64, 1, 1> : launch<64, 1, 2>);
+  cudaError_t e = run(k, v, a, p.cs > 0 ? dim3(p.cs, Hkv * p.mblocks, B) : dim3(p.ctas), p.cs, st);
+  if (e == cudaSuccess && p.ws_bytes > 0 && p.ctas > 1) {
+    const long long rows = std::min<long long>(p.rows, static_cast<long long>(a.G) * R);
     e = sd_launch_pdl(D == 128 ? tree_join_kernel<128> : tree_join_kernel<64>,
-                      dim3(p.ctas - 1, static_cast<unsigned>((std::min<long long>(p.rows, static_cast<long long>(a.G) * R) * (D / 4) + kJoin - 1) / kJoin)),
-                      dim3(kJoin), 0, st, a, p.ctas);
+                      dim3(p.ctas - 1, static_cast<unsigned>((rows * (D / 4) + kJoin - 1) / kJoin)), dim3(kJoin), 0, st, a, p.ctas);
+  }
   if (e != cudaSuccess) {
     (void)cudaGetLastError();
     return SD_ERR_CUDA;

@@ -6,9 +6,9 @@
 // 256 of them (an m-block):
 //     S[128 rows][128 keys] = Q K^T        (both from shared memory, K-major)
 //     O[128 rows][D]       += P V          (P from tensor memory, V MN-major)
-// with one running maximum and sum a row. A row's maximum moves only when a score passes it
-// by more than 2^8 (O is then scaled in place, seldom after the first tile): weights stay
-// below 2^8 and sums far inside fp32. P is bf16, and the sum is taken over the rounded
+// with one running reference and sum a row. The reference is the maximum of the row's first
+// tile and moves only when a score passes it by more than 64 (log2 units; O is then scaled in
+// place): weights stay below 2^64 and sums far inside fp32. P is bf16, and the sum is taken over the rounded
 // weights, so that they add up to 1 whatever their rounding.
 //
 // Two softmax groups of four warps, each with an S | P buffer and an O accumulator of its
@@ -41,9 +41,10 @@ namespace {
 constexpr int kMaxRows = 256;    // rows of a tree
 constexpr int kTile = 128;       // keys a tile
 constexpr int kSoft = 256;       // softmax threads
-constexpr int kProducer = 8, kProduct = 9;  // warps
-constexpr int kThreads = kSoft + 64;
-constexpr float kSlack = 8.f;    // log2 units that a score may pass its row's reference by
+constexpr int kProducer = 8, kProduct = 9, kCleaner = 10;  // warps; two of the last
+constexpr int kClean = 64;       // its threads
+constexpr int kThreads = kSoft + 64 + kClean;
+constexpr float kSlack = 64.f;   // log2 units that a score may pass its row's reference by
 constexpr int kJoin = 256;       // threads of the joining kernel
 constexpr int kMaxCtas = 192;    // shares
 
@@ -226,7 +227,7 @@ struct Cfg {
   static constexpr int kOffParent = kOffQ + kQ * kTileBytes;     // [256] int16
   static constexpr int kOffMl = kOffParent + kMaxRows * 2;       // [2][128] float2
   static constexpr int kOffBar = kOffMl + 2 * kTile * 8;
-  static constexpr int kBars = 2 * (kKSlots + kVSlots) + 7;
+  static constexpr int kBars = 2 * (kKSlots + kVSlots) + 11;
   static constexpr int kOffMisc = kOffBar + kBars * 8;           // tensor memory, bad pages, [8] rows with bad values
   static constexpr int kSmem = kOffMisc + 48;
   static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -285,6 +286,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto PFULL = [&](int g) { return bar(2 * (kKS + kVS) + 2 + g); };
   auto PVDONE = [&](int g) { return bar(2 * (kKS + kVS) + 4 + g); };
   const uint32_t QFULL = bar(2 * (kKS + kVS) + 6);  // a run's query tile, and O may be written
+  // tiles with new rows, one after the other: the scores of the j-th are under way (so that its
+  // values may be waited for), and its values are all numbers
+  auto VTOLD = [&](int j) { return bar(2 * (kKS + kVS) + 7 + (j & 1)); };
+  auto VCLEAN = [&](int j) { return bar(2 * (kKS + kVS) + 9 + (j & 1)); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
   volatile uint32_t* bad_page = reinterpret_cast<uint32_t*>(smem + C::kOffMisc + 4);  // bit: a run's number mod 32
   uint32_t* bad_rows = reinterpret_cast<uint32_t*>(smem + C::kOffMisc + 8);           // [8]
@@ -307,6 +312,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(PVDONE(g), 1);
     }
     mbar_init(QFULL, 1);
+    for (int j = 0; j < 2; ++j) {
+      mbar_init(VTOLD(j), 1);
+      mbar_init(VCLEAN(j), kClean / 32);
+    }
     *const_cast<uint32_t*>(bad_page) = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -328,6 +337,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = *tmem_slot;
   const uint32_t tmem_o = tmem + 256;  // S | P of group g at column 128 g, O at 256 + kDim g
 
+  // whether tile t of a run holds new rows (or rows behind the last key)
+  auto new_rows = [](const Run& x, int t) { return (x.tile0 + t + 1) * kTile > x.n_keys - x.m; };
   Run r;
   if (warp == kProducer) {
     // -------------------------------------------------------------- producer
@@ -376,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr uint32_t kIdescS = umma_idesc(128, kTile, 0, 0), kIdescO = umma_idesc(128, kDim, 0, 1);
     const uint64_t dK = umma_desc(base, 16, 1024), dV = umma_desc(base + C::kOffV, C::kHalf, 1024);
     const uint64_t dQ = umma_desc(base + C::kOffQ, 16, 1024);
-    int n0 = 0, n1 = 0, T0 = 0, run = 0;  // n0, n1: products of the groups so far
+    int n0 = 0, n1 = 0, T0 = 0, run = 0, told = 0, cleaned = 0;  // n0, n1: products of the groups so far
     while (walk.next(a, r)) {
       // item x: group x mod 2, of tile x / 2 (two row tiles) or x. The first group's wait for a
       // tile stands for the second's.
@@ -400,6 +411,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           umma_commit(FREEK(ks));
         }
         __syncwarp();
+        if ((kQ == 1 || g == 0) && new_rows(r, tile_of(x) - T0)) {
+          if (lane == 0) mbar_arrive(VTOLD(told));
+          ++told;
+        }
       };
       mbar_wait(QFULL, run & 1);
       for (int x = 0; x < min(2, items); ++x) {
@@ -408,7 +423,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       for (int x = 0; x < items; ++x) {
         const int g = x & 1, T = tile_of(x), vs = T % kVS, n = g ? n1 : n0;
-        if (kQ == 1 || g == 0) mbar_wait(FULLV(vs), (T / kVS) & 1);
+        if (kQ == 1 || g == 0) {
+          mbar_wait(FULLV(vs), (T / kVS) & 1);
+          if (new_rows(r, T - T0)) {
+            mbar_wait(VCLEAN(cleaned), (cleaned >> 1) & 1);
+            ++cleaned;
+          }
+        }
         mbar_wait(PFULL(g), n & 1);
         tc_fence_after();
         if (elect_one()) {
@@ -431,6 +452,53 @@ __global__ void __launch_bounds__(kThreads, 1)
       T0 += r.n_tiles;
       ++run;
     }
+  } else if (warp >= kCleaner) {
+    // -------------------------------------------------------------- values of the last tiles
+    // V rows behind the last key become 0 (whatever they hold), and so do values of new rows
+    // that are no numbers: 0 times them would be NaN
+    const int th = threadIdx.x - 32 * kCleaner;
+    int T0 = 0, cleaned = 0;
+    while (walk.next(a, r)) {
+      const int prefix = r.n_keys - r.m;
+      for (int t = 0; t < r.n_tiles; ++t) {
+        if (!new_rows(r, t)) continue;
+        const int T = T0 + t, key0 = (r.tile0 + t) * kTile;
+        mbar_wait(VTOLD(cleaned), (cleaned >> 1) & 1);
+        mbar_wait(FULLV(T % kVS), (T / kVS) & 1);
+        const uint32_t tile = base + C::kOffV + (T % kVS) * C::kTileBytes;
+#pragma unroll 1
+        for (int row = max(0, prefix - key0) + th / 8; row < kTile; row += kClean / 8) {
+          const int key = key0 + row;
+          bool bad = false;
+#pragma unroll
+          for (int h = 0; h < kDim / 64; ++h) {
+            const uint32_t at = tile + h * C::kHalf + row * 128 + ((th & 7) << 4);
+            if (key >= r.n_keys) {
+              st_shared_v4(at, 0u, 0u, 0u, 0u);
+              continue;
+            }
+            uint32_t w[4];
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+            if (bad_pair(w[0]) || bad_pair(w[1]) || bad_pair(w[2]) || bad_pair(w[3])) {
+              bad = true;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
+                if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0x0000ffffu;
+              }
+              st_shared_v4(at, w[0], w[1], w[2], w[3]);
+            }
+          }
+          if (bad) atomicOr(&bad_rows[(key - prefix) >> 5], 1u << ((key - prefix) & 31));
+        }
+        __syncwarp();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(VCLEAN(cleaned));
+        ++cleaned;
+      }
+      T0 += r.n_tiles;
+    }
   } else {
     // -------------------------------------------------------------- softmax
     const int g = warp >> 2, rl = threadIdx.x & 127;      // lane of the 128-row tile
@@ -439,13 +507,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t ts = tmem + 128 * g + lane_off, to = tmem_o + lane_off;
     const float sl = a.scale_log2;
     constexpr int kWords = C::kCols / 32;
-    int n = 0, T0 = 0, run = 0;
+    int n = 0, run = 0;
     while (walk.next(a, r)) {
       const int prefix = r.n_keys - r.m, M = r.m * a.G, p = r.mb * a.rows + row;
       const bool live = p < M;
       auto gdiv = [&](int x) { return __float2int_rz((static_cast<float>(x) + 0.5f) * a.inv_g); };  // exact below 2^21
       const int node = live ? gdiv(p) : 0;
-      const bool masked_run = (r.tile0 + r.n_tiles) * kTile > prefix;
+      const bool masked_run = new_rows(r, r.n_tiles - 1);
       // ---- the packed queries; the tree where the run reaches the new rows
       constexpr int kChunks = kQ * C::kRows * (kDim / 8) / kSoft, kBatch = kChunks < 8 ? kChunks : 8;  // a thread's
 #pragma unroll 1
@@ -488,8 +556,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       // ---- tiles
       float m_ref = -INFINITY, l = 0.f;
       for (int t = kQ == 1 ? g : 0; t < r.n_tiles; t += 3 - kQ, ++n) {
-        const int T = T0 + t, key0 = (r.tile0 + t) * kTile;
-        const bool masked = key0 + kTile > prefix;
+        const int key0 = (r.tile0 + t) * kTile;
+        const bool masked = new_rows(r, t);
         uint32_t see[kWords];
         if (masked) {
           const int c0 = key0 + copy * C::kCols;  // the lane's first key
@@ -583,48 +651,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int c = 1; c < kCopies; ++c) tmem_store(ts + (copy ^ c) * (C::kCols / 2), none);
         }
-        if (masked) {
-          // V rows behind the last key become 0 (whatever they hold), and so do values of new
-          // rows that are no numbers
-          mbar_wait(FULLV(T % kVS), (T / kVS) & 1);
-          const int kk = kQ == 1 ? rl : 64 * g + rl, key = key0 + kk;
-          const uint32_t vrow = base + C::kOffV + (T % kVS) * C::kTileBytes + kk * 128;
-          if ((kQ == 1 || rl < 64) && key >= prefix) {
-            bool bad = false;
-#pragma unroll
-            for (int h = 0; h < kDim / 64; ++h)
-#pragma unroll
-              for (int c = 0; c < 8; ++c) {
-                const uint32_t at = vrow + h * C::kHalf + ((c ^ (kk & 7)) << 4);
-                if (key >= r.n_keys) {
-                  st_shared_v4(at, 0u, 0u, 0u, 0u);
-                } else {
-                  uint32_t w[4];
-                  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
-                  if (bad_pair(w[0]) || bad_pair(w[1]) || bad_pair(w[2]) || bad_pair(w[3])) {
-                    bad = true;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                      if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
-                      if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0x0000ffffu;
-                    }
-                    st_shared_v4(at, w[0], w[1], w[2], w[3]);
-                  }
-                }
-              }
-            if (bad) atomicOr(&bad_rows[(key - prefix) >> 5], 1u << ((key - prefix) & 31));
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (kQ == 2) named_bar_sync(1, kSoft);  // both halves, before either group's product
-        }
         __syncwarp();
         tmem_wait_store();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(PFULL(g));
       }
-      T0 += r.n_tiles;
       // ---- the run's end: the groups and copies join
       const int own = kQ == 2 ? r.n_tiles : (r.n_tiles + 1 - g) / 2;
       if (own > 0) mbar_wait(PVDONE(g), (n - 1) & 1);
@@ -812,7 +844,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
       float top = -INFINITY, total = 0.f;
       bool skip = false;
-      constexpr int kBatch = 4;
+      constexpr int kBatch = 16;
       for (int k0 = 0; k0 < n; k0 += kBatch) {
         float4 v[kBatch];
         float2 ml[kBatch];

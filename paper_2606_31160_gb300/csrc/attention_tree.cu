@@ -13,9 +13,11 @@
 //
 // Two softmax groups of four warps, each with an S | P buffer and an O accumulator of its
 // own. Up to 128 packed rows the groups take alternate key tiles of the same rows; with more,
-// the same tile for 128 rows each. One warp issues all products, a group's PV and then its
-// next S (which goes where P was, so PV has to be done), then the other's: while one group's
-// products run, the other's softmax does. Few rows leave most of the 128 lanes idle, so up to
+// the same tile for 128 rows each. A group's next S goes where P was, so it is issued when PV
+// is done; while one group's products run, the other's softmax does. With two row tiles each
+// group has a warp that issues its products (a wait on a barrier, even one that is over, takes
+// such a warp ~135 cycles, a commit ~150: one for both groups took 1900 cycles a product pair
+// of 1024). Few rows leave most of the 128 lanes idle, so up to
 // 64 (32) of them are put into the tile two (four) times, each copy with its own half
 // (quarter) of the keys: its weights for the other keys are 0, and copies, groups and shares
 // join at the end by one rule
@@ -41,9 +43,9 @@ namespace {
 constexpr int kMaxRows = 256;    // rows of a tree
 constexpr int kTile = 128;       // keys a tile
 constexpr int kSoft = 256;       // softmax threads
-constexpr int kProducer = 8, kProduct = 9, kCleaner = 10;  // warps; two of the last
-constexpr int kClean = 64;       // its threads
-constexpr int kThreads = kSoft + 64 + kClean;
+constexpr int kProducer = 8, kProduct = 9, kCleaner = 11;  // warps: one, two, two
+constexpr int kClean = 64;       // the cleaners' threads
+constexpr int kThreads = kSoft + 96 + kClean;
 constexpr float kSlack = 64.f;   // log2 units that a score may pass its row's reference by
 constexpr int kJoin = 256;       // threads of the joining kernel
 constexpr int kMaxCtas = 192;    // shares
@@ -80,6 +82,10 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       : "=f"(d.x), "=f"(d.y)
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return d;
+}
+
+__device__ __forceinline__ void named_bar_arrive(int id, int threads) {
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
 // ------------------------------------------------------------------ shares
@@ -263,6 +269,35 @@ __device__ __noinline__ float bad_values(const TreeArgs& a, const int16_t* paren
   return sum;
 }
 
+// Four columns of a row, joined from its parts.
+struct Joined {
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float top = -INFINITY, total = 0.f;
+  bool skip = false;  // its tree is not valid
+  template <int kN>
+  __device__ __forceinline__ void add(const float2 (&ml)[kN], const float4 (&v)[kN]) {
+    float now = top;
+#pragma unroll
+    for (int u = 0; u < kN; ++u) {
+      skip |= ml[u].x != ml[u].x;
+      now = fmaxf(now, ml[u].x);
+    }
+    const float ref = now == -INFINITY ? 0.f : now, f0 = ex2(top - ref);
+    o.x *= f0, o.y *= f0, o.z *= f0, o.w *= f0, total *= f0;
+    top = now;
+#pragma unroll
+    for (int u = 0; u < kN; ++u) {
+      const float f = ex2(ml[u].x - ref);
+      total = fmaf(f, ml[u].y, total);
+      o.x = fmaf(f, v[u].x, o.x), o.y = fmaf(f, v[u].y, o.y), o.z = fmaf(f, v[u].z, o.z), o.w = fmaf(f, v[u].w, o.w);
+    }
+  }
+  __device__ __forceinline__ void store(__nv_bfloat16* out) const {
+    const float inv = 1.f / total;
+    if (!skip) *reinterpret_cast<uint2*>(out) = make_uint2(cvt_bf16x2(o.x * inv, o.y * inv), cvt_bf16x2(o.z * inv, o.w * inv));
+  }
+};
+
 // ------------------------------------------------------------------ kernel
 // kCluster: grid (cluster size, KV heads x m-blocks, scenes), else (shares).
 template <int kDim, int kCopies, int kQ, bool kCluster>
@@ -313,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     mbar_init(QFULL, 1);
     for (int j = 0; j < 2; ++j) {
-      mbar_init(VTOLD(j), 1);
+      mbar_init(VTOLD(j), kQ);
       mbar_init(VCLEAN(j), kClean / 32);
     }
     *const_cast<uint32_t*>(bad_page) = 0;
@@ -379,23 +414,28 @@ __global__ void __launch_bounds__(kThreads, 1)
         load(&tm_k, FULLK(T % kKS), base + (T % kKS) * C::kTileBytes);
         if (T >= kVS) mbar_wait(FREEV(T % kVS), (T / kVS - 1) & 1);
         load(&tm_v, FULLV(T % kVS), base + C::kOffV + (T % kVS) * C::kTileBytes);
+        // the first queries do not queue behind all the slots' keys
+        if (T == 0 && r.n_tiles > 1) mbar_wait(QFULL, 0);
       }
       ++run;
     }
-  } else if (warp == kProduct) {
+  } else if (warp >= kProduct && warp < kCleaner) {
     // -------------------------------------------------------------- products
+    // of group warp - kProduct with two row tiles, else of both by the first warp
+    const int x0 = kQ == 2 ? warp - kProduct : 0;
+    constexpr int kStep = kQ;
+    if (kQ == 1 && warp > kProduct) walk.left = 0;
     constexpr uint32_t kIdescS = umma_idesc(128, kTile, 0, 0), kIdescO = umma_idesc(128, kDim, 0, 1);
     const uint64_t dK = umma_desc(base, 16, 1024), dV = umma_desc(base + C::kOffV, C::kHalf, 1024);
     const uint64_t dQ = umma_desc(base + C::kOffQ, 16, 1024);
     int n0 = 0, n1 = 0, T0 = 0, run = 0, told = 0, cleaned = 0;  // n0, n1: products of the groups so far
     while (walk.next(a, r)) {
-      // item x: group x mod 2, of tile x / 2 (two row tiles) or x. The first group's wait for a
-      // tile stands for the second's.
+      // item x: group x mod 2, of tile x / 2 (two row tiles) or x
       const int items = kQ * r.n_tiles;
       auto tile_of = [&](int x) { return T0 + (kQ == 2 ? x >> 1 : x); };
       auto wait_k = [&](int x) {
         const int T = tile_of(x);
-        if (kQ == 1 || !(x & 1)) mbar_wait(FULLK(T % kKS), (T / kKS) & 1);
+        mbar_wait(FULLK(T % kKS), (T / kKS) & 1);
       };
       auto scores = [&](int x) {
         const int g = x & 1, ks = tile_of(x) % kKS;
@@ -411,24 +451,22 @@ __global__ void __launch_bounds__(kThreads, 1)
           umma_commit(FREEK(ks));
         }
         __syncwarp();
-        if ((kQ == 1 || g == 0) && new_rows(r, tile_of(x) - T0)) {
+        if (new_rows(r, tile_of(x) - T0)) {
           if (lane == 0) mbar_arrive(VTOLD(told));
           ++told;
         }
       };
       mbar_wait(QFULL, run & 1);
-      for (int x = 0; x < min(2, items); ++x) {
+      for (int x = x0; x < min(2, items); x += kStep) {
         wait_k(x);
         scores(x);
       }
-      for (int x = 0; x < items; ++x) {
+      for (int x = x0; x < items; x += kStep) {
         const int g = x & 1, T = tile_of(x), vs = T % kVS, n = g ? n1 : n0;
-        if (kQ == 1 || g == 0) {
-          mbar_wait(FULLV(vs), (T / kVS) & 1);
-          if (new_rows(r, T - T0)) {
-            mbar_wait(VCLEAN(cleaned), (cleaned >> 1) & 1);
-            ++cleaned;
-          }
+        mbar_wait(FULLV(vs), (T / kVS) & 1);
+        if (new_rows(r, T - T0)) {
+          mbar_wait(VCLEAN(cleaned), (cleaned >> 1) & 1);
+          ++cleaned;
         }
         mbar_wait(PFULL(g), n & 1);
         tc_fence_after();
@@ -553,7 +591,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       const bool tree_ok = !named_bar_or(1, kSoft, wrong);
       if (threadIdx.x == 0) mbar_arrive(QFULL);
-      // ---- tiles
+      // ---- tiles. Two row tiles: the groups' weights in turn, so that one group's products run
+      // meanwhile
+      if (kQ == 2 && g == 1) named_bar_arrive(2, kSoft);
       float m_ref = -INFINITY, l = 0.f;
       for (int t = kQ == 1 ? g : 0; t < r.n_tiles; t += 3 - kQ, ++n) {
         const int key0 = (r.tile0 + t) * kTile;
@@ -577,6 +617,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         mbar_wait(SREADY(g), n & 1);
         __syncwarp();
+        if (kQ == 2) named_bar_sync(2 + g, kSoft);  // the other group's weights are done
         tc_fence_after();
         // 32 scores of the lane, hidden ones as -inf
         auto scores = [&](int c, uint32_t (&s)[32]) {
@@ -656,6 +697,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(PFULL(g));
+        if (kQ == 2 && (g == 0 || t + 1 < r.n_tiles)) named_bar_arrive(3 - g, kSoft);
       }
       // ---- the run's end: the groups and copies join
       const int own = kQ == 2 ? r.n_tiles : (r.n_tiles + 1 - g) / 2;
@@ -752,10 +794,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (live && (kQ == 2 || g == 0)) put_ml(row, make_float2(top, total));
         } else if (tree_ok) {
           constexpr int kPer = kWide / 8;  // 16-byte chunks a row
-#pragma unroll 1
+#pragma unroll 4
           for (int x = lane; x < 32 * kPer; x += 32) {
             const int at = (warp & 3) * 32 + x / kPer, c = c0 / 8 + x % kPer, pr = r.mb * a.rows + (kQ == 2 ? g * kTile : 0) + at;
-            if (pr >= M) break;
+            if (pr >= M) continue;
             uint4 v;
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                          : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
@@ -841,9 +883,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int x = threadIdx.x; x < mine * (kDim / 4); x += kThreads) {
       const int row = row0 + x / (kDim / 4), c4 = x % (kDim / 4);
       const uint32_t at = base + cluster_o<kDim>(row, c4), at_ml = base + cluster_ml<kDim>(a.rows, row);
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      float top = -INFINITY, total = 0.f;
-      bool skip = false;
+      Joined j;
       constexpr int kBatch = 16;
       for (int k0 = 0; k0 < n; k0 += kBatch) {
         float4 v[kBatch];
@@ -859,28 +899,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                          : "r"(cluster_map(at, k0 + u)));
           }
         }
-        float now = top;
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          skip |= ml[u].x != ml[u].x;  // its tree is not valid
-          now = fmaxf(now, ml[u].x);
-        }
-        const float ref = now == -INFINITY ? 0.f : now, f0 = ex2(top - ref);
-        o.x *= f0, o.y *= f0, o.z *= f0, o.w *= f0, total *= f0;
-        top = now;
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          const float f = ex2(ml[u].x - ref);
-          total = fmaf(f, ml[u].y, total);
-          o.x = fmaf(f, v[u].x, o.x), o.y = fmaf(f, v[u].y, o.y), o.z = fmaf(f, v[u].z, o.z), o.w = fmaf(f, v[u].w, o.w);
-        }
+        j.add(ml, v);
       }
-      if (!skip) {
-        const float inv = 1.f / total;
-        const int pr = mb * a.rows + row, i = pr / a.G;
-        *reinterpret_cast<uint2*>(a.out + ((static_cast<long long>(blockIdx.z) * a.R + i) * a.Hq + (blockIdx.y / a.mblocks) * a.G + pr - i * a.G) * kDim +
-                                  c4 * 4) = make_uint2(cvt_bf16x2(o.x * inv, o.y * inv), cvt_bf16x2(o.z * inv, o.w * inv));
-      }
+      const int pr = mb * a.rows + row, i = pr / a.G;
+      j.store(a.out + ((static_cast<long long>(blockIdx.z) * a.R + i) * a.Hq + (blockIdx.y / a.mblocks) * a.G + pr - i * a.G) * kDim + c4 * 4);
     }
     __syncwarp();
     cluster_arrive_relaxed();  // (its reads are done; nobody's memory goes before)
@@ -889,13 +911,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // The units that a share's border cuts: border c lies between shares c - 1 and c, and the
-// first one that cuts a unit joins its parts.
-// A thread takes four columns of a row, rows along the lanes (as the parts lie), and eight
-// parts at once.
+// first one that cuts a unit joins its parts. A thread takes four columns of a row, rows along
+// the lanes (as the parts lie), and eight parts at once.
 template <int kDim>
 __global__ void __launch_bounds__(kJoin) tree_join_kernel(const __grid_constant__ TreeArgs a, int ctas) {
   constexpr int kRowsJ = kJoin / (kDim / 4), kBatch = 8;
-  __shared__ float2 s_ml[kMaxCtas][kRowsJ];
   sd_pdl_enter();
   const int lane = threadIdx.x & 31, c = blockIdx.x + 1;
   Walk walk;
@@ -904,47 +924,33 @@ __global__ void __launch_bounds__(kJoin) tree_join_kernel(const __grid_constant_
   if (!walk.next(a, r)) return;
   if (r.first == plan.begin(c) || plan.begin(c - 1) > r.first) return;
   const int share = c - 1, n = plan.cta_of(r.first + r.tiles - 1) - share + 1;  // its first share, its parts
-  const int row0 = blockIdx.y * kRowsJ, row = row0 + threadIdx.x % kRowsJ, c4 = threadIdx.x / kRowsJ;
-  if (row0 >= a.rows || r.mb * a.rows + row0 >= r.m * a.G) return;
+  const int c4 = threadIdx.x / kRowsJ, rows = min(a.rows, r.m * a.G - r.mb * a.rows);
   const size_t pf = part_floats(a.rows, kDim);
   // (the unit begins in its first share's second part, and goes on in the others' first)
-  auto part = [&](int k) { return a.part + (2 * static_cast<size_t>(share + k) + (k == 0 ? 1 : 0)) * pf; };
-  for (int x = threadIdx.x; x < n * kRowsJ; x += kJoin) {
-    const int k = x / kRowsJ, rr = x % kRowsJ;
-    s_ml[k][rr] = __ldcg(reinterpret_cast<const float2*>(part(k) + static_cast<size_t>(a.rows) * kDim) + row0 + rr);
-  }
-  __syncthreads();
-  const int p = r.mb * a.rows + row, rr = threadIdx.x % kRowsJ;
-  if (p >= r.m * a.G) return;
-  float top = -INFINITY;
-  bool skip = false;  // its tree is not valid
-  for (int k = 0; k < n; ++k) {
-    const float m = s_ml[k][rr].x;
-    skip |= m != m;
-    top = fmaxf(top, m);
-  }
-  if (skip) return;
-  const float ref = top == -INFINITY ? 0.f : top;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  float total = 0.f;
-  for (int k0 = 0; k0 < n; k0 += kBatch) {
-    float4 x[kBatch];
+  const float* part0 = a.part + 2 * static_cast<size_t>(share) * pf;
+  for (int row = blockIdx.y * kRowsJ + threadIdx.x % kRowsJ; row < rows; row += gridDim.y * kRowsJ) {
+    const float* at = part0 + (static_cast<size_t>(c4) * a.rows + row) * 4;
+    const float* at_ml = part0 + static_cast<size_t>(a.rows) * kDim + 2 * row;
+    Joined j;
+    for (int k0 = 0; k0 < n; k0 += kBatch) {
+      float4 v[kBatch];
+      float2 ml[kBatch];
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (k0 + u < n) x[u] = __ldcg(reinterpret_cast<const float4*>(part(k0 + u)) + static_cast<size_t>(c4) * a.rows + row);
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (k0 + u < n) {
-        const float2 y = s_ml[k0 + u][rr];
-        const float f = ex2(y.x - ref);
-        total = fmaf(f, y.y, total);
-        o.x = fmaf(f, x[u].x, o.x), o.y = fmaf(f, x[u].y, o.y), o.z = fmaf(f, x[u].z, o.z), o.w = fmaf(f, x[u].w, o.w);
+      for (int u = 0; u < kBatch; ++u) {
+        const int k = k0 + u;
+        const size_t off = (2 * static_cast<size_t>(k) + (k == 0 ? 1 : 0)) * pf;
+        ml[u] = make_float2(-INFINITY, 0.f);
+        v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (k < n) {
+          ml[u] = __ldcg(reinterpret_cast<const float2*>(at_ml + off));
+          v[u] = __ldcg(reinterpret_cast<const float4*>(at + off));
+        }
       }
+      j.add(ml, v);
+    }
+    const int p = r.mb * a.rows + row, i = p / a.G;
+    j.store(a.out + ((static_cast<long long>(r.b) * a.R + i) * a.Hq + r.kvh * a.G + p - i * a.G) * kDim + c4 * 4);
   }
-  const float inv = 1.f / total;
-  const int i = p / a.G;
-  *reinterpret_cast<uint2*>(a.out + ((static_cast<long long>(r.b) * a.R + i) * a.Hq + r.kvh * a.G + p - i * a.G) * kDim + c4 * 4) =
-      make_uint2(cvt_bf16x2(o.x * inv, o.y * inv), cvt_bf16x2(o.z * inv, o.w * inv));
 }
 
 // ------------------------------------------------------------------ host
@@ -1121,7 +1127,8 @@ extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const 
   if (e == cudaSuccess && p.ws_bytes > 0 && p.ctas > 1) {
     const long long rows = std::min<long long>(p.rows, static_cast<long long>(a.G) * R);
     e = sd_launch_pdl(D == 128 ? tree_join_kernel<128> : tree_join_kernel<64>,
-                      dim3(p.ctas - 1, static_cast<unsigned>((rows * (D / 4) + kJoin - 1) / kJoin)), dim3(kJoin), 0, st, a, p.ctas);
+                      dim3(p.ctas - 1, static_cast<unsigned>(std::min<long long>((rows * (D / 4) + kJoin - 1) / kJoin, 4))), dim3(kJoin), 0,
+                      st, a, p.ctas);
   }
   if (e != cudaSuccess) {
     (void)cudaGetLastError();

@@ -6,9 +6,10 @@
 // 256 of them (an m-block):
 //     S[128 rows][128 keys] = Q K^T        (both from shared memory, K-major)
 //     O[128 rows][D]       += P V          (P from tensor memory, V MN-major)
-// with one running reference and sum a row. The reference is the maximum of the row's first
-// tile and moves only when a score passes it by more than 64 (log2 units; O is then scaled in
-// place): weights stay below 2^64 and sums far inside fp32. P is bf16, and the sum is taken over the rounded
+// with one running reference and sum a row. The reference is the maximum of the first tile in
+// which the row sees a key, and moves only where a later tile's weights sum to more than 2^16
+// relative to it (O is then scaled in place): sums stay far inside fp32, and no tile but the
+// first looks for its maximum. P is bf16, and the sum is taken over the rounded
 // weights, so that they add up to 1 whatever their rounding.
 //
 // Two softmax groups of four warps, each with an S | P buffer and an O accumulator of its
@@ -43,10 +44,8 @@ namespace {
 constexpr int kMaxRows = 256;    // rows of a tree
 constexpr int kTile = 128;       // keys a tile
 constexpr int kSoft = 256;       // softmax threads
-constexpr int kProducer = 8, kProduct = 9, kCleaner = 11;  // warps: one, two, two
-constexpr int kClean = 64;       // the cleaners' threads
-constexpr int kThreads = kSoft + 96 + kClean;
-constexpr float kSlack = 64.f;   // log2 units that a score may pass its row's reference by
+constexpr int kProducer = 8, kProduct = 9;  // warps; the last ones clean
+constexpr int kThreads = kSoft + 128;
 constexpr int kJoin = 256;       // threads of the joining kernel
 constexpr int kMaxCtas = 192;    // shares
 
@@ -61,7 +60,7 @@ struct TreeArgs {
   float scale_log2, inv_g;
 };
 
-// The largest of three (NaN loses), and sums and products of pairs.
+// The largest of three (NaN loses); products and sums of pairs.
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -75,15 +74,13 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return d;
 }
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
-      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
+// Adds the two bf16 numbers of w, each to a sum of its own.
+__device__ __forceinline__ void add_pair(uint32_t w, float& lo, float& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\t"
+      "add.rn.f32.bf16 %0, a, %0;\n\tadd.rn.f32.bf16 %1, b, %1;\n\t}"
+      : "+f"(lo), "+f"(hi)
+      : "r"(w));
 }
-
 __device__ __forceinline__ void named_bar_arrive(int id, int threads) {
   asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
@@ -223,6 +220,8 @@ struct Walk {
 template <int kDim, int kCopies, int kQ>
 struct Cfg {
   static_assert(kCopies == 1 || kQ == 1, "copies of one tile");
+  static constexpr int kCleaner = kProduct + kQ;           // first of the cleaning warps
+  static constexpr int kClean = kThreads - 32 * kCleaner;  // their threads
   static constexpr int kRows = kTile / kCopies;            // packed rows a tile
   static constexpr int kCols = kTile / kCopies;            // keys of a tile that a lane looks at
   static constexpr int kHalf = kTile * 128;                // 64 columns of 128 rows
@@ -349,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(QFULL, 1);
     for (int j = 0; j < 2; ++j) {
       mbar_init(VTOLD(j), kQ);
-      mbar_init(VCLEAN(j), kClean / 32);
+      mbar_init(VCLEAN(j), C::kClean / 32);
     }
     *const_cast<uint32_t*>(bad_page) = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -419,12 +418,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       ++run;
     }
-  } else if (warp >= kProduct && warp < kCleaner) {
+  } else if (warp >= kProduct && warp < C::kCleaner) {
     // -------------------------------------------------------------- products
-    // of group warp - kProduct with two row tiles, else of both by the first warp
-    const int x0 = kQ == 2 ? warp - kProduct : 0;
+    // of group warp - kProduct with two row tiles, else of both
+    const int x0 = warp - kProduct;
     constexpr int kStep = kQ;
-    if (kQ == 1 && warp > kProduct) walk.left = 0;
     constexpr uint32_t kIdescS = umma_idesc(128, kTile, 0, 0), kIdescO = umma_idesc(128, kDim, 0, 1);
     const uint64_t dK = umma_desc(base, 16, 1024), dV = umma_desc(base + C::kOffV, C::kHalf, 1024);
     const uint64_t dQ = umma_desc(base + C::kOffQ, 16, 1024);
@@ -490,11 +488,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       T0 += r.n_tiles;
       ++run;
     }
-  } else if (warp >= kCleaner) {
+  } else if (warp >= C::kCleaner) {
     // -------------------------------------------------------------- values of the last tiles
     // V rows behind the last key become 0 (whatever they hold), and so do values of new rows
     // that are no numbers: 0 times them would be NaN
-    const int th = threadIdx.x - 32 * kCleaner;
+    const int th = threadIdx.x - 32 * C::kCleaner;
     int T0 = 0, cleaned = 0;
     while (walk.next(a, r)) {
       const int prefix = r.n_keys - r.m;
@@ -505,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_wait(FULLV(T % kVS), (T / kVS) & 1);
         const uint32_t tile = base + C::kOffV + (T % kVS) * C::kTileBytes;
 #pragma unroll 1
-        for (int row = max(0, prefix - key0) + th / 8; row < kTile; row += kClean / 8) {
+        for (int row = max(0, prefix - key0) + th / 8; row < kTile; row += C::kClean / 8) {
           const int key = key0 + row;
           bool bad = false;
 #pragma unroll
@@ -619,22 +617,31 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (kQ == 2) named_bar_sync(2 + g, kSoft);  // the other group's weights are done
         tc_fence_after();
-        // 32 scores of the lane, hidden ones as -inf
-        auto scores = [&](int c, uint32_t (&s)[32]) {
-          tmem_load(ts + copy * C::kCols + 32 * c, s);
+        // of 32 scores of the lane, hidden ones become -inf
+        auto hide = [&](int c, uint32_t (&s)[32]) {
           if (masked) {
+            uint32_t w = see[0];
 #pragma unroll
-            for (int w = 0; w < kWords; ++w)
-              if (w == c)
+            for (int x = 1; x < kWords; ++x)
+              if (c == x) w = see[x];
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                  if (!(see[w] >> j & 1)) s[j] = 0xff800000u;
+            for (int j = 0; j < 32; ++j)
+              if (!(w >> j & 1)) s[j] = 0xff800000u;
           }
         };
-        auto passes = [&](float top) { return top > m_ref + kSlack || (m_ref == -INFINITY && top > m_ref); };
-        // the row's reference moves to `top`, and with it what was summed
-        auto move_reference = [&](float top) {
-          const float now = fmaxf(m_ref, top), f = m_ref == -INFINITY ? 0.f : ex2(m_ref - now);
+        // the row's reference moves to the tile's maximum where that is higher, and with it what
+        // was summed
+        auto move_reference = [&] {
+          float mx = -INFINITY;
+#pragma unroll 1
+          for (int c = 0; c < kWords; ++c) {
+            uint32_t s[32];
+            tmem_load(ts + copy * C::kCols + 32 * c, s);
+            hide(c, s);
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) mx = max3(mx, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
+          }
+          const float now = fmaxf(m_ref, mx * sl), f = m_ref == -INFINITY ? 0.f : ex2(m_ref - now);
           m_ref = now;
           l *= f;
           if (t >= 3 - kQ) {  // the group's PV of the tile before is done: S came after it
@@ -648,44 +655,36 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         };
-        if (t < 3 - kQ) {  // the first tile: its maximum
-          float mx = -INFINITY;
-#pragma unroll
-          for (int c = 0; c < kWords; ++c) {
-            uint32_t s[32];
-            scores(c, s);
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) mx = max3(mx, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
-          }
-          move_reference(mx * sl);
-        }
-        // weights relative to the reference, and the tile's maximum with them; where that
-        // passes the reference by too much (seldom), once more with it
+        if (__any_sync(0xffffffffu, m_ref == -INFINITY)) move_reference();
+        // weights relative to the reference; where their sum passes 2^16 (seldom), once more
+        // relative to the tile's maximum
         uint32_t pw[C::kCols / 2];
-        float2 sum;
+        float sum[4];
 #pragma unroll 1
-        for (;;) {
+        for (bool again = false;; again = true) {
           const float sub = m_ref == -INFINITY ? 0.f : -m_ref;
-          float mx = -INFINITY;
-          sum = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sum[j] = 0.f;
+          uint32_t s[2][32];
+          tmem_load_begin(ts + copy * C::kCols, s[0]);
 #pragma unroll
           for (int c = 0; c < kWords; ++c) {
-            uint32_t s[32];
-            scores(c, s);
+            tmem_wait_load(s[c & 1]);
+            if (c + 1 < kWords) tmem_load_begin(ts + copy * C::kCols + 32 * (c + 1), s[(c + 1) & 1]);
+            hide(c, s[c & 1]);
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
-              mx = max3(mx, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
-              const float2 y = fma2(make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), make_float2(sl, sl), make_float2(sub, sub));
+              const float2 y = fma2(make_float2(__uint_as_float(s[c & 1][j]), __uint_as_float(s[c & 1][j + 1])),
+                                    make_float2(sl, sl), make_float2(sub, sub));
               const uint32_t w = cvt_bf16x2(ex2(y.x), ex2(y.y));
               pw[16 * c + j / 2] = w;
-              sum = add2(sum, make_float2(sd_bf16_lo(w), sd_bf16_hi(w)));
+              add_pair(w, sum[j & 2], sum[(j & 2) + 1]);
             }
           }
-          const float top = mx * sl;
-          if (!__any_sync(0xffffffffu, passes(top))) break;
-          move_reference(top);
+          if (again || !__any_sync(0xffffffffu, (sum[0] + sum[1]) + (sum[2] + sum[3]) > 0x1p16f)) break;
+          move_reference();
         }
-        l += sum.x + sum.y;
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         tmem_store(ts + copy * (C::kCols / 2), pw);
         if (kCopies > 1) {
           const uint32_t none[C::kCols / 2] = {};

@@ -27,21 +27,22 @@ struct AcceptArgs {
   int R, V;
 };
 
-// The walk of scene b over its n rows, by one CTA. keys: the rows' maxima.
-__device__ void walk(const AcceptArgs& a, int b, int n) {
+// The walk of scene b over its n rows, by one CTA; p and t: the parent and token of the
+// thread's row.
+static_assert(kMaxRows <= kThreads, "a row a thread");
+__device__ void walk(const AcceptArgs& a, int b, int n, int p, int t) {
   __shared__ int s_star[kMaxRows], s_parent[kMaxRows], s_token[kMaxRows];
   const long long row0 = static_cast<long long>(b) * a.R;
   bool tree_ok = true, range_ok = true;
-  for (int i = threadIdx.x; i < n; i += kThreads) {
+  const int i = threadIdx.x;
+  if (i < n) {
     unsigned long long* key = a.keys + row0 + i;
     s_star[i] = static_cast<int>(0xffffffffu - static_cast<uint32_t>(__ldcg(key)));
     *key = 0ull;  // re-armed for the next call
-    const int p = a.parents ? __ldcg(a.parents + row0 + i) : i - 1;
-    const int t = i > 0 ? __ldcg(a.tokens + row0 + i) : 0;
     s_parent[i] = p;
     s_token[i] = t;
-    tree_ok &= p >= -1 && p < i;
-    range_ok &= t >= 0 && t < a.V;
+    tree_ok = p >= -1 && p < i;
+    range_ok = t >= 0 && t < a.V;
   }
   tree_ok = __syncthreads_and(tree_ok) != 0;
   range_ok = __syncthreads_and(range_ok) != 0;
@@ -50,8 +51,7 @@ __device__ void walk(const AcceptArgs& a, int b, int n) {
     return;
   }
   if (!range_ok && threadIdx.x == 0) sd_set_error(SD_DEVERR_TOKEN_RANGE);
-  for (int i = threadIdx.x; i < n; i += kThreads)
-    if (a.argmax) a.argmax[row0 + i] = s_star[i];
+  if (i < n && a.argmax) a.argmax[row0 + i] = s_star[i];
   if (threadIdx.x >= 32) return;
   const int lane = threadIdx.x;
   int count = 0, at = n > 0 ? 0 : -1;
@@ -69,7 +69,7 @@ __device__ void walk(const AcceptArgs& a, int b, int n) {
     }
     at = next;
   }
-  for (int i = count + lane; i < a.R; i += 32) a.path[row0 + i] = a.out[row0 + i] = -1;
+  for (int c = count + lane; c < a.R; c += 32) a.path[row0 + c] = a.out[row0 + c] = -1;
   if (lane == 0) a.n_emit[b] = count;
 }
 
@@ -89,6 +89,11 @@ __global__ void __launch_bounds__(kThreads) accept_tree_kernel(const T* logits, 
   const long long at = static_cast<long long>(b) * a.R + r;
   unsigned long long best = 0;
   if (n > 0) best = scan_segment(logits + at * a.stride, a.V, static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x), vps, s_best, &s_index);
+  // (the tree travels with the ticket: any CTA may come to walk it)
+  const int own = threadIdx.x;
+  const long long row0 = static_cast<long long>(b) * a.R;
+  const int p = own < n && a.parents ? __ldcg(a.parents + row0 + own) : own - 1;
+  const int t = own > 0 && own < n ? __ldcg(a.tokens + row0 + own) : 0;
   if (threadIdx.x == 0) {
     if (n > 0) atomicMax(&a.keys[at], best);
     __threadfence();
@@ -97,7 +102,7 @@ __global__ void __launch_bounds__(kThreads) accept_tree_kernel(const T* logits, 
     __threadfence();
   }
   __syncthreads();
-  if (s_last) walk(a, b, n);
+  if (s_last) walk(a, b, n, p, t);
 }
 
 // Vectors a segment: about six CTAs an SM over all rows and at least 16 KB (one step of every

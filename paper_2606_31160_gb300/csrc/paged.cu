@@ -16,12 +16,14 @@
 #include "common.cuh"
 
 #include <math.h>
+#include <algorithm>
 
 SD_DEFINE_ERROR_ACCESSOR(sd_take_error_paged)
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;  // of an append
+constexpr int kCtas = 14;      // CTAs an SM of a long append
 
 struct Paged {
   const int32_t* table;
@@ -57,66 +59,50 @@ __device__ __forceinline__ bool pages_ok(const Paged& p, int b, int first, int n
   return __syncthreads_and(ok) != 0;
 }
 
-// Grid (chunks of a scene's rows, scenes). A thread takes the same 16-byte chunk of kPer
-// heads of one row, queries first, then keys, then values.
+// Grid (CTAs of a scene, scenes). A thread takes the same 16-byte chunk of kPer heads of one
+// row, queries first, then keys, then values, and then of the row so many further on.
 template <int D, int kPer>
 __global__ void __launch_bounds__(kThreads) paged_append_kernel(const __grid_constant__ AppendArgs a,
                                                                 const __grid_constant__ RopeTable tab) {
-  constexpr int kVec = D / 8;
+  constexpr int kVec = D / 8, kItems = kThreads / kVec;  // items (a row's kPer heads) of a CTA at once
   const int b = blockIdx.y, vec = threadIdx.x % kVec;
   const RopeChunk chunk = sd_rope_chunk(vec, tab);
-  const int heads = a.Hq + 2 * a.pg.Hkv, groups = (heads + kPer - 1) / kPer;
+  const int heads = a.Hq + 2 * a.pg.Hkv, rotated = a.pos ? a.Hq + a.pg.Hkv : 0, groups = (heads + kPer - 1) / kPer;
   sd_pdl_enter();
   const int l0 = __ldcg(a.len + b), n = a.n_new ? __ldcg(a.n_new + b) : a.R;
   const bool count_ok = n >= 0 && n <= a.R && l0 >= 0;
   const bool fits = count_ok && static_cast<long long>(l0) + n <= static_cast<long long>(a.pg.max_pages) << a.pg.shift;
+  uint4 x[kPer];
+  int page = 0, p[3] = {0, 0, 0};
+  auto place = [&](long long item, int& r, int& h0) {
+    r = static_cast<int>(item / groups);
+    h0 = static_cast<int>(item - static_cast<long long>(r) * groups) * kPer;
+  };
+  auto load = [&](int r, int h0) {
+    const long long row = static_cast<long long>(b) * a.R + r;
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int h = h0 + u;
+      const uint4* src = h < a.Hq ? a.q + row * a.qs + h * kVec
+                         : h < a.Hq + a.pg.Hkv ? a.k_new + row * a.ks + (h - a.Hq) * kVec
+                                               : a.v_new + row * a.vs + (h - a.Hq - a.pg.Hkv) * kVec;
+      if (h < heads) x[u] = __ldcg(src + vec);
+    }
+    page = __ldcg(a.pg.table + static_cast<long long>(b) * a.pg.max_pages + ((l0 + r) >> a.pg.shift));
+    if (h0 < rotated)
+#pragma unroll
+      for (int j = 0; j < 3; ++j) p[j] = __ldcg(a.pos + row * 3 + j);
+  };
+  // the first row travels while the CTA looks at the pages
+  const long long step = static_cast<long long>(gridDim.x) * kItems, items = fits ? static_cast<long long>(n) * groups : 0;
+  long long item = blockIdx.x * static_cast<long long>(kItems) + threadIdx.x / kVec;
+  int r = 0, h0 = 0;
+  if (item < items) {
+    place(item, r, h0);
+    load(r, h0);
+  }
   // (also the barrier between this CTA's reads of the length and its ticket)
   const bool paged = pages_ok(a.pg, b, l0, fits ? n : 0);
-  if (fits && paged) {
-    const long long item = blockIdx.x * static_cast<long long>(kThreads / kVec) + threadIdx.x / kVec;
-    const int r = static_cast<int>(item / groups), h0 = static_cast<int>(item - static_cast<long long>(r) * groups) * kPer;
-    if (r < n) {
-      const long long row = static_cast<long long>(b) * a.R + r;
-      uint4 x[kPer];
-#pragma unroll
-      for (int u = 0; u < kPer; ++u) {
-        const int h = h0 + u;
-        const uint4* src = h < a.Hq ? a.q + row * a.qs + h * kVec
-                           : h < a.Hq + a.pg.Hkv ? a.k_new + row * a.ks + (h - a.Hq) * kVec
-                                                 : a.v_new + row * a.vs + (h - a.Hq - a.pg.Hkv) * kVec;
-        if (h < heads) x[u] = __ldcg(src + vec);
-      }
-      const int at = l0 + r;
-      const int page = __ldcg(a.pg.table + static_cast<long long>(b) * a.pg.max_pages + (at >> a.pg.shift));
-      if (a.pos && h0 < a.Hq + a.pg.Hkv) {
-        const int32_t* p3 = a.pos + row * 3;
-        const int p[3] = {__ldcg(p3), __ldcg(p3 + 1), __ldcg(p3 + 2)};
-        float c[4], s[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float t = static_cast<float>(chunk.axis[j] == 0 ? p[0] : (chunk.axis[j] == 1 ? p[1] : p[2]));
-          sincospif(2.0f * sd_frac_turns(t, chunk.hi[j], chunk.lo[j]), &s[j], &c[j]);
-        }
-#pragma unroll
-        for (int u = 0; u < kPer; ++u)
-          if (h0 + u < a.Hq + a.pg.Hkv)
-            x[u] = make_uint4(sd_rope_pair(x[u].x, c[0], s[0]), sd_rope_pair(x[u].y, c[1], s[1]),
-                              sd_rope_pair(x[u].z, c[2], s[2]), sd_rope_pair(x[u].w, c[3], s[3]));
-      }
-#pragma unroll
-      for (int u = 0; u < kPer; ++u) {
-        const int h = h0 + u;
-        if (h >= heads) break;
-        if (h < a.Hq) {
-          a.q_out[row * a.qos + h * kVec + vec] = x[u];
-        } else {
-          const bool key = h < a.Hq + a.pg.Hkv;
-          const int g = h - a.Hq - (key ? 0 : a.pg.Hkv);
-          (key ? a.k : a.v)[paged_row(a.pg, page, g, at) * kVec + vec] = x[u];
-        }
-      }
-    }
-  }
   if (threadIdx.x == 0) {
     __threadfence();
     if (atomicAdd(&a.ticket[b], 1u) == gridDim.x - 1) {
@@ -125,10 +111,45 @@ __global__ void __launch_bounds__(kThreads) paged_append_kernel(const __grid_con
       else sd_set_error(!count_ok ? SD_DEVERR_LENGTH : (fits ? SD_DEVERR_PAGE : SD_DEVERR_KV_OVERFLOW));
     }
   }
+  if (!paged) return;
+  while (item < items) {
+    if (h0 < rotated) {
+      float c[4], s[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float t = static_cast<float>(chunk.axis[j] == 0 ? p[0] : (chunk.axis[j] == 1 ? p[1] : p[2]));
+        sincospif(2.0f * sd_frac_turns(t, chunk.hi[j], chunk.lo[j]), &s[j], &c[j]);
+      }
+#pragma unroll
+      for (int u = 0; u < kPer; ++u)
+        if (h0 + u < rotated)
+          x[u] = make_uint4(sd_rope_pair(x[u].x, c[0], s[0]), sd_rope_pair(x[u].y, c[1], s[1]),
+                            sd_rope_pair(x[u].z, c[2], s[2]), sd_rope_pair(x[u].w, c[3], s[3]));
+    }
+    const long long row = static_cast<long long>(b) * a.R + r;
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int h = h0 + u;
+      if (h >= heads) break;
+      if (h < a.Hq) {
+        a.q_out[row * a.qos + h * kVec + vec] = x[u];
+      } else {
+        const bool key = h < a.Hq + a.pg.Hkv;
+        const int g = h - a.Hq - (key ? 0 : a.pg.Hkv);
+        (key ? a.k : a.v)[paged_row(a.pg, page, g, l0 + r) * kVec + vec] = x[u];
+      }
+    }
+    item += step;
+    if (item < items) {
+      place(item, r, h0);
+      load(r, h0);
+    }
+  }
 }
 
 // ------------------------------------------------------------------ commit
 constexpr int kCaches = 48;  // caches a launch
+constexpr int kRows = 256;   // threads, and rows of a path looked at together
 
 struct CommitArgs {
   struct {
@@ -142,61 +163,82 @@ struct CommitArgs {
   int R, Hkv, shift;
 };
 
-// Grid (columns of one cache's keys and values, scenes, caches).
+// Grid (columns of one cache's keys and values, scenes, caches). A CTA takes kRows rows of
+// the path at a time: their places into shared memory, checked, then the rows.
 template <int D>
-__global__ void __launch_bounds__(kThreads) paged_commit_kernel(const __grid_constant__ CommitArgs a) {
+__global__ void __launch_bounds__(kRows) paged_commit_kernel(const __grid_constant__ CommitArgs a) {
   constexpr int kVec = D / 8;
   constexpr int kBatch = 8;  // rows a thread has in flight
+  __shared__ long long s_src[kRows], s_dst[kRows];  // rows of the pools; s_src -1: in its place
   const int b = blockIdx.y;
   const auto& c = a.c[blockIdx.z];
   const Paged pg = {c.table, a.Hkv, c.n_pages, a.shift, c.max_pages};
   sd_pdl_enter();
   const int32_t* path = a.path + static_cast<long long>(b) * a.R;
+  const int32_t* table = c.table + static_cast<long long>(b) * c.max_pages;
   const int l = __ldcg(c.len + b), n = a.n_new ? __ldcg(a.n_new + b) : a.R, m = __ldcg(a.n_emit + b);
+  // (the first rows of the path travel with the lengths)
+  int from = static_cast<int>(threadIdx.x) < a.R ? __ldcg(path + threadIdx.x) : 0;
+  int before = threadIdx.x > 0 && static_cast<int>(threadIdx.x) < a.R ? __ldcg(path + threadIdx.x - 1) : -1;
   const bool len_ok = n >= 0 && n <= a.R && l >= n && l <= static_cast<long long>(c.max_pages) << a.shift;
   const bool m_ok = m >= 0 && m <= n;
-  const int first = l - n;
-  const int32_t* table = c.table + static_cast<long long>(b) * c.max_pages;
+  const int first = l - n, rows = len_ok && m_ok ? m : 0;
   bool path_ok = true, page_ok = true;
-  if (len_ok && m_ok) {
-    for (int i = threadIdx.x; i < m; i += kThreads) {
-      const int from = __ldcg(path + i), before = i > 0 ? __ldcg(path + i - 1) : -1;
-      const bool ok = from > before && from < n;
-      path_ok &= ok;
-      const int src = __ldcg(table + ((first + (ok ? from : 0)) >> a.shift)), dst = __ldcg(table + ((first + i) >> a.shift));
-      page_ok &= src >= 0 && src < c.n_pages && dst >= 0 && dst < c.n_pages;
-    }
+  // where row i of the path comes from and goes to
+  auto place = [&](int i) {
+    const bool ok = from > before && from < n;
+    path_ok &= ok;
+    const int src = __ldcg(table + ((first + (ok ? from : 0)) >> a.shift)), dst = __ldcg(table + ((first + i) >> a.shift));
+    page_ok &= src >= 0 && src < c.n_pages && dst >= 0 && dst < c.n_pages;
+    s_src[threadIdx.x] = from == i ? -1 : paged_row(pg, src, 0, first + from);
+    s_dst[threadIdx.x] = paged_row(pg, dst, 0, first + i);
+  };
+  auto load = [&](int i) {
+    from = __ldcg(path + i);
+    before = i > 0 ? __ldcg(path + i - 1) : -1;
+  };
+  for (int i = static_cast<int>(threadIdx.x) + kRows; i < rows; i += kRows) {  // (long paths: checked first)
+    load(i);
+    place(i);
+  }
+  if (static_cast<int>(threadIdx.x) < rows) {
+    if (rows > kRows) load(threadIdx.x);
+    place(threadIdx.x);
   }
   path_ok = __syncthreads_and(path_ok) != 0;
   page_ok = __syncthreads_and(page_ok) != 0;
   const bool ok = len_ok && m_ok && path_ok && page_ok;
-  const int col = blockIdx.x * kThreads + threadIdx.x;  // [k, v][head][chunk]
-  if (ok && col < 2 * a.Hkv * kVec) {
-    const int vec = col % kVec, h = col / kVec, g = h % a.Hkv;
-    uint4* pool = (h < a.Hkv ? c.k : c.v) + vec;
-    for (int i0 = 0; i0 < m; i0 += kBatch) {
-      uint4 x[kBatch];
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int i = i0 + u;
-        if (i >= m) break;
-        const int from = __ldcg(path + i);
-        if (from != i) x[u] = __ldcg(pool + paged_row(pg, __ldcg(table + ((first + from) >> a.shift)), g, first + from) * kVec);
-      }
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int i = i0 + u;
-        if (i >= m) break;
-        if (__ldcg(path + i) != i) pool[paged_row(pg, __ldcg(table + ((first + i) >> a.shift)), g, first + i) * kVec] = x[u];
-      }
-    }
-  }
   if (threadIdx.x == 0) {
     __threadfence();
     if (atomicAdd(&c.ticket[b], 1u) == gridDim.x - 1) {
       c.ticket[b] = 0;
       if (ok) c.len[b] = first + m;
       else sd_set_error(!len_ok ? SD_DEVERR_LENGTH : (m_ok && path_ok ? SD_DEVERR_PAGE : SD_DEVERR_ROLLBACK));
+    }
+  }
+  if (!ok) return;
+  const int col = blockIdx.x * kRows + threadIdx.x;  // [k, v][head][chunk]
+  const int vec = col % kVec, h = col / kVec, g = h % a.Hkv;
+  uint4* pool = (h < a.Hkv ? c.k : c.v) + ((static_cast<long long>(g) << a.shift) * kVec + vec);
+  for (int i0 = 0; i0 < m; i0 += kRows) {
+    if (i0 > 0) {
+      __syncthreads();
+      if (i0 + static_cast<int>(threadIdx.x) < m) {
+        load(i0 + threadIdx.x);
+        place(i0 + threadIdx.x);
+      }
+      __syncthreads();
+    }
+    const int here = min(m - i0, kRows);
+    if (h >= 2 * a.Hkv) continue;
+    for (int i = 0; i < here; i += kBatch) {
+      uint4 x[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        if (i + u < here && s_src[i + u] >= 0) x[u] = __ldcg(pool + s_src[i + u] * kVec);
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        if (i + u < here && s_src[i + u] >= 0) pool[s_dst[i + u] * kVec] = x[u];
     }
   }
 }
@@ -256,14 +298,17 @@ extern "C" sd_status sd_paged_append(const sd_paged_cache* cache, const void* k_
   a.pos = pos;
   a.R = R;
   a.Hq = Hq;
-  // heads a thread: one where the call is short, so that many threads share its latency; eight
-  // where it is long: the angles of a row are taken once for eight heads
-  const long long heads = Hq + 2ll * Hkv, per_cta = kThreads / (D / 8);
-  const int per = static_cast<long long>(B) * R * heads >= 16 * per_cta * sd_num_sms() ? 8 : 1;
-  const long long blocks = (R * ((heads + per - 1) / per) + per_cta - 1) / per_cta;
-  if (blocks > 0x7fffffffll) return SD_ERR_UNSUPPORTED;
-  if (sd_launch_pdl(D == 64 ? (per == 8 ? paged_append_kernel<64, 8> : paged_append_kernel<64, 1>)
-                            : (per == 8 ? paged_append_kernel<128, 8> : paged_append_kernel<128, 1>),
+  // heads a thread: one where the call is short, so that many threads share its latency; four
+  // or eight where it is long: the angles of a row are taken once for them
+  const long long heads = Hq + 2ll * Hkv, per_cta = kThreads / (D / 8), sms = sd_num_sms();
+  const long long ctas = static_cast<long long>(B) * R * heads / per_cta;
+  const int per = ctas >= 16 * sms ? 8 : ctas >= 4 * sms ? 4 : 1;
+  // as many CTAs as are resident (seven an SM, at 72 registers), twice, and each goes on from
+  // there. 201 MB: 36.2 us; one CTA for each 128 items 43.9, CTAs of 256 threads, three an SM, 38.4
+  const long long blocks = std::min((R * ((heads + per - 1) / per) + per_cta - 1) / per_cta, std::max<long long>((kCtas * sms + B - 1) / B, 1));
+  const auto kernel = D == 64 ? (per == 8 ? paged_append_kernel<64, 8> : per == 4 ? paged_append_kernel<64, 4> : paged_append_kernel<64, 1>)
+                              : (per == 8 ? paged_append_kernel<128, 8> : per == 4 ? paged_append_kernel<128, 4> : paged_append_kernel<128, 1>);
+  if (sd_launch_pdl(kernel,
                     dim3(static_cast<unsigned>(blocks), B), dim3(kThreads), 0, reinterpret_cast<cudaStream_t>(stream), a,
                     tab) != cudaSuccess) {
     (void)cudaGetLastError();
@@ -297,7 +342,7 @@ extern "C" sd_status sd_paged_commit(const sd_paged_cache* caches, int count, co
   a.R = R;
   a.Hkv = caches[0].n_kv_heads;
   a.shift = log2_of(caches[0].page);
-  const int blocks = (2 * a.Hkv * (D / 8) + kThreads - 1) / kThreads;
+  const int blocks = (2 * a.Hkv * (D / 8) + kRows - 1) / kRows;
   for (int i0 = 0; i0 < count; i0 += kCaches) {
     const int n = count - i0 < kCaches ? count - i0 : kCaches;
     for (int i = 0; i < n; ++i) {
@@ -305,7 +350,7 @@ extern "C" sd_status sd_paged_commit(const sd_paged_cache* caches, int count, co
       a.c[i] = {static_cast<uint4*>(c.k), static_cast<uint4*>(c.v), c.table, c.len, c.ticket, c.n_pages, c.max_pages};
     }
     if (sd_launch_pdl(D == 64 ? paged_commit_kernel<64> : paged_commit_kernel<128>, dim3(blocks, caches[0].batch, n),
-                      dim3(kThreads), 0, reinterpret_cast<cudaStream_t>(stream), a) != cudaSuccess) {
+                      dim3(kRows), 0, reinterpret_cast<cudaStream_t>(stream), a) != cudaSuccess) {
       (void)cudaGetLastError();
       return SD_ERR_CUDA;
     }

@@ -622,20 +622,23 @@ class PagedKVCacheGroup:
         self._structs = (PagedCacheStruct * len(self.caches))(*(c._struct for c in self.caches))
 
 
-def _current_device(index):
-    """Kernels launch on the current device, on its current stream."""
-    if index != (torch.cuda.current_device() if _raw_device is None else _raw_device()):
+def _stream_on(index):
+    """The current stream, of the device that the tensors are on: kernels launch on the current one."""
+    at = torch.cuda.current_device() if _raw_device is None else _raw_device()
+    if index != at:
         raise ValueError("the tensors must be on the current device")
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(at)
 
 
 def _ints(t, name, shape, device):
     """Address of an int32 tensor of this shape on this device, None for None."""
     if t is None:
         return None
-    p = _dev(t, name, torch.int32)
-    if t.shape != shape or t.device.index != device:
-        raise ValueError("%s must be %s on the caller's device" % (name, tuple(shape)))
-    return p
+    if t.__class__ is not _Tensor or t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        _dev(t, name, torch.int32)
+        if t.shape != shape or t.get_device() != device:
+            raise ValueError("%s must be %s on the caller's device" % (name, tuple(shape)))
+    return t.data_ptr()
 
 
 def _row_stride(t, name, shape, device):
@@ -643,12 +646,12 @@ def _row_stride(t, name, shape, device):
     and whose rows are evenly spaced (part of a projection's output)."""
     if not isinstance(t, _Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
-    if not t.is_cuda or t.dtype is not torch.bfloat16 or t.shape != shape or t.device.index != device:
+    if t.dtype is not torch.bfloat16 or t.shape != shape or t.get_device() != device:
         raise ValueError("%s must be %s bf16 on the caller's CUDA device" % (name, tuple(shape)))
     B, R, H, D = shape
-    sb, sr, sh, sd_ = t.stride()
     if t.is_contiguous():
         return t.data_ptr(), H * D
+    sb, sr, sh, sd_ = t.stride()
     if (D > 1 and sd_ != 1) or (H > 1 and sh != D):
         raise ValueError("%s: a row's heads must be contiguous" % name)
     step = sr if R > 1 else sb
@@ -667,7 +670,7 @@ def paged_append(cache, k_new, v_new, q=None, pos=None, sections=None, interleav
     rotated queries."""
     B, H, _, D = cache._shape
     dev = cache._device
-    _current_device(dev)
+    stream = _stream_on(dev)
     if len(k_new.shape) != 4:
         raise ValueError("k_new must be [B, R, Hkv, D]")
     R = k_new.shape[1]
@@ -689,7 +692,7 @@ def paged_append(cache, k_new, v_new, q=None, pos=None, sections=None, interleav
         raise ValueError("pos without sections")
     sec = None if pos is None else _sections(tuple(int(x) for x in sections))
     _check(lib().sd_paged_append(cache._ref, kp, ks, vp, vs, qp, qs, op, R, Hq, _ints(pos, "pos", (B, R, 3), dev), sec,
-                                 int(interleaved), float(base), _ints(n_new, "n_new", (B,), dev), _stream()),
+                                 int(interleaved), float(base), _ints(n_new, "n_new", (B,), dev), stream),
            "sd_paged_append")
     return q if q_out is None else q_out
 
@@ -707,7 +710,7 @@ def tree_attention(q, cache, parents=None, n_new=None, out=None, scale=0.0, ws=N
     stream."""
     B, H, cap, D = cache._shape
     dev = cache._device
-    _current_device(dev)
+    stream = _stream_on(dev)
     if len(q.shape) != 4:
         raise ValueError("q must be [B, R, Hq, D]")
     R, Hq = q.shape[1], q.shape[2]
@@ -723,7 +726,7 @@ def tree_attention(q, cache, parents=None, n_new=None, out=None, scale=0.0, ws=N
     _check(lib().sd_tree_attention(qp, qs, cache._ref, _ints(parents, "parents", (B, R), dev),
                                    _ints(n_new, "n_new", (B,), dev), _dev(out, "out", torch.bfloat16), R, Hq, float(scale),
                                    None if ws is None else _dev(ws, "ws"), 0 if ws is None else ws.numel() * ws.element_size(),
-                                   _stream()), "sd_tree_attention")
+                                   stream), "sd_tree_attention")
     return out
 
 
@@ -746,7 +749,7 @@ def accept_tree(logits, tokens, parents=None, n_new=None, ws=None, n_emit=None, 
     else:
         ptr, stride = _padded_rows(logits, B * R)
     dev = logits.device
-    _current_device(dev.index)
+    stream = _stream_on(dev.index)
     if ws is None:
         ws = workspace(accept_tree_workspace_bytes(B, R, V), dev)
     n_emit = torch.empty(B, dtype=torch.int32, device=dev) if n_emit is None else n_emit
@@ -757,7 +760,7 @@ def accept_tree(logits, tokens, parents=None, n_new=None, ws=None, n_emit=None, 
     _check(lib().sd_accept_tree(ptr, dt, B, R, V, stride, _ints(tokens, "tokens", wide, at), _ints(parents, "parents", wide, at),
                                 _ints(n_new, "n_new", (B,), at), _ints(n_emit, "n_emit", (B,), at), _ints(path, "path", wide, at),
                                 _ints(out, "out", wide, at), _ints(argmax, "argmax", wide, at), _dev(ws, "ws"),
-                                ws.numel() * ws.element_size(), _stream()), "sd_accept_tree")
+                                ws.numel() * ws.element_size(), stream), "sd_accept_tree")
     return n_emit, path, out, argmax
 
 
@@ -769,12 +772,12 @@ def paged_commit(caches, path, n_emit, n_new=None):
         caches = PagedKVCacheGroup([caches] if isinstance(caches, PagedKVCache) else caches)
     first = caches.caches[0]
     B, dev = first._shape[0], first._device
-    _current_device(dev)
+    stream = _stream_on(dev)
     if len(path.shape) != 2:
         raise ValueError("path must be [B, R]")
     R = path.shape[1]
     _check(lib().sd_paged_commit(caches._structs, len(caches.caches), _ints(path, "path", (B, R), dev),
-                                 _ints(n_emit, "n_emit", (B,), dev), _ints(n_new, "n_new", (B,), dev), R, _stream()),
+                                 _ints(n_emit, "n_emit", (B,), dev), _ints(n_new, "n_new", (B,), dev), R, stream),
            "sd_paged_commit")
 
 

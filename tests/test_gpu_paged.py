@@ -162,6 +162,7 @@ def _path(rng, n):
     (6, 61, 4, 64, 16, 3, True),
     (3, 256, 2, 128, 32, 2, True),
     (2, 9, 3, 128, 128, 50, False),
+    (2, 700, 2, 64, 64, 2, True),
 ])
 def test_commit(B, R, Hkv, D, page, layers, ragged):
     g = torch.Generator(device="cuda").manual_seed(R)

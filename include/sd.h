@@ -548,7 +548,7 @@ sd_status sd_token_logprobs(const void* logits, sd_dtype dtype, int rows, int V,
  * bf16; row n of scene b is row n % page of page table[b][n / page], so a scene
  * holds up to max_pages * page rows (fewer than 2^31). table: device int32
  * [batch][max_pages], which no call writes; several caches (the layers of a model)
- * may share one. Entries past a scene's rows are never read. len as in
+ * may share one. Entries past a scene's rows may be anything. len as in
  * sd_kv_cache; every cache has its own. Rows at or past len[b] are never read.
  * ticket: device uint32 [batch], zero-filled before the cache's first use and left
  * zeroed by every completed call; calls that share it must not overlap on the device.

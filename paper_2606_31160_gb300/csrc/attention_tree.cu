@@ -44,7 +44,9 @@ namespace {
 constexpr int kMaxRows = 256;    // rows of a tree
 constexpr int kTile = 128;       // keys a tile
 constexpr int kSoft = 256;       // softmax threads
-constexpr int kProducer = 8, kProduct = 9;  // warps; the last ones clean
+// warps: 8 brings keys, 9 issues products, 10 brings values (one row tile) or issues the second
+// group's products (and warp 8 brings both), 11 cleans
+constexpr int kProducer = 8, kProduct = 9, kSecond = 10, kCleaner = 11;
 constexpr int kThreads = kSoft + 128;
 constexpr int kJoin = 256;       // threads of the joining kernel
 constexpr int kMaxCtas = 192;    // shares
@@ -220,8 +222,6 @@ struct Walk {
 template <int kDim, int kCopies, int kQ>
 struct Cfg {
   static_assert(kCopies == 1 || kQ == 1, "copies of one tile");
-  static constexpr int kCleaner = kProduct + kQ;           // first of the cleaning warps
-  static constexpr int kClean = kThreads - 32 * kCleaner;  // their threads
   static constexpr int kRows = kTile / kCopies;            // packed rows a tile
   static constexpr int kCols = kTile / kCopies;            // keys of a tile that a lane looks at
   static constexpr int kHalf = kTile * 128;                // 64 columns of 128 rows
@@ -348,14 +348,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(QFULL, 1);
     for (int j = 0; j < 2; ++j) {
       mbar_init(VTOLD(j), kQ);
-      mbar_init(VCLEAN(j), C::kClean / 32);
+      mbar_init(VCLEAN(j), 1);
     }
     *const_cast<uint32_t*>(bad_page) = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  int early[4] = {};
   // tensor memory is taken after the wait for the kernel before (which may hold some) and
   // before the next kernel may come
   griddep_wait();
+  if (kCluster && (warp == kProducer || warp == kSecond) && a.max_pages <= 128) {
+    const int32_t* table = a.table + static_cast<long long>(blockIdx.z) * a.max_pages;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (lane + 32 * k < a.max_pages) early[k] = __ldcg(table + lane + 32 * k);
+  }
   if (warp == kProduct) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_slot)), "r"(512)
                  : "memory");
@@ -374,9 +381,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   // whether tile t of a run holds new rows (or rows behind the last key)
   auto new_rows = [](const Run& x, int t) { return (x.tile0 + t + 1) * kTile > x.n_keys - x.m; };
   Run r;
-  if (warp == kProducer) {
-    // -------------------------------------------------------------- producer
-    if (kCluster ? blockIdx.x == 0 && blockIdx.y == 0 : blockIdx.x == 0)
+  if (warp == kProducer || (kQ == 1 && warp == kSecond)) {
+    // -------------------------------------------------------------- producers
+    // of keys and values: with one row tile and many copies a tile (~60 cycles each to issue;
+    // pages of 16 rows take 16) each its own
+    const bool keys = warp == kProducer;
+    const bool apart = kQ == 1 && (kTile >> a.shift) * (kDim / 64) >= 8, values = keys != apart;
+    if (!keys && !values) walk.left = 0;
+    if (keys && (kCluster ? blockIdx.x == 0 && blockIdx.y == 0 : blockIdx.x == 0))
       for (int b = kCluster ? blockIdx.z + 32 * lane : lane; b < (kCluster ? blockIdx.z + 1 : a.B); b += 32)
         if (length_error(a, b)) sd_set_error(SD_DEVERR_LENGTH);
     const uint64_t evict_first = l2_evict_first_policy();
@@ -384,15 +396,27 @@ __global__ void __launch_bounds__(kThreads, 1)
     int T = 0, run = 0;
     while (walk.next(a, r)) {
       const int32_t* table = a.table + static_cast<long long>(r.b) * a.max_pages;
-      auto page_id = [&](int t) {  // the lane's page of tile t, or -2: none
+      auto page_id = [&](int t) {  // the lane's page of tile t
         const int at = t * pages + lane;
         return lane < pages && (at << a.shift) < r.n_keys ? __ldcg(table + at) : INT32_MIN;
       };
-      int id = page_id(r.tile0);
+      int id;
+      if (kCluster && a.max_pages <= 128) {
+        // the scene's pages were on their way before its length was known
+        const int at = r.tile0 * pages + lane;
+        id = INT32_MIN;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int x = __shfl_sync(0xffffffffu, early[k], at & 31);
+          if ((at >> 5) == k) id = x;
+        }
+      } else {
+        id = page_id(r.tile0);
+      }
       for (int t = 0; t < r.n_tiles; ++t, ++T) {
         const int tile = r.tile0 + t;
         const bool need = lane < pages && ((tile * pages + lane) << a.shift) < r.n_keys, ok = need && id >= 0 && id < a.n_pages;
-        if (__any_sync(0xffffffffu, need && !ok) && lane == 0) {
+        if (keys && __any_sync(0xffffffffu, need && !ok) && lane == 0) {
           atomicOr(const_cast<uint32_t*>(bad_page), 1u << (run & 31));
           sd_set_error(SD_DEVERR_PAGE);
         }
@@ -409,16 +433,20 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           __syncwarp();
         };
-        if (T >= kKS) mbar_wait(FREEK(T % kKS), (T / kKS - 1) & 1);
-        load(&tm_k, FULLK(T % kKS), base + (T % kKS) * C::kTileBytes);
-        if (T >= kVS) mbar_wait(FREEV(T % kVS), (T / kVS - 1) & 1);
-        load(&tm_v, FULLV(T % kVS), base + C::kOffV + (T % kVS) * C::kTileBytes);
+        if (keys) {
+          if (T >= kKS) mbar_wait(FREEK(T % kKS), (T / kKS - 1) & 1);
+          load(&tm_k, FULLK(T % kKS), base + (T % kKS) * C::kTileBytes);
+        }
+        if (values) {
+          if (T >= kVS) mbar_wait(FREEV(T % kVS), (T / kVS - 1) & 1);
+          load(&tm_v, FULLV(T % kVS), base + C::kOffV + (T % kVS) * C::kTileBytes);
+        }
         // the first queries do not queue behind all the slots' keys
-        if (T == 0 && r.n_tiles > 1) mbar_wait(QFULL, 0);
+        if (!kCluster && T == 0 && r.n_tiles > 1) mbar_wait(QFULL, 0);
       }
       ++run;
     }
-  } else if (warp >= kProduct && warp < C::kCleaner) {
+  } else if (warp == kProduct || (kQ == 2 && warp == kSecond)) {
     // -------------------------------------------------------------- products
     // of group warp - kProduct with two row tiles, else of both
     const int x0 = warp - kProduct;
@@ -461,6 +489,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       for (int x = x0; x < items; x += kStep) {
         const int g = x & 1, T = tile_of(x), vs = T % kVS, n = g ? n1 : n0;
+        const int steps = (min(r.n_keys - (r.tile0 + T - T0) * kTile, kTile) + 15) / 16;  // 16 keys each
         mbar_wait(FULLV(vs), (T / kVS) & 1);
         if (new_rows(r, T - T0)) {
           mbar_wait(VCLEAN(cleaned), (cleaned >> 1) & 1);
@@ -469,10 +498,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_wait(PFULL(g), n & 1);
         tc_fence_after();
         if (elect_one()) {
-#pragma unroll
-          for (int kk = 0; kk < kTile / 16; ++kk)
+          auto product = [&](int kk) {
             umma_ta(tmem_o + kDim * g, tmem + 128 * g + kk * 8, dV + ((vs * C::kTileBytes + kk * 2048) >> 4), kIdescO,
                     x >= 2 || kk > 0 ? 1 : 0);
+          };
+          if (steps == kTile / 16) {
+#pragma unroll
+            for (int kk = 0; kk < kTile / 16; ++kk) product(kk);
+          } else {
+#pragma unroll 1
+            for (int kk = 0; kk < steps; ++kk) product(kk);
+          }
           umma_commit(PVDONE(g));
           umma_commit(FREEV(vs));
         }
@@ -488,11 +524,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       T0 += r.n_tiles;
       ++run;
     }
-  } else if (warp >= C::kCleaner) {
+  } else if (warp == kCleaner) {
     // -------------------------------------------------------------- values of the last tiles
-    // V rows behind the last key become 0 (whatever they hold), and so do values of new rows
-    // that are no numbers: 0 times them would be NaN
-    const int th = threadIdx.x - 32 * C::kCleaner;
+    // V rows behind the last key (of its 16) become 0, whatever they hold, and so do values of
+    // new rows that are no numbers: 0 times them would be NaN
     int T0 = 0, cleaned = 0;
     while (walk.next(a, r)) {
       const int prefix = r.n_keys - r.m;
@@ -502,13 +537,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_wait(VTOLD(cleaned), (cleaned >> 1) & 1);
         mbar_wait(FULLV(T % kVS), (T / kVS) & 1);
         const uint32_t tile = base + C::kOffV + (T % kVS) * C::kTileBytes;
-#pragma unroll 1
-        for (int row = max(0, prefix - key0) + th / 8; row < kTile; row += C::kClean / 8) {
+        const int rows = min((r.n_keys - key0 + 15) / 16 * 16, kTile);  // that the product reads
+#pragma unroll 2
+        for (int row = max(0, prefix - key0) + lane / 8; row < rows; row += 4) {
           const int key = key0 + row;
           bool bad = false;
 #pragma unroll
           for (int h = 0; h < kDim / 64; ++h) {
-            const uint32_t at = tile + h * C::kHalf + row * 128 + ((th & 7) << 4);
+            const uint32_t at = tile + h * C::kHalf + row * 128 + ((lane & 7) << 4);
             if (key >= r.n_keys) {
               st_shared_v4(at, 0u, 0u, 0u, 0u);
               continue;
@@ -806,42 +842,39 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       } else {
-        // the copies' sums through the query tile (its products are done): [128 lanes][kDim / 2]
-        constexpr int kC = kDim / 4;  // columns a group and round
-        float* stage = reinterpret_cast<float*>(smem + C::kOffQ);
+        // the copies' sums through shared memory: [128 lanes][columns of a round]; the query tile
+        // (its products are done) holds half of them, a cluster's slots all, behind the part
+        constexpr int kRounds = kCluster ? 1 : 2, kWide = kDim / kRounds;
+        static_assert(!kCluster || C::kRows * (kDim + 2) * 4 + kTile * kDim * 4 <= C::kOffQ, "part and columns");
+        float* stage = reinterpret_cast<float*>(smem + (kCluster ? (C::kRows * (kDim + 2) * 4 + 127) / 128 * 128 : C::kOffQ));
 #pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-          if (kC == 32) {
+        for (int round = 0; round < kRounds; ++round) {
+#pragma unroll 1
+          for (int c = g * 32; c < kWide; c += 64) {  // 32 columns a group
             float x[32];
-            joined(half * 2 * kC + g * kC, x);
+            joined(round * kWide + c, x);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-              *reinterpret_cast<float4*>(stage + rl * 2 * kC + (((g * (kC / 4) + j) ^ (rl & 7)) << 2)) =
+              *reinterpret_cast<float4*>(stage + rl * kWide + ((((c >> 2) + j) ^ (rl & 7)) << 2)) =
                   make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
-          } else if (g == 0) {  // head dim 64: one group's 32 columns a round
-            float x[32];
-            joined(half * 32, x);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              *reinterpret_cast<float4*>(stage + rl * 32 + ((j ^ (rl & 7)) << 2)) = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
           }
           __syncwarp();
           named_bar_sync(1, kSoft);
-          for (int x = threadIdx.x; x < C::kRows * (kC / 2); x += kSoft) {
+          for (int x = threadIdx.x; x < C::kRows * (kWide / 4); x += kSoft) {
             // (rows along the lanes for the parts, columns for the output)
-            const int rr = whole ? x / (kC / 2) : x % C::kRows, c4 = whole ? x % (kC / 2) : x / C::kRows, pr = r.mb * a.rows + rr;
+            const int rr = whole ? x / (kWide / 4) : x % C::kRows, c4 = whole ? x % (kWide / 4) : x / C::kRows;
+            const int pr = r.mb * a.rows + rr, d = round * kWide + c4 * 4;
             if (pr >= M) continue;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int cp = 0; cp < kCopies; ++cp) {
               const int at = cp * C::kRows + rr;
-              const float4 y = *reinterpret_cast<const float4*>(stage + at * 2 * kC + ((c4 ^ (at & 7)) << 2));
+              const float4 y = *reinterpret_cast<const float4*>(stage + at * kWide + ((c4 ^ (at & 7)) << 2));
               v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
             }
-            const int d = half * 2 * kC + c4 * 4;
             if (!whole) {
               put_o(rr, d, v);
-              if (half == 0 && c4 == 0) {
+              if (d == 0) {
                 float2 fin;
                 joined_ml(rr, fin.x, fin.y);
                 put_ml(rr, fin);
@@ -865,18 +898,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   tc_fence_before();
-  __syncthreads();
+  const int cs = gridDim.x, parts = kCluster ? min(cs, walk.s.tiles) : 1;  // CTAs that had tiles: the first ones
+  __syncwarp();
+  if (parts > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // (the same for the whole cluster)
+  else __syncthreads();
+  if (parts > 1) cluster_wait();
   if (warp == kProduct) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
-  if (kCluster) {
+  if (kCluster && parts > 1) {
     // ---- the cluster's parts: a CTA joins its share of the rows, a thread four columns of one
-    const int cs = gridDim.x, n = min(cs, walk.s.tiles);  // CTAs that had tiles: the first n
-    if (n <= 1) return;                                    // (the same for the whole cluster)
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    cluster_wait();
+    const int n = parts;
     const int M = walk.s.m * a.G, mb = blockIdx.y % a.mblocks, rows = min(a.rows, M - mb * a.rows), each = (rows + cs - 1) / cs;
     const int row0 = blockIdx.x * each, mine = min(each, rows - row0);
     for (int x = threadIdx.x; x < mine * (kDim / 4); x += kThreads) {

@@ -251,7 +251,8 @@ __device__ __forceinline__ uint32_t cluster_ml(int rows, int row) {
   return static_cast<uint32_t>(rows * kDim * 4 + row * 8);
 }
 
-__device__ __forceinline__ bool bad_pair(uint32_t w) { return __vcmpeq2(w & 0x7f807f80u, 0x7f807f80u) != 0; }
+// Nonzero where one of the two bf16 numbers of w is no number: its exponent, all ones, carries.
+__device__ __forceinline__ uint32_t bad_pair(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 
 // Sum of the values that are no numbers at column d of the bad rows that row i of scene b sees.
 __device__ __noinline__ float bad_values(const TreeArgs& a, const int16_t* parent, const uint32_t* bad, int b, int kvh, int prefix,
@@ -538,30 +539,40 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_wait(FULLV(T % kVS), (T / kVS) & 1);
         const uint32_t tile = base + C::kOffV + (T % kVS) * C::kTileBytes;
         const int rows = min((r.n_keys - key0 + 15) / 16 * 16, kTile);  // that the product reads
-#pragma unroll 2
-        for (int row = max(0, prefix - key0) + lane / 8; row < rows; row += 4) {
-          const int key = key0 + row;
-          bool bad = false;
+        // rows lane / 8, + 4, + 8, + 12 at once, a chunk of each half a lane
+        constexpr int kAt = 4, kHalves = kDim / 64;
+#pragma unroll 1
+        for (int row0 = max(0, prefix - key0) + lane / 8; row0 < rows; row0 += 4 * kAt) {
+          uint32_t w[kAt][kHalves][4];
+          auto chunk = [&](int i, int h) { return tile + h * C::kHalf + (row0 + 4 * i) * 128 + ((lane & 7) << 4); };
 #pragma unroll
-          for (int h = 0; h < kDim / 64; ++h) {
-            const uint32_t at = tile + h * C::kHalf + row * 128 + ((lane & 7) << 4);
-            if (key >= r.n_keys) {
-              st_shared_v4(at, 0u, 0u, 0u, 0u);
-              continue;
-            }
-            uint32_t w[4];
-            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
-            if (bad_pair(w[0]) || bad_pair(w[1]) || bad_pair(w[2]) || bad_pair(w[3])) {
-              bad = true;
+          for (int i = 0; i < kAt; ++i)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                if ((w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
-                if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= 0x0000ffffu;
+            for (int h = 0; h < kHalves; ++h)
+              if (key0 + row0 + 4 * i < r.n_keys)
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(w[i][h][0]), "=r"(w[i][h][1]), "=r"(w[i][h][2]), "=r"(w[i][h][3])
+                             : "r"(chunk(i, h)));
+#pragma unroll
+          for (int i = 0; i < kAt; ++i) {
+            const int row = row0 + 4 * i, node = key0 + row - prefix;
+            if (row >= rows) break;
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+              uint32_t(&x)[4] = w[i][h];
+              if (key0 + row >= r.n_keys) {
+                st_shared_v4(chunk(i, h), 0u, 0u, 0u, 0u);
+              } else if (bad_pair(x[0]) | bad_pair(x[1]) | bad_pair(x[2]) | bad_pair(x[3])) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  if ((x[j] & 0x7f80u) == 0x7f80u) x[j] &= 0xffff0000u;
+                  if ((x[j] & 0x7f800000u) == 0x7f800000u) x[j] &= 0x0000ffffu;
+                }
+                st_shared_v4(chunk(i, h), x[0], x[1], x[2], x[3]);
+                atomicOr(&bad_rows[node >> 5], 1u << (node & 31));
               }
-              st_shared_v4(at, w[0], w[1], w[2], w[3]);
             }
           }
-          if (bad) atomicOr(&bad_rows[(key - prefix) >> 5], 1u << ((key - prefix) & 31));
         }
         __syncwarp();
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -587,13 +598,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int node = live ? gdiv(p) : 0;
       const bool masked_run = new_rows(r, r.n_tiles - 1);
       // ---- the packed queries; the tree where the run reaches the new rows
-      constexpr int kChunks = kQ * C::kRows * (kDim / 8) / kSoft, kBatch = kChunks < 8 ? kChunks : 8;  // a thread's
-#pragma unroll 1
-      for (int x0 = 0; x0 < kChunks; x0 += kBatch) {
+      static_assert(kMaxRows <= kSoft, "a row a thread");
+      int up = -1;
+      if (masked_run && a.parents && static_cast<int>(threadIdx.x) < r.m)
+        up = __ldcg(a.parents + static_cast<long long>(r.b) * a.R + threadIdx.x);
+      constexpr int kBatch = kQ * C::kRows * (kDim / 8) / kSoft;  // 16-byte chunks a thread
+      {
         uint4 v[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-          const int x = threadIdx.x + (x0 + u) * kSoft, qr = x / (kDim / 8), c = x % (kDim / 8), pq = r.mb * a.rows + qr;
+          const int x = threadIdx.x + u * kSoft, qr = x / (kDim / 8), c = x % (kDim / 8), pq = r.mb * a.rows + qr;
           v[u] = make_uint4(0, 0, 0, 0);
           if (pq < M) {
             const int i = gdiv(pq);
@@ -603,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-          const int x = threadIdx.x + (x0 + u) * kSoft, qr = x / (kDim / 8), c = x % (kDim / 8);
+          const int x = threadIdx.x + u * kSoft, qr = x / (kDim / 8), c = x % (kDim / 8);
 #pragma unroll
           for (int cp = 0; cp < kCopies; ++cp) {
             const int at = cp * C::kRows + (qr & 127);
@@ -613,12 +627,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
-      bool wrong = false;
-      if (masked_run && a.parents && static_cast<int>(threadIdx.x) < r.m) {
-        const int up = __ldcg(a.parents + static_cast<long long>(r.b) * a.R + threadIdx.x);
-        wrong = up < -1 || up >= static_cast<int>(threadIdx.x);
-        s_parent[threadIdx.x] = static_cast<int16_t>(wrong ? -1 : up);
-      }
+      const bool wrong = up < -1 || up >= static_cast<int>(threadIdx.x);
+      if (masked_run && a.parents) s_parent[threadIdx.x] = static_cast<int16_t>(wrong ? -1 : up);
       if (threadIdx.x < 8) bad_rows[threadIdx.x] = 0;
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       tc_fence_before();  // (the run before: its O has been read)

@@ -1087,17 +1087,28 @@ sd_status host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) 
   if (units > 0x7fffffffll / tiles) return SD_ERR_UNSUPPORTED;
   p->mblocks = static_cast<int>(blocks);
   p->ctas = static_cast<int>(std::min<long long>(std::min(sd_num_sms(), kMaxCtas), units * tiles));
-  // in tiles: waves x (tiles a CTA + a fixed cost), or all tiles over all CTAs, the second
-  // units' costs and the joining kernel's
+  // The way of least estimated time, in us, from what each took over 1 to 32 scenes of 512 to
+  // 8192 keys: a CTA's tile, its first queries to its last output, the exchange in a cluster,
+  // the joining kernel; and never less than all tiles' bytes take. (32 query / 8 KV heads x 128,
+  // clusters / even shares: 26 rows and 4096 keys, 1 scene 16 / 37, 12 scenes 43 / 50, 20
+  // scenes 81 / 71; 61 rows, 32 scenes of 512 keys 46 / 65, of 8192 233 / 216.)
+  struct Cost {
+    double tile, unit, exchange, join;
+  };
+  static constexpr Cost kCosts[2][4] = {{{0.7, 7.5, 1.0, 2.0}, {0.7, 7.5, 1.5, 3.0}, {0.72, 9.0, 1.5, 5.0}, {1.3, 12.0, 4.0, 10.0}},
+                                        {{0.93, 7.5, 2.0, 2.0}, {0.95, 7.5, 3.0, 4.0}, {1.0, 8.0, 4.5, 7.0}, {1.64, 12.5, 6.0, 15.0}}};
+  const Cost& c = kCosts[D == 128][p->variant];
   const int* active = dev->active[D == 128][p->variant];
-  double best = static_cast<double>(tiles) * units / p->ctas + 4.0 * std::min<long long>(units, p->ctas) / p->ctas + (tiles > 1 ? 6.0 : 0.0);
+  const double all = static_cast<double>(units) * tiles, stream = all * (4.0 * kTile * D / 6.7e6);
+  const double runs = static_cast<double>((units + p->ctas - 1) / p->ctas);  // that a share begins beside its first
+  double best = std::max(stream, all / p->ctas * c.tile + runs * c.unit) + c.unit + (tiles > 1 ? c.join : 0.0);
   p->cs = 0;
   if (blocks * Hkv <= 65535)
     for (int i = 0; i < kNumSizes; ++i) {
       const int cs = kSizes[i];
       if (active[i] <= 0 || cs > tiles) continue;
-      const long long waves = (units + active[i] - 1) / active[i];
-      const double cost = static_cast<double>(waves) * ((tiles + cs - 1) / cs + (waves > 1 ? 4.0 : 0.0));
+      const double waves = static_cast<double>((units + active[i] - 1) / active[i]);
+      const double cost = std::max(stream + c.unit, waves * ((tiles + cs - 1) / cs * c.tile + c.unit + (cs > 1 ? c.exchange : 0.0)));
       if (cost < best) best = cost, p->cs = cs;
     }
   // one tile a unit: no share's border cuts one

@@ -243,6 +243,25 @@ __global__ void __launch_bounds__(kRows) paged_commit_kernel(const __grid_consta
   }
 }
 
+// The rotation's table, kept from call to call of a thread with the same numbers (64 powers take
+// 3 us).
+const RopeTable* table_of(int D, const int32_t* sections, int interleaved, float base) {
+  struct Kept {
+    bool valid = false;
+    int D, sections[3], interleaved;
+    float base;
+    RopeTable tab;
+  };
+  static thread_local Kept k;
+  if (!k.valid || k.D != D || k.sections[0] != sections[0] || k.sections[1] != sections[1] || k.sections[2] != sections[2] ||
+      k.interleaved != interleaved || k.base != base) {
+    k.valid = sd_internal_rope_table(D, sections, interleaved, base, &k.tab);
+    k.D = D, k.interleaved = interleaved, k.base = base;
+    for (int i = 0; i < 3; ++i) k.sections[i] = sections[i];
+  }
+  return k.valid ? &k.tab : nullptr;
+}
+
 int log2_of(int page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
 
 }  // namespace
@@ -269,10 +288,12 @@ extern "C" sd_status sd_paged_append(const sd_paged_cache* cache, const void* k_
   const int B = cache->batch, Hkv = cache->n_kv_heads, D = cache->head_dim;
   if (R < 0 || Hq < 0 || (Hq > 0) != (q != nullptr) || (q_out && !q) || (q && !pos)) return SD_ERR_INVALID_ARG;
   if (interleaved != 0 && interleaved != 1) return SD_ERR_INVALID_ARG;
-  RopeTable tab = {};
+  static const RopeTable kNone = {};
+  const RopeTable* tab = &kNone;
   if (pos) {
     if (!sections || !(base > 1.0f) || !isfinite(base)) return SD_ERR_INVALID_ARG;
-    if (!sd_internal_rope_table(D, sections, interleaved, base, &tab)) return SD_ERR_INVALID_ARG;
+    tab = table_of(D, sections, interleaved, base);
+    if (!tab) return SD_ERR_INVALID_ARG;
   }
   if (k_stride < static_cast<long long>(Hkv) * D || v_stride < static_cast<long long>(Hkv) * D || k_stride % 8 || v_stride % 8 ||
       (q && (q_stride < static_cast<long long>(Hq) * D || q_stride % 8)))
@@ -310,7 +331,7 @@ extern "C" sd_status sd_paged_append(const sd_paged_cache* cache, const void* k_
                               : (per == 8 ? paged_append_kernel<128, 8> : per == 4 ? paged_append_kernel<128, 4> : paged_append_kernel<128, 1>);
   if (sd_launch_pdl(kernel,
                     dim3(static_cast<unsigned>(blocks), B), dim3(kThreads), 0, reinterpret_cast<cudaStream_t>(stream), a,
-                    tab) != cudaSuccess) {
+                    *tab) != cudaSuccess) {
     (void)cudaGetLastError();
     return SD_ERR_CUDA;
   }

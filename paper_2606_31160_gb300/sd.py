@@ -684,13 +684,13 @@ def paged_append(cache, k_new, v_new, q=None, pos=None, sections=None, interleav
         qp, qs = _row_stride(q, "q", (B, R, Hq, D), dev)
         if q_out is not None:
             op = _dev(q_out, "q_out", torch.bfloat16)
-            if q_out.shape != q.shape or q_out.device.index != dev:
+            if q_out.shape != q.shape or q_out.get_device() != dev:
                 raise ValueError("q_out must have q's shape and device")
     elif q_out is not None:
         raise ValueError("q_out without q")
     if pos is not None and sections is None:
         raise ValueError("pos without sections")
-    sec = None if pos is None else _sections(tuple(int(x) for x in sections))
+    sec = None if pos is None else _sections(sections if sections.__class__ is tuple else tuple(int(x) for x in sections))
     _check(lib().sd_paged_append(cache._ref, kp, ks, vp, vs, qp, qs, op, R, Hq, _ints(pos, "pos", (B, R, 3), dev), sec,
                                  int(interleaved), float(base), _ints(n_new, "n_new", (B,), dev), stream),
            "sd_paged_append")
@@ -717,7 +717,7 @@ def tree_attention(q, cache, parents=None, n_new=None, out=None, scale=0.0, ws=N
     qp, qs = _row_stride(q, "q", (B, R, Hq, D), dev)
     if out is None:
         out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-    elif out.shape != q.shape or out.device.index != dev:
+    elif out.shape != q.shape or out.get_device() != dev:
         raise ValueError("out must have q's shape and device")
     if ws is None:
         need = lib().sd_tree_attention_workspace(B, R, Hq, H, D, cap)

@@ -1138,6 +1138,9 @@ extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const 
   if (B == 0) return SD_OK;
   if (!q || !out || !sd_aligned16(q) || !sd_aligned16(out)) return SD_ERR_INVALID_ARG;
   if (workspace && !sd_aligned16(workspace)) return SD_ERR_INVALID_ARG;
+  const double sc = scale > 0.f ? scale : 1.0 / sqrt(static_cast<double>(D));
+  const float scale_log2 = static_cast<float>(sc * 1.4426950408889634);
+  if (!isfinite(scale_log2)) return SD_ERR_INVALID_ARG;
   const int cap = cache->max_pages * cache->page;
   HostPlan p = {};
   const sd_status planned = host_plan(B, R, Hq, Hkv, D, cap, &p);
@@ -1164,8 +1167,7 @@ extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const 
   a.cap = cap;
   a.rows = p.rows;
   a.mblocks = p.mblocks;
-  const double sc = scale > 0.f ? scale : 1.0 / sqrt(static_cast<double>(D));
-  a.scale_log2 = static_cast<float>(sc * 1.4426950408889634);
+  a.scale_log2 = scale_log2;
   a.inv_g = 1.0f / static_cast<float>(a.G);
   CUtensorMap k, v;
   if (!make_map(&k, cache->k, cache->page, cache->n_pages * Hkv, cache->page, D) ||

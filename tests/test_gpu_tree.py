@@ -159,6 +159,93 @@ def test_scores_far_from_zero_and_rising(R, D):
         check_scene(out, q, cache, 0, np.arange(R) - 1, R)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("R", [1, 24, 60, 110])
+def test_references_that_move_in_a_run(R, D):
+    """Scores that rise over many tiles of a CTA, by little and by much, in every row tile: the
+    references move and what was summed with them."""
+    g = torch.Generator(device="cuda").manual_seed(R)
+    Hq, Hkv, L = 8, 4, 20000
+    q = _randn(g, 1, R, Hq, D)
+    q[..., 0] = 4.0
+    up = torch.arange(L, device="cuda") / L
+    for shape in (up * 120, (up * 8).floor() * 90, torch.where((up > 0.6) & (up < 0.6001), 300.0, 0.0)):
+        cache = make_cache(g, [L], L, Hkv, D, 64)
+        at = torch.arange(L, device="cuda")
+        cache.k[cache.table[0, at // 64].long(), :, at % 64, 0] = (shape / 4 * (D / 64) ** 0.5)[:, None].to(torch.bfloat16).expand(-1, Hkv)
+        out = sd.tree_attention(q, cache)
+        assert sd.get_device_error() == 0
+        check_scene(out, q, cache, 0, np.arange(R) - 1, R)
+
+
+@pytest.mark.parametrize("B,R,Hq,Hkv,D,L", [(100, 5, 4, 2, 64, 3000), (80, 15, 8, 2, 64, 4000), (80, 30, 8, 2, 128, 3000),
+                                              (40, 33, 16, 4, 128, 5000), (42, 70, 8, 4, 64, 3500)])
+def test_attention_of_many_scenes(B, R, Hq, Hkv, D, L):
+    """More than 32 scenes, in even shares (the way that takes a workspace), some with nothing
+    new and some not valid; the workspace of any content, the results the same every time."""
+    assert sd.tree_attention_workspace_bytes(B, R, Hq, Hkv, D, -(-(L + R) // 64) * 64) > 0
+    g = torch.Generator(device="cuda").manual_seed(B)
+    rng = np.random.default_rng(B)
+    n_new = rng.integers(0, R + 1, B)
+    n_new[0], n_new[-1] = R, R
+    lens = rng.integers(0, L + 1, B) + n_new
+    cache = make_cache(g, lens, L + R, Hkv, D, 64)
+    parents = np.stack([make_tree(rng, R, forest=True) for _ in range(B)])
+    bad_len, bad_tree, bad_page = 7, B // 2, B - 2
+    n_new[bad_tree] = n_new[bad_page] = R
+    lens[bad_tree], lens[bad_page] = L + R, L + R
+    cache.len.copy_(_i32(lens))
+    cache.len[bad_len] = -1
+    parents[bad_tree, R // 2] = R
+    cache.table[bad_page, 3] = -1
+    q = _randn(g, B, R, Hq, D)
+    ws = torch.full((sd.tree_attention_workspace_bytes(B, R, Hq, Hkv, D, cache.shape[2]),), 0xFF, dtype=torch.uint8, device="cuda")
+    out = torch.full((B, R, Hq, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    sd.tree_attention(q, cache, parents=_i32(parents), n_new=_i32(n_new), out=out, ws=ws)
+    assert sd.get_device_error() == sd.SD_DEVERR_LENGTH | sd.SD_DEVERR_TREE | sd.SD_DEVERR_PAGE
+    for b in range(B):
+        if b in (bad_len, bad_tree):
+            assert (out[b] == 7.0).all()
+        elif b == bad_page:
+            assert out[b].isnan().all()
+        else:
+            check_scene(out, q, cache, b, parents[b], n_new[b])
+            assert (out[b, n_new[b]:] == 7.0).all()
+    again = sd.tree_attention(q, cache, parents=_i32(parents), n_new=_i32(n_new), out=torch.full_like(out, 7.0))
+    assert torch.equal(again.view(torch.int16), out.view(torch.int16))
+    sd.get_device_error()
+
+
+def test_two_graphs_and_a_workspace_of_ones_own():
+    """Two captured graphs that share a workspace, replayed in turn, each the same as its call;
+    a workspace that is too short is refused."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    B, R, Hq, Hkv, D, L = 40, 6, 8, 4, 128, 1500
+    need = sd.tree_attention_workspace_bytes(B, R, Hq, Hkv, D, -(-L // 32) * 32)
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    sides = []
+    for _ in range(2):
+        cache = make_cache(g, [L - 7 * b for b in range(B)], L, Hkv, D, 32)
+        sides.append((_randn(g, B, R, Hq, D), cache, torch.zeros((B, R, Hq, D), dtype=torch.bfloat16, device="cuda")))
+    want = [sd.tree_attention(q, cache) for q, cache, _ in sides]
+    torch.cuda.synchronize()
+    graphs = []
+    for q, cache, out in sides:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            sd.tree_attention(q, cache, out=out, ws=ws)
+        graphs.append(graph)
+    for _ in range(3):
+        for i, graph in enumerate(graphs):
+            graph.replay()
+            assert torch.equal(sides[i][2], want[i])
+    assert sd.get_device_error() == 0
+    with pytest.raises(sd.SDError) as e:
+        sd.tree_attention(sides[0][0], sides[0][1], ws=ws[:need - 16])
+    assert e.value.status == 3
+
+
 def test_a_long_tail_beside_one_key():
     """One key that holds most of a row over thousands that share the rest."""
     g = torch.Generator(device="cuda").manual_seed(6)

@@ -65,6 +65,7 @@ def test_attention(lib):
     assert _attend(lib, c, R=0) == 1 and _attend(lib, c, Hq=30) == 1 and _attend(lib, c, Hq=0) == 1
     assert _attend(lib, c, R=257) == 2
     assert _attend(lib, c, scale=-1.0) == 1 and _attend(lib, c, scale=float("nan")) == 1 and _attend(lib, c, scale=float("inf")) == 1
+    assert _attend(lib, c, scale=3e38) == 1                                     # past fp32 in the units of the exponent
     assert _attend(lib, c, qs=4088) == 1 and _attend(lib, c, qs=4097) == 1
     assert _attend(lib, c, q=0) == 1 and _attend(lib, c, out=0) == 1 and _attend(lib, c, q=8) == 1 and _attend(lib, c, out=8) == 1
     assert _attend(lib, c, ws=24) == 1

@@ -58,7 +58,7 @@ struct TreeArgs {
   const int32_t *table, *len, *parents, *n_new;
   long long q_stride;
   float* part;              // even shares: per CTA two parts, O [D / 4][rows][4], then (m, l) [rows][2]
-  int B, R, Hq, Hkv, G, n_pages, shift, max_pages, cap, rows, mblocks;  // rows: of an m-block
+  int B, R, Hq, Hkv, G, n_pages, shift, max_pages, cap, rows, row_shift, mblocks;  // rows (1 << row_shift): of an m-block
   float scale_log2, inv_g;
 };
 
@@ -89,7 +89,7 @@ __device__ __forceinline__ void named_bar_arrive(int id, int threads) {
 
 // ------------------------------------------------------------------ shares
 struct Scene {
-  int n_keys, m, tiles, units;  // tiles 0: not valid, or no rows that count
+  int n_keys, m, tiles, mblocks;  // tiles 0: not valid, or no rows that count
 };
 __device__ __forceinline__ Scene scene_of(const TreeArgs& a, int b) {
   Scene s;
@@ -97,8 +97,8 @@ __device__ __forceinline__ Scene scene_of(const TreeArgs& a, int b) {
   s.m = a.n_new ? __ldcg(a.n_new + b) : a.R;
   const bool ok = s.m > 0 && s.m <= a.R && s.n_keys >= s.m && s.n_keys <= a.cap;
   s.tiles = ok ? (s.n_keys + kTile - 1) / kTile : 0;
-  s.units = a.Hkv * ((s.m * a.G + a.rows - 1) / a.rows);
-  if (!ok) s.n_keys = s.m = s.units = 0;
+  s.mblocks = (s.m * a.G + a.rows - 1) >> a.row_shift;
+  if (!ok) s.n_keys = s.m = s.mblocks = 0;
   return s;
 }
 __device__ __forceinline__ bool length_error(const TreeArgs& a, int b) {
@@ -122,7 +122,7 @@ struct Run {
   int first;                         // the unit's first tile among all
 };
 struct Walk {
-  int b, unit, tile, first, left;
+  int b, kvh, mb, tile, first, left;
   Scene s;
   // Cuts all tiles into even shares of `ctas` CTAs and stands at the first tile of share
   // `cta`, with its tiles to go (kOn: with all that follow). A warp; up to 32 scenes are
@@ -131,10 +131,10 @@ struct Walk {
   __device__ __forceinline__ Plan begin(const TreeArgs& a, int cta, int ctas, int lane) {
     Scene mine = {};
     if (lane < a.B) mine = scene_of(a, lane);
-    int n = mine.tiles * mine.units;
+    int n = mine.tiles * mine.mblocks * a.Hkv;
     for (int b0 = lane + 32; b0 < a.B; b0 += 32) {
       const Scene x = scene_of(a, b0);
-      n += x.tiles * x.units;
+      n += x.tiles * x.mblocks * a.Hkv;
     }
     Plan p;
     p.total = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<uint32_t>(n)));
@@ -149,7 +149,7 @@ struct Walk {
         mine = Scene{};
         if (b0 + lane < a.B) mine = scene_of(a, b0 + lane);
       }
-      const int own = mine.tiles * mine.units;
+      const int own = mine.tiles * mine.mblocks * a.Hkv;
       int upto = own;
 #pragma unroll
       for (int x = 1; x < 32; x <<= 1) {
@@ -163,9 +163,11 @@ struct Walk {
         s.n_keys = __shfl_sync(0xffffffffu, mine.n_keys, at);
         s.m = __shfl_sync(0xffffffffu, mine.m, at);
         s.tiles = __shfl_sync(0xffffffffu, mine.tiles, at);
-        s.units = __shfl_sync(0xffffffffu, mine.units, at);
+        s.mblocks = __shfl_sync(0xffffffffu, mine.mblocks, at);
         const int in = pos - before - __shfl_sync(0xffffffffu, upto - own, at);
-        unit = in / s.tiles;
+        const int unit = in / s.tiles;
+        kvh = unit / s.mblocks;
+        mb = unit - kvh * s.mblocks;
         tile = in - unit * s.tiles;
         first = pos - tile;
         return p;
@@ -175,14 +177,11 @@ struct Walk {
     left = 0;  // (only if a length changed under the kernel)
     return p;
   }
-  // Stands at the tiles that CTA `rank` of a cluster of `cs` takes of its unit. kvh, mb: the
-  // unit's place in scene b
-  __device__ __forceinline__ void begin_part(const TreeArgs& a, int scene, int kvh, int mb, int rank, int cs) {
-    b = scene;
+  // Stands at the tiles that CTA `rank` of a cluster of `cs` takes of a unit.
+  __device__ __forceinline__ void begin_part(const TreeArgs& a, int scene, int head, int block, int rank, int cs) {
+    b = scene, kvh = head, mb = block;
     s = scene_of(a, b);
-    const int mblocks = s.units / a.Hkv;
-    if (mb >= mblocks) s.tiles = 0;
-    unit = kvh * mblocks + mb;
+    if (mb >= s.mblocks) s.tiles = 0;
     const int each = s.tiles / cs, rest = s.tiles - each * cs;
     tile = rank * each + min(rank, rest);
     first = 0;
@@ -193,18 +192,20 @@ struct Walk {
     if (tile == s.tiles) {
       first += s.tiles;
       tile = 0;
-      if (++unit == s.units) {
-        unit = 0;
-        do {
-          if (++b >= a.B) return false;  // (only if a length changed under the kernel)
-          s = scene_of(a, b);
-        } while (s.tiles == 0);
+      if (++mb == s.mblocks) {
+        mb = 0;
+        if (++kvh == a.Hkv) {
+          kvh = 0;
+          do {
+            if (++b >= a.B) return false;  // (only if a length changed under the kernel)
+            s = scene_of(a, b);
+          } while (s.tiles == 0);
+        }
       }
     }
-    const int mblocks = s.units / a.Hkv;
     r.b = b;
-    r.kvh = unit / mblocks;
-    r.mb = unit - r.kvh * mblocks;
+    r.kvh = kvh;
+    r.mb = mb;
     r.n_keys = s.n_keys;
     r.m = s.m;
     r.tiles = s.tiles;
@@ -370,7 +371,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   Walk walk;
-  if (kCluster) walk.begin_part(a, blockIdx.z, blockIdx.y / a.mblocks, blockIdx.y % a.mblocks, blockIdx.x, gridDim.x);
+  const int unit_head = a.mblocks == 1 ? blockIdx.y : blockIdx.y / a.mblocks, unit_block = blockIdx.y - unit_head * a.mblocks;
+  if (kCluster) walk.begin_part(a, blockIdx.z, unit_head, unit_block, blockIdx.x, gridDim.x);
   else walk.begin<false>(a, blockIdx.x, gridDim.x, lane);
   tc_fence_before();
   __syncthreads();
@@ -920,7 +922,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (kCluster && parts > 1) {
     // ---- the cluster's parts: a CTA joins its share of the rows, a thread four columns of one
     const int n = parts;
-    const int M = walk.s.m * a.G, mb = blockIdx.y % a.mblocks, rows = min(a.rows, M - mb * a.rows), each = (rows + cs - 1) / cs;
+    const int M = walk.s.m * a.G, mb = unit_block, rows = min(a.rows, M - mb * a.rows), each = (rows + cs - 1) / cs;
     const int row0 = blockIdx.x * each, mine = min(each, rows - row0);
     for (int x = threadIdx.x; x < mine * (kDim / 4); x += kThreads) {
       const int row = row0 + x / (kDim / 4), c4 = x % (kDim / 4);
@@ -944,7 +946,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         j.add(ml, v);
       }
       const int pr = mb * a.rows + row, i = pr / a.G;
-      j.store(a.out + ((static_cast<long long>(blockIdx.z) * a.R + i) * a.Hq + (blockIdx.y / a.mblocks) * a.G + pr - i * a.G) * kDim + c4 * 4);
+      j.store(a.out + ((static_cast<long long>(blockIdx.z) * a.R + i) * a.Hq + unit_head * a.G + pr - i * a.G) * kDim + c4 * 4);
     }
     __syncwarp();
     cluster_arrive_relaxed();  // (its reads are done; nobody's memory goes before)
@@ -1166,6 +1168,7 @@ extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const 
   a.max_pages = cache->max_pages;
   a.cap = cap;
   a.rows = p.rows;
+  a.row_shift = 5 + p.variant;
   a.mblocks = p.mblocks;
   a.scale_log2 = scale_log2;
   a.inv_g = 1.0f / static_cast<float>(a.G);

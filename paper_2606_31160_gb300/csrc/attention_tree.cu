@@ -36,6 +36,7 @@
 
 #include <math.h>
 #include <algorithm>
+#include <type_traits>
 
 SD_DEFINE_ERROR_ACCESSOR(sd_take_error_attention_tree)
 
@@ -956,10 +957,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // The units that a share's border cuts: border c lies between shares c - 1 and c, and the
 // first one that cuts a unit joins its parts. A thread takes four columns of a row, rows along
-// the lanes (as the parts lie), and eight parts at once.
+// the lanes (as the parts lie), and eight parts, or four rows of two, at once.
 template <int kDim>
 __global__ void __launch_bounds__(kJoin) tree_join_kernel(const __grid_constant__ TreeArgs a, int ctas) {
-  constexpr int kRowsJ = kJoin / (kDim / 4), kBatch = 8;
+  constexpr int kRowsJ = kJoin / (kDim / 4);
   sd_pdl_enter();
   const int lane = threadIdx.x & 31, c = blockIdx.x + 1;
   Walk walk;
@@ -972,29 +973,43 @@ __global__ void __launch_bounds__(kJoin) tree_join_kernel(const __grid_constant_
   const size_t pf = part_floats(a.rows, kDim);
   // (the unit begins in its first share's second part, and goes on in the others' first)
   const float* part0 = a.part + 2 * static_cast<size_t>(share) * pf;
-  for (int row = blockIdx.y * kRowsJ + threadIdx.x % kRowsJ; row < rows; row += gridDim.y * kRowsJ) {
-    const float* at = part0 + (static_cast<size_t>(c4) * a.rows + row) * 4;
-    const float* at_ml = part0 + static_cast<size_t>(a.rows) * kDim + 2 * row;
-    Joined j;
-    for (int k0 = 0; k0 < n; k0 += kBatch) {
-      float4 v[kBatch];
-      float2 ml[kBatch];
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int k = k0 + u;
-        const size_t off = (2 * static_cast<size_t>(k) + (k == 0 ? 1 : 0)) * pf;
-        ml[u] = make_float2(-INFINITY, 0.f);
-        v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (k < n) {
-          ml[u] = __ldcg(reinterpret_cast<const float2*>(at_ml + off));
-          v[u] = __ldcg(reinterpret_cast<const float4*>(at + off));
-        }
-      }
-      j.add(ml, v);
-    }
+  const int step = gridDim.y * kRowsJ;
+  auto out_of = [&](int row) {
     const int p = r.mb * a.rows + row, i = p / a.G;
-    j.store(a.out + ((static_cast<long long>(r.b) * a.R + i) * a.Hq + r.kvh * a.G + p - i * a.G) * kDim + c4 * 4);
-  }
+    return a.out + ((static_cast<long long>(r.b) * a.R + i) * a.Hq + r.kvh * a.G + p - i * a.G) * kDim + c4 * 4;
+  };
+  // kRows rows and kParts parts at once
+  auto join = [&](auto rows_at, auto parts_at) {
+    constexpr int kRows = decltype(rows_at)::value, kParts = decltype(parts_at)::value;
+    for (int row0 = blockIdx.y * kRowsJ + threadIdx.x % kRowsJ; row0 < rows; row0 += kRows * step) {
+      Joined j[kRows];
+      for (int k0 = 0; k0 < n; k0 += kParts) {
+        float4 v[kRows][kParts];
+        float2 ml[kRows][kParts];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+#pragma unroll
+          for (int u = 0; u < kParts; ++u) {
+            const int row = row0 + i * step, k = k0 + u;
+            ml[i][u] = make_float2(-INFINITY, 0.f);
+            v[i][u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (k < n && row < rows) {
+              const float* part = part0 + (2 * static_cast<size_t>(k) + (k == 0 ? 1 : 0)) * pf;
+              ml[i][u] = __ldcg(reinterpret_cast<const float2*>(part + static_cast<size_t>(a.rows) * kDim) + row);
+              v[i][u] = __ldcg(reinterpret_cast<const float4*>(part) + static_cast<size_t>(c4) * a.rows + row);
+            }
+          }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) j[i].add(ml[i], v[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kRows; ++i)
+        if (row0 + i * step < rows) j[i].store(out_of(row0 + i * step));
+    }
+  };
+  // (a unit cut once has two parts: then more rows instead)
+  if (n == 2) join(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
+  else join(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
 }
 
 // ------------------------------------------------------------------ host

@@ -587,7 +587,8 @@ typedef struct {
  *   k_new, v_new: [B][R][Hkv][D] bf16, read only; row (b, i) begins k_stride (v_stride)
  *   elements after the one before it, a multiple of 8, at least Hkv * D.
  *   q: [B][R][Hq][D] bf16, rows q_stride elements apart, or NULL (with Hq = 0): no queries.
- *   q_out: the rotated queries, [B][R][Hq][D] contiguous; NULL: in place of q.
+ *   q_out: the rotated queries, [B][R][Hq][D] contiguous; NULL: in place of q. It must not
+ *   overlap k_new, v_new or (but for q_out = q, rows Hq * D apart) q.
  *   pos, sections, interleaved, base: as for sd_rope_apply; pos NULL: nothing is
  *   rotated (then q must be NULL).
  * Writes row i of scene b at position len[b] + i, then len[b] += n_new[b]. A scene with
@@ -607,7 +608,9 @@ sd_status sd_paged_append(const sd_paged_cache* cache, const void* k_new, long l
  * ancestors j of row i. With parents NULL it is sd_verify_attention's causal mask.
  *   q: [B][R][Hq][D] bf16 (rotated), rows q_stride elements apart, a multiple of 8;
  *   out: [B][R][Hq][D] bf16, contiguous; scale: 0 selects 1/sqrt(D).
- * What a row does not see does not reach it, infinities and NaN included.
+ * What a row does not see does not reach it, infinities and NaN included; an infinite
+ * value that it sees makes that column infinite or NaN. Weights are bf16 (relative to the
+ * row's reference), scores and sums fp32, and the sum is of the rounded weights.
  * workspace: sd_tree_attention_workspace bytes (0: none is used) of device memory,
  * 16-byte aligned, of any content; calls that share one must not overlap on the device.
  * Hq % Hkv == 0, R <= 256. A scene with len[b] < n_new[b] or len[b] > max_pages * page

@@ -8,6 +8,9 @@
 // scene's last CTA (a ticket, no spin) walks the tree over the keys and re-arms the
 // workspace. The order of the keys is total, so the result does not depend on the order in
 // which they come. CTAs of rows that do not count end at once.
+// Bound by the logits' bytes where they are many (16 ragged scenes of up to 61 rows x 151936
+// fp32, 329 MB: 56 us, 0.88 of a copy's rate); one scene's 26 rows of bf16 (7.9 MB) take 8.7 us:
+// the scan, the ticket, the keys, the walk, one after the other.
 #include "row_scan.cuh"
 
 #include <algorithm>
@@ -106,7 +109,8 @@ __global__ void __launch_bounds__(kThreads) accept_tree_kernel(const T* logits, 
 }
 
 // Vectors a segment: about six CTAs an SM over all rows and at least 16 KB (one step of every
-// thread) a segment; where rows do not count the CTAs left would be uneven, so three times as many.
+// thread) a segment; where rows do not count the CTAs left would be uneven, so three times as many
+// (16 ragged scenes: 57.4 -> 56.1 us; 26 rows that all count 8.7 -> 8.8).
 int segment_vectors(int B, int R, int V, int elem_bytes, bool ragged) {
   const long long row = (static_cast<long long>(V) * elem_bytes + 15) / 16;
   const long long ctas = (ragged ? 18LL : 6LL) * sd_num_sms();

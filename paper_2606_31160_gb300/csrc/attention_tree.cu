@@ -29,6 +29,15 @@
 // of all units, one unit after the other, in one even share each; a unit that a share's border
 // cuts leaves its parts in the workspace, and a second kernel joins them.
 //
+// What it takes on a GB300 (cold inputs, the device alone), and what bounds it. 32 ragged scenes
+// of up to 8192 keys, 61 rows, 32 / 8 heads x 128 (1.0 GB): 209 us, 4.8 TB/s or 0.72 of a copy's
+// rate. A pair of row tiles takes ~3350 cycles a key tile, of which the exponentials (16 a cycle
+// and SM) need 2048 and the products 2048: a group's weights (~1400) wait for its S, and its PV
+// and next S (~1400) for the weights, and only the other group's stand between. One scene of
+// 131072 keys and 8 rows: 94 us, 0.86 of the copy's rate on 96 SMs. One scene of 4096 keys is
+// one launch of dependent phases, 1 row 10.2 us, 26 rows 13.8 (the cluster's join of 104 rows a
+// head, ~10 bytes a cycle and SM, a quarter of it).
+//
 // What a row does not see does not reach it: hidden scores are replaced before the maximum,
 // and in the tiles that hold new rows, values that are no numbers are taken out of V (0 times
 // them would be NaN) and added at the end to the rows that see them.
@@ -388,7 +397,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == kProducer || (kQ == 1 && warp == kSecond)) {
     // -------------------------------------------------------------- producers
     // of keys and values: with one row tile and many copies a tile (~60 cycles each to issue;
-    // pages of 16 rows take 16) each its own
+    // pages of 16 rows take 16) each its own (one scene of 4096 keys in such pages, 1 row: 10.5 ->
+    // 10.2 us; with pages of 64 and 128 rows no difference)
     const bool keys = warp == kProducer;
     const bool apart = kQ == 1 && (kTile >> a.shift) * (kDim / 64) >= 8, values = keys != apart;
     if (!keys && !values) walk.left = 0;
@@ -957,7 +967,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // The units that a share's border cuts: border c lies between shares c - 1 and c, and the
 // first one that cuts a unit joins its parts. A thread takes four columns of a row, rows along
-// the lanes (as the parts lie), and eight parts, or four rows of two, at once.
+// the lanes (as the parts lie), and eight parts, or four rows of two, at once: with 39 MB of parts
+// of two (32 scenes, 61 rows) it waits for memory, 15 us cold, 22 with one row at a time.
 template <int kDim>
 __global__ void __launch_bounds__(kJoin) tree_join_kernel(const __grid_constant__ TreeArgs a, int ctas) {
   constexpr int kRowsJ = kJoin / (kDim / 4);
@@ -1098,6 +1109,8 @@ sd_status host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) 
   if (cap > 0x7fffff00) return SD_ERR_UNSUPPORTED;
   DevState* dev = state();
   if (!dev) return SD_ERR_CUDA;
+  // copies where they fit (4096 keys, 4 packed rows: 10.8 -> 10.2 us; 131072 keys, 32: 98.6 ->
+  // 93.7), two row tiles past one (32 scenes, 244 rows: 209 us, as two m-blocks 263)
   p->variant = M <= 32 ? 0 : M <= 64 ? 1 : M <= 128 ? 2 : 3;
   p->rows = 32 << p->variant;
   const long long blocks = (M + p->rows - 1) / p->rows, units = blocks * B * Hkv;
@@ -1108,7 +1121,8 @@ sd_status host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) 
   // 8192 keys: a CTA's tile, its first queries to its last output, the exchange in a cluster,
   // the joining kernel; and never less than all tiles' bytes take. (32 query / 8 KV heads x 128,
   // clusters / even shares: 26 rows and 4096 keys, 1 scene 16 / 37, 12 scenes 43 / 50, 20
-  // scenes 81 / 71; 61 rows, 32 scenes of 512 keys 46 / 65, of 8192 233 / 216.)
+  // scenes 81 / 71; 61 rows, 32 scenes of 512 keys 46 / 65, of 8192 233 / 209; 8 rows, 131072
+  // keys 94 / 100, where clusters of 8 take 129, of 16 146.)
   struct Cost {
     double tile, unit, exchange, join;
   };

@@ -9,10 +9,13 @@
 // chunks are rotated between (the angles as in the rotation kernel, bit for bit). A scene
 // with a page out of range is left untouched, so every CTA looks at all the pages that the
 // scene's new rows take before it writes. The scene's last CTA (a ticket) moves the length.
+// Long calls are bound by the bytes: 8192 rows of 32 + 8 + 8 heads x 128, 201 MB, 36.2 us, 0.83 of
+// a copy's rate. 8 rows take 4.4 us: length, pages, rows, ticket.
 //
 // Commit. Row first + path[i] moves to first + i. The path ascends, so path[i] >= i, and a
 // thread that takes one 16-byte column of a head's rows in order, some at a time, never
-// reads a row that it has written.
+// reads a row that it has written. 36 caches at once: one scene 7.8 us, 32 scenes of up to 61
+// rows 13 us; round trips (length, path, pages, rows, ticket), not bytes (0.9 and 18 MB).
 #include "common.cuh"
 
 #include <math.h>
@@ -320,7 +323,8 @@ extern "C" sd_status sd_paged_append(const sd_paged_cache* cache, const void* k_
   a.R = R;
   a.Hq = Hq;
   // heads a thread: one where the call is short, so that many threads share its latency; four
-  // or eight where it is long: the angles of a row are taken once for them
+  // or eight where it is long: the angles of a row are taken once for them (1, 4, 8 heads: 8 rows
+  // of 48 heads 4.4, 5.1, 5.6 us; 32 ragged trees of 36 heads x 64 10.0, 7.4, 7.8; 8192 rows of 48 92, 38.2, 36.2)
   const long long heads = Hq + 2ll * Hkv, per_cta = kThreads / (D / 8), sms = sd_num_sms();
   const long long ctas = static_cast<long long>(B) * R * heads / per_cta;
   const int per = ctas >= 16 * sms ? 8 : ctas >= 4 * sms ? 4 : 1;

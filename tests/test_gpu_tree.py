@@ -141,6 +141,26 @@ def test_masked_infinities_and_nan(Hq, Hkv, R, D):
 
 
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("R", [1, 14, 30, 60])
+@pytest.mark.parametrize("at", [0, 200])
+def test_values_of_the_prefix_that_are_no_numbers(R, D, at):
+    """They reach every row of their KV head, in their column alone; a key's, all columns."""
+    g = torch.Generator(device="cuda").manual_seed(R)
+    prefix, parents = 300, make_tree(np.random.default_rng(R), R)
+    cache = make_cache(g, [prefix + R], prefix + R, 3, D, 32)
+    t = cache.table[0]
+    cache.v[t[at // 32], 0, at % 32, 7] = float("inf")
+    cache.v[t[at // 32], 1, at % 32, 9] = float("nan")
+    cache.k[t[at // 32], 2, at % 32, 5] = float("nan")
+    q = _randn(g, 1, R, 12, D)
+    out = sd.tree_attention(q, cache, parents=_i32(parents[None]))
+    assert sd.get_device_error() == 0
+    want = torch.ones((R, 12, D), dtype=torch.bool, device="cuda")
+    want[:, :4, 7] = want[:, 4:8, 9] = want[:, 8:] = False
+    assert torch.equal(out[0].isfinite(), want)
+
+
+@pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("R", [1, 9, 40])
 def test_scores_far_from_zero_and_rising(R, D):
     """Keys whose scores rise along the cache, jump late, or lie far below 0; -inf scores."""

@@ -35,8 +35,8 @@
 // and SM) need 2048 and the products 2048: a group's weights (~1400) wait for its S, and its PV
 // and next S (~1400) for the weights, and only the other group's stand between. One scene of
 // 131072 keys and 8 rows: 94 us, 0.86 of the copy's rate on 96 SMs. One scene of 4096 keys is
-// one launch of dependent phases, 1 row 10.2 us, 26 rows 13.8 (the cluster's join of 104 rows a
-// head, ~10 bytes a cycle and SM, a quarter of it).
+// one launch of dependent phases, 1 row 9.8 us, 26 rows 13.6 (the cluster's join of 104 rows a
+// head, 55 KB into every CTA at ~16 bytes a cycle, a quarter of it).
 //
 // What a row does not see does not reach it: hidden scores are replaced before the maximum,
 // and in the tiles that hold new rows, values that are no numbers are taken out of V (0 times
@@ -876,6 +876,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int c = g * 32; c < kWide; c += 64) {  // 32 columns a group
             float x[32];
             joined(round * kWide + c, x);
+            if (live)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
               *reinterpret_cast<float4*>(stage + rl * kWide + ((((c >> 2) + j) ^ (rl & 7)) << 2)) =
@@ -883,9 +884,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           __syncwarp();
           named_bar_sync(1, kSoft);
-          for (int x = threadIdx.x; x < C::kRows * (kWide / 4); x += kSoft) {
-            // (rows along the lanes for the parts, columns for the output)
-            const int rr = whole ? x / (kWide / 4) : x % C::kRows, c4 = whole ? x % (kWide / 4) : x / C::kRows;
+          const bool wide = kCluster || whole;
+          for (int x = threadIdx.x; x < (wide ? min(C::kRows, M - r.mb * a.rows) : C::kRows) * (kWide / 4); x += kSoft) {
+            // (rows along the lanes for the workspace's parts, else columns)
+            const int rr = wide ? x / (kWide / 4) : x % C::kRows, c4 = wide ? x % (kWide / 4) : x / C::kRows;
             const int pr = r.mb * a.rows + rr, d = round * kWide + c4 * 4;
             if (pr >= M) continue;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -939,7 +941,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int row = row0 + x / (kDim / 4), c4 = x % (kDim / 4);
       const uint32_t at = base + cluster_o<kDim>(row, c4), at_ml = base + cluster_ml<kDim>(a.rows, row);
       Joined j;
-      constexpr int kBatch = 16;
+      constexpr int kBatch = 4;  // (in a loop: 16 at once, in line, took 13.8 for 13.6 us)
+#pragma unroll 1
       for (int k0 = 0; k0 < n; k0 += kBatch) {
         float4 v[kBatch];
         float2 ml[kBatch];

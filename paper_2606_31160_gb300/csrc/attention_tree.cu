@@ -30,12 +30,12 @@
 // cuts leaves its parts in the workspace, and a second kernel joins them.
 //
 // What it takes on a GB300 (cold inputs, the device alone), and what bounds it. 32 ragged scenes
-// of up to 8192 keys, 61 rows, 32 / 8 heads x 128 (1.0 GB): 209 us, 4.8 TB/s or 0.72 of a copy's
-// rate. A pair of row tiles takes ~3350 cycles a key tile, of which the exponentials (16 a cycle
-// and SM) need 2048 and the products 2048: a group's weights (~1400) wait for its S, and its PV
-// and next S (~1400) for the weights, and only the other group's stand between. One scene of
+// of up to 8192 keys, 61 rows, 32 / 8 heads x 128 (1.0 GB): 204 us, 4.9 TB/s or 0.74 of a copy's
+// rate. A pair of row tiles takes ~2960 cycles a key tile, of which the exponentials (16 a cycle
+// and SM) need 2048 and the products 2048: a group's weights (1280) wait for its S, and its PV
+// and next S (1650) for the weights, and only the other group's stand between. One scene of
 // 131072 keys and 8 rows: 94 us, 0.86 of the copy's rate on 96 SMs. One scene of 4096 keys is
-// one launch of dependent phases, 1 row 9.8 us, 26 rows 13.6 (the cluster's join of 104 rows a
+// one launch of dependent phases, 1 row 9.8 us, 26 rows 13.3 (the cluster's join of 104 rows a
 // head, 55 KB into every CTA at ~16 bytes a cycle, a quarter of it).
 //
 // What a row does not see does not reach it: hidden scores are replaced before the maximum,
@@ -724,21 +724,28 @@ __global__ void __launch_bounds__(kThreads, 1)
           const float sub = m_ref == -INFINITY ? 0.f : -m_ref;
 #pragma unroll
           for (int j = 0; j < 4; ++j) sum[j] = 0.f;
-          uint32_t s[2][32];
-          tmem_load_begin(ts + copy * C::kCols, s[0]);
+          // (32 scores at a time left gaps at their waits: a turn took 1430 cycles for 1203; 128: 1315)
+          constexpr int kAtOnce = kWords < 2 ? 1 : 2;
 #pragma unroll
-          for (int c = 0; c < kWords; ++c) {
-            tmem_wait_load(s[c & 1]);
-            if (c + 1 < kWords) tmem_load_begin(ts + copy * C::kCols + 32 * (c + 1), s[(c + 1) & 1]);
-            hide(c, s[c & 1]);
+          for (int c0 = 0; c0 < kWords; c0 += kAtOnce) {
+            uint32_t s[kAtOnce][32];
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float2 y = fma2(make_float2(__uint_as_float(s[c & 1][j]), __uint_as_float(s[c & 1][j + 1])),
-                                    make_float2(sl, sl), make_float2(sub, sub));
-              const uint32_t w = cvt_bf16x2(ex2(y.x), ex2(y.y));
-              pw[16 * c + j / 2] = w;
-              add_pair(w, sum[j & 2], sum[(j & 2) + 1]);
+            for (int c = 0; c < kAtOnce; ++c) tmem_load_begin(ts + copy * C::kCols + 32 * (c0 + c), s[c]);
+#pragma unroll
+            for (int c = 0; c < kAtOnce; ++c) {
+              tmem_wait_load(s[c]);
+              hide(c0 + c, s[c]);
             }
+#pragma unroll
+            for (int c = 0; c < kAtOnce; ++c)
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) {
+                const float2 y = fma2(make_float2(__uint_as_float(s[c][j]), __uint_as_float(s[c][j + 1])),
+                                      make_float2(sl, sl), make_float2(sub, sub));
+                const uint32_t w = cvt_bf16x2(ex2(y.x), ex2(y.y));
+                pw[16 * (c0 + c) + j / 2] = w;
+                add_pair(w, sum[j & 2], sum[(j & 2) + 1]);
+              }
           }
           if (again || !__any_sync(0xffffffffu, (sum[0] + sum[1]) + (sum[2] + sum[3]) > 0x1p16f)) break;
           move_reference();

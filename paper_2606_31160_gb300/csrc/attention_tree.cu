@@ -30,12 +30,12 @@
 // cuts leaves its parts in the workspace, and a second kernel joins them.
 //
 // What it takes on a GB300 (cold inputs, the device alone), and what bounds it. 32 ragged scenes
-// of up to 8192 keys, 61 rows, 32 / 8 heads x 128 (1.0 GB): 204 us, 4.9 TB/s or 0.74 of a copy's
+// of up to 8192 keys, 61 rows, 32 / 8 heads x 128 (1.0 GB): 205 us, 4.9 TB/s or 0.73 of a copy's
 // rate. A pair of row tiles takes ~2960 cycles a key tile, of which the exponentials (16 a cycle
 // and SM) need 2048 and the products 2048: a group's weights (1280) wait for its S, and its PV
 // and next S (1650) for the weights, and only the other group's stand between. One scene of
 // 131072 keys and 8 rows: 94 us, 0.86 of the copy's rate on 96 SMs. One scene of 4096 keys is
-// one launch of dependent phases, 1 row 9.8 us, 26 rows 13.3 (the cluster's join of 104 rows a
+// one launch of dependent phases, 1 row 9.8 us, 26 rows 13.2 (the cluster's join of 104 rows a
 // head, 55 KB into every CTA at ~16 bytes a cycle, a quarter of it).
 //
 // What a row does not see does not reach it: hidden scores are replaced before the maximum,
@@ -1120,7 +1120,7 @@ sd_status host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) 
   DevState* dev = state();
   if (!dev) return SD_ERR_CUDA;
   // copies where they fit (4096 keys, 4 packed rows: 10.8 -> 10.2 us; 131072 keys, 32: 98.6 ->
-  // 93.7), two row tiles past one (32 scenes, 244 rows: 209 us, as two m-blocks 263)
+  // 93.7), two row tiles past one (32 scenes, 244 rows: 209 us, as two m-blocks 263; 205 now)
   p->variant = M <= 32 ? 0 : M <= 64 ? 1 : M <= 128 ? 2 : 3;
   p->rows = 32 << p->variant;
   const long long blocks = (M + p->rows - 1) / p->rows, units = blocks * B * Hkv;
@@ -1131,7 +1131,7 @@ sd_status host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) 
   // 8192 keys: a CTA's tile, its first queries to its last output, the exchange in a cluster,
   // the joining kernel; and never less than all tiles' bytes take. (32 query / 8 KV heads x 128,
   // clusters / even shares: 26 rows and 4096 keys, 1 scene 16 / 37, 12 scenes 43 / 50, 20
-  // scenes 81 / 71; 61 rows, 32 scenes of 512 keys 46 / 65, of 8192 233 / 209; 8 rows, 131072
+  // scenes 81 / 71; 61 rows, 32 scenes of 512 keys 46 / 65, of 8192 232 / 205; 8 rows, 131072
   // keys 94 / 100, where clusters of 8 take 129, of 16 146.)
   struct Cost {
     double tile, unit, exchange, join;

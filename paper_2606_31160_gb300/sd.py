@@ -641,6 +641,14 @@ def _ints(t, name, shape, device):
     return t.data_ptr()
 
 
+def _ws(ws, device):
+    """Address and bytes of a workspace on this device."""
+    ptr = _dev(ws, "ws")
+    if ws.get_device() != device:
+        raise ValueError("ws must be on the caller's device")
+    return ptr, ws.numel() * ws.element_size()
+
+
 def _row_stride(t, name, shape, device):
     """Address and row stride of bf16 rows [B, R, H, D] whose last two dims are contiguous
     and whose rows are evenly spaced (part of a projection's output)."""
@@ -723,10 +731,10 @@ def tree_attention(q, cache, parents=None, n_new=None, out=None, scale=0.0, ws=N
         need = lib().sd_tree_attention_workspace(B, R, Hq, H, D, cap)
         if need:
             ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    wp, nbytes = (None, 0) if ws is None else _ws(ws, dev)
     _check(lib().sd_tree_attention(qp, qs, cache._ref, _ints(parents, "parents", (B, R), dev),
                                    _ints(n_new, "n_new", (B,), dev), _dev(out, "out", torch.bfloat16), R, Hq, float(scale),
-                                   None if ws is None else _dev(ws, "ws"), 0 if ws is None else ws.numel() * ws.element_size(),
-                                   stream), "sd_tree_attention")
+                                   wp, nbytes, stream), "sd_tree_attention")
     return out
 
 
@@ -759,8 +767,8 @@ def accept_tree(logits, tokens, parents=None, n_new=None, ws=None, n_emit=None, 
     wide, at = (B, R), dev.index
     _check(lib().sd_accept_tree(ptr, dt, B, R, V, stride, _ints(tokens, "tokens", wide, at), _ints(parents, "parents", wide, at),
                                 _ints(n_new, "n_new", (B,), at), _ints(n_emit, "n_emit", (B,), at), _ints(path, "path", wide, at),
-                                _ints(out, "out", wide, at), _ints(argmax, "argmax", wide, at), _dev(ws, "ws"),
-                                ws.numel() * ws.element_size(), stream), "sd_accept_tree")
+                                _ints(out, "out", wide, at), _ints(argmax, "argmax", wide, at), *_ws(ws, at), stream),
+           "sd_accept_tree")
     return n_emit, path, out, argmax
 
 

@@ -49,7 +49,9 @@ class PagedTreeTarget:
 
 def depths(parents):
     """Rows between each row and the prefix, [B, R]: its position is the prefix's length plus
-    that."""
+    that. Parents of rows that do not count may be anything: one that is not an earlier row is
+    not followed."""
+    parents = torch.where(parents < torch.arange(parents.shape[1], device=parents.device), parents, -1)
     at, depth = parents, torch.zeros_like(parents)
     while bool((at >= 0).any()):
         depth += (at >= 0).to(depth.dtype)

@@ -611,8 +611,12 @@ sd_status sd_paged_append(const sd_paged_cache* cache, const void* k_new, long l
  * What a row does not see does not reach it, infinities and NaN included; an infinite
  * value that it sees makes that column infinite or NaN. Weights are bf16 (relative to the
  * row's reference), scores and sums fp32, and the sum is of the rounded weights.
- * workspace: sd_tree_attention_workspace bytes (0: none is used) of device memory,
- * 16-byte aligned, of any content; calls that share one must not overlap on the device.
+ * workspace: device memory, 16-byte aligned, of any content; calls that share one must not
+ * overlap on the device. sd_tree_attention_workspace gives the most bytes that a call of up to
+ * B scenes and R rows takes over a cache of these heads whose max_pages * page is at most
+ * `capacity`, on the current device (0: none), so that one workspace serves every smaller call
+ * too. Many calls (those of few scenes) take none, and then it may be NULL or too short; one
+ * that needs more than ws_bytes returns SD_ERR_WORKSPACE.
  * Hq % Hkv == 0, R <= 256. A scene with len[b] < n_new[b] or len[b] > max_pages * page
  * sets SD_DEVERR_LENGTH; its output, as that of one whose tree is not valid, is left
  * unwritten. Where a page is not valid the scene's output is NaN.

@@ -1111,22 +1111,36 @@ DevState* state() {
 struct HostPlan {
   int variant, rows, mblocks;  // copies 4, 2, 1, two row tiles; packed rows of an m-block
   int cs, ctas;                // CTAs a cluster; 0: even shares over ctas
-  size_t ws_bytes;
+  long long units, tiles;
+  size_t ws_bytes;             // what even shares leave to the joining kernel
 };
 
-sd_status host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) {
-  const long long M = static_cast<long long>(Hq / Hkv) * R, tiles = (static_cast<long long>(cap) + kTile - 1) / kTile;
+// What does not hang on the way that is chosen, for a device of `sms` SMs. ws_bytes grows with
+// each of B, R and cap.
+sd_status host_shape(int B, int R, int Hq, int Hkv, int D, int cap, int sms, HostPlan* p) {
+  const long long M = static_cast<long long>(Hq / Hkv) * R;
+  p->tiles = (static_cast<long long>(cap) + kTile - 1) / kTile;
   if (cap > 0x7fffff00) return SD_ERR_UNSUPPORTED;
-  DevState* dev = state();
-  if (!dev) return SD_ERR_CUDA;
   // copies where they fit (4096 keys, 4 packed rows: 10.8 -> 10.2 us; 131072 keys, 32: 98.6 ->
   // 93.7), two row tiles past one (32 scenes, 244 rows: 209 us, as two m-blocks 263; 205 now)
   p->variant = M <= 32 ? 0 : M <= 64 ? 1 : M <= 128 ? 2 : 3;
   p->rows = 32 << p->variant;
-  const long long blocks = (M + p->rows - 1) / p->rows, units = blocks * B * Hkv;
-  if (units > 0x7fffffffll / tiles) return SD_ERR_UNSUPPORTED;
+  const long long blocks = (M + p->rows - 1) / p->rows;
+  p->units = blocks * B * Hkv;
+  if (p->units > 0x7fffffffll / p->tiles) return SD_ERR_UNSUPPORTED;
   p->mblocks = static_cast<int>(blocks);
-  p->ctas = static_cast<int>(std::min<long long>(std::min(sd_num_sms(), kMaxCtas), units * tiles));
+  p->ctas = static_cast<int>(std::min<long long>(std::min(sms, kMaxCtas), p->units * p->tiles));
+  // (one tile a unit: no share's border cuts one)
+  p->ws_bytes = p->tiles > 1 ? 2 * static_cast<size_t>(p->ctas) * part_floats(p->rows, D) * sizeof(float) : 0;
+  return SD_OK;
+}
+
+sd_status host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) {
+  const sd_status s = host_shape(B, R, Hq, Hkv, D, cap, sd_num_sms(), p);
+  if (s != SD_OK) return s;
+  const long long units = p->units, tiles = p->tiles, blocks = p->mblocks;
+  DevState* dev = state();
+  if (!dev) return SD_ERR_CUDA;
   // The way of least estimated time, in us, from what each took over 1 to 32 scenes of 512 to
   // 8192 keys: a CTA's tile, its first queries to its last output, the exchange in a cluster,
   // the joining kernel; and never less than all tiles' bytes take. (32 query / 8 KV heads x 128,
@@ -1152,8 +1166,7 @@ sd_status host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) 
       const double cost = std::max(stream + c.unit, waves * ((tiles + cs - 1) / cs * c.tile + c.unit + (cs > 1 ? c.exchange : 0.0)));
       if (cost < best) best = cost, p->cs = cs;
     }
-  // one tile a unit: no share's border cuts one
-  p->ws_bytes = p->cs == 0 && tiles > 1 ? 2 * static_cast<size_t>(p->ctas) * part_floats(p->rows, D) * sizeof(float) : 0;
+  if (p->cs > 0) p->ws_bytes = 0;
   return SD_OK;
 }
 
@@ -1162,8 +1175,10 @@ sd_status host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) 
 extern "C" size_t sd_tree_attention_workspace(int B, int R, int Hq, int Hkv, int D, int capacity) {
   if (B <= 0 || R <= 0 || R > kMaxRows || Hkv <= 0 || Hq <= 0 || Hq % Hkv || Hq / Hkv > 4095 || (D != 64 && D != 128) || capacity <= 0)
     return 0;
+  // enough for even shares, whatever the way: the estimate goes from one to the other and back as B
+  // and R grow, and a workspace of the largest call has to serve the smaller ones
   HostPlan p = {};
-  return host_plan(B, R, Hq, Hkv, D, capacity, &p) == SD_OK ? p.ws_bytes : 0;
+  return host_shape(B, R, Hq, Hkv, D, capacity, state() ? sd_num_sms() : kMaxCtas, &p) == SD_OK ? p.ws_bytes : 0;
 }
 
 extern "C" sd_status sd_tree_attention(const void* q, long long q_stride, const sd_paged_cache* cache,

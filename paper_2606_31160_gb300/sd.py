@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(_PKG, "libsd.so")
 HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "sd.h")
 
 SD_BF16, SD_F32 = 0, 1
+SD_ERR_WORKSPACE = 3
 SD_DEVERR_KV_OVERFLOW = 0x1
 SD_DEVERR_ROLLBACK = 0x2
 SD_DEVERR_TOKEN_RANGE = 0x4
@@ -706,6 +707,7 @@ def paged_append(cache, k_new, v_new, q=None, pos=None, sections=None, interleav
 
 
 def tree_attention_workspace_bytes(B, R, Hq, Hkv, D, capacity):
+    """The most that a call of up to B scenes, R rows and capacity (max_pages * page) rows takes."""
     return int(lib().sd_tree_attention_workspace(B, R, Hq, Hkv, D, capacity))
 
 
@@ -714,8 +716,8 @@ def tree_attention(q, cache, parents=None, n_new=None, out=None, scale=0.0, ws=N
     holds them: a row sees the prefix, its ancestors and itself. parents [B,R] int32: the
     earlier row that each row follows, -1 for the prefix; None: a chain. n_new: int32 [B]
     rows of each scene that count, or all. ws: tree_attention_workspace_bytes of device
-    memory; when None a call that takes one has it from torch's allocator, on the current
-    stream."""
+    memory (of the largest call, where it serves several); when None a call that takes one has
+    it from torch's allocator, on the current stream."""
     B, H, cap, D = cache._shape
     dev = cache._device
     stream = _stream_on(dev)
@@ -727,14 +729,13 @@ def tree_attention(q, cache, parents=None, n_new=None, out=None, scale=0.0, ws=N
         out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
     elif out.shape != q.shape or out.get_device() != dev:
         raise ValueError("out must have q's shape and device")
-    if ws is None:
-        need = lib().sd_tree_attention_workspace(B, R, Hq, H, D, cap)
-        if need:
-            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-    wp, nbytes = (None, 0) if ws is None else _ws(ws, dev)
-    _check(lib().sd_tree_attention(qp, qs, cache._ref, _ints(parents, "parents", (B, R), dev),
-                                   _ints(n_new, "n_new", (B,), dev), _dev(out, "out", torch.bfloat16), R, Hq, float(scale),
-                                   wp, nbytes, stream), "sd_tree_attention")
+    args = (qp, qs, cache._ref, _ints(parents, "parents", (B, R), dev), _ints(n_new, "n_new", (B,), dev),
+            _dev(out, "out", torch.bfloat16), R, Hq, float(scale))
+    status = lib().sd_tree_attention(*args, *((None, 0) if ws is None else _ws(ws, dev)), stream)
+    if status == SD_ERR_WORKSPACE and ws is None:  # (nothing was launched; most calls take none)
+        ws = torch.empty(tree_attention_workspace_bytes(B, R, Hq, H, D, cap), dtype=torch.uint8, device=q.device)
+        status = lib().sd_tree_attention(*args, *_ws(ws, dev), stream)
+    _check(status, "sd_tree_attention")
     return out
 
 

@@ -593,7 +593,8 @@ typedef struct {
  *   rotated (then q must be NULL).
  * Writes row i of scene b at position len[b] + i, then len[b] += n_new[b]. A scene with
  * len[b] + n_new[b] > max_pages * page sets SD_DEVERR_KV_OVERFLOW; it, and one with
- * another error, is left untouched, its queries too.
+ * another error, is left untouched, its queries too. With no rows or no scenes nothing is
+ * done, and the addresses of rows (positions and queries among them) may be NULL.
  */
 sd_status sd_paged_append(const sd_paged_cache* cache, const void* k_new, long long k_stride, const void* v_new,
                           long long v_stride, void* q, long long q_stride, void* q_out, int R, int Hq,

@@ -289,7 +289,7 @@ extern "C" sd_status sd_paged_append(const sd_paged_cache* cache, const void* k_
   const sd_status s = sd_internal_paged_check(cache);
   if (s != SD_OK) return s;
   const int B = cache->batch, Hkv = cache->n_kv_heads, D = cache->head_dim;
-  if (R < 0 || Hq < 0 || (Hq > 0) != (q != nullptr) || (q_out && !q) || (q && !pos)) return SD_ERR_INVALID_ARG;
+  if (R < 0 || Hq < 0) return SD_ERR_INVALID_ARG;
   if (interleaved != 0 && interleaved != 1) return SD_ERR_INVALID_ARG;
   static const RopeTable kNone = {};
   const RopeTable* tab = &kNone;
@@ -301,7 +301,8 @@ extern "C" sd_status sd_paged_append(const sd_paged_cache* cache, const void* k_
   if (k_stride < static_cast<long long>(Hkv) * D || v_stride < static_cast<long long>(Hkv) * D || k_stride % 8 || v_stride % 8 ||
       (q && (q_stride < static_cast<long long>(Hq) * D || q_stride % 8)))
     return SD_ERR_INVALID_ARG;
-  if (B == 0 || R == 0) return SD_OK;
+  if (B == 0 || R == 0) return SD_OK;  // (the addresses of nothing may be NULL)
+  if ((Hq > 0) != (q != nullptr) || (q_out && !q) || (q && !pos)) return SD_ERR_INVALID_ARG;
   if (!k_new || !v_new || !sd_aligned16(k_new) || !sd_aligned16(v_new) || !sd_aligned16(q) || !sd_aligned16(q_out))
     return SD_ERR_INVALID_ARG;
   AppendArgs a = {};

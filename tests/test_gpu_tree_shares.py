@@ -78,3 +78,43 @@ def test_no_numbers_in_shares(B, R, Hq, Hkv, D, L):
     assert sd.get_device_error() == 0
     for b in range(0, B, 3):
         check_scene(out, q, cache, b, parents[b], R)
+
+
+WIDE = [(1, 1, 16, 4, 128, 300, 131072), (1, 9, 16, 4, 128, 2000, 131072), (2, 26, 32, 8, 128, 129, 65536),
+        (3, 61, 16, 4, 128, 640, 65536), (2, 130, 8, 2, 128, 1500, 131072), (1, 5, 8, 4, 64, 1, 131072),
+        (2, 13, 28, 4, 64, 777, 131072), (3, 40, 32, 4, 64, 513, 131072), (4, 12, 32, 8, 64, 128, 65536)]
+
+
+@pytest.mark.parametrize("B,R,Hq,Hkv,D,keys,width", WIDE)
+def test_tables_wider_than_the_keys(B, R, Hq, Hkv, D, keys, width):
+    """A table as wide as a long context, with few keys in it. Most of these are served in shares,
+    fewer tiles than CTAs, one a share, units of many parts; the others in clusters of which not
+    every CTA has a tile. What lies past a scene's pages is anything."""
+    g = torch.Generator(device="cuda").manual_seed(keys)
+    rng = np.random.default_rng(keys)
+    lens = rng.integers(0, keys + 1, B) + R
+    lens[-1] = keys + R
+    small = make_cache(g, lens, keys + R, Hkv, D, 64)
+    table = torch.full((B, width // 64), -1, dtype=torch.int32, device="cuda")
+    table[:, 1::2] = 1 << 30
+    table[:, :small.table.shape[1]] = small.table
+    cache = sd.PagedKVCache(small.k, small.v, table, small.len)
+    parents = np.stack([make_tree(rng, R, forest=True) for _ in range(B)])
+    q = _randn(g, B, R, Hq, D)
+    ws = torch.full((sd.tree_attention_workspace_bytes(B, R, Hq, Hkv, D, width),), 0xFF, dtype=torch.uint8, device="cuda")
+    out = sd.tree_attention(q, cache, parents=_i32(parents), ws=ws)
+    assert sd.get_device_error() == 0
+    for b in range(B):
+        check_scene(out, q, cache, b, parents[b], R)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_wide_tables_are_served_in_shares(D):
+    """Some of the shapes above, for each head dim."""
+    def shares(B, R, Hq, Hkv, D, keys, width):
+        pool = torch.zeros((1, Hkv, 64, D), dtype=torch.bfloat16, device="cuda")
+        cache = sd.PagedKVCache(pool, pool.clone(), torch.zeros((B, width // 64), dtype=torch.int32, device="cuda"),
+                                torch.full((B,), R, dtype=torch.int32, device="cuda"))
+        return takes_shares(torch.zeros((B, R, Hq, D), dtype=torch.bfloat16, device="cuda"), cache)
+    ways = [shares(*s) for s in WIDE if s[4] == D]
+    assert sum(ways) >= 2

@@ -31,9 +31,12 @@
 //
 // What it takes on a GB300 (cold inputs, the device alone), and what bounds it. 32 ragged scenes
 // of up to 8192 keys, 61 rows, 32 / 8 heads x 128 (1.0 GB): 205 us, 4.9 TB/s or 0.73 of a copy's
-// rate. A pair of row tiles takes ~2960 cycles a key tile, of which the exponentials (16 a cycle
-// and SM) need 2048 and the products 2048: a group's weights (1280) wait for its S, and its PV
-// and next S (1650) for the weights, and only the other group's stand between. One scene of
+// rate. About 160 of them are the tile loop (98.6 tiles a CTA): a pair of row tiles takes 1.61 to
+// 1.65 us, ~2960 cycles, a key tile, of which the exponentials (16 a cycle and SM) need 2048 and the products
+// 2048: a group's weights (1280) wait for its S, and its PV and next S (1650) for the weights,
+// and only the other group's stand between. The launch, a CTA's first queries and its last
+// output take 15, every further run's end and start 9.8 (two row tiles; 6.5 at head dim 64), 1.7
+// times a CTA here, and the parts of cut units and their joining 12 to 15. One scene of
 // 131072 keys and 8 rows: 94 us, 0.86 of the copy's rate on 96 SMs. One scene of 4096 keys is
 // one launch of dependent phases, 1 row 9.8 us, 26 rows 13.2 (the cluster's join of 104 rows a
 // head, 55 KB into every CTA at ~16 bytes a cycle, a quarter of it).
@@ -1146,7 +1149,10 @@ sd_status host_plan(int B, int R, int Hq, int Hkv, int D, int cap, HostPlan* p) 
   // the joining kernel; and never less than all tiles' bytes take. (32 query / 8 KV heads x 128,
   // clusters / even shares: 26 rows and 4096 keys, 1 scene 16 / 37, 12 scenes 43 / 50, 20
   // scenes 81 / 71; 61 rows, 32 scenes of 512 keys 46 / 65, of 8192 232 / 205; 8 rows, 131072
-  // keys 94 / 100, where clusters of 8 take 129, of 16 146.)
+  // keys 94 / 100, where clusters of 8 take 129, of 16 146.) The keys are not known here, so it
+  // is the table's width that counts: measured for tables as wide as their longest scene. In one
+  // 16 times as wide few scenes take even shares too: 1 row over 4096 keys 7.4 -> 12.1 us, 26
+  // rows 11.9 -> 25.9, 32 scenes of 512 keys with 61 rows 33.7 -> 45.2.
   struct Cost {
     double tile, unit, exchange, join;
   };

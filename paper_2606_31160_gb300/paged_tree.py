@@ -9,6 +9,9 @@ its own ancestors (`sd.tree_attention`). The target's logits then pick a path
 (`sd.accept_tree`), and its rows move together behind the prefix in every layer's cache
 (`sd.paged_commit`).
 
+Trees are accepted greedily only, and the command fills the prefix with random rows: the
+attention of a prompt's own rows would go in calls of up to 256 rows, a chain each.
+
     python -m paper_2606_31160_gb300.paged_tree [--prefix 1000 --nodes 26 --steps 4]
 """
 
